@@ -1,0 +1,89 @@
+// net_common.cuh -- what the network operators (net_scan.cu, net_norm.cu, net_drop.cu) share: moves of a thread's
+// channels between memory and fp32 registers, the gate function, and the checks of an argument block.
+#pragma once
+
+#include <cstdint>
+#include <cstdio>
+#include <cstdlib>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include "auvenv.h"
+#include "auvnet.h"
+
+namespace auv {
+namespace net {
+
+// A thread's piece of a row in memory: E channels of type T in one access.
+template <int BYTES> struct Word;
+template <> struct Word<2> { using type = uint16_t; };
+template <> struct Word<4> { using type = uint32_t; };
+template <> struct Word<8> { using type = uint2; };
+template <> struct Word<16> { using type = uint4; };
+
+template <typename T, int E> using Raw = typename Word<(int)sizeof(T) * E>::type;
+
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
+__device__ __forceinline__ void from_float(float x, float& r) { r = x; }
+__device__ __forceinline__ void from_float(float x, __nv_bfloat16& r) { r = __float2bfloat16_rn(x); }
+__device__ __forceinline__ void from_float(float x, __half& r) { r = __float2half_rn(x); }
+
+template <typename T, int E>
+__device__ __forceinline__ void unpack(const Raw<T, E>& w, float (&x)[E]) {
+  union { Raw<T, E> w; T t[E]; } u;
+  u.w = w;
+#pragma unroll
+  for (int e = 0; e < E; ++e) x[e] = to_float(u.t[e]);
+}
+
+template <typename T, int E>
+__device__ __forceinline__ Raw<T, E> pack(const float (&x)[E]) {
+  union U { Raw<T, E> w; T t[E]; __device__ U() {} } u;
+#pragma unroll
+  for (int e = 0; e < E; ++e) from_float(x[e], u.t[e]);
+  return u.w;
+}
+
+template <typename T, int E>
+__device__ __forceinline__ void load(const T* p, float (&x)[E]) {
+  unpack<T, E>(*reinterpret_cast<const Raw<T, E>*>(p), x);
+}
+
+template <typename T, int E>
+__device__ __forceinline__ void store(T* p, const float (&x)[E]) {
+  *reinterpret_cast<Raw<T, E>*>(p) = pack<T, E>(x);
+}
+
+// sigmoid(x) and sigmoid(-x) from one exponential; both are exact to a few
+// ulp, which 1 - sigmoid(x) is not where the gate is nearly shut.
+__device__ __forceinline__ void gates(float x, float& a, float& b) {
+  const float e = __expf(-fabsf(x));
+  const float r = __fdividef(1.0f, 1.0f + e);
+  const float q = e * r;
+  a = x >= 0.0f ? r : q;
+  b = x >= 0.0f ? q : r;
+}
+
+// ---------------------------------------------------------------- host side
+int fail(int code, const char* fmt, ...);
+int cuda_fail(cudaError_t e, const char* what);
+// Device memory of the current device, aligned to `align`.
+int need(const void* p, const char* name, size_t align);
+// The same for rows (ni x nj rows of nk elements of `size` bytes): strides not
+// negative; of an output, no two rows on the same memory.
+int need_rows(const net_rows& r, const char* name, int64_t ni, int64_t nj, int64_t nk, int size, bool output);
+int sm_count();
+
+// Whether every access of E channels of r is aligned.
+inline bool aligned(const net_rows& r, int64_t ni, int64_t nj, int size, int e) {
+  return reinterpret_cast<uintptr_t>(r.data) % ((size_t)size * e) == 0 && (ni <= 1 || r.outer % e == 0) &&
+         (nj <= 1 || r.inner % e == 0);
+}
+
+inline int type_size(uint32_t dtype) { return dtype == NET_FP32 ? 4 : 2; }
+
+}  // namespace net
+}  // namespace auv
