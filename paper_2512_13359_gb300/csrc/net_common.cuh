@@ -57,11 +57,14 @@ __device__ __forceinline__ void store(T* p, const float (&x)[E]) {
   *reinterpret_cast<Raw<T, E>*>(p) = pack<T, E>(x);
 }
 
-// sigmoid(x) and sigmoid(-x) from one exponential; both are exact to a few
-// ulp, which 1 - sigmoid(x) is not where the gate is nearly shut.
+// sigmoid(x) and sigmoid(-x) from one exponential; both are right to a few
+// ulp, which 1 - sigmoid(x) is not where the gate is nearly shut.  Eight
+// instructions: the flush of what is below 2^-126 spares the scalings around
+// the two approximations.
 __device__ __forceinline__ void gates(float x, float& a, float& b) {
-  const float e = __expf(-fabsf(x));
-  const float r = __fdividef(1.0f, 1.0f + e);
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fabsf(x) * -1.44269504088896341f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
   const float q = e * r;
   a = x >= 0.0f ? r : q;
   b = x >= 0.0f ? q : r;

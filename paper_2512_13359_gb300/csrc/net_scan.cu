@@ -1,82 +1,310 @@
-// net_scan.cu -- gated linear recurrence along a trajectory (auvnet.h, net_gate_scan): h[t] = a c[t] + (1 - a) v[t],
-// a = sigmoid(f[t]), c[t] = h[t - 1] or 0 where an episode ended.
-#include "net_common.cuh"
+// net_scan.cu -- gated linear recurrence along a trajectory (auvnet.h, net_gate_scan).
+//
+// h[t] = a c[t] + b v[t] with a = sigmoid(f[t]), b = 1 - a, c[t] = h[t - 1] or 0 where an episode ended: per channel a
+// chain of affine maps.  The backward pass is the same chain from the last step to the first, in g[t], the gradient of
+// c[t]: d[t] = dy[t] + g[t + 1], g[t] = a d[t] or 0.  Both move bytes and compute little (3 arrays of T N D forward, 6
+// backward), so two kernels share the work by how much parallelism the channels give:
+//
+//  k_steps  one thread per E adjacent channels walks the steps.  Its inputs of the next 8 steps are on their way to
+//           shared memory (cp.async to slots of its own: no barrier), so few threads keep HBM busy.
+//  k_one    the same for a single step.
+//  k_pieces few channels, many steps: the steps are split too (net_pieces.cu).
+#include "net_scan.cuh"
 
 namespace auv {
 namespace net {
 namespace {
 
-struct Scan {
-  int64_t T, N, D;
-  net_rows f, v, y, dy, df, dv;
-  const float* h0;
-  float* hT;
-  const float* dhT;
-  float* dh0;
-  const uint8_t *done, *done_prev;
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* dst, const void* src) {
+  const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(src) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(d), "l"(src), "n"(BYTES) : "memory");
+}
+// Two-byte pieces (odd widths or strides of 16-bit types) have no asynchronous copy.
+template <typename T, int E> constexpr bool kAsync = sizeof(T) * E >= 4;
+
+template <int E>
+__device__ __forceinline__ void load_state(const float* p, float (&x)[E]) {
+  if (p && E >= 4 && reinterpret_cast<uintptr_t>(p) % 16 == 0) {
+#pragma unroll
+    for (int e = 0; e + 3 < E; e += 4) {
+      const float4 w = *reinterpret_cast<const float4*>(p + e);
+      x[e] = w.x, x[e + 1] = w.y, x[e + 2] = w.z, x[e + 3] = w.w;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = p ? p[e] : 0.0f;
+  }
+}
+template <int E>
+__device__ __forceinline__ void store_state(float* p, const float (&x)[E]) {
+  if (E >= 4 && reinterpret_cast<uintptr_t>(p) % 16 == 0) {
+#pragma unroll
+    for (int e = 0; e + 3 < E; e += 4) *reinterpret_cast<float4*>(p + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e) p[e] = x[e];
+  }
+}
+
+// One step of E channels: h (forward) or g (backward) is taken through it and its outputs are stored at y, or dv and
+// df.  before: the state before step 0, asked for at that step alone (first).  ends: bit e for channel e.
+template <typename T, int E, bool BACK>
+__device__ __forceinline__ void step(const float (&ga)[E], const float (&gb)[E], const Raw<T, E>& rv, const Raw<T, E>& ry,
+                                     const Raw<T, E>& rdy, bool first, const float* before, uint32_t ends, T* y, T* z,
+                                     float (&h)[E]) {
+  float v[E];
+  unpack<T, E>(rv, v);
+  if constexpr (!BACK) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) h[e] = fmaf(ga[e], ends >> e & 1u ? 0.0f : h[e], gb[e] * v[e]);
+    store<T, E>(y, h);
+  } else {
+    float c[E], dy[E], df[E], dv[E];
+    if (!first) unpack<T, E>(ry, c);
+    else load_state<E>(before, c);
+    unpack<T, E>(rdy, dy);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const bool end = ends >> e & 1u;
+      const float q = dy[e] + h[e];
+      dv[e] = gb[e] * q;
+      df[e] = ga[e] * dv[e] * ((end ? 0.0f : c[e]) - v[e]);
+      h[e] = end ? 0.0f : ga[e] * q;
+    }
+    store<T, E>(y, dv);
+    store<T, E>(z, df);
+  }
+}
+
+// Whose flags a thread's channels follow: those of its first channel's env, and of the next env from some channel on
+// (MIXED: arrays whose rows follow each other in memory are taken as one row, whose pieces may belong to two envs).
+template <int E, bool MIXED>
+struct Owner {
+  int64_t env;
+  uint32_t second;      // bits of the channels of the next env
+  __device__ Owner(int64_t first, int64_t per) {
+    env = first / per;
+    const int split = (int)min((int64_t)E, (env + 1) * per - first);
+    second = MIXED ? ((1u << E) - 1) & ~((1u << split) - 1) : 0u;
+  }
+  // The flags of step t as they are in memory, and from them bit e: channel e's episode ended before it.  Apart, since
+  // the first is done long before the second: nothing may wait for the load in between.
+  __device__ uint32_t load(const Scan& a, int t) const {
+    const uint32_t one = end_flag(a, t, env);
+    if constexpr (MIXED) return second ? one | end_flag(a, t, env + 1) << 8 : one;
+    return one;
+  }
+  __device__ uint32_t ends(uint32_t flag) const {
+    if constexpr (MIXED) return ((flag & 255u) ? ((1u << E) - 1) & ~second : 0u) | (flag >> 8 ? second : 0u);
+    return flag ? (1u << E) - 1 : 0u;
+  }
 };
 
-__device__ __forceinline__ bool ended(const Scan& a, int64_t t, int64_t n) {
-  const uint8_t* p = t ? (a.done ? a.done + (t - 1) * a.N + n : nullptr) : (a.done_prev ? a.done_prev + n : nullptr);
-  return p && *p;
+// T = 1, a rollout's step: nothing to walk, so few registers and many threads.
+template <typename T, int E, bool BACK, bool MIXED>
+__global__ void __launch_bounds__(256) k_one(Scan a, int64_t width) {
+  const int64_t m = blockIdx.x * (int64_t)256 + threadIdx.x, per = a.D / E;
+  if (m >= a.N * per) return;
+  const int64_t n = m / per, d = (m - n * per) * E;
+  using W = Raw<T, E>;
+  auto get = [&](const net_rows& r) { return *reinterpret_cast<const W*>(base<T>(r, n, d)); };
+  const W rf = get(a.f), rv = get(a.v), rdy = BACK ? get(a.dy) : rf;
+  const float* const from = BACK ? a.dhT : a.h0;
+  float h[E], f[E], ga[E], gb[E];
+  load_state<E>(from ? from + m * E : nullptr, h);
+  const Owner<E, MIXED> owner(m * E, width);
+  const uint32_t ends = owner.ends(owner.load(a, 0));
+  unpack<T, E>(rf, f);
+#pragma unroll
+  for (int e = 0; e < E; ++e) gates(f[e], ga[e], gb[e]);
+  step<T, E, BACK>(ga, gb, rv, rv, rdy, true, a.h0 ? a.h0 + m * E : nullptr, ends,
+                   const_cast<T*>(base<T>(BACK ? a.dv : a.y, n, d)), BACK ? const_cast<T*>(base<T>(a.df, n, d)) : nullptr,
+                   h);
+  float* const out = BACK ? a.dh0 : a.hT;
+  if (out) store_state<E>(out + m * E, h);
 }
 
-template <typename T>
-__device__ __forceinline__ T* at(const net_rows& r, int64_t t, int64_t n, int64_t d) {
-  return reinterpret_cast<T*>(r.data) + t * r.outer + n * r.inner + d;
-}
+constexpr int kStepThreads = 128;
+// Steps on their way: of narrow pieces more, since few channels make few threads.
+template <int E> constexpr int kAheadOf = E >= 4 ? 8 : 16;
+// Steps whose gates are computed side by side before the chain runs through them: narrow pieces, of which few channels
+// make few warps, wait for each other's latency otherwise.
+template <int E> constexpr int kGroup = E == 4 ? 2 : 4;
 
-// One channel of one env a thread, step after step.
-template <typename T>
-__global__ void k_scan(Scan a) {
-  const int64_t m = blockIdx.x * (int64_t)blockDim.x + threadIdx.x;
-  if (m >= a.N * a.D) return;
-  const int64_t n = m / a.D, d = m % a.D;
-  float h = a.h0 ? a.h0[m] : 0.0f;
-  for (int64_t t = 0; t < a.T; ++t) {
-    float f[1], v[1], ga, gb;
-    load<T, 1>(at<T>(a.f, t, n, d), f);
-    load<T, 1>(at<T>(a.v, t, n, d), v);
-    gates(f[0], ga, gb);
-    if (ended(a, t, n)) h = 0.0f;
-    h = fmaf(ga, h, gb * v[0]);
-    const float o[1] = {h};
-    store<T, 1>(at<T>(a.y, t, n, d), o);
+template <typename T, int E, bool BACK, bool MIXED>
+__global__ void __launch_bounds__(kStepThreads) k_steps(Scan a, int64_t width) {
+  using W = Raw<T, E>;
+  using In = Inputs<T, BACK>;
+  constexpr int K = In::kN, kAhead = kAsync<T, E> ? kAheadOf<E> : 8, kG = kAsync<T, E> ? kGroup<E> : kAhead;
+  extern __shared__ uint4 smem[];
+  W* const ring = reinterpret_cast<W*>(smem) + threadIdx.x;    // slot (u, i) at (u * K + i) * kStepThreads
+  const int64_t m = blockIdx.x * (int64_t)kStepThreads + threadIdx.x, per = a.D / E;
+  if (m >= a.N * per) return;
+  const int64_t n = m / per, d = (m - n * per) * E;
+  In in(a, n, d);
+  const int T_ = a.T;
+  static_assert(kAhead * E <= 32, "the flags of a round are one word");
+  [[maybe_unused]] W reg[kAhead][K];
+  auto fetch = [&](int u, int s) {      // the s-th step of the chain, in order
+    if (s < T_) {
+#pragma unroll
+      for (int i = 0; i < K; ++i) {
+        if (i != 2 || s < T_ - 1) {
+          if constexpr (kAsync<T, E>) copy_async<sizeof(W)>(ring + (u * K + i) * kStepThreads, in.p[i]);
+          else reg[u][i] = *reinterpret_cast<const W*>(in.p[i]);
+        }
+        in.p[i] += in.by[i];
+      }
+    }
+  };
+  const bool flags = a.done || a.done_prev;
+  const Owner<E, MIXED> owner(m * E, width);
+  auto flag_of = [&](int s) { return flags && s < T_ ? owner.load(a, BACK ? T_ - 1 - s : s) : 0u; };
+  uint32_t flag[kAhead];
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) {
+    fetch(u, u);
+    if (kAsync<T, E> && u % kG == kG - 1) copy_commit();
+    flag[u] = flag_of(u);
   }
-  if (a.hT) a.hT[m] = h;
-}
-
-template <typename T>
-__global__ void k_scan_back(Scan a) {
-  const int64_t m = blockIdx.x * (int64_t)blockDim.x + threadIdx.x;
-  if (m >= a.N * a.D) return;
-  const int64_t n = m / a.D, d = m % a.D;
-  float g = a.dhT ? a.dhT[m] : 0.0f;
-  for (int64_t t = a.T - 1; t >= 0; --t) {
-    float f[1], v[1], dy[1], c[1], ga, gb;
-    load<T, 1>(at<T>(a.f, t, n, d), f);
-    load<T, 1>(at<T>(a.v, t, n, d), v);
-    load<T, 1>(at<T>(a.dy, t, n, d), dy);
-    if (t) load<T, 1>(at<T>(a.y, t - 1, n, d), c);
-    else c[0] = a.h0 ? a.h0[m] : 0.0f;
-    gates(f[0], ga, gb);
-    const bool e = ended(a, t, n);
-    if (e) c[0] = 0.0f;
-    const float q = dy[0] + g;
-    const float dv[1] = {gb * q}, df[1] = {ga * gb * (c[0] - v[0]) * q};
-    store<T, 1>(at<T>(a.dv, t, n, d), dv);
-    store<T, 1>(at<T>(a.df, t, n, d), df);
-    g = e ? 0.0f : ga * q;
+  float h[E];
+  load_state<E>(BACK ? (a.dhT ? a.dhT + m * E : nullptr) : (a.h0 ? a.h0 + m * E : nullptr), h);
+  const float* const h0 = a.h0 ? a.h0 + m * E : nullptr;
+  const net_rows &ro = BACK ? a.dv : a.y, &rz = BACK ? a.df : a.y;
+  T* y = const_cast<T*>(base<T>(ro, n, d)) + (BACK ? (T_ - 1) * ro.outer : 0);
+  T* z = BACK ? const_cast<T*>(base<T>(rz, n, d)) + (T_ - 1) * rz.outer : nullptr;
+  const int64_t ys = BACK ? -ro.outer : ro.outer, zs = -rz.outer;
+  for (int s0 = 0; s0 < T_; s0 += kAhead) {
+    uint32_t ends = 0;
+    if (flags) {
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) ends |= owner.ends(flag[u]) << (u * E);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) flag[u] = flag_of(s0 + kAhead + u);
+    }
+#pragma unroll
+    for (int u0 = 0; u0 < kAhead; u0 += kG) {
+      if (s0 + u0 >= T_) break;
+      W w[kG][K];
+      if constexpr (kAsync<T, E>) copy_wait<kAhead / kG - 1>();
+#pragma unroll
+      for (int u = 0; u < kG; ++u)
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+          if constexpr (kAsync<T, E>) w[u][i] = ring[((u0 + u) * K + i) * kStepThreads];
+          else w[u][i] = reg[u][i];
+        }
+#pragma unroll
+      for (int u = 0; u < kG; ++u) fetch(u0 + u, s0 + u0 + u + kAhead);
+      if constexpr (kAsync<T, E>) copy_commit();
+      float ga[kG][E], gb[kG][E];
+#pragma unroll
+      for (int u = 0; u < kG; ++u) {
+        float f[E];
+        unpack<T, E>(w[u][0], f);
+#pragma unroll
+        for (int e = 0; e < E; ++e) gates(f[e], ga[u][e], gb[u][e]);
+      }
+#pragma unroll
+      for (int u = 0; u < kG; ++u) {
+        const int s = s0 + u0 + u;
+        if (s < T_) {
+          step<T, E, BACK>(ga[u], gb[u], w[u][1], w[u][BACK ? 2 : 0], w[u][BACK ? 3 : 0], s == T_ - 1, h0,
+                           ends >> ((u0 + u) * E), y, z, h);
+          y += ys;
+          if constexpr (BACK) z += zs;
+        }
+      }
+    }
   }
-  if (a.dh0) a.dh0[m] = g;
+  if constexpr (kAsync<T, E>) copy_wait<0>();
+  float* const out = BACK ? a.dh0 : a.hT;
+  if (out) store_state<E>(out + m * E, h);
 }
 
-template <typename T>
-cudaError_t launch(const Scan& a, bool back, cudaStream_t s) {
-  const int64_t blocks = (a.N * a.D + 127) / 128;
-  if (back) k_scan_back<T><<<(unsigned)blocks, 128, 0, s>>>(a);
-  else k_scan<T><<<(unsigned)blocks, 128, 0, s>>>(a);
+template <typename T, int E, bool BACK, bool MIXED>
+cudaError_t launch_steps(const Scan& a, int64_t width, cudaStream_t s) {
+  const int64_t blocks = (a.N * (a.D / E) + kStepThreads - 1) / kStepThreads;
+  // slots: of a short sequence as many as it has steps, whole groups of them (a group is read whole)
+  constexpr int kAhead = kAheadOf<E>, kG = kGroup<E>;
+  const int ahead = a.T < kAhead ? (a.T + kG - 1) / kG * kG : kAhead;
+  const int smem = kAsync<T, E> ? ahead * Inputs<T, BACK>::kN * kStepThreads * (int)sizeof(T) * E : 0;
+  const auto kern = k_steps<T, E, BACK, MIXED>;
+  if (smem > 48 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+  }
+  kern<<<(unsigned)blocks, kStepThreads, smem, s>>>(a, width);
   return cudaGetLastError();
+}
+
+template <typename T, int E, bool BACK, bool MIXED>
+cudaError_t launch_walk(const Scan& a, int64_t width, cudaStream_t s) {
+  if (a.T == 1) {
+    k_one<T, E, BACK, MIXED><<<(unsigned)((a.N * (a.D / E) + 255) / 256), 256, 0, s>>>(a, width);
+    return cudaGetLastError();
+  }
+  if constexpr (E <= 4) return launch_steps<T, E, BACK, MIXED>(a, width, s);
+  else return cudaErrorInvalidValue;   // not asked for
+}
+
+template <typename T, bool BACK, bool MIXED>
+cudaError_t launch_width(const Scan& a, int64_t width, int e, cudaStream_t s) {
+  if constexpr (sizeof(T) == 2)
+    if (e == 8) return launch_walk<T, 8, BACK, MIXED>(a, width, s);
+  if (e == 4) return launch_walk<T, 4, BACK, MIXED>(a, width, s);
+  if (e == 2) return launch_walk<T, 2, BACK, MIXED>(a, width, s);
+  return launch_walk<T, 1, BACK, false>(a, width, s);
+}
+
+// T = 0: the state passes as it is.
+__global__ void k_none(int64_t m, const float* from, float* to) {
+  const int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x;
+  if (i < m) to[i] = from ? from[i] : 0.0f;
+}
+
+template <typename T, bool BACK>
+cudaError_t launch(const Scan& a, cudaStream_t s) {
+  const int64_t m = a.N * a.D, sms = sm_count();
+  if (a.T == 0) {
+    float* const to = BACK ? a.dh0 : a.hT;
+    if (to) k_none<<<(unsigned)((m + 255) / 256), 256, 0, s>>>(m, BACK ? a.dhT : a.h0, to);
+    return cudaGetLastError();
+  }
+  // Walking the steps takes some 100 ns a step forward and 190 backward, whatever the channels (up to HBM's pace);
+  // splitting them 4 us for every round of pieces (32 channels x 256 steps, 128 backward in fp32) that the SMs' two
+  // blocks (one) take.  512 steps of bf16, forward: 32,768 channels 49 and 34 us, 131,072 channels 87 and 121.
+  if (a.T >= 32) {
+    constexpr bool kLarge = BACK && sizeof(T) == 4;
+    const int64_t rows = kLarge ? 128 : 256, blocks = kLarge ? sms : 2 * sms;
+    const int64_t rounds = ((m + 31) / 32 * ((a.T + rows - 1) / rows) + blocks - 1) / blocks;
+    if ((int64_t)a.T * (BACK ? 190 : 100) > 4000 * rounds) return launch_pieces<T>(a, BACK, s);
+  }
+  // Channels of a thread: for one step as many as 16 bytes hold; over many steps four, since half as many bytes a
+  // thread make twice the threads (4,096 envs x 256 channels x 128 steps of bf16: 127 us, 137 with eight), and two
+  // where four would leave fewer than 160 threads an SM (512 steps, 65,536 channels: 55 us, 75 with four; 131,072: 99
+  // and 86).
+  int most = 16 / (int)sizeof(T);
+  if (a.T > 1) most = m >= 4 * 160 * sms ? 4 : 2;
+  const net_rows* rows[] = {&a.f, &a.v, &a.y, &a.dy, &a.df, &a.dv};
+  constexpr int kArrays = BACK ? 6 : 3;
+  auto fits = [&](int e, int64_t n) {
+    for (int i = 0; i < kArrays; ++i)
+      if (!aligned(*rows[i], a.T, n, sizeof(T), e)) return false;
+    return true;
+  };
+  // Rows that follow each other in every array are one row.
+  Scan flat = a;
+  bool one_row = a.N > 1;
+  for (int i = 0; i < kArrays; ++i) one_row = one_row && rows[i]->inner == a.D;
+  flat.D = m, flat.N = 1;
+  for (int e = most; e > 1; e /= 2) {
+    if (a.D % e == 0 && fits(e, a.N)) return launch_width<T, BACK, false>(a, a.D, e, s);
+    if (one_row && m % e == 0 && a.D >= e && fits(e, 1)) return launch_width<T, BACK, true>(flat, a.D, e, s);
+  }
+  return launch_width<T, BACK, false>(a, a.D, 1, s);
 }
 
 int run(const net_scan* p, bool back, void* stream) {
@@ -86,8 +314,8 @@ int run(const net_scan* p, bool back, void* stream) {
   if (p->dtype > NET_FP16) return fail(AUV_ERR_INVALID, "dtype %u unknown", p->dtype);
   if (p->T < 0 || p->N < 0 || p->D < 0) return fail(AUV_ERR_INVALID, "negative size");
   const int64_t most = (int64_t)1 << 37;   // channels of a call: blocks stay below 2^31
-  if (p->N > most || p->D > most || (p->N && p->D > most / p->N) || p->T > ((int64_t)1 << 50))
-    return fail(AUV_ERR_UNSUPPORTED, "N * D past 2^37 or T past 2^50");
+  if (p->N > most || p->D > most || (p->N && p->D > most / p->N) || p->T > INT32_MAX)
+    return fail(AUV_ERR_UNSUPPORTED, "N * D past 2^37 or T past 2^31");
   const int64_t M = p->N * p->D;
   if (M == 0) return AUV_OK;
   const int z = type_size(p->dtype);
@@ -103,12 +331,18 @@ int run(const net_scan* p, bool back, void* stream) {
       {p->done, "done", 1, true}, {p->done_prev, "done_prev", 1, true}};
   for (const auto& q : flat)
     if (q.p && q.used && (rc = need(q.p, q.name, q.align))) return rc;
-  const Scan a = {p->T, p->N, p->D, p->f, p->v, p->y, p->dy, p->df, p->dv, p->h0, p->hT, p->dhT, p->dh0, p->done,
-                  p->done_prev};
+  const Scan a = {(int)p->T, p->N, p->D, p->f, p->v, p->y, p->dy, p->df, p->dv, p->h0, p->hT, p->dhT, p->dh0, p->done,
+                  p->done_prev, p->N};
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = p->dtype == NET_FP32   ? launch<float>(a, back, s)
-                        : p->dtype == NET_BF16 ? launch<__nv_bfloat16>(a, back, s)
-                                               : launch<__half>(a, back, s);
+  cudaError_t e;
+  if (back)
+    e = p->dtype == NET_FP32   ? launch<float, true>(a, s)
+        : p->dtype == NET_BF16 ? launch<__nv_bfloat16, true>(a, s)
+                               : launch<__half, true>(a, s);
+  else
+    e = p->dtype == NET_FP32   ? launch<float, false>(a, s)
+        : p->dtype == NET_BF16 ? launch<__nv_bfloat16, false>(a, s)
+                               : launch<__half, false>(a, s);
   return e == cudaSuccess ? AUV_OK : cuda_fail(e, back ? "net_gate_scan_backward" : "net_gate_scan");
 }
 

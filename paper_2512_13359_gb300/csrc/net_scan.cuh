@@ -1,0 +1,58 @@
+// net_scan.cuh -- what the two kernels of the gated recurrence (net_scan.cu, net_pieces.cu) share.
+#pragma once
+
+#include "net_common.cuh"
+
+namespace auv {
+namespace net {
+
+struct Scan {
+  int T;
+  int64_t N, D;
+  net_rows f, v, y, dy, df, dv;
+  const float* h0;
+  float* hT;
+  const float* dhT;
+  float* dh0;
+  const uint8_t *done, *done_prev;
+  int64_t envs;          // of done: N, whatever of it has become channels
+};
+
+template <typename T>
+__device__ __forceinline__ const T* base(const net_rows& r, int64_t n, int64_t d) {
+  return reinterpret_cast<const T*>(r.data) + n * r.inner + d;
+}
+
+// The flag of step t of env n (0 where there are none).
+__device__ __forceinline__ uint32_t end_flag(const Scan& a, int t, int64_t n) {
+  const uint8_t* p = t ? a.done : a.done_prev;
+  return p ? (uint32_t)__ldg(p + (t ? (t - 1) * a.envs : 0) + n) : 0u;
+}
+
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+
+// The arrays of one step that a thread reads: f, v, and backward the state before the step and dy; from the chain's
+// first step on (the last of the sequence backward).
+template <typename T, bool BACK>
+struct Inputs {
+  static constexpr int kN = BACK ? 4 : 2;
+  const T* p[kN];       // of the chain's first step (i = 2: the state before it)
+  int64_t by[kN];       // from one step to the next
+  __device__ Inputs(const Scan& a, int64_t n, int64_t d) {
+    const net_rows* r[4] = {&a.f, &a.v, &a.y, &a.dy};
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      p[i] = base<T>(*r[i], n, d) + (BACK ? (a.T - 1 - (i == 2)) * r[i]->outer : 0);
+      by[i] = BACK ? -r[i]->outer : r[i]->outer;
+    }
+  }
+};
+
+// Few channels, many steps (net_pieces.cu); back: the gradients.
+constexpr int kPieceThreads = 256;
+template <typename T> cudaError_t launch_pieces(const Scan& a, bool back, cudaStream_t s);
+
+}  // namespace net
+}  // namespace auv
