@@ -1,4 +1,18 @@
 // net_norm.cu -- group norm with an activation, channels last (auvnet.h, net_group_norm).
+//
+// Two arrays of B S C forward, three backward, and a reduction over each group (S positions x C / G channels) before
+// the elements can be finished: bytes again, if they are read once.
+//
+//  k_team, k_team_back      groups of a few thousand values: a team of lanes (of a warp, or a whole block) keeps a group
+//                           in registers and goes from instance to instance.  A team's channels stay the same, so the
+//                           backward pass sums dgamma and dbeta in registers and joins them once at its end.
+//  k_part, k_stats, k_apply larger groups: sums by chunk and channel, joined, and the elements read once more.
+//  (.._back)
+//
+// Variances are those of deviations: in registers from the mean, over chunks from each channel's first value, joined
+// by the distances of the means.  All sums have a fixed order.
+#include <algorithm>
+
 #include "net_common.cuh"
 
 namespace auv {
@@ -14,29 +28,57 @@ struct Norm {
   uint32_t act;
 };
 
-// act(u) and act'(u); the slope of relu at 0 is 0.
-__device__ __forceinline__ float act_value(uint32_t act, float u) {
-  if (act == NET_ACT_RELU) return u > 0.0f || u != u ? u : 0.0f;
-  if (act == NET_ACT_SILU) {
+// tanh: the difference of the gates is exact to 2^-22, which is enough ahead of a 16-bit store.
+template <typename T>
+__device__ __forceinline__ float tanh_of(float u) {
+  if constexpr (sizeof(T) == 4) {
+    return tanhf(u);
+  } else {
     float s, r;
-    gates(u, s, r);
-    return u * s;
+    gates(2.0f * u, s, r);
+    return s - r;
   }
-  return act == NET_ACT_TANH ? tanhf(u) : u;
 }
 
-__device__ __forceinline__ float act_slope(uint32_t act, float u) {
-  if (act == NET_ACT_RELU) return u > 0.0f ? 1.0f : 0.0f;
-  if (act == NET_ACT_SILU) {
-    float s, r;
-    gates(u, s, r);
-    return s * fmaf(u, r, 1.0f);
+// act(u); NaN passes relu.
+template <typename T, int E>
+__device__ __forceinline__ void activate(uint32_t act, float (&u)[E]) {
+  if (act == NET_ACT_RELU) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) u[e] = u[e] <= 0.0f ? 0.0f : u[e];
+  } else if (act == NET_ACT_SILU) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      float s, r;
+      gates(u[e], s, r);
+      u[e] *= s;
+    }
+  } else if (act == NET_ACT_TANH) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) u[e] = tanh_of<T>(u[e]);
   }
-  if (act == NET_ACT_TANH) {
-    const float t = tanhf(u);
-    return fmaf(-t, t, 1.0f);
+}
+
+// dz = dy act'(u) in place of dy; the slope of relu at 0 is 0.
+template <typename T, int E>
+__device__ __forceinline__ void slope(uint32_t act, const float (&u)[E], float (&dy)[E]) {
+  if (act == NET_ACT_RELU) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) dy[e] = u[e] > 0.0f ? dy[e] : 0.0f;
+  } else if (act == NET_ACT_SILU) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      float s, r;
+      gates(u[e], s, r);
+      dy[e] *= s * fmaf(u[e], r, 1.0f);
+    }
+  } else if (act == NET_ACT_TANH) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const float t = tanh_of<T>(u[e]);
+      dy[e] *= fmaf(-t, t, 1.0f);
+    }
   }
-  return 1.0f;
 }
 
 template <typename T>
@@ -44,117 +86,645 @@ __device__ __forceinline__ T* at(const net_rows& r, int64_t i, int64_t j, int64_
   return reinterpret_cast<T*>(r.data) + i * r.outer + j * r.inner + k;
 }
 
-constexpr int kThreads = 128;
+template <int E>
+__device__ __forceinline__ void load_weights(const float* w, int64_t c, float none, float (&x)[E]) {
+#pragma unroll
+  for (int e = 0; e < E; ++e) x[e] = w ? __ldg(w + c + e) : none;
+}
 
-__device__ float block_sum(float x) {
-  __shared__ float part[kThreads / 32];
-  for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+// ------------------------------------------------------------------ teams
+constexpr int kThreads = 256;
+
+// How teams cover a call: a group is `pieces` pieces of E channels, `wide` of them a position; a team has `lanes` lanes
+// (a power of two up to 32, or all of a block); a block has `groups` x `rows` teams, for that many adjacent groups of
+// as many instances, and goes on by gridDim.x * rows instances.
+struct Teams {
+  int lanes, pieces, wide, groups, rows;
+};
+
+// The sum over a team, in all its lanes.
+template <bool BLOCK>
+__device__ __forceinline__ void team_sum(float (&x)[2], int lanes) {
+  if constexpr (!BLOCK) {
+    for (int o = lanes / 2; o; o /= 2) {
+      x[0] += __shfl_xor_sync(0xffffffffu, x[0], o);
+      x[1] += __shfl_xor_sync(0xffffffffu, x[1], o);
+    }
+  } else {
+    __shared__ float2 part[kThreads / 32];
+#pragma unroll
+    for (int o = 16; o; o /= 2) {
+      x[0] += __shfl_xor_sync(0xffffffffu, x[0], o);
+      x[1] += __shfl_xor_sync(0xffffffffu, x[1], o);
+    }
+    __syncthreads();
+    if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = make_float2(x[0], x[1]);
+    __syncthreads();
+    x[0] = x[1] = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) x[0] += part[w].x, x[1] += part[w].y;
+  }
+}
+template <bool BLOCK>
+__device__ __forceinline__ float team_sum(float x, int lanes) {
+  float v[2] = {x, 0.0f};
+  team_sum<BLOCK>(v, lanes);
+  return v[0];
+}
+
+// What a lane of a team works on.
+template <int E, int SLOTS>
+struct Lane {
+  int lane, row;           // in the team; its instance among the block's
+  int64_t g, c0;           // group, its first channel
+  bool on;                 // whether the team has a group
+  bool has[SLOTS];         // pieces that the lane has
+  int64_t s[SLOTS];        // their position
+  int c[SLOTS];            // and first channel in the group
+  __device__ Lane(const Norm& a, const Teams& t) {
+    lane = threadIdx.x % t.lanes;
+    const int team = threadIdx.x / t.lanes;
+    row = team / t.groups;
+    g = blockIdx.y * (int64_t)t.groups + team % t.groups;
+    on = row < t.rows && g < a.G;
+    c0 = on ? g * (a.C / a.G) : 0;
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j) {
+      const int i = j * t.lanes + lane;
+      has[j] = on && i < t.pieces;
+      s[j] = i / t.wide;
+      c[j] = i % t.wide * E;
+    }
+  }
+};
+
+template <typename T, int E, int SLOTS, bool BLOCK>
+__global__ void __launch_bounds__(kThreads) k_team(Norm a, Teams t) {
+  const Lane<E, SLOTS> me(a, t);
+  const float n = (float)max((int64_t)1, a.S * (a.C / a.G));
+  float gamma[SLOTS][E], beta[SLOTS][E];
+#pragma unroll
+  for (int j = 0; j < SLOTS; ++j) {
+    load_weights<E>(me.has[j] ? a.gamma : nullptr, me.c0 + me.c[j], 1.0f, gamma[j]);
+    load_weights<E>(me.has[j] ? a.beta : nullptr, me.c0 + me.c[j], 0.0f, beta[j]);
+  }
+  Raw<T, E> next[SLOTS];
+  auto fetch = [&](int64_t b) {
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j)
+      if (me.has[j] && b < a.B)
+        next[j] = *reinterpret_cast<const Raw<T, E>*>(at<T>(a.x, b, me.s[j], me.c0 + me.c[j]));
+  };
+  const int64_t step = (int64_t)gridDim.x * t.rows;
+  fetch(blockIdx.x * (int64_t)t.rows + me.row);
+  for (int64_t b0 = blockIdx.x * (int64_t)t.rows; b0 < a.B; b0 += step) {
+    const int64_t b = b0 + me.row;
+    float x[SLOTS][E];
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j) unpack<T, E>(next[j], x[j]);
+    fetch(b + step);
+    float sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j)
+#pragma unroll
+      for (int e = 0; e < E; ++e) sum += me.has[j] ? x[j][e] : 0.0f;
+    const float mean = team_sum<BLOCK>(sum, t.lanes) / n;
+    sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j)
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        x[j][e] -= mean;
+        sum += me.has[j] ? x[j][e] * x[j][e] : 0.0f;
+      }
+    const float rstd = 1.0f / sqrtf(team_sum<BLOCK>(sum, t.lanes) / n + a.eps);
+    if (me.on && me.lane == 0 && b < a.B) {
+      a.mean[b * a.G + me.g] = mean;
+      a.rstd[b * a.G + me.g] = rstd;
+    }
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[j][e] = fmaf(gamma[j][e], x[j][e] * rstd, beta[j][e]);
+      activate<T, E>(a.act, x[j]);
+      if (me.has[j] && b < a.B) store<T, E>(at<T>(a.y, b, me.s[j], me.c0 + me.c[j]), x[j]);
+    }
+  }
+}
+
+// partial: [2][gridDim.x][C], dbeta's and dgamma's sums by block (NULL: not wanted).
+template <typename T, int E, int SLOTS, bool BLOCK>
+__global__ void __launch_bounds__(kThreads) k_team_back(Norm a, Teams t, float* partial) {
+  extern __shared__ float sums[];          // [2][teams of a block][lanes * SLOTS * E]
+  const Lane<E, SLOTS> me(a, t);
+  const float inv = 1.0f / (float)(a.S * (a.C / a.G));
+  float gamma[SLOTS][E], beta[SLOTS][E], db[SLOTS][E] = {}, dg[SLOTS][E] = {};
+#pragma unroll
+  for (int j = 0; j < SLOTS; ++j) {
+    load_weights<E>(me.has[j] ? a.gamma : nullptr, me.c0 + me.c[j], 1.0f, gamma[j]);
+    load_weights<E>(me.has[j] ? a.beta : nullptr, me.c0 + me.c[j], 0.0f, beta[j]);
+  }
+  Raw<T, E> nx[SLOTS], ny[SLOTS];
+  float nm = 0.0f, nr = 0.0f;
+  auto fetch = [&](int64_t b) {
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j)
+      if (me.has[j] && b < a.B) {
+        nx[j] = *reinterpret_cast<const Raw<T, E>*>(at<T>(a.x, b, me.s[j], me.c0 + me.c[j]));
+        ny[j] = *reinterpret_cast<const Raw<T, E>*>(at<T>(a.dy, b, me.s[j], me.c0 + me.c[j]));
+      }
+    if (me.on && b < a.B) nm = a.mean[b * a.G + me.g], nr = a.rstd[b * a.G + me.g];
+  };
+  const int64_t step = (int64_t)gridDim.x * t.rows;
+  fetch(blockIdx.x * (int64_t)t.rows + me.row);
+  for (int64_t b0 = blockIdx.x * (int64_t)t.rows; b0 < a.B; b0 += step) {
+    const int64_t b = b0 + me.row;
+    float xh[SLOTS][E], dz[SLOTS][E];
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j) {
+      unpack<T, E>(nx[j], xh[j]);
+      unpack<T, E>(ny[j], dz[j]);
+    }
+    const float mean = nm, rstd = nr;
+    fetch(b + step);
+    const bool in = b < a.B;
+    float w[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j) {
+      float u[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        xh[j][e] = (xh[j][e] - mean) * rstd;
+        u[e] = fmaf(gamma[j][e], xh[j][e], beta[j][e]);
+      }
+      slope<T, E>(a.act, u, dz[j]);
+      if (me.has[j] && in) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          db[j][e] += dz[j][e];
+          dg[j][e] = fmaf(dz[j][e], xh[j][e], dg[j][e]);
+          dz[j][e] *= gamma[j][e];
+          w[0] += dz[j][e];
+          w[1] = fmaf(dz[j][e], xh[j][e], w[1]);
+        }
+      }
+    }
+    team_sum<BLOCK>(w, t.lanes);
+    w[0] *= inv;
+    w[1] *= inv;
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j) {
+      float o[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] = rstd * (dz[j][e] - w[0] - xh[j][e] * w[1]);
+      if (me.has[j] && in) store<T, E>(at<T>(a.dx, b, me.s[j], me.c0 + me.c[j]), o);
+    }
+  }
+  if (!partial) return;
+  // Each channel's sums: over the lanes that had it (a position each) and the block's instances.
+  const int team = threadIdx.x / t.lanes, held = t.lanes * SLOTS * E, all = kThreads / t.lanes * held;
+#pragma unroll
+  for (int j = 0; j < SLOTS; ++j)
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      sums[team * held + (j * t.lanes + me.lane) * E + e] = db[j][e];
+      sums[all + team * held + (j * t.lanes + me.lane) * E + e] = dg[j][e];
+    }
   __syncthreads();
-  if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = x;
-  __syncthreads();
+  const int width = t.wide * E;
+  for (int i = threadIdx.x; i < t.groups * width; i += kThreads) {
+    const int64_t g = blockIdx.y * (int64_t)t.groups + i / width;
+    if (g >= a.G) break;
+    float b = 0.0f, w = 0.0f;
+    for (int r = 0; r < t.rows; ++r)
+      for (int k = i % width; k < t.pieces * E; k += width) {
+        b += sums[(r * t.groups + i / width) * held + k];
+        w += sums[all + (r * t.groups + i / width) * held + k];
+      }
+    const int64_t c = g * width + i % width;
+    partial[blockIdx.x * a.C + c] = b;
+    partial[((int64_t)gridDim.x + blockIdx.x) * a.C + c] = w;
+  }
+}
+
+// The sum of column c of [rows][C], 32 columns a block, eight warps over the rows.
+__device__ __forceinline__ float column_sum(const float* p, int64_t rows, int64_t C, int64_t c) {
+  __shared__ float part[kThreads / 32][32];
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   float s = 0.0f;
-  for (int w = 0; w < kThreads / 32; ++w) s += part[w];
+  if (c < C) {
+#pragma unroll 8
+    for (int64_t r = warp; r < rows; r += kThreads / 32) s += p[r * C + c];
+  }
+  __syncthreads();
+  part[warp][lane] = s;
+  __syncthreads();
+  s = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kThreads / 32; ++w) s += part[w][lane];
   return s;
 }
 
-template <typename T>
-__device__ __forceinline__ float value(const net_rows& r, int64_t i, int64_t j, int64_t k) {
-  return to_float(*at<T>(r, i, j, k));
+// dbeta and dgamma from [2][rows][C].
+__global__ void __launch_bounds__(kThreads) k_weights(Norm a, const float* partial, int64_t rows) {
+  const int64_t c = blockIdx.x * (int64_t)32 + threadIdx.x % 32;
+  const float b = column_sum(partial, rows, a.C, c), g = column_sum(partial + rows * a.C, rows, a.C, c);
+  if (threadIdx.x < 32 && c < a.C) {
+    if (a.dbeta) a.dbeta[c] = b;
+    if (a.dgamma) a.dgamma[c] = g;
+  }
 }
 
-// One group of one instance a block.
-template <typename T>
-__global__ void k_norm(Norm a) {
-  const int64_t W = a.C / a.G, n = a.S * W;
+// ------------------------------------------------------------------ chunks
+// Larger groups: a block takes `rows` positions of `cols` pieces of E channels, kThreads / cols rows side by side.
+struct Chunks {
+  int cols;             // pieces of a block, a power of two up to 32
+  int rows;             // positions of a block
+  int64_t count;        // chunks of an instance
+};
+
+template <int E>
+struct Place {
+  int64_t b, chunk, c, s0, s1;
+  int row, rows;        // the thread's first, and how many are side by side
+  bool on;
+  __device__ Place(const Norm& a, const Chunks& k) {
+    b = blockIdx.x / k.count;
+    chunk = blockIdx.x - b * k.count;
+    c = (blockIdx.y * (int64_t)k.cols + threadIdx.x % k.cols) * E;
+    on = c < a.C;
+    row = threadIdx.x / k.cols;
+    rows = kThreads / k.cols;
+    s0 = chunk * k.rows;
+    s1 = min(a.S, s0 + k.rows);
+  }
+};
+
+// Adds up the block's rows: x of the threads of a column, in the first row's.
+template <int E>
+__device__ __forceinline__ void join_rows(float (&x)[E], int cols) {
+  __shared__ float part[E][kThreads];
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < E; ++e) part[e][threadIdx.x] = x[e];
+  __syncthreads();
+  if ((int)threadIdx.x < cols) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      float s = 0.0f;
+      for (int i = threadIdx.x; i < kThreads; i += cols) s += part[e][i];
+      x[e] = s;
+    }
+  }
+}
+
+// Mean and sum of squared deviations of each chunk's channels: part[2][B * count][C].
+template <typename T, int E>
+__global__ void __launch_bounds__(kThreads) k_part(Norm a, Chunks k, float* part) {
+  const Place<E> me(a, k);
+  float first[E] = {}, s1[E] = {}, s2[E] = {};
+  if (me.on) {
+    const T* p = at<T>(a.x, me.b, me.s0, me.c);
+    load<T, E>(p, first);          // deviations from the chunk's first value: no large sums to cancel
+    const int64_t by = me.rows * a.x.inner;
+    p += me.row * a.x.inner;
+#pragma unroll 4
+    for (int64_t s = me.s0 + me.row; s < me.s1; s += me.rows, p += by) {
+      float x[E];
+      load<T, E>(p, x);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float d = x[e] - first[e];
+        s1[e] += d;
+        s2[e] = fmaf(d, d, s2[e]);
+      }
+    }
+  }
+  join_rows<E>(s1, k.cols);
+  join_rows<E>(s2, k.cols);
+  if (me.on && (int)threadIdx.x < k.cols) {
+    const float n = (float)(me.s1 - me.s0);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const float m = s1[e] / n;
+      part[blockIdx.x * a.C + me.c + e] = first[e] + m;
+      part[((int64_t)gridDim.x + blockIdx.x) * a.C + me.c + e] = fmaxf(fmaf(-m, s1[e], s2[e]), 0.0f);
+    }
+  }
+}
+
+// Mean and rstd of a group, a block each, from its channels' chunks.
+__global__ void __launch_bounds__(kThreads) k_stats(Norm a, Chunks k, const float* part) {
+  const int64_t W = a.C / a.G, all = k.count * W;
   for (int64_t q = blockIdx.x; q < a.B * a.G; q += gridDim.x) {
     const int64_t b = q / a.G, c0 = q % a.G * W;
-    float s = 0.0f;
-    for (int64_t i = threadIdx.x; i < n; i += kThreads) s += value<T>(a.x, b, i / W, c0 + i % W);
-    const float mean = block_sum(s) / (float)max(n, (int64_t)1);
-    s = 0.0f;
-    for (int64_t i = threadIdx.x; i < n; i += kThreads) {
-      const float d = value<T>(a.x, b, i / W, c0 + i % W) - mean;
-      s = fmaf(d, d, s);
+    const float* m = part + b * k.count * a.C + c0;
+    const float* m2 = m + a.B * k.count * a.C;
+    auto size = [&](int64_t chunk) { return (float)(min(a.S, (chunk + 1) * k.rows) - chunk * k.rows); };
+    const float shift = m[0];
+    float s[2] = {0.0f, 0.0f};
+    for (int64_t i = threadIdx.x; i < all; i += kThreads) s[0] += size(i / W) * (m[i / W * a.C + i % W] - shift);
+    team_sum<true>(s, 0);
+    const float n = (float)a.S * (float)W, mean = shift + s[0] / n;
+    s[0] = s[1] = 0.0f;
+    for (int64_t i = threadIdx.x; i < all; i += kThreads) {
+      const float d = m[i / W * a.C + i % W] - mean;
+      s[0] += m2[i / W * a.C + i % W];
+      s[1] = fmaf(size(i / W) * d, d, s[1]);
     }
-    const float rstd = 1.0f / sqrtf(block_sum(s) / (float)max(n, (int64_t)1) + a.eps);
-    for (int64_t i = threadIdx.x; i < n; i += kThreads) {
-      const int64_t j = i / W, c = c0 + i % W;
-      const float xh = (value<T>(a.x, b, j, c) - mean) * rstd;
-      from_float(act_value(a.act, fmaf(a.gamma ? a.gamma[c] : 1.0f, xh, a.beta ? a.beta[c] : 0.0f)),
-                 *at<T>(a.y, b, j, c));
-    }
+    team_sum<true>(s, 0);
     if (threadIdx.x == 0) {
       a.mean[q] = mean;
-      a.rstd[q] = rstd;
+      a.rstd[q] = 1.0f / sqrtf((s[0] + s[1]) / n + a.eps);
     }
   }
 }
 
-template <typename T>
-__device__ __forceinline__ void slope_at(const Norm& a, int64_t b, int64_t j, int64_t c, float mean, float rstd,
-                                         float& dz, float& xh) {
-  xh = (value<T>(a.x, b, j, c) - mean) * rstd;
-  dz = value<T>(a.dy, b, j, c) *
-       act_slope(a.act, fmaf(a.gamma ? a.gamma[c] : 1.0f, xh, a.beta ? a.beta[c] : 0.0f));
+template <int E>
+struct Weights {
+  float gamma[E], beta[E], mean[E], rstd[E];
+  __device__ Weights(const Norm& a, int64_t b, int64_t c) {
+    load_weights<E>(a.gamma, c, 1.0f, gamma);
+    load_weights<E>(a.beta, c, 0.0f, beta);
+    const int64_t W = a.C / a.G;
+    int64_t g = c / W, left = (g + 1) * W - c;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      if (left-- == 0) ++g, left = W - 1;
+      mean[e] = a.mean[b * a.G + g];
+      rstd[e] = a.rstd[b * a.G + g];
+    }
+  }
+};
+
+template <typename T, int E>
+__global__ void __launch_bounds__(kThreads) k_apply(Norm a, Chunks k) {
+  const Place<E> me(a, k);
+  if (!me.on) return;
+  const Weights<E> w(a, me.b, me.c);
+  const T* p = at<T>(a.x, me.b, me.s0 + me.row, me.c);
+  T* o = at<T>(a.y, me.b, me.s0 + me.row, me.c);
+  const int64_t by = me.rows * a.x.inner, oy = me.rows * a.y.inner;
+#pragma unroll 4
+  for (int64_t s = me.s0 + me.row; s < me.s1; s += me.rows, p += by, o += oy) {
+    float x[E];
+    load<T, E>(p, x);
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = fmaf(w.gamma[e], (x[e] - w.mean[e]) * w.rstd[e], w.beta[e]);
+    activate<T, E>(a.act, x);
+    store<T, E>(o, x);
+  }
 }
 
-template <typename T>
-__global__ void k_norm_dx(Norm a) {
-  const int64_t W = a.C / a.G, n = a.S * W;
-  for (int64_t q = blockIdx.x; q < a.B * a.G; q += gridDim.x) {
+// Sums of dz and dz xh of each chunk's channels: part[2][B * count][C].
+template <typename T, int E>
+__global__ void __launch_bounds__(kThreads) k_part_back(Norm a, Chunks k, float* part) {
+  const Place<E> me(a, k);
+  float db[E] = {}, dg[E] = {};
+  if (me.on) {
+    const Weights<E> w(a, me.b, me.c);
+    const T* p = at<T>(a.x, me.b, me.s0 + me.row, me.c);
+    const T* y = at<T>(a.dy, me.b, me.s0 + me.row, me.c);
+    const int64_t by = me.rows * a.x.inner, yy = me.rows * a.dy.inner;
+#pragma unroll 4
+    for (int64_t s = me.s0 + me.row; s < me.s1; s += me.rows, p += by, y += yy) {
+      float xh[E], dz[E], u[E];
+      load<T, E>(p, xh);
+      load<T, E>(y, dz);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        xh[e] = (xh[e] - w.mean[e]) * w.rstd[e];
+        u[e] = fmaf(w.gamma[e], xh[e], w.beta[e]);
+      }
+      slope<T, E>(a.act, u, dz);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        db[e] += dz[e];
+        dg[e] = fmaf(dz[e], xh[e], dg[e]);
+      }
+    }
+  }
+  join_rows<E>(db, k.cols);
+  join_rows<E>(dg, k.cols);
+  if (me.on && (int)threadIdx.x < k.cols) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      part[blockIdx.x * a.C + me.c + e] = db[e];
+      part[((int64_t)gridDim.x + blockIdx.x) * a.C + me.c + e] = dg[e];
+    }
+  }
+}
+
+// avg(w) and avg(w xh) of a group, a block each: avg[2][B * G].  The blocks after those sum dbeta and dgamma.
+__global__ void __launch_bounds__(kThreads) k_stats_back(Norm a, Chunks k, const float* part, float* avg, int64_t groups) {
+  const int64_t rows = a.B * k.count;
+  if (blockIdx.x >= groups) {
+    const int64_t c = (blockIdx.x - groups) * 32 + threadIdx.x % 32;
+    const float b = column_sum(part, rows, a.C, c), g = column_sum(part + rows * a.C, rows, a.C, c);
+    if (threadIdx.x < 32 && c < a.C) {
+      if (a.dbeta) a.dbeta[c] = b;
+      if (a.dgamma) a.dgamma[c] = g;
+    }
+    return;
+  }
+  const int64_t W = a.C / a.G, all = k.count * W;
+  for (int64_t q = blockIdx.x; q < a.B * a.G; q += groups) {
     const int64_t b = q / a.G, c0 = q % a.G * W;
-    const float mean = a.mean[q], rstd = a.rstd[q];
-    float s1 = 0.0f, s2 = 0.0f;
-    for (int64_t i = threadIdx.x; i < n; i += kThreads) {
-      const int64_t c = c0 + i % W;
-      float dz, xh;
-      slope_at<T>(a, b, i / W, c, mean, rstd, dz, xh);
-      const float w = (a.gamma ? a.gamma[c] : 1.0f) * dz;
-      s1 += w;
-      s2 = fmaf(w, xh, s2);
+    const float* db = part + b * k.count * a.C + c0;
+    const float* dg = db + rows * a.C;
+    float s[2] = {0.0f, 0.0f};
+    for (int64_t i = threadIdx.x; i < all; i += kThreads) {
+      const float g = a.gamma ? a.gamma[c0 + i % W] : 1.0f;
+      s[0] = fmaf(g, db[i / W * a.C + i % W], s[0]);
+      s[1] = fmaf(g, dg[i / W * a.C + i % W], s[1]);
     }
-    s1 = block_sum(s1) / (float)n;
-    s2 = block_sum(s2) / (float)n;
-    for (int64_t i = threadIdx.x; i < n; i += kThreads) {
-      const int64_t j = i / W, c = c0 + i % W;
-      float dz, xh;
-      slope_at<T>(a, b, j, c, mean, rstd, dz, xh);
-      from_float(rstd * ((a.gamma ? a.gamma[c] : 1.0f) * dz - s1 - xh * s2), *at<T>(a.dx, b, j, c));
+    team_sum<true>(s, 0);
+    if (threadIdx.x == 0) {
+      const float inv = 1.0f / ((float)a.S * (float)W);
+      avg[q] = s[0] * inv;
+      avg[a.B * a.G + q] = s[1] * inv;
     }
   }
 }
 
-// One channel a block.
-template <typename T>
-__global__ void k_norm_dparam(Norm a) {
-  const int64_t c = blockIdx.x, g = c / (a.C / a.G), n = a.B * a.S;
-  float s1 = 0.0f, s2 = 0.0f;
-  for (int64_t i = threadIdx.x; i < n; i += kThreads) {
-    const int64_t b = i / a.S;
-    float dz, xh;
-    slope_at<T>(a, b, i % a.S, c, a.mean[b * a.G + g], a.rstd[b * a.G + g], dz, xh);
-    s1 += dz;
-    s2 = fmaf(dz, xh, s2);
+template <typename T, int E>
+__global__ void __launch_bounds__(kThreads) k_apply_back(Norm a, Chunks k, const float* avg) {
+  const Place<E> me(a, k);
+  if (!me.on) return;
+  const Weights<E> w(a, me.b, me.c);
+  float m1[E], m2[E];
+  const int64_t W = a.C / a.G;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    m1[e] = avg[me.b * a.G + (me.c + e) / W];
+    m2[e] = avg[(a.B + me.b) * a.G + (me.c + e) / W];
   }
-  s1 = block_sum(s1);
-  s2 = block_sum(s2);
-  if (threadIdx.x == 0) {
-    if (a.dbeta) a.dbeta[c] = s1;
-    if (a.dgamma) a.dgamma[c] = s2;
+  const T* p = at<T>(a.x, me.b, me.s0 + me.row, me.c);
+  const T* y = at<T>(a.dy, me.b, me.s0 + me.row, me.c);
+  T* o = at<T>(a.dx, me.b, me.s0 + me.row, me.c);
+  const int64_t by = me.rows * a.x.inner, yy = me.rows * a.dy.inner, oy = me.rows * a.dx.inner;
+#pragma unroll 4
+  for (int64_t s = me.s0 + me.row; s < me.s1; s += me.rows, p += by, y += yy, o += oy) {
+    float xh[E], dz[E], u[E];
+    load<T, E>(p, xh);
+    load<T, E>(y, dz);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      xh[e] = (xh[e] - w.mean[e]) * w.rstd[e];
+      u[e] = fmaf(w.gamma[e], xh[e], w.beta[e]);
+    }
+    slope<T, E>(a.act, u, dz);
+#pragma unroll
+    for (int e = 0; e < E; ++e) dz[e] = w.rstd[e] * (w.gamma[e] * dz[e] - m1[e] - xh[e] * m2[e]);
+    store<T, E>(o, dz);
   }
 }
 
-template <typename T>
-cudaError_t launch(const Norm& a, bool back, cudaStream_t s) {
-  const int64_t q = a.B * a.G;
-  const unsigned blocks = (unsigned)(q < (1 << 30) ? q : (1 << 30));
+// No positions: the mean is 0, the variance too.
+__global__ void k_empty(Norm a) {
+  const int64_t i = blockIdx.x * (int64_t)kThreads + threadIdx.x;
+  if (i < a.B * a.G) {
+    a.mean[i] = 0.0f;
+    a.rstd[i] = 1.0f / sqrtf(a.eps);
+  }
+}
+
+// ------------------------------------------------------------------ plans
+struct Plan {
+  bool team;
+  int e, slots;
+  bool block;
+  Teams t;
+  dim3 grid;
+  Chunks k;
+  int64_t stats;        // blocks that join groups
+  size_t bytes;
+};
+
+int pow2_at_least(int64_t n) {
+  int p = 1;
+  while (p < n) p *= 2;
+  return p;
+}
+
+// Sizes and strides alone: the same for the workspace and the call.
+Plan make_plan(const net_norm* p, bool back) {
+  Plan q = {};
+  const int size = type_size(p->dtype), sms = sm_count();
+  const int64_t W = p->C / p->G;
+  const net_rows* rows[2][2] = {{&p->x, &p->y}, {&p->x, &p->dy}};
+  auto fits = [&](int e) {
+    bool ok = true;
+    for (const net_rows* r : rows[back])
+      ok = ok && (p->B <= 1 || r->outer % e == 0) && (p->S <= 1 || r->inner % e == 0) &&
+           reinterpret_cast<uintptr_t>(r->data) % ((size_t)size * e) == 0;
+    if (back)
+      ok = ok && (p->B <= 1 || p->dx.outer % e == 0) && (p->S <= 1 || p->dx.inner % e == 0) &&
+           reinterpret_cast<uintptr_t>(p->dx.data) % ((size_t)size * e) == 0;
+    return ok;
+  };
+  const int widest = 16 / size;
+  // teams: pieces within a group
+  q.e = widest;
+  while (q.e > 1 && (W % q.e || !fits(q.e))) q.e = q.e > 2 ? 2 : 1;
+  const int64_t pieces = W / q.e * (p->S < (1 << 20) ? p->S : 1 << 20);
+  const int most = 4;
+  q.team = pieces <= (int64_t)kThreads * most && p->G <= 65535 * (kThreads / 32);
+  if (q.team) {
+    // two pieces a lane until a warp is full, then four, then blocks
+    q.block = pieces > 32 * most;
+    const int lanes = q.block ? kThreads : std::min(32, pow2_at_least((pieces + 1) / 2));
+    q.slots = std::max(1, pow2_at_least((pieces + lanes - 1) / lanes));
+    const int teams = kThreads / lanes;
+    const int groups = (int)std::min<int64_t>(p->G, teams), per = teams / groups;
+    q.t = {lanes, (int)pieces, (int)(W / q.e), groups, per};
+    const int64_t gy = (p->G + groups - 1) / groups, gx = (p->B + per - 1) / per;
+    // enough blocks for every SM's share, and few partial sums
+    const int64_t want = std::max<int64_t>(1, (int64_t)sms * (back ? 4 : 8) / gy);
+    q.grid = dim3((unsigned)std::min(gx, want), (unsigned)gy);
+    if (back && (p->dgamma || p->dbeta)) q.bytes = sizeof(float) * 2 * q.grid.x * (size_t)p->C;
+    return q;
+  }
+  q.e = p->C % widest == 0 && fits(widest) ? widest : 1;
+  const int64_t cols = (p->C + q.e - 1) / q.e;
+  q.k.cols = std::min(32, pow2_at_least(cols));
+  const int64_t across = (cols + q.k.cols - 1) / q.k.cols;
+  const int side = kThreads / q.k.cols;
+  int64_t want = std::max<int64_t>(1, (int64_t)sms * 8 / std::max<int64_t>(1, across * p->B));
+  want = std::min(want, std::max<int64_t>(1, p->S / (side * 4)));
+  int64_t per = (p->S + want - 1) / want;
+  per = std::min<int64_t>(std::max<int64_t>(per, 1), 1 << 20);
+  q.k.rows = (int)per;
+  q.k.count = (p->S + per - 1) / per;
+  q.grid = dim3((unsigned)(p->B * q.k.count), (unsigned)across);
+  q.stats = std::min<int64_t>(p->B * p->G, 1 << 20);
+  q.bytes = sizeof(float) * 2 * ((size_t)p->B * q.k.count * p->C + (back ? (size_t)p->B * p->G : 0));
+  return q;
+}
+
+template <typename T, int E, int SLOTS, bool BLOCK>
+cudaError_t launch_team(const Norm& a, const Plan& q, bool back, float* ws, cudaStream_t s) {
   if (!back) {
-    if (q) k_norm<T><<<blocks, kThreads, 0, s>>>(a);
-  } else {
-    if (q && a.S) k_norm_dx<T><<<blocks, kThreads, 0, s>>>(a);
-    if (a.dgamma || a.dbeta) k_norm_dparam<T><<<(unsigned)a.C, kThreads, 0, s>>>(a);
+    k_team<T, E, SLOTS, BLOCK><<<q.grid, kThreads, 0, s>>>(a, q.t);
+    return cudaGetLastError();
   }
+  const bool weights = a.dgamma || a.dbeta;
+  const int smem = weights ? 2 * kThreads * SLOTS * E * (int)sizeof(float) : 0;
+  const auto kern = k_team_back<T, E, SLOTS, BLOCK>;
+  if (smem > 48 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+  }
+  kern<<<q.grid, kThreads, smem, s>>>(a, q.t, weights ? ws : nullptr);
+  cudaError_t e = cudaGetLastError();
+  if (e == cudaSuccess && weights) {
+    k_weights<<<(unsigned)((a.C + 31) / 32), kThreads, 0, s>>>(a, ws, q.grid.x);
+    e = cudaGetLastError();
+  }
+  return e;
+}
+
+template <typename T, int E>
+cudaError_t launch_teams(const Norm& a, const Plan& q, bool back, float* ws, cudaStream_t s) {
+  if (q.block) {
+    if (q.slots == 1) return launch_team<T, E, 1, true>(a, q, back, ws, s);
+    if (q.slots == 2) return launch_team<T, E, 2, true>(a, q, back, ws, s);
+    return launch_team<T, E, 4, true>(a, q, back, ws, s);
+  }
+  if (q.slots == 1) return launch_team<T, E, 1, false>(a, q, back, ws, s);
+  if (q.slots == 2) return launch_team<T, E, 2, false>(a, q, back, ws, s);
+  return launch_team<T, E, 4, false>(a, q, back, ws, s);
+}
+
+template <typename T, int E>
+cudaError_t launch_chunks(const Norm& a, const Plan& q, bool back, float* ws, cudaStream_t s) {
+  if (!back) {
+    k_part<T, E><<<q.grid, kThreads, 0, s>>>(a, q.k, ws);
+    k_stats<<<(unsigned)q.stats, kThreads, 0, s>>>(a, q.k, ws);
+    k_apply<T, E><<<q.grid, kThreads, 0, s>>>(a, q.k);
+    return cudaGetLastError();
+  }
+  float* const avg = ws + 2 * a.B * q.k.count * a.C;
+  const int64_t columns = a.dgamma || a.dbeta ? (a.C + 31) / 32 : 0;
+  k_part_back<T, E><<<q.grid, kThreads, 0, s>>>(a, q.k, ws);
+  k_stats_back<<<(unsigned)(q.stats + columns), kThreads, 0, s>>>(a, q.k, ws, avg, q.stats);
+  k_apply_back<T, E><<<q.grid, kThreads, 0, s>>>(a, q.k, avg);
   return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t launch(const Norm& a, const Plan& q, bool back, void* ws, cudaStream_t s) {
+  constexpr int kWide = 16 / sizeof(T);
+  float* const w = static_cast<float*>(ws);
+  if (a.B == 0 || a.S == 0) {
+    if (!back && a.B) k_empty<<<(unsigned)((a.B * a.G + kThreads - 1) / kThreads), kThreads, 0, s>>>(a);
+    if (back && (a.dgamma || a.dbeta)) k_weights<<<(unsigned)((a.C + 31) / 32), kThreads, 0, s>>>(a, nullptr, 0);
+    return cudaGetLastError();
+  }
+  if (!q.team) return q.e > 1 ? launch_chunks<T, kWide>(a, q, back, w, s) : launch_chunks<T, 1>(a, q, back, w, s);
+  if (q.e == kWide) return launch_teams<T, kWide>(a, q, back, w, s);
+  if (q.e == 2) return launch_teams<T, 2>(a, q, back, w, s);
+  return launch_teams<T, 1>(a, q, back, w, s);
 }
 
 int check(const net_norm* p, bool back) {
@@ -166,9 +736,8 @@ int check(const net_norm* p, bool back) {
   if (p->B < 0 || p->S < 0 || p->C < 0) return fail(AUV_ERR_INVALID, "negative size");
   if (p->G < 1 || p->C % p->G) return fail(AUV_ERR_INVALID, "G < 1, or C not a multiple of G");
   if (!back && !(p->eps >= 0.0f && p->eps < INFINITY)) return fail(AUV_ERR_INVALID, "eps negative or not finite");
-  const int64_t most = (int64_t)1 << 50;
-  if (p->C > (1 << 24) || p->G > (1 << 24) || p->B > most || p->S > most || (p->B && p->S > most / p->B))
-    return fail(AUV_ERR_UNSUPPORTED, "C or G past 2^24, or B * S past 2^50");
+  if (p->C > (1 << 20) || p->B > INT32_MAX / 2 || p->S > INT32_MAX || p->B * p->G > INT32_MAX)
+    return fail(AUV_ERR_UNSUPPORTED, "C past 2^20, B past 2^30, or S or B * G past 2^31");
   return AUV_OK;
 }
 
@@ -188,7 +757,8 @@ int run(const net_norm* p, bool back, void* stream) {
   if ((p->gamma && (rc = need(p->gamma, "gamma", 4))) || (p->beta && (rc = need(p->beta, "beta", 4)))) return rc;
   if (back && ((p->dgamma && (rc = need(p->dgamma, "dgamma", 4))) || (p->dbeta && (rc = need(p->dbeta, "dbeta", 4)))))
     return rc;
-  const size_t ws = net_group_norm_workspace_bytes(p, back);
+  const Plan q = make_plan(p, back);
+  const size_t ws = p->B && p->S ? q.bytes : 0;
   if (ws) {
     if (p->workspace_bytes < ws)
       return fail(AUV_ERR_SIZE, "workspace of %zu bytes, %zu needed", p->workspace_bytes, ws);
@@ -197,9 +767,9 @@ int run(const net_norm* p, bool back, void* stream) {
   const Norm a = {p->B, p->S, p->C, p->G, p->x, p->y, p->dy, p->dx, p->gamma, p->beta, p->mean, p->rstd,
                   p->dgamma, p->dbeta, p->eps, p->act};
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = p->dtype == NET_FP32   ? launch<float>(a, back, s)
-                        : p->dtype == NET_BF16 ? launch<__nv_bfloat16>(a, back, s)
-                                               : launch<__half>(a, back, s);
+  const cudaError_t e = p->dtype == NET_FP32   ? launch<float>(a, q, back, p->workspace, s)
+                        : p->dtype == NET_BF16 ? launch<__nv_bfloat16>(a, q, back, p->workspace, s)
+                                               : launch<__half>(a, q, back, p->workspace, s);
   return e == cudaSuccess ? AUV_OK : cuda_fail(e, back ? "net_group_norm_backward" : "net_group_norm");
 }
 
@@ -210,9 +780,9 @@ int run(const net_norm* p, bool back, void* stream) {
 extern "C" {
 
 size_t net_group_norm_workspace_bytes(const net_norm* a, int backward) {
-  (void)a;
-  (void)backward;
-  return 0;
+  using namespace auv::net;
+  if (!a || check(a, backward) || !a->B || !a->S || !a->C) return 0;
+  return make_plan(a, backward).bytes;
 }
 
 int net_group_norm(const net_norm* a, void* stream) { return auv::net::run(a, false, stream); }
