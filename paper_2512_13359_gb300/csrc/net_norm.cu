@@ -28,6 +28,73 @@ struct Norm {
   uint32_t act;
 };
 
+// Pairs of fp32 operations in one instruction, where there are pairs.
+template <int E>
+__device__ __forceinline__ void mul(float (&x)[E], const float (&y)[E]) {
+  if constexpr (E == 1) {
+    x[0] *= y[0];
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; e += 2) {
+      const float2 r = __fmul2_rn(make_float2(x[e], x[e + 1]), make_float2(y[e], y[e + 1]));
+      x[e] = r.x, x[e + 1] = r.y;
+    }
+  }
+}
+template <int E>
+__device__ __forceinline__ void fma(const float (&x)[E], const float (&y)[E], const float (&z)[E], float (&o)[E]) {
+  if constexpr (E == 1) {
+    o[0] = fmaf(x[0], y[0], z[0]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; e += 2) {
+      const float2 r = __ffma2_rn(make_float2(x[e], x[e + 1]), make_float2(y[e], y[e + 1]), make_float2(z[e], z[e + 1]));
+      o[e] = r.x, o[e + 1] = r.y;
+    }
+  }
+}
+template <int E>
+__device__ __forceinline__ void add(float (&x)[E], const float (&y)[E]) {
+  if constexpr (E == 1) {
+    x[0] += y[0];
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; e += 2) {
+      const float2 r = __fadd2_rn(make_float2(x[e], x[e + 1]), make_float2(y[e], y[e + 1]));
+      x[e] = r.x, x[e + 1] = r.y;
+    }
+  }
+}
+// The sum of x's values, halves together.
+template <int E>
+__device__ __forceinline__ float total(const float (&x)[E]) {
+  if constexpr (E == 1) {
+    return x[0];
+  } else {
+    float h[E / 2];
+#pragma unroll
+    for (int e = 0; e < E / 2; ++e) h[e] = x[e];
+    float g[E / 2];
+#pragma unroll
+    for (int e = 0; e < E / 2; ++e) g[e] = x[E / 2 + e];
+    add<E / 2>(h, g);
+    return total<E / 2>(h);
+  }
+}
+template <int E>
+__device__ __forceinline__ void fill(float (&x)[E], float v) {
+#pragma unroll
+  for (int e = 0; e < E; ++e) x[e] = v;
+}
+
+// sigmoid alone: four instructions.  Where its exponential overflows it is 0.
+__device__ __forceinline__ float sigmoid(float u) {
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(u * -1.44269504088896341f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+  return r;
+}
+
 // tanh: the difference of the gates is exact to 2^-22, which is enough ahead of a 16-bit store.
 template <typename T>
 __device__ __forceinline__ float tanh_of(float u) {
@@ -45,14 +112,10 @@ template <typename T, int E>
 __device__ __forceinline__ void activate(uint32_t act, float (&u)[E]) {
   if (act == NET_ACT_RELU) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) u[e] = u[e] <= 0.0f ? 0.0f : u[e];
+    for (int e = 0; e < E; ++e) asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(u[e]) : "f"(u[e]));
   } else if (act == NET_ACT_SILU) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      float s, r;
-      gates(u[e], s, r);
-      u[e] *= s;
-    }
+    for (int e = 0; e < E; ++e) u[e] *= sigmoid(u[e]);
   } else if (act == NET_ACT_TANH) {
 #pragma unroll
     for (int e = 0; e < E; ++e) u[e] = tanh_of<T>(u[e]);
@@ -66,18 +129,21 @@ __device__ __forceinline__ void slope(uint32_t act, const float (&u)[E], float (
 #pragma unroll
     for (int e = 0; e < E; ++e) dy[e] = u[e] > 0.0f ? dy[e] : 0.0f;
   } else if (act == NET_ACT_SILU) {
+    float v[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      float s, r;
-      gates(u[e], s, r);
-      dy[e] *= s * fmaf(u[e], r, 1.0f);
+    for (int e = 0; e < E; ++e) {      // s (1 + u (1 - s))
+      const float s = sigmoid(u[e]);
+      v[e] = fmaf(fmaf(-u[e], s, u[e]), s, s);
     }
+    mul<E>(dy, v);
   } else if (act == NET_ACT_TANH) {
+    float v[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const float t = tanh_of<T>(u[e]);
-      dy[e] *= fmaf(-t, t, 1.0f);
+      v[e] = fmaf(-t, t, 1.0f);
     }
+    mul<E>(dy, v);
   }
 }
 
@@ -86,50 +152,74 @@ __device__ __forceinline__ T* at(const net_rows& r, int64_t i, int64_t j, int64_
   return reinterpret_cast<T*>(r.data) + i * r.outer + j * r.inner + k;
 }
 
+// E weights from channel c on (a multiple of E), or what stands for none.
 template <int E>
 __device__ __forceinline__ void load_weights(const float* w, int64_t c, float none, float (&x)[E]) {
+  fill<E>(x, none);
+  if (!w) return;
+  if (E >= 4 && reinterpret_cast<uintptr_t>(w + c) % 16 == 0) {
 #pragma unroll
-  for (int e = 0; e < E; ++e) x[e] = w ? __ldg(w + c + e) : none;
+    for (int e = 0; e + 3 < E; e += 4) {
+      const float4 v = __ldg(reinterpret_cast<const float4*>(w + c + e));
+      x[e] = v.x, x[e + 1] = v.y, x[e + 2] = v.z, x[e + 3] = v.w;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = __ldg(w + c + e);
+  }
 }
 
 // ------------------------------------------------------------------ teams
 constexpr int kThreads = 256;
+constexpr int kMostLanes = 512;      // of a team that is a block
 
-// How teams cover a call: a group is `pieces` pieces of E channels, `wide` of them a position; a team has `lanes` lanes
-// (a power of two up to 32, or all of a block); a block has `groups` x `rows` teams, for that many adjacent groups of
-// as many instances, and goes on by gridDim.x * rows instances.
+// How teams cover a call: a group is `pieces` pieces of E channels, `wide` of them a position; a team has `lanes` lanes,
+// a power of two: up to 32, or more, which are then a whole block.  A block has `groups` x `rows` teams, for that many
+// adjacent groups of as many instances, and goes on by gridDim.x * rows instances.
 struct Teams {
   int lanes, pieces, wide, groups, rows;
 };
 
-// The sum over a team, in all its lanes.
-template <bool BLOCK>
-__device__ __forceinline__ void team_sum(float (&x)[2], int lanes) {
-  if constexpr (!BLOCK) {
+// How a team is made: LANES = 32 a whole warp, kAny some lanes of one, kBlock a block.
+constexpr int kAny = 0, kBlock = -1;
+
+// The sums over a team, in all its lanes.
+template <int LANES, int N>
+__device__ __forceinline__ void team_sum(float (&x)[N], int lanes) {
+  if constexpr (LANES == kAny) {
     for (int o = lanes / 2; o; o /= 2) {
-      x[0] += __shfl_xor_sync(0xffffffffu, x[0], o);
-      x[1] += __shfl_xor_sync(0xffffffffu, x[1], o);
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] += __shfl_xor_sync(0xffffffffu, x[i], o);
     }
   } else {
-    __shared__ float2 part[kThreads / 32];
 #pragma unroll
     for (int o = 16; o; o /= 2) {
-      x[0] += __shfl_xor_sync(0xffffffffu, x[0], o);
-      x[1] += __shfl_xor_sync(0xffffffffu, x[1], o);
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] += __shfl_xor_sync(0xffffffffu, x[i], o);
+    }
+  }
+  if constexpr (LANES == kBlock) {
+    __shared__ float part[kMostLanes / 32][N];
+    const int warps = blockDim.x / 32;
+    __syncthreads();
+    if (threadIdx.x % 32 == 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) part[threadIdx.x / 32][i] = x[i];
     }
     __syncthreads();
-    if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = make_float2(x[0], x[1]);
-    __syncthreads();
-    x[0] = x[1] = 0.0f;
+    fill<N>(x, 0.0f);
+    for (int w = 0; w < warps; ++w) {
 #pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) x[0] += part[w].x, x[1] += part[w].y;
+      for (int i = 0; i < N; ++i) x[i] += part[w][i];
+    }
   }
 }
-template <bool BLOCK>
-__device__ __forceinline__ float team_sum(float x, int lanes) {
-  float v[2] = {x, 0.0f};
-  team_sum<BLOCK>(v, lanes);
-  return v[0];
+
+// 1 / sqrt(v): the approximation and a step of Newton's method.
+__device__ __forceinline__ float inverse_root(float v) {
+  const float r = rsqrtf(v);
+  const float q = fmaf(-v * r, r, 1.0f);
+  return v > 1e-30f ? fmaf(0.5f * r, q, r) : r;
 }
 
 // What a lane of a team works on.
@@ -139,7 +229,7 @@ struct Lane {
   int64_t g, c0;           // group, its first channel
   bool on;                 // whether the team has a group
   bool has[SLOTS];         // pieces that the lane has
-  int64_t s[SLOTS];        // their position
+  int s[SLOTS];            // their position
   int c[SLOTS];            // and first channel in the group
   __device__ Lane(const Norm& a, const Teams& t) {
     lane = threadIdx.x % t.lanes;
@@ -152,137 +242,171 @@ struct Lane {
     for (int j = 0; j < SLOTS; ++j) {
       const int i = j * t.lanes + lane;
       has[j] = on && i < t.pieces;
-      s[j] = i / t.wide;
-      c[j] = i % t.wide * E;
+      s[j] = has[j] ? i / t.wide : 0;
+      c[j] = has[j] ? i - s[j] * t.wide : 0;
+      c[j] *= E;
     }
+  }
+  // Where piece j of an array is, for instance 0.
+  template <typename T>
+  __device__ T* piece(const net_rows& r, int j) const {
+    return at<T>(r, 0, s[j], c0 + c[j]);
   }
 };
 
-template <typename T, int E, int SLOTS, bool BLOCK>
-__global__ void __launch_bounds__(kThreads) k_team(Norm a, Teams t) {
+template <typename T, int E, int SLOTS, int LANES>
+__global__ void __launch_bounds__(LANES == kBlock ? kMostLanes : kThreads) k_team(Norm a, Teams t) {
   const Lane<E, SLOTS> me(a, t);
-  const float n = (float)max((int64_t)1, a.S * (a.C / a.G));
+  const float inv = 1.0f / (float)(a.S * (a.C / a.G));
   float gamma[SLOTS][E], beta[SLOTS][E];
+  const T* px[SLOTS];
+  T* py[SLOTS];
+  const int first = blockIdx.x * t.rows + me.row, step = gridDim.x * t.rows, B = (int)a.B;
+  const int64_t by = step * a.x.outer, yy = step * a.y.outer;
 #pragma unroll
   for (int j = 0; j < SLOTS; ++j) {
     load_weights<E>(me.has[j] ? a.gamma : nullptr, me.c0 + me.c[j], 1.0f, gamma[j]);
     load_weights<E>(me.has[j] ? a.beta : nullptr, me.c0 + me.c[j], 0.0f, beta[j]);
+    px[j] = me.template piece<const T>(a.x, j) + first * a.x.outer;
+    py[j] = me.template piece<T>(a.y, j) + first * a.y.outer;
   }
-  Raw<T, E> next[SLOTS];
-  auto fetch = [&](int64_t b) {
-#pragma unroll
-    for (int j = 0; j < SLOTS; ++j)
-      if (me.has[j] && b < a.B)
-        next[j] = *reinterpret_cast<const Raw<T, E>*>(at<T>(a.x, b, me.s[j], me.c0 + me.c[j]));
-  };
-  const int64_t step = (int64_t)gridDim.x * t.rows;
-  fetch(blockIdx.x * (int64_t)t.rows + me.row);
-  for (int64_t b0 = blockIdx.x * (int64_t)t.rows; b0 < a.B; b0 += step) {
-    const int64_t b = b0 + me.row;
-    float x[SLOTS][E];
-#pragma unroll
-    for (int j = 0; j < SLOTS; ++j) unpack<T, E>(next[j], x[j]);
-    fetch(b + step);
-    float sum = 0.0f;
-#pragma unroll
-    for (int j = 0; j < SLOTS; ++j)
-#pragma unroll
-      for (int e = 0; e < E; ++e) sum += me.has[j] ? x[j][e] : 0.0f;
-    const float mean = team_sum<BLOCK>(sum, t.lanes) / n;
-    sum = 0.0f;
-#pragma unroll
-    for (int j = 0; j < SLOTS; ++j)
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        x[j][e] -= mean;
-        sum += me.has[j] ? x[j][e] * x[j][e] : 0.0f;
-      }
-    const float rstd = 1.0f / sqrtf(team_sum<BLOCK>(sum, t.lanes) / n + a.eps);
-    if (me.on && me.lane == 0 && b < a.B) {
-      a.mean[b * a.G + me.g] = mean;
-      a.rstd[b * a.G + me.g] = rstd;
-    }
+  int64_t at_stats = first * a.G + me.g;
+  const bool writes = me.on && me.lane == 0;
+  Raw<T, E> next[SLOTS] = {};
+  auto fetch = [&](int b) {
 #pragma unroll
     for (int j = 0; j < SLOTS; ++j) {
+      if (me.has[j] && b < B) next[j] = *reinterpret_cast<const Raw<T, E>*>(px[j]);
+      px[j] += by;
+    }
+  };
+  fetch(first);
+  // all lanes go round as often, for the shuffles
+  int b = first;
+  for (int left = (B - (int)blockIdx.x * t.rows + step - 1) / step; left > 0; --left, b += step) {
+    float x[SLOTS][E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) x[j][e] = fmaf(gamma[j][e], x[j][e] * rstd, beta[j][e]);
+    for (int j = 0; j < SLOTS; ++j) unpack<T, E>(next[j], x[j]);    // 0 where the lane has none
+    fetch(b + step);
+    float part[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) part[e] = x[0][e];
+#pragma unroll
+    for (int j = 1; j < SLOTS; ++j) add<E>(part, x[j]);
+    float sum[1] = {total<E>(part)};
+    team_sum<LANES, 1>(sum, t.lanes);
+    const float mean = sum[0] * inv;
+    fill<E>(part, -mean);
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j) add<E>(x[j], part);
+    fill<E>(part, 0.0f);
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j)
+      if (me.has[j]) fma<E>(x[j], x[j], part, part);
+    sum[0] = total<E>(part);
+    team_sum<LANES, 1>(sum, t.lanes);
+    const float rstd = inverse_root(fmaf(sum[0], inv, a.eps));
+    if (writes && b < B) {
+      a.mean[at_stats] = mean;
+      a.rstd[at_stats] = rstd;
+    }
+    at_stats += step * a.G;
+    fill<E>(part, rstd);
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j) {
+      mul<E>(x[j], part);
+      fma<E>(gamma[j], x[j], beta[j], x[j]);
       activate<T, E>(a.act, x[j]);
-      if (me.has[j] && b < a.B) store<T, E>(at<T>(a.y, b, me.s[j], me.c0 + me.c[j]), x[j]);
+      if (me.has[j] && b < B) store<T, E>(py[j], x[j]);
+      py[j] += yy;
     }
   }
 }
 
-// partial: [2][gridDim.x][C], dbeta's and dgamma's sums by block (NULL: not wanted).
-template <typename T, int E, int SLOTS, bool BLOCK>
-__global__ void __launch_bounds__(kThreads) k_team_back(Norm a, Teams t, float* partial) {
+// partial: [2][gridDim.x][C], dbeta's and dgamma's sums by block (NULL: not wanted); of one block dbeta and dgamma.
+template <typename T, int E, int SLOTS, int LANES>
+__global__ void __launch_bounds__(LANES == kBlock ? kMostLanes : kThreads) k_team_back(Norm a, Teams t, float* partial) {
   extern __shared__ float sums[];          // [2][teams of a block][lanes * SLOTS * E]
   const Lane<E, SLOTS> me(a, t);
   const float inv = 1.0f / (float)(a.S * (a.C / a.G));
   float gamma[SLOTS][E], beta[SLOTS][E], db[SLOTS][E] = {}, dg[SLOTS][E] = {};
+  const T *px[SLOTS], *py[SLOTS];
+  T* pd[SLOTS];
+  const int first = blockIdx.x * t.rows + me.row, step = gridDim.x * t.rows, B = (int)a.B;
+  const int64_t by = step * a.x.outer, yy = step * a.dy.outer, dd = step * a.dx.outer;
 #pragma unroll
   for (int j = 0; j < SLOTS; ++j) {
     load_weights<E>(me.has[j] ? a.gamma : nullptr, me.c0 + me.c[j], 1.0f, gamma[j]);
     load_weights<E>(me.has[j] ? a.beta : nullptr, me.c0 + me.c[j], 0.0f, beta[j]);
+    px[j] = me.template piece<const T>(a.x, j) + first * a.x.outer;
+    py[j] = me.template piece<const T>(a.dy, j) + first * a.dy.outer;
+    pd[j] = me.template piece<T>(a.dx, j) + first * a.dx.outer;
   }
-  Raw<T, E> nx[SLOTS], ny[SLOTS];
+  int64_t at_stats = first * a.G + me.g;
+  Raw<T, E> nx[SLOTS] = {}, ny[SLOTS] = {};
   float nm = 0.0f, nr = 0.0f;
-  auto fetch = [&](int64_t b) {
+  auto fetch = [&](int b) {
 #pragma unroll
-    for (int j = 0; j < SLOTS; ++j)
-      if (me.has[j] && b < a.B) {
-        nx[j] = *reinterpret_cast<const Raw<T, E>*>(at<T>(a.x, b, me.s[j], me.c0 + me.c[j]));
-        ny[j] = *reinterpret_cast<const Raw<T, E>*>(at<T>(a.dy, b, me.s[j], me.c0 + me.c[j]));
+    for (int j = 0; j < SLOTS; ++j) {
+      if (me.has[j]) {
+        if (b < B) {
+          nx[j] = *reinterpret_cast<const Raw<T, E>*>(px[j]);
+          ny[j] = *reinterpret_cast<const Raw<T, E>*>(py[j]);
+        } else {
+          ny[j] = {};             // past the last instance: adds nothing
+        }
       }
-    if (me.on && b < a.B) nm = a.mean[b * a.G + me.g], nr = a.rstd[b * a.G + me.g];
+      px[j] += by;
+      py[j] += yy;
+    }
+    if (me.on && b < B) nm = a.mean[at_stats], nr = a.rstd[at_stats];
+    at_stats += step * a.G;
   };
-  const int64_t step = (int64_t)gridDim.x * t.rows;
-  fetch(blockIdx.x * (int64_t)t.rows + me.row);
-  for (int64_t b0 = blockIdx.x * (int64_t)t.rows; b0 < a.B; b0 += step) {
-    const int64_t b = b0 + me.row;
-    float xh[SLOTS][E], dz[SLOTS][E];
+  fetch(first);
+  int b = first;
+  for (int left = (B - (int)blockIdx.x * t.rows + step - 1) / step; left > 0; --left, b += step) {
+    float xh[SLOTS][E], dz[SLOTS][E], m[E], r[E];
 #pragma unroll
     for (int j = 0; j < SLOTS; ++j) {
       unpack<T, E>(nx[j], xh[j]);
       unpack<T, E>(ny[j], dz[j]);
     }
-    const float mean = nm, rstd = nr;
+    fill<E>(m, -nm);
+    fill<E>(r, nr);
     fetch(b + step);
-    const bool in = b < a.B;
-    float w[2] = {0.0f, 0.0f};
+    float p0[E] = {}, p1[E] = {};
 #pragma unroll
     for (int j = 0; j < SLOTS; ++j) {
       float u[E];
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        xh[j][e] = (xh[j][e] - mean) * rstd;
-        u[e] = fmaf(gamma[j][e], xh[j][e], beta[j][e]);
-      }
+      add<E>(xh[j], m);
+      mul<E>(xh[j], r);
+      fma<E>(gamma[j], xh[j], beta[j], u);
       slope<T, E>(a.act, u, dz[j]);
-      if (me.has[j] && in) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          db[j][e] += dz[j][e];
-          dg[j][e] = fmaf(dz[j][e], xh[j][e], dg[j][e]);
-          dz[j][e] *= gamma[j][e];
-          w[0] += dz[j][e];
-          w[1] = fmaf(dz[j][e], xh[j][e], w[1]);
-        }
+      if (me.has[j] && b < B) {
+        add<E>(db[j], dz[j]);
+        fma<E>(dz[j], xh[j], dg[j], dg[j]);
+        mul<E>(dz[j], gamma[j]);
+        add<E>(p0, dz[j]);
+        fma<E>(dz[j], xh[j], p1, p1);
       }
     }
-    team_sum<BLOCK>(w, t.lanes);
-    w[0] *= inv;
-    w[1] *= inv;
+    float w[2] = {total<E>(p0), total<E>(p1)};
+    team_sum<LANES, 2>(w, t.lanes);
+    // rstd (dz - avg(w) - xh avg(w xh))
+    fill<E>(p0, -w[0] * inv);
+    fill<E>(p1, -w[1] * inv);
 #pragma unroll
     for (int j = 0; j < SLOTS; ++j) {
-      float o[E];
-#pragma unroll
-      for (int e = 0; e < E; ++e) o[e] = rstd * (dz[j][e] - w[0] - xh[j][e] * w[1]);
-      if (me.has[j] && in) store<T, E>(at<T>(a.dx, b, me.s[j], me.c0 + me.c[j]), o);
+      add<E>(dz[j], p0);
+      fma<E>(xh[j], p1, dz[j], dz[j]);
+      mul<E>(dz[j], r);
+      if (me.has[j] && b < B) store<T, E>(pd[j], dz[j]);
+      pd[j] += dd;
     }
   }
   if (!partial) return;
   // Each channel's sums: over the lanes that had it (a position each) and the block's instances.
-  const int team = threadIdx.x / t.lanes, held = t.lanes * SLOTS * E, all = kThreads / t.lanes * held;
+  const int team = threadIdx.x / t.lanes, held = t.lanes * SLOTS * E, all = blockDim.x / t.lanes * held;
 #pragma unroll
   for (int j = 0; j < SLOTS; ++j)
 #pragma unroll
@@ -292,7 +416,7 @@ __global__ void __launch_bounds__(kThreads) k_team_back(Norm a, Teams t, float* 
     }
   __syncthreads();
   const int width = t.wide * E;
-  for (int i = threadIdx.x; i < t.groups * width; i += kThreads) {
+  for (int i = threadIdx.x; i < t.groups * width; i += blockDim.x) {
     const int64_t g = blockIdx.y * (int64_t)t.groups + i / width;
     if (g >= a.G) break;
     float b = 0.0f, w = 0.0f;
@@ -302,37 +426,40 @@ __global__ void __launch_bounds__(kThreads) k_team_back(Norm a, Teams t, float* 
         w += sums[all + (r * t.groups + i / width) * held + k];
       }
     const int64_t c = g * width + i % width;
-    partial[blockIdx.x * a.C + c] = b;
-    partial[((int64_t)gridDim.x + blockIdx.x) * a.C + c] = w;
+    if (gridDim.x == 1) {
+      if (a.dbeta) a.dbeta[c] = b;
+      if (a.dgamma) a.dgamma[c] = w;
+    } else {
+      partial[blockIdx.x * a.C + c] = b;
+      partial[((int64_t)gridDim.x + blockIdx.x) * a.C + c] = w;
+    }
   }
 }
 
-// The sum of column c of [rows][C], 32 columns a block, eight warps over the rows.
-__device__ __forceinline__ float column_sum(const float* p, int64_t rows, int64_t C, int64_t c) {
-  __shared__ float part[kThreads / 32][32];
-  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+// dbeta and dgamma from [2][rows][C]: 32 columns of one a block, its warps over the rows.
+constexpr int kJoinThreads = 1024;
+__device__ __forceinline__ void join_weights(const Norm& a, const float* partial, int64_t rows, int64_t block, int which) {
+  __shared__ float part[kJoinThreads / 32][32];
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, warps = blockDim.x / 32;
+  const int64_t c = block * 32 + lane;
   float s = 0.0f;
-  if (c < C) {
+  if (c < a.C) {
+    const float* p = partial + which * rows * a.C + c;
 #pragma unroll 8
-    for (int64_t r = warp; r < rows; r += kThreads / 32) s += p[r * C + c];
+    for (int64_t r = warp; r < rows; r += warps) s += p[r * a.C];
   }
-  __syncthreads();
   part[warp][lane] = s;
   __syncthreads();
-  s = 0.0f;
-#pragma unroll
-  for (int w = 0; w < kThreads / 32; ++w) s += part[w][lane];
-  return s;
+  if (warp == 0 && c < a.C) {
+    s = 0.0f;
+    for (int w = 0; w < warps; ++w) s += part[w][lane];
+    float* const out = which ? a.dgamma : a.dbeta;
+    if (out) out[c] = s;
+  }
 }
 
-// dbeta and dgamma from [2][rows][C].
-__global__ void __launch_bounds__(kThreads) k_weights(Norm a, const float* partial, int64_t rows) {
-  const int64_t c = blockIdx.x * (int64_t)32 + threadIdx.x % 32;
-  const float b = column_sum(partial, rows, a.C, c), g = column_sum(partial + rows * a.C, rows, a.C, c);
-  if (threadIdx.x < 32 && c < a.C) {
-    if (a.dbeta) a.dbeta[c] = b;
-    if (a.dgamma) a.dgamma[c] = g;
-  }
+__global__ void __launch_bounds__(kJoinThreads) k_weights(Norm a, const float* partial, int64_t rows) {
+  join_weights(a, partial, rows, blockIdx.x, blockIdx.y);
 }
 
 // ------------------------------------------------------------------ chunks
@@ -424,7 +551,7 @@ __global__ void __launch_bounds__(kThreads) k_stats(Norm a, Chunks k, const floa
     const float shift = m[0];
     float s[2] = {0.0f, 0.0f};
     for (int64_t i = threadIdx.x; i < all; i += kThreads) s[0] += size(i / W) * (m[i / W * a.C + i % W] - shift);
-    team_sum<true>(s, 0);
+    team_sum<kBlock, 2>(s, 0);
     const float n = (float)a.S * (float)W, mean = shift + s[0] / n;
     s[0] = s[1] = 0.0f;
     for (int64_t i = threadIdx.x; i < all; i += kThreads) {
@@ -432,7 +559,7 @@ __global__ void __launch_bounds__(kThreads) k_stats(Norm a, Chunks k, const floa
       s[0] += m2[i / W * a.C + i % W];
       s[1] = fmaf(size(i / W) * d, d, s[1]);
     }
-    team_sum<true>(s, 0);
+    team_sum<kBlock, 2>(s, 0);
     if (threadIdx.x == 0) {
       a.mean[q] = mean;
       a.rstd[q] = 1.0f / sqrtf((s[0] + s[1]) / n + a.eps);
@@ -519,12 +646,7 @@ __global__ void __launch_bounds__(kThreads) k_part_back(Norm a, Chunks k, float*
 __global__ void __launch_bounds__(kThreads) k_stats_back(Norm a, Chunks k, const float* part, float* avg, int64_t groups) {
   const int64_t rows = a.B * k.count;
   if (blockIdx.x >= groups) {
-    const int64_t c = (blockIdx.x - groups) * 32 + threadIdx.x % 32;
-    const float b = column_sum(part, rows, a.C, c), g = column_sum(part + rows * a.C, rows, a.C, c);
-    if (threadIdx.x < 32 && c < a.C) {
-      if (a.dbeta) a.dbeta[c] = b;
-      if (a.dgamma) a.dgamma[c] = g;
-    }
+    join_weights(a, part, rows, (blockIdx.x - groups) / 2, (int)((blockIdx.x - groups) % 2));
     return;
   }
   const int64_t W = a.C / a.G, all = k.count * W;
@@ -538,7 +660,7 @@ __global__ void __launch_bounds__(kThreads) k_stats_back(Norm a, Chunks k, const
       s[0] = fmaf(g, db[i / W * a.C + i % W], s[0]);
       s[1] = fmaf(g, dg[i / W * a.C + i % W], s[1]);
     }
-    team_sum<true>(s, 0);
+    team_sum<kBlock, 2>(s, 0);
     if (threadIdx.x == 0) {
       const float inv = 1.0f / ((float)a.S * (float)W);
       avg[q] = s[0] * inv;
@@ -592,7 +714,7 @@ __global__ void k_empty(Norm a) {
 // ------------------------------------------------------------------ plans
 struct Plan {
   bool team;
-  int e, slots;
+  int e, slots, threads;
   bool block;
   Teams t;
   dim3 grid;
@@ -628,19 +750,21 @@ Plan make_plan(const net_norm* p, bool back) {
   q.e = widest;
   while (q.e > 1 && (W % q.e || !fits(q.e))) q.e = q.e > 2 ? 2 : 1;
   const int64_t pieces = W / q.e * (p->S < (1 << 20) ? p->S : 1 << 20);
-  const int most = 4;
-  q.team = pieces <= (int64_t)kThreads * most && p->G <= 65535 * (kThreads / 32);
+  // Eight values a lane (four single ones): backward, six registers a value are weights, their sums and what comes next.
+  const int most = std::min(4, 8 / q.e);
+  q.team = pieces <= (int64_t)kMostLanes * most && p->G <= 65535;
   if (q.team) {
-    // two pieces a lane until a warp is full, then four, then blocks
     q.block = pieces > 32 * most;
-    const int lanes = q.block ? kThreads : std::min(32, pow2_at_least((pieces + 1) / 2));
+    int lanes = pow2_at_least((pieces + most - 1) / most);
+    lanes = std::min(lanes, q.block ? kMostLanes : 32);
     q.slots = std::max(1, pow2_at_least((pieces + lanes - 1) / lanes));
-    const int teams = kThreads / lanes;
+    q.threads = q.block ? lanes : kThreads;
+    const int teams = q.threads / lanes;
     const int groups = (int)std::min<int64_t>(p->G, teams), per = teams / groups;
     q.t = {lanes, (int)pieces, (int)(W / q.e), groups, per};
     const int64_t gy = (p->G + groups - 1) / groups, gx = (p->B + per - 1) / per;
-    // enough blocks for every SM's share, and few partial sums
-    const int64_t want = std::max<int64_t>(1, (int64_t)sms * (back ? 4 : 8) / gy);
+    // as many blocks as the SMs hold at a time, or so: each goes from instance to instance
+    const int64_t want = std::max<int64_t>(1, (int64_t)sms * (1024 / q.threads) / gy);
     q.grid = dim3((unsigned)std::min(gx, want), (unsigned)gy);
     if (back && (p->dgamma || p->dbeta)) q.bytes = sizeof(float) * 2 * q.grid.x * (size_t)p->C;
     return q;
@@ -662,38 +786,42 @@ Plan make_plan(const net_norm* p, bool back) {
   return q;
 }
 
-template <typename T, int E, int SLOTS, bool BLOCK>
+template <typename T, int E, int SLOTS, int LANES>
 cudaError_t launch_team(const Norm& a, const Plan& q, bool back, float* ws, cudaStream_t s) {
   if (!back) {
-    k_team<T, E, SLOTS, BLOCK><<<q.grid, kThreads, 0, s>>>(a, q.t);
+    k_team<T, E, SLOTS, LANES><<<q.grid, q.threads, 0, s>>>(a, q.t);
     return cudaGetLastError();
   }
   const bool weights = a.dgamma || a.dbeta;
-  const int smem = weights ? 2 * kThreads * SLOTS * E * (int)sizeof(float) : 0;
-  const auto kern = k_team_back<T, E, SLOTS, BLOCK>;
+  const int smem = weights ? 2 * q.threads * SLOTS * E * (int)sizeof(float) : 0;
+  const auto kern = k_team_back<T, E, SLOTS, LANES>;
   if (smem > 48 * 1024) {
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
   }
-  kern<<<q.grid, kThreads, smem, s>>>(a, q.t, weights ? ws : nullptr);
+  kern<<<q.grid, q.threads, smem, s>>>(a, q.t, weights ? ws : nullptr);
   cudaError_t e = cudaGetLastError();
-  if (e == cudaSuccess && weights) {
-    k_weights<<<(unsigned)((a.C + 31) / 32), kThreads, 0, s>>>(a, ws, q.grid.x);
+  if (e == cudaSuccess && weights && q.grid.x > 1) {
+    k_weights<<<dim3((unsigned)((a.C + 31) / 32), 2), kJoinThreads, 0, s>>>(a, ws, q.grid.x);
     e = cudaGetLastError();
   }
   return e;
 }
 
+template <typename T, int E, int SLOTS>
+cudaError_t launch_teams(const Norm& a, const Plan& q, bool back, float* ws, cudaStream_t s) {
+  if (q.block) return launch_team<T, E, SLOTS, kBlock>(a, q, back, ws, s);
+  if (q.t.lanes == 32) return launch_team<T, E, SLOTS, 32>(a, q, back, ws, s);
+  return launch_team<T, E, SLOTS, kAny>(a, q, back, ws, s);
+}
+
 template <typename T, int E>
 cudaError_t launch_teams(const Norm& a, const Plan& q, bool back, float* ws, cudaStream_t s) {
-  if (q.block) {
-    if (q.slots == 1) return launch_team<T, E, 1, true>(a, q, back, ws, s);
-    if (q.slots == 2) return launch_team<T, E, 2, true>(a, q, back, ws, s);
-    return launch_team<T, E, 4, true>(a, q, back, ws, s);
-  }
-  if (q.slots == 1) return launch_team<T, E, 1, false>(a, q, back, ws, s);
-  if (q.slots == 2) return launch_team<T, E, 2, false>(a, q, back, ws, s);
-  return launch_team<T, E, 4, false>(a, q, back, ws, s);
+  if constexpr (E <= 2)
+    if (q.slots == 4) return launch_teams<T, E, 4>(a, q, back, ws, s);
+  if constexpr (E <= 4)
+    if (q.slots == 2) return launch_teams<T, E, 2>(a, q, back, ws, s);
+  return launch_teams<T, E, 1>(a, q, back, ws, s);
 }
 
 template <typename T, int E>
@@ -705,7 +833,7 @@ cudaError_t launch_chunks(const Norm& a, const Plan& q, bool back, float* ws, cu
     return cudaGetLastError();
   }
   float* const avg = ws + 2 * a.B * q.k.count * a.C;
-  const int64_t columns = a.dgamma || a.dbeta ? (a.C + 31) / 32 : 0;
+  const int64_t columns = a.dgamma || a.dbeta ? (a.C + 31) / 32 * 2 : 0;
   k_part_back<T, E><<<q.grid, kThreads, 0, s>>>(a, q.k, ws);
   k_stats_back<<<(unsigned)(q.stats + columns), kThreads, 0, s>>>(a, q.k, ws, avg, q.stats);
   k_apply_back<T, E><<<q.grid, kThreads, 0, s>>>(a, q.k, avg);
@@ -718,7 +846,7 @@ cudaError_t launch(const Norm& a, const Plan& q, bool back, void* ws, cudaStream
   float* const w = static_cast<float*>(ws);
   if (a.B == 0 || a.S == 0) {
     if (!back && a.B) k_empty<<<(unsigned)((a.B * a.G + kThreads - 1) / kThreads), kThreads, 0, s>>>(a);
-    if (back && (a.dgamma || a.dbeta)) k_weights<<<(unsigned)((a.C + 31) / 32), kThreads, 0, s>>>(a, nullptr, 0);
+    if (back && (a.dgamma || a.dbeta)) k_weights<<<dim3((unsigned)((a.C + 31) / 32), 2), kJoinThreads, 0, s>>>(a, nullptr, 0);
     return cudaGetLastError();
   }
   if (!q.team) return q.e > 1 ? launch_chunks<T, kWide>(a, q, back, w, s) : launch_chunks<T, 1>(a, q, back, w, s);
