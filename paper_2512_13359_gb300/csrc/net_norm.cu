@@ -6,7 +6,9 @@
 //  k_team, k_team_back      groups of a few thousand values: a team of lanes (of a warp, or a whole block) keeps a group
 //                           in registers and goes from instance to instance.  A team's channels stay the same, so the
 //                           backward pass sums dgamma and dbeta in registers and joins them once at its end.
-//  k_part, k_stats, k_apply larger groups: sums by chunk and channel, joined, and the elements read once more.
+//  k_slab, k_slab_back      larger groups, as long as a cluster of blocks holds some adjacent ones of an instance in shared
+//                           memory, each block some positions: statistics are joined through distributed shared memory.
+//  k_part, k_stats, k_apply the rest: sums by chunk and channel, joined, and the elements read once more.
 //  (.._back)
 //
 // Variances are those of deviations: in registers from the mean, over chunks from each channel's first value, joined
@@ -462,6 +464,258 @@ __global__ void __launch_bounds__(kJoinThreads) k_weights(Norm a, const float* p
   join_weights(a, partial, rows, blockIdx.x, blockIdx.y);
 }
 
+// ------------------------------------------------------------------ slabs
+// A cluster holds S positions x `cols` pieces of E channels (whole groups of `wide` pieces, `groups` of them), each of
+// its blocks `rows` positions; `side` rows of threads, a thread a piece of each `side`-th position.
+struct Slab {
+  int cols, wide, groups, side, rows, ranks, tiles;
+};
+constexpr int kSlabGroups = 4;             // of a slab at most
+constexpr int kSlabRanks = 16;
+
+__device__ __forceinline__ uint32_t slab_rank() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void slab_arrive(int ranks) {
+  if (ranks > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+}
+// Stores v at this block's address p in the shared memory of every block of the cluster, all of which have started
+// (slab_arrive, a while ago), and waits for the others' stores.
+__device__ __forceinline__ void exchange(float2* p, float2 v, bool mine, int ranks) {
+  if (ranks > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+  if (mine) {
+    const uint32_t local = (uint32_t)__cvta_generic_to_shared(p);
+    for (int r = 0; r < ranks; ++r) {
+      uint32_t there;
+      asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(local), "r"(r));
+      asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(v.x), "f"(v.y) : "memory");
+    }
+  }
+  if (ranks > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  else __syncthreads();
+}
+
+template <typename T, int E>
+struct SlabThread {
+  int col, row, g, rank;       // piece, row of threads, group of the slab, block of the cluster
+  int64_t b, c, s0, s1;        // instance, first channel, the block's positions
+  bool on;
+  __device__ SlabThread(const Norm& a, const Slab& k) {
+    rank = (int)slab_rank();
+    const int64_t q = blockIdx.x / k.ranks;
+    b = q / k.tiles;
+    const int64_t tile = q - b * k.tiles;
+    row = threadIdx.x / k.cols;
+    col = threadIdx.x - row * k.cols;
+    g = col / k.wide;
+    c = (tile * k.cols + col) * E;
+    on = row < k.side && c < a.C;
+    s0 = min(a.S, (int64_t)rank * k.rows);
+    s1 = min(a.S, s0 + k.rows);
+  }
+  // Copies the thread's pieces of an array.
+  __device__ void fetch(const net_rows& r, uint4* to, const Slab& k) const {
+    if (!on) return;
+    const T* p = at<const T>(r, b, s0 + row, c);
+    const int64_t by = k.side * r.inner;
+    to += threadIdx.x;
+    for (int64_t s = s0 + row; s < s1; s += k.side, p += by, to += k.side * k.cols)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(p)
+                   : "memory");
+  }
+};
+
+// Sums x over the threads of each group of the slab (in order), to group[g].
+__device__ __forceinline__ void group_sums(float x, float* threads, float* group, const Slab& k) {
+  threads[threadIdx.x] = x;
+  __syncthreads();
+  const int lane = threadIdx.x % 32, n = k.side * k.wide;
+  for (int g = threadIdx.x / 32; g < k.groups; g += kThreads / 32) {
+    float s = 0.0f;
+    for (int i = lane; i < n; i += 32) s += threads[i / k.wide * k.cols + g * k.wide + i % k.wide];
+#pragma unroll
+    for (int o = 16; o; o /= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (lane == 0) group[g] = s;
+  }
+  __syncthreads();
+}
+
+template <typename T, int E>
+__global__ void __launch_bounds__(kThreads) k_slab(Norm a, Slab k) {
+  extern __shared__ uint4 data[];
+  __shared__ float threads[kThreads], group[kSlabGroups];
+  __shared__ float2 from[kSlabRanks][kSlabGroups];     // mean and squared deviations of each block's part
+  slab_arrive(k.ranks);
+  const SlabThread<T, E> me(a, k);
+  me.fetch(a.x, data, k);
+  float gamma[E], beta[E];
+  load_weights<E>(me.on ? a.gamma : nullptr, me.c, 1.0f, gamma);
+  load_weights<E>(me.on ? a.beta : nullptr, me.c, 0.0f, beta);
+  asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
+  const uint4* const mine = data + threadIdx.x;
+  const int n = me.on ? (int)max((int64_t)0, (me.s1 - me.s0 - me.row + k.side - 1) / k.side) : 0, by = k.side * k.cols;
+  const int W = k.wide * E;
+  float part[E] = {};
+#pragma unroll 4
+  for (int i = 0; i < n; ++i) {
+    float x[E];
+    unpack<T, E>(mine[i * by], x);
+    add<E>(part, x);
+  }
+  group_sums(total<E>(part), threads, group, k);
+  const float here = (float)((me.s1 - me.s0) * W), inv = here > 0.0f ? 1.0f / here : 0.0f;
+  const float mean0 = group[me.g < k.groups ? me.g : 0] * inv;
+  float shift[E];
+  fill<E>(shift, -mean0);
+  fill<E>(part, 0.0f);
+#pragma unroll 4
+  for (int i = 0; i < n; ++i) {
+    float x[E];
+    unpack<T, E>(mine[i * by], x);
+    add<E>(x, shift);
+    fma<E>(x, x, part, part);
+  }
+  __syncthreads();           // all have read the sums
+  const int mg = threadIdx.x;
+  const float mean_of = mg < k.groups ? group[mg] * inv : 0.0f;
+  __syncthreads();
+  group_sums(total<E>(part), threads, group, k);
+  exchange(&from[me.rank][mg], make_float2(mean_of, mg < k.groups ? group[mg] : 0.0f), mg < k.groups, k.ranks);
+  // joined by the distances of the parts' means from the first's, which is a block with positions
+  const int g = me.g < k.groups ? me.g : 0;
+  const float all = 1.0f / (float)(a.S * W), m0 = from[0][g].x;
+  float mean = 0.0f, sq = 0.0f;
+  for (int r = 0; r < k.ranks; ++r) {
+    const float w = (float)(min(a.S, (int64_t)(r + 1) * k.rows) - min(a.S, (int64_t)r * k.rows)) * (float)W;
+    mean = fmaf(w, from[r][g].x - m0, mean);
+  }
+  mean = fmaf(mean, all, m0);
+  for (int r = 0; r < k.ranks; ++r) {
+    const float w = (float)(min(a.S, (int64_t)(r + 1) * k.rows) - min(a.S, (int64_t)r * k.rows)) * (float)W;
+    const float d = from[r][g].x - mean;
+    sq += w > 0.0f ? fmaf(w * d, d, from[r][g].y) : 0.0f;
+  }
+  const float rstd = inverse_root(fmaf(sq, all, a.eps));
+  if (!me.on) return;
+  if (me.rank == 0 && me.row == 0 && me.col % k.wide == 0) {
+    a.mean[me.b * a.G + me.c / W] = mean;
+    a.rstd[me.b * a.G + me.c / W] = rstd;
+  }
+  float scale[E];
+  fill<E>(shift, -mean);
+  fill<E>(scale, rstd);
+  T* o = at<T>(a.y, me.b, me.s0 + me.row, me.c);
+  const int64_t oy = k.side * a.y.inner;
+#pragma unroll 2
+  for (int i = 0; i < n; ++i, o += oy) {
+    float x[E];
+    unpack<T, E>(mine[i * by], x);
+    add<E>(x, shift);
+    mul<E>(x, scale);
+    fma<E>(gamma, x, beta, x);
+    activate<T, E>(a.act, x);
+    store<T, E>(o, x);
+  }
+}
+
+// partial: [2][B * ranks][C], or NULL.
+template <typename T, int E>
+__global__ void __launch_bounds__(kThreads) k_slab_back(Norm a, Slab k, float* partial) {
+  extern __shared__ uint4 data[];
+  __shared__ float sums[2][E][kThreads];
+  __shared__ float2 from[kSlabRanks][kSlabGroups];
+  slab_arrive(k.ranks);
+  const SlabThread<T, E> me(a, k);
+  const int held = k.rows * k.cols;
+  me.fetch(a.x, data, k);
+  me.fetch(a.dy, data + held, k);
+  float gamma[E], beta[E], shift[E], scale[E];
+  load_weights<E>(me.on ? a.gamma : nullptr, me.c, 1.0f, gamma);
+  load_weights<E>(me.on ? a.beta : nullptr, me.c, 0.0f, beta);
+  const int W = k.wide * E;
+  const int64_t stats = me.b * a.G + me.c / W;
+  const float rstd = me.on ? a.rstd[stats] : 0.0f;
+  fill<E>(shift, me.on ? -a.mean[stats] : 0.0f);
+  fill<E>(scale, rstd);
+  asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
+  const uint4 *const mx = data + threadIdx.x, *const my = mx + held;
+  const int n = me.on ? (int)max((int64_t)0, (me.s1 - me.s0 - me.row + k.side - 1) / k.side) : 0, by = k.side * k.cols;
+  float db[E] = {}, dg[E] = {};
+  auto piece = [&](int i, float (&xh)[E], float (&dz)[E]) {
+    float u[E];
+    unpack<T, E>(mx[i * by], xh);
+    unpack<T, E>(my[i * by], dz);
+    add<E>(xh, shift);
+    mul<E>(xh, scale);
+    fma<E>(gamma, xh, beta, u);
+    slope<T, E>(a.act, u, dz);
+  };
+#pragma unroll 2
+  for (int i = 0; i < n; ++i) {
+    float xh[E], dz[E];
+    piece(i, xh, dz);
+    add<E>(db, dz);
+    fma<E>(dz, xh, dg, dg);
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) sums[0][e][threadIdx.x] = db[e], sums[1][e][threadIdx.x] = dg[e];
+  __syncthreads();
+  // each channel's sums over the rows of threads: to the first row's places, and out
+  const int64_t row = (int64_t)(blockIdx.x / k.ranks / k.tiles) * k.ranks + me.rank;
+  const int64_t c0 = (blockIdx.x / k.ranks % k.tiles) * (int64_t)k.cols * E, rows = a.B * k.ranks;
+  for (int i = threadIdx.x; i < 2 * E * k.cols; i += kThreads) {
+    const int col = i % k.cols, e = i / k.cols % E, which = i / (k.cols * E);
+    float v = 0.0f;
+    for (int r = 0; r < k.side; ++r) v += sums[which][e][r * k.cols + col];
+    sums[which][e][col] = v;
+    const int64_t c = c0 + col * E + e;
+    if (partial && c < a.C) partial[(which * rows + row) * a.C + c] = v;
+  }
+  __syncthreads();
+  // and each group's, weighted
+  const int lane = threadIdx.x % 32;
+  for (int g = threadIdx.x / 32; g < k.groups; g += kThreads / 32) {
+    float2 v = make_float2(0.0f, 0.0f);
+    for (int i = lane; i < W; i += 32) {
+      const int col = g * k.wide + i / E, e = i % E;
+      const int64_t c = c0 + col * E + e;
+      const float w = c < a.C ? (a.gamma ? __ldg(a.gamma + c) : 1.0f) : 0.0f;
+      v.x = fmaf(w, sums[0][e][col], v.x);
+      v.y = fmaf(w, sums[1][e][col], v.y);
+    }
+#pragma unroll
+    for (int o = 16; o; o /= 2) {
+      v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
+      v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+    }
+    if (lane == 0) from[me.rank][g] = v;
+  }
+  __syncthreads();
+  const int mg = threadIdx.x;
+  const float2 own = mg < k.groups ? from[me.rank][mg] : make_float2(0.0f, 0.0f);
+  exchange(&from[me.rank][mg], own, mg < k.groups, k.ranks);
+  if (!me.on) return;
+  float2 w = make_float2(0.0f, 0.0f);
+  for (int r = 0; r < k.ranks; ++r) w.x += from[r][me.g].x, w.y += from[r][me.g].y;
+  const float all = 1.0f / (float)(a.S * W);
+  float m1[E], m2[E];
+  fill<E>(m1, -w.x * all);
+  fill<E>(m2, -w.y * all);
+  T* o = at<T>(a.dx, me.b, me.s0 + me.row, me.c);
+  const int64_t oy = k.side * a.dx.inner;
+#pragma unroll 2
+  for (int i = 0; i < n; ++i, o += oy) {
+    float xh[E], dz[E];
+    piece(i, xh, dz);
+    fma<E>(dz, gamma, m1, dz);
+    fma<E>(xh, m2, dz, dz);
+    mul<E>(dz, scale);
+    store<T, E>(o, dz);
+  }
+}
+
 // ------------------------------------------------------------------ chunks
 // Larger groups: a block takes `rows` positions of `cols` pieces of E channels, kThreads / cols rows side by side.
 struct Chunks {
@@ -718,6 +972,9 @@ struct Plan {
   bool block;
   Teams t;
   dim3 grid;
+  bool slab;
+  Slab sl;
+  int smem;
   Chunks k;
   int64_t stats;        // blocks that join groups
   size_t bytes;
@@ -768,6 +1025,34 @@ Plan make_plan(const net_norm* p, bool back) {
     q.grid = dim3((unsigned)std::min(gx, want), (unsigned)gy);
     if (back && (p->dgamma || p->dbeta)) q.bytes = sizeof(float) * 2 * q.grid.x * (size_t)p->C;
     return q;
+  }
+  // slabs: whole groups side by side, 64 bytes of a row at least, in as few blocks as leave three an SM (72 KB each,
+  // backward 16 of them for sums; then two, and clusters of 16).  Aligned pieces within a group alone.
+  if (W % widest == 0 && fits(widest) && W / widest <= kThreads) {
+    const int wide = (int)(W / widest);
+    const int groups = (int)std::min<int64_t>(p->G, std::max(1, kSlabGroups / wide));
+    const int cols = wide * groups, side = kThreads / cols, arrays = back ? 2 : 1;
+    const int64_t row = (int64_t)cols * 16 * arrays;
+    auto ranks_for = [&](int64_t bytes) {
+      const int64_t rows = std::max<int64_t>(1, bytes / row);
+      return (p->S + rows - 1) / rows;
+    };
+    int64_t ranks = ranks_for(back ? 56 * 1024 : 72 * 1024);
+    if (ranks > 8) ranks = ranks_for(back ? 92 * 1024 : 108 * 1024);
+    if (ranks <= kSlabRanks) {
+      const int64_t tiles = (p->G + groups - 1) / groups;
+      int r = pow2_at_least(ranks);
+      // more blocks where there are few
+      while (r < 8 && p->B * tiles * r < sms && p->S >= 2 * r * side) r *= 2;
+      const int64_t rows = (p->S + r - 1) / r;
+      q.slab = p->B * tiles * r <= INT32_MAX;
+      q.e = widest;
+      q.sl = {cols, wide, groups, side, (int)rows, r, (int)tiles};
+      q.grid = dim3((unsigned)(p->B * tiles * r));
+      q.smem = (int)(rows * row);
+      if (back && (p->dgamma || p->dbeta)) q.bytes = sizeof(float) * 2 * (size_t)(p->B * r) * p->C;
+      if (q.slab) return q;
+    }
   }
   q.e = p->C % widest == 0 && fits(widest) ? widest : 1;
   const int64_t cols = (p->C + q.e - 1) / q.e;
@@ -824,6 +1109,33 @@ cudaError_t launch_teams(const Norm& a, const Plan& q, bool back, float* ws, cud
   return launch_teams<T, E, 1>(a, q, back, ws, s);
 }
 
+template <typename T>
+cudaError_t launch_slab(const Norm& a, const Plan& q, bool back, float* ws, cudaStream_t s) {
+  constexpr int E = 16 / sizeof(T);
+  const bool weights = back && (a.dgamma || a.dbeta);
+  const void* const kern = back ? (const void*)k_slab_back<T, E> : (const void*)k_slab<T, E>;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, q.smem);
+  if (e == cudaSuccess && q.sl.ranks > 8)
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = q.grid;
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = q.smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = q.sl.ranks;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (back) e = cudaLaunchKernelEx(&cfg, k_slab_back<T, E>, a, q.sl, weights ? ws : (float*)nullptr);
+  else e = cudaLaunchKernelEx(&cfg, k_slab<T, E>, a, q.sl);
+  if (e == cudaSuccess && weights)
+    k_weights<<<dim3((unsigned)((a.C + 31) / 32), 2), kJoinThreads, 0, s>>>(a, ws, a.B * q.sl.ranks);
+  return e == cudaSuccess ? cudaGetLastError() : e;
+}
+
 template <typename T, int E>
 cudaError_t launch_chunks(const Norm& a, const Plan& q, bool back, float* ws, cudaStream_t s) {
   if (!back) {
@@ -849,6 +1161,7 @@ cudaError_t launch(const Norm& a, const Plan& q, bool back, void* ws, cudaStream
     if (back && (a.dgamma || a.dbeta)) k_weights<<<dim3((unsigned)((a.C + 31) / 32), 2), kJoinThreads, 0, s>>>(a, nullptr, 0);
     return cudaGetLastError();
   }
+  if (q.slab) return launch_slab<T>(a, q, back, w, s);
   if (!q.team) return q.e > 1 ? launch_chunks<T, kWide>(a, q, back, w, s) : launch_chunks<T, 1>(a, q, back, w, s);
   if (q.e == kWide) return launch_teams<T, kWide>(a, q, back, w, s);
   if (q.e == 2) return launch_teams<T, 2>(a, q, back, w, s);

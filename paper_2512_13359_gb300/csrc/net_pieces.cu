@@ -135,6 +135,7 @@ __global__ void __launch_bounds__(Shape<T, E, CH, BACK>::kThreads) k_pieces(Scan
   const bool flags = a.done || a.done_prev;
   fetch(0, first);
   if (flags && one_env) fetch_flags(first + run * R);
+  if (ranks > 1) cluster_sync();       // all blocks have started: their shared memory may be written
   const float* const h0 = a.h0 ? a.h0 + m : nullptr;
   // The state before the cluster's piece is the first warp's, a lane a channel.
   float carry = 0.0f;
