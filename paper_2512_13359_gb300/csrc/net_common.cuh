@@ -8,6 +8,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
+#include <type_traits>
 
 #include "auvenv.h"
 #include "auvnet.h"
@@ -31,20 +32,52 @@ __device__ __forceinline__ void from_float(float x, float& r) { r = x; }
 __device__ __forceinline__ void from_float(float x, __nv_bfloat16& r) { r = __float2bfloat16_rn(x); }
 __device__ __forceinline__ void from_float(float x, __half& r) { r = __float2half_rn(x); }
 
+// Pairs of 16-bit values by words: a shift and a mask, or one conversion, for two.
+template <typename T>
+__device__ __forceinline__ void unpack_pair(uint32_t w, float& lo, float& hi) {
+  if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+    lo = __uint_as_float(w << 16);
+    hi = __uint_as_float(w & 0xffff0000u);
+  } else {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+    lo = f.x, hi = f.y;
+  }
+}
+template <typename T>
+__device__ __forceinline__ uint32_t pack_pair(float lo, float hi) {
+  if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+  } else {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+  }
+}
+
 template <typename T, int E>
 __device__ __forceinline__ void unpack(const Raw<T, E>& w, float (&x)[E]) {
-  union { Raw<T, E> w; T t[E]; } u;
-  u.w = w;
+  union { Raw<T, E> w; T t[E]; uint32_t u[(sizeof(T) * E + 3) / 4]; } v;
+  v.w = w;
+  if constexpr (sizeof(T) == 4 || E == 1) {
 #pragma unroll
-  for (int e = 0; e < E; ++e) x[e] = to_float(u.t[e]);
+    for (int e = 0; e < E; ++e) x[e] = to_float(v.t[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; e += 2) unpack_pair<T>(v.u[e / 2], x[e], x[e + 1]);
+  }
 }
 
 template <typename T, int E>
 __device__ __forceinline__ Raw<T, E> pack(const float (&x)[E]) {
-  union U { Raw<T, E> w; T t[E]; __device__ U() {} } u;
+  union U { Raw<T, E> w; T t[E]; uint32_t u[(sizeof(T) * E + 3) / 4]; __device__ U() {} } v;
+  if constexpr (sizeof(T) == 4 || E == 1) {
 #pragma unroll
-  for (int e = 0; e < E; ++e) from_float(x[e], u.t[e]);
-  return u.w;
+    for (int e = 0; e < E; ++e) from_float(x[e], v.t[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; e += 2) v.u[e / 2] = pack_pair<T>(x[e], x[e + 1]);
+  }
+  return v.w;
 }
 
 template <typename T, int E>
@@ -69,6 +102,19 @@ __device__ __forceinline__ void gates(float x, float& a, float& b) {
   a = x >= 0.0f ? r : q;
   b = x >= 0.0f ? q : r;
 }
+
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* dst, const void* src) {
+  const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(src) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(d), "l"(src), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+
+// Two-byte pieces (odd widths or strides of 16-bit types) have no asynchronous copy.
+template <typename T, int E> constexpr bool kAsync = sizeof(T) * E >= 4;
 
 // ---------------------------------------------------------------- host side
 int fail(int code, const char* fmt, ...);

@@ -256,40 +256,88 @@ struct Lane {
   }
 };
 
+// What a lane reads of its next instances: N arrays' pieces of 16 bytes on their way to slots of its own in shared memory
+// (65,536 x 256 bf16 forward: 12.8 us, 15.8 with registers), narrower ones in registers one instance ahead (65,536 x 250:
+// 17.5 us, 21.1 with slots).
+constexpr int kStages = 3;
+template <typename T, int E, int SLOTS, int N>
+struct Ahead {
+  using W = Raw<T, E>;
+  static constexpr bool kRing = sizeof(W) == 16;
+  static constexpr int kDepth = kRing ? kStages : 1;
+  const T* p[N][SLOTS];
+  int64_t by[N];
+  W* slots;              // (stage, i, j) at ((stage * N + i) * SLOTS + j) * blockDim.x
+  W next[kRing ? 1 : N][kRing ? 1 : SLOTS];
+  int stage;
+  __device__ void begin(uint4* smem) { slots = reinterpret_cast<W*>(smem) + threadIdx.x, stage = 0; }
+  static __host__ __device__ constexpr int bytes(int threads) {
+    return kRing ? kStages * N * SLOTS * threads * (int)sizeof(W) : 0;
+  }
+  // The instance `kDepth` on from the one just taken (or the first few).
+  __device__ void fetch(const bool (&has)[SLOTS], bool there, int to) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int j = 0; j < SLOTS; ++j) {
+        if (has[j] && there) {
+          if constexpr (kRing) copy_async<sizeof(W)>(slots + ((to * N + i) * SLOTS + j) * blockDim.x, p[i][j]);
+          else next[i][j] = *reinterpret_cast<const W*>(p[i][j]);
+        }
+        p[i][j] += by[i];
+      }
+    if constexpr (kRing) copy_commit();
+  }
+  __device__ void wait() {
+    if constexpr (kRing) copy_wait<kStages - 1>();
+  }
+  __device__ void take(int i, int j, bool has, float (&x)[E]) {
+    W w = {};
+    if constexpr (kRing) {
+      if (has) w = slots[((stage * N + i) * SLOTS + j) * blockDim.x];
+    } else {
+      if (has) w = next[i][j];
+    }
+    unpack<T, E>(w, x);
+  }
+  __device__ void step() { stage = stage + 1 == kDepth ? 0 : stage + 1; }
+};
+
 template <typename T, int E, int SLOTS, int LANES>
 __global__ void __launch_bounds__(LANES == kBlock ? kMostLanes : kThreads) k_team(Norm a, Teams t) {
   const Lane<E, SLOTS> me(a, t);
   const float inv = 1.0f / (float)(a.S * (a.C / a.G));
+  extern __shared__ uint4 smem[];
   float gamma[SLOTS][E], beta[SLOTS][E];
-  const T* px[SLOTS];
+  Ahead<T, E, SLOTS, 1> in;
   T* py[SLOTS];
   const int first = blockIdx.x * t.rows + me.row, step = gridDim.x * t.rows, B = (int)a.B;
-  const int64_t by = step * a.x.outer, yy = step * a.y.outer;
+  const int64_t yy = step * a.y.outer;
+  in.begin(smem);
+  in.by[0] = step * a.x.outer;
+#pragma unroll
+  for (int j = 0; j < SLOTS; ++j) {
+    in.p[0][j] = me.template piece<const T>(a.x, j) + first * a.x.outer;
+    py[j] = me.template piece<T>(a.y, j) + first * a.y.outer;
+  }
+#pragma unroll
+  for (int k = 0; k < in.kDepth; ++k) in.fetch(me.has, first + k * (int64_t)step < B, k);
 #pragma unroll
   for (int j = 0; j < SLOTS; ++j) {
     load_weights<E>(me.has[j] ? a.gamma : nullptr, me.c0 + me.c[j], 1.0f, gamma[j]);
     load_weights<E>(me.has[j] ? a.beta : nullptr, me.c0 + me.c[j], 0.0f, beta[j]);
-    px[j] = me.template piece<const T>(a.x, j) + first * a.x.outer;
-    py[j] = me.template piece<T>(a.y, j) + first * a.y.outer;
   }
   int64_t at_stats = first * a.G + me.g;
   const bool writes = me.on && me.lane == 0;
-  Raw<T, E> next[SLOTS] = {};
-  auto fetch = [&](int b) {
-#pragma unroll
-    for (int j = 0; j < SLOTS; ++j) {
-      if (me.has[j] && b < B) next[j] = *reinterpret_cast<const Raw<T, E>*>(px[j]);
-      px[j] += by;
-    }
-  };
-  fetch(first);
   // all lanes go round as often, for the shuffles
   int b = first;
   for (int left = (B - (int)blockIdx.x * t.rows + step - 1) / step; left > 0; --left, b += step) {
     float x[SLOTS][E];
+    in.wait();
 #pragma unroll
-    for (int j = 0; j < SLOTS; ++j) unpack<T, E>(next[j], x[j]);    // 0 where the lane has none
-    fetch(b + step);
+    for (int j = 0; j < SLOTS; ++j) in.take(0, j, me.has[j], x[j]);    // 0 where the lane has none
+    in.fetch(me.has, b + in.kDepth * (int64_t)step < B, in.stage);
+    in.step();
     float part[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) part[e] = x[0][e];
@@ -328,54 +376,50 @@ __global__ void __launch_bounds__(LANES == kBlock ? kMostLanes : kThreads) k_tea
 // partial: [2][gridDim.x][C], dbeta's and dgamma's sums by block (NULL: not wanted); of one block dbeta and dgamma.
 template <typename T, int E, int SLOTS, int LANES>
 __global__ void __launch_bounds__(LANES == kBlock ? kMostLanes : kThreads) k_team_back(Norm a, Teams t, float* partial) {
-  extern __shared__ float sums[];          // [2][teams of a block][lanes * SLOTS * E]
+  extern __shared__ uint4 smem[];
   const Lane<E, SLOTS> me(a, t);
   const float inv = 1.0f / (float)(a.S * (a.C / a.G));
   float gamma[SLOTS][E], beta[SLOTS][E], db[SLOTS][E] = {}, dg[SLOTS][E] = {};
-  const T *px[SLOTS], *py[SLOTS];
+  Ahead<T, E, SLOTS, 2> in;
   T* pd[SLOTS];
   const int first = blockIdx.x * t.rows + me.row, step = gridDim.x * t.rows, B = (int)a.B;
-  const int64_t by = step * a.x.outer, yy = step * a.dy.outer, dd = step * a.dx.outer;
+  const int64_t dd = step * a.dx.outer;
+  in.begin(smem);
+  in.by[0] = step * a.x.outer, in.by[1] = step * a.dy.outer;
+#pragma unroll
+  for (int j = 0; j < SLOTS; ++j) {
+    in.p[0][j] = me.template piece<const T>(a.x, j) + first * a.x.outer;
+    in.p[1][j] = me.template piece<const T>(a.dy, j) + first * a.dy.outer;
+    pd[j] = me.template piece<T>(a.dx, j) + first * a.dx.outer;
+  }
+#pragma unroll
+  for (int k = 0; k < in.kDepth; ++k) in.fetch(me.has, first + k * (int64_t)step < B, k);
+  int64_t at_stats = first * a.G + me.g;
+  float nm = 0.0f, nr = 0.0f;
+  auto fetch_stats = [&](int b) {
+    if (me.on && b < B) nm = a.mean[at_stats], nr = a.rstd[at_stats];
+    at_stats += step * a.G;
+  };
+  fetch_stats(first);
 #pragma unroll
   for (int j = 0; j < SLOTS; ++j) {
     load_weights<E>(me.has[j] ? a.gamma : nullptr, me.c0 + me.c[j], 1.0f, gamma[j]);
     load_weights<E>(me.has[j] ? a.beta : nullptr, me.c0 + me.c[j], 0.0f, beta[j]);
-    px[j] = me.template piece<const T>(a.x, j) + first * a.x.outer;
-    py[j] = me.template piece<const T>(a.dy, j) + first * a.dy.outer;
-    pd[j] = me.template piece<T>(a.dx, j) + first * a.dx.outer;
   }
-  int64_t at_stats = first * a.G + me.g;
-  Raw<T, E> nx[SLOTS] = {}, ny[SLOTS] = {};
-  float nm = 0.0f, nr = 0.0f;
-  auto fetch = [&](int b) {
-#pragma unroll
-    for (int j = 0; j < SLOTS; ++j) {
-      if (me.has[j]) {
-        if (b < B) {
-          nx[j] = *reinterpret_cast<const Raw<T, E>*>(px[j]);
-          ny[j] = *reinterpret_cast<const Raw<T, E>*>(py[j]);
-        } else {
-          ny[j] = {};             // past the last instance: adds nothing
-        }
-      }
-      px[j] += by;
-      py[j] += yy;
-    }
-    if (me.on && b < B) nm = a.mean[at_stats], nr = a.rstd[at_stats];
-    at_stats += step * a.G;
-  };
-  fetch(first);
   int b = first;
   for (int left = (B - (int)blockIdx.x * t.rows + step - 1) / step; left > 0; --left, b += step) {
     float xh[SLOTS][E], dz[SLOTS][E], m[E], r[E];
+    in.wait();
 #pragma unroll
     for (int j = 0; j < SLOTS; ++j) {
-      unpack<T, E>(nx[j], xh[j]);
-      unpack<T, E>(ny[j], dz[j]);
+      in.take(0, j, me.has[j], xh[j]);
+      in.take(1, j, me.has[j], dz[j]);
     }
+    in.fetch(me.has, b + in.kDepth * (int64_t)step < B, in.stage);
+    in.step();
     fill<E>(m, -nm);
     fill<E>(r, nr);
-    fetch(b + step);
+    fetch_stats(b + step);
     float p0[E] = {}, p1[E] = {};
 #pragma unroll
     for (int j = 0; j < SLOTS; ++j) {
@@ -407,6 +451,9 @@ __global__ void __launch_bounds__(LANES == kBlock ? kMostLanes : kThreads) k_tea
     }
   }
   if (!partial) return;
+  if constexpr (in.kRing) copy_wait<0>();
+  __syncthreads();
+  float* const sums = reinterpret_cast<float*>(smem);     // [2][teams of a block][lanes * SLOTS * E]
   // Each channel's sums: over the lanes that had it (a position each) and the block's instances.
   const int team = threadIdx.x / t.lanes, held = t.lanes * SLOTS * E, all = blockDim.x / t.lanes * held;
 #pragma unroll
@@ -500,41 +547,40 @@ __device__ __forceinline__ void exchange(float2* p, float2 v, bool mine, int ran
 template <typename T, int E>
 struct SlabThread {
   int col, row, g, rank;       // piece, row of threads, group of the slab, block of the cluster
-  int64_t b, c, s0, s1;        // instance, first channel, the block's positions
+  int b, tile, c, s0, s1, n;   // instance, slab of it, first channel, the block's positions, the thread's pieces
   bool on;
   __device__ SlabThread(const Norm& a, const Slab& k) {
     rank = (int)slab_rank();
-    const int64_t q = blockIdx.x / k.ranks;
-    b = q / k.tiles;
-    const int64_t tile = q - b * k.tiles;
-    row = threadIdx.x / k.cols;
+    const unsigned q = blockIdx.x / (unsigned)k.ranks, i = q / (unsigned)k.tiles;
+    b = (int)i;
+    tile = (int)(q - i * k.tiles);
+    row = threadIdx.x / (unsigned)k.cols;
     col = threadIdx.x - row * k.cols;
-    g = col / k.wide;
+    g = col / (unsigned)k.wide;
     c = (tile * k.cols + col) * E;
-    on = row < k.side && c < a.C;
-    s0 = min(a.S, (int64_t)rank * k.rows);
-    s1 = min(a.S, s0 + k.rows);
+    on = row < k.side && c < (int)a.C;
+    s0 = (int)min(a.S, (int64_t)rank * k.rows);
+    s1 = (int)min(a.S, (int64_t)s0 + k.rows);
+    n = on && s0 + row < s1 ? (int)((unsigned)(s1 - s0 - row + k.side - 1) / (unsigned)k.side) : 0;
   }
   // Copies the thread's pieces of an array.
   __device__ void fetch(const net_rows& r, uint4* to, const Slab& k) const {
-    if (!on) return;
     const T* p = at<const T>(r, b, s0 + row, c);
     const int64_t by = k.side * r.inner;
     to += threadIdx.x;
-    for (int64_t s = s0 + row; s < s1; s += k.side, p += by, to += k.side * k.cols)
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(p)
-                   : "memory");
+#pragma unroll 4
+    for (int i = 0; i < n; ++i, p += by, to += k.side * k.cols) copy_async<16>(to, p);
   }
 };
 
-// Sums x over the threads of each group of the slab (in order), to group[g].
+// The sums of x over the threads of each group of the slab (in order), to group[g].
 __device__ __forceinline__ void group_sums(float x, float* threads, float* group, const Slab& k) {
   threads[threadIdx.x] = x;
   __syncthreads();
   const int lane = threadIdx.x % 32, n = k.side * k.wide;
   for (int g = threadIdx.x / 32; g < k.groups; g += kThreads / 32) {
     float s = 0.0f;
-    for (int i = lane; i < n; i += 32) s += threads[i / k.wide * k.cols + g * k.wide + i % k.wide];
+    for (int i = lane; i < n; i += 32) s += threads[(unsigned)i / (unsigned)k.wide * k.cols + g * k.wide + (unsigned)i % (unsigned)k.wide];
 #pragma unroll
     for (int o = 16; o; o /= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
     if (lane == 0) group[g] = s;
@@ -542,78 +588,87 @@ __device__ __forceinline__ void group_sums(float x, float* threads, float* group
   __syncthreads();
 }
 
+// A thread's values are summed once, as distances from its first piece; its mean and squared deviations from that mean
+// are joined over the threads of a group, and over the cluster's blocks, by the distances of the means.
 template <typename T, int E>
-__global__ void __launch_bounds__(kThreads) k_slab(Norm a, Slab k) {
+__global__ void __launch_bounds__(kThreads, 3) k_slab(Norm a, Slab k) {
   extern __shared__ uint4 data[];
-  __shared__ float threads[kThreads], group[kSlabGroups];
-  __shared__ float2 from[kSlabRanks][kSlabGroups];     // mean and squared deviations of each block's part
+  __shared__ float threads[2][kThreads], group[2][kSlabGroups];
+  __shared__ float2 from[kSlabRanks][kSlabGroups], stats[kSlabGroups];   // mean, squared deviations; mean, rstd
   slab_arrive(k.ranks);
   const SlabThread<T, E> me(a, k);
   me.fetch(a.x, data, k);
+  copy_commit();
   float gamma[E], beta[E];
   load_weights<E>(me.on ? a.gamma : nullptr, me.c, 1.0f, gamma);
   load_weights<E>(me.on ? a.beta : nullptr, me.c, 0.0f, beta);
-  asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
+  copy_wait<0>();
   const uint4* const mine = data + threadIdx.x;
-  const int n = me.on ? (int)max((int64_t)0, (me.s1 - me.s0 - me.row + k.side - 1) / k.side) : 0, by = k.side * k.cols;
-  const int W = k.wide * E;
-  float part[E] = {};
+  const int n = me.n, by = k.side * k.cols, W = k.wide * E;
+  float first[E] = {}, s1[E] = {}, s2[E] = {};
+  if (n) {
+    unpack<T, E>(mine[0], first);
+#pragma unroll
+    for (int e = 0; e < E; ++e) first[e] = -first[e];
+  }
 #pragma unroll 4
   for (int i = 0; i < n; ++i) {
     float x[E];
     unpack<T, E>(mine[i * by], x);
-    add<E>(part, x);
+    add<E>(x, first);
+    add<E>(s1, x);
+    fma<E>(x, x, s2, s2);
   }
-  group_sums(total<E>(part), threads, group, k);
-  const float here = (float)((me.s1 - me.s0) * W), inv = here > 0.0f ? 1.0f / here : 0.0f;
-  const float mean0 = group[me.g < k.groups ? me.g : 0] * inv;
-  float shift[E];
-  fill<E>(shift, -mean0);
-  fill<E>(part, 0.0f);
-#pragma unroll 4
-  for (int i = 0; i < n; ++i) {
-    float x[E];
-    unpack<T, E>(mine[i * by], x);
-    add<E>(x, shift);
-    fma<E>(x, x, part, part);
-  }
-  __syncthreads();           // all have read the sums
-  const int mg = threadIdx.x;
-  const float mean_of = mg < k.groups ? group[mg] * inv : 0.0f;
-  __syncthreads();
-  group_sums(total<E>(part), threads, group, k);
-  exchange(&from[me.rank][mg], make_float2(mean_of, mg < k.groups ? group[mg] : 0.0f), mg < k.groups, k.ranks);
-  // joined by the distances of the parts' means from the first's, which is a block with positions
-  const int g = me.g < k.groups ? me.g : 0;
-  const float all = 1.0f / (float)(a.S * W), m0 = from[0][g].x;
+  const float inv = n ? 1.0f / (float)n : 0.0f;
   float mean = 0.0f, sq = 0.0f;
-  for (int r = 0; r < k.ranks; ++r) {
-    const float w = (float)(min(a.S, (int64_t)(r + 1) * k.rows) - min(a.S, (int64_t)r * k.rows)) * (float)W;
-    mean = fmaf(w, from[r][g].x - m0, mean);
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    s2[e] = fmaxf(fmaf(-s1[e] * inv, s1[e], s2[e]), 0.0f);
+    s1[e] = fmaf(s1[e], inv, -first[e]);       // the channel's mean
+    mean += s1[e];
+    sq += s2[e];
   }
-  mean = fmaf(mean, all, m0);
-  for (int r = 0; r < k.ranks; ++r) {
-    const float w = (float)(min(a.S, (int64_t)(r + 1) * k.rows) - min(a.S, (int64_t)r * k.rows)) * (float)W;
-    const float d = from[r][g].x - mean;
-    sq += w > 0.0f ? fmaf(w * d, d, from[r][g].y) : 0.0f;
+  mean *= 1.0f / E;
+#pragma unroll
+  for (int e = 0; e < E; ++e) sq = fmaf((s1[e] - mean) * (float)n, s1[e] - mean, sq);
+  group_sums(mean * (float)(n * E), threads[0], group[0], k);
+  const float here = (float)(me.s1 - me.s0) * (float)W;
+  const float block = here > 0.0f ? group[0][me.g] / here : 0.0f;
+  group_sums(fmaf((mean - block) * (float)(n * E), mean - block, sq), threads[1], group[1], k);
+  const int mg = threadIdx.x;
+  const bool joins = mg < k.groups;
+  exchange(&from[me.rank][joins ? mg : 0],
+           joins && here > 0.0f ? make_float2(group[0][mg] / here, group[1][mg]) : make_float2(0.0f, 0.0f), joins, k.ranks);
+  if (joins) {
+    const float all = 1.0f / ((float)a.S * (float)W), m0 = from[0][mg].x;
+    auto size = [&](int r) { return (float)max((int64_t)0, min((int64_t)k.rows, a.S - (int64_t)r * k.rows)) * (float)W; };
+    float m = 0.0f, v = 0.0f;
+    for (int r = 0; r < k.ranks; ++r) m = fmaf(size(r), from[r][mg].x - m0, m);
+    m = fmaf(m, all, m0);
+    for (int r = 0; r < k.ranks; ++r) {
+      const float d = from[r][mg].x - m, w = size(r);
+      if (w > 0.0f) v += fmaf(w * d, d, from[r][mg].y);
+    }
+    const float rstd = inverse_root(fmaf(v, all, a.eps));
+    stats[mg] = make_float2(m, rstd);
+    const int64_t g = me.tile * (int64_t)k.groups + mg;
+    if (me.rank == 0 && g < a.G) {
+      a.mean[me.b * a.G + g] = m;
+      a.rstd[me.b * a.G + g] = rstd;
+    }
   }
-  const float rstd = inverse_root(fmaf(sq, all, a.eps));
+  __syncthreads();
   if (!me.on) return;
-  if (me.rank == 0 && me.row == 0 && me.col % k.wide == 0) {
-    a.mean[me.b * a.G + me.c / W] = mean;
-    a.rstd[me.b * a.G + me.c / W] = rstd;
-  }
-  float scale[E];
-  fill<E>(shift, -mean);
-  fill<E>(scale, rstd);
+  fill<E>(s1, -stats[me.g].x);
+  fill<E>(s2, stats[me.g].y);
+  mul<E>(gamma, s2);
   T* o = at<T>(a.y, me.b, me.s0 + me.row, me.c);
   const int64_t oy = k.side * a.y.inner;
-#pragma unroll 2
+#pragma unroll 4
   for (int i = 0; i < n; ++i, o += oy) {
     float x[E];
     unpack<T, E>(mine[i * by], x);
-    add<E>(x, shift);
-    mul<E>(x, scale);
+    add<E>(x, s1);
     fma<E>(gamma, x, beta, x);
     activate<T, E>(a.act, x);
     store<T, E>(o, x);
@@ -622,7 +677,7 @@ __global__ void __launch_bounds__(kThreads) k_slab(Norm a, Slab k) {
 
 // partial: [2][B * ranks][C], or NULL.
 template <typename T, int E>
-__global__ void __launch_bounds__(kThreads) k_slab_back(Norm a, Slab k, float* partial) {
+__global__ void __launch_bounds__(kThreads, 3) k_slab_back(Norm a, Slab k, float* partial) {
   extern __shared__ uint4 data[];
   __shared__ float sums[2][E][kThreads];
   __shared__ float2 from[kSlabRanks][kSlabGroups];
@@ -635,13 +690,14 @@ __global__ void __launch_bounds__(kThreads) k_slab_back(Norm a, Slab k, float* p
   load_weights<E>(me.on ? a.gamma : nullptr, me.c, 1.0f, gamma);
   load_weights<E>(me.on ? a.beta : nullptr, me.c, 0.0f, beta);
   const int W = k.wide * E;
-  const int64_t stats = me.b * a.G + me.c / W;
+  const int64_t stats = me.b * a.G + me.c / (unsigned)W;
   const float rstd = me.on ? a.rstd[stats] : 0.0f;
   fill<E>(shift, me.on ? -a.mean[stats] : 0.0f);
   fill<E>(scale, rstd);
-  asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
+  copy_commit();
+  copy_wait<0>();
   const uint4 *const mx = data + threadIdx.x, *const my = mx + held;
-  const int n = me.on ? (int)max((int64_t)0, (me.s1 - me.s0 - me.row + k.side - 1) / k.side) : 0, by = k.side * k.cols;
+  const int n = me.n, by = k.side * k.cols;
   float db[E] = {}, dg[E] = {};
   auto piece = [&](int i, float (&xh)[E], float (&dz)[E]) {
     float u[E];
@@ -663,14 +719,14 @@ __global__ void __launch_bounds__(kThreads) k_slab_back(Norm a, Slab k, float* p
   for (int e = 0; e < E; ++e) sums[0][e][threadIdx.x] = db[e], sums[1][e][threadIdx.x] = dg[e];
   __syncthreads();
   // each channel's sums over the rows of threads: to the first row's places, and out
-  const int64_t row = (int64_t)(blockIdx.x / k.ranks / k.tiles) * k.ranks + me.rank;
-  const int64_t c0 = (blockIdx.x / k.ranks % k.tiles) * (int64_t)k.cols * E, rows = a.B * k.ranks;
+  const int64_t row = (int64_t)me.b * k.ranks + me.rank, rows = a.B * k.ranks;
+  const int c0 = me.tile * k.cols * E;
   for (int i = threadIdx.x; i < 2 * E * k.cols; i += kThreads) {
-    const int col = i % k.cols, e = i / k.cols % E, which = i / (k.cols * E);
+    const int e2 = (unsigned)i / (unsigned)k.cols, col = i - e2 * k.cols, e = e2 % E, which = e2 / E;
     float v = 0.0f;
     for (int r = 0; r < k.side; ++r) v += sums[which][e][r * k.cols + col];
     sums[which][e][col] = v;
-    const int64_t c = c0 + col * E + e;
+    const int c = c0 + col * E + e;
     if (partial && c < a.C) partial[(which * rows + row) * a.C + c] = v;
   }
   __syncthreads();
@@ -680,7 +736,7 @@ __global__ void __launch_bounds__(kThreads) k_slab_back(Norm a, Slab k, float* p
     float2 v = make_float2(0.0f, 0.0f);
     for (int i = lane; i < W; i += 32) {
       const int col = g * k.wide + i / E, e = i % E;
-      const int64_t c = c0 + col * E + e;
+      const int c = c0 + col * E + e;
       const float w = c < a.C ? (a.gamma ? __ldg(a.gamma + c) : 1.0f) : 0.0f;
       v.x = fmaf(w, sums[0][e][col], v.x);
       v.y = fmaf(w, sums[1][e][col], v.y);
@@ -1020,8 +1076,10 @@ Plan make_plan(const net_norm* p, bool back) {
     const int groups = (int)std::min<int64_t>(p->G, teams), per = teams / groups;
     q.t = {lanes, (int)pieces, (int)(W / q.e), groups, per};
     const int64_t gy = (p->G + groups - 1) / groups, gx = (p->B + per - 1) / per;
-    // as many blocks as the SMs hold at a time, or so: each goes from instance to instance
-    const int64_t want = std::max<int64_t>(1, (int64_t)sms * (1024 / q.threads) / gy);
+    // as many blocks as the SMs hold at a time: each goes from instance to instance (a second round of blocks cost 8 us
+    // of 29 backward at 65,536 x 256 bf16)
+    const int resident = back ? 512 : q.e == 8 && !q.block ? 1280 : 1024;
+    const int64_t want = std::max<int64_t>(1, (int64_t)sms * (resident / q.threads) / gy);
     q.grid = dim3((unsigned)std::min(gx, want), (unsigned)gy);
     if (back && (p->dgamma || p->dbeta)) q.bytes = sizeof(float) * 2 * q.grid.x * (size_t)p->C;
     return q;
@@ -1073,19 +1131,26 @@ Plan make_plan(const net_norm* p, bool back) {
 
 template <typename T, int E, int SLOTS, int LANES>
 cudaError_t launch_team(const Norm& a, const Plan& q, bool back, float* ws, cudaStream_t s) {
+  auto allow = [](const void* kern, int bytes) {
+    return bytes <= 40 * 1024 ? cudaSuccess   // 48 KB with what a kernel declares itself
+                              : cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  };
   if (!back) {
-    k_team<T, E, SLOTS, LANES><<<q.grid, q.threads, 0, s>>>(a, q.t);
+    constexpr auto kern = k_team<T, E, SLOTS, LANES>;
+    const int smem = Ahead<T, E, SLOTS, 1>::bytes(q.threads);
+    const cudaError_t e = allow((const void*)kern, smem);
+    if (e != cudaSuccess) return e;
+    kern<<<q.grid, q.threads, smem, s>>>(a, q.t);
     return cudaGetLastError();
   }
   const bool weights = a.dgamma || a.dbeta;
-  const int smem = weights ? 2 * q.threads * SLOTS * E * (int)sizeof(float) : 0;
+  const int smem = std::max(weights ? 2 * q.threads * SLOTS * E * (int)sizeof(float) : 0,
+                            Ahead<T, E, SLOTS, 2>::bytes(q.threads));
   const auto kern = k_team_back<T, E, SLOTS, LANES>;
-  if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e != cudaSuccess) return e;
-  }
+  cudaError_t e = allow((const void*)kern, smem);
+  if (e != cudaSuccess) return e;
   kern<<<q.grid, q.threads, smem, s>>>(a, q.t, weights ? ws : nullptr);
-  cudaError_t e = cudaGetLastError();
+  e = cudaGetLastError();
   if (e == cudaSuccess && weights && q.grid.x > 1) {
     k_weights<<<dim3((unsigned)((a.C + 31) / 32), 2), kJoinThreads, 0, s>>>(a, ws, q.grid.x);
     e = cudaGetLastError();

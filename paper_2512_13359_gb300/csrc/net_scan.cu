@@ -15,15 +15,6 @@ namespace auv {
 namespace net {
 namespace {
 
-template <int BYTES>
-__device__ __forceinline__ void copy_async(void* dst, const void* src) {
-  const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);
-  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(src) : "memory");
-  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(d), "l"(src), "n"(BYTES) : "memory");
-}
-// Two-byte pieces (odd widths or strides of 16-bit types) have no asynchronous copy.
-template <typename T, int E> constexpr bool kAsync = sizeof(T) * E >= 4;
-
 template <int E>
 __device__ __forceinline__ void load_state(const float* p, float (&x)[E]) {
   if (p && E >= 4 && reinterpret_cast<uintptr_t>(p) % 16 == 0) {

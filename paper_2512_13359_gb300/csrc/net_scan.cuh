@@ -29,10 +29,6 @@ __device__ __forceinline__ uint32_t end_flag(const Scan& a, int t, int64_t n) {
   return p ? (uint32_t)__ldg(p + (t ? (t - 1) * a.envs : 0) + n) : 0u;
 }
 
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int LEFT>
-__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
-
 // The arrays of one step that a thread reads: f, v, and backward the state before the step and dy; from the chain's
 // first step on (the last of the sequence backward).
 template <typename T, bool BACK>
