@@ -171,6 +171,24 @@ __device__ __forceinline__ void load_weights(const float* w, int64_t c, float no
   }
 }
 
+// Kernels of one call follow each other closely: the next one's blocks are set up while the last of the one before run,
+// and wait here for its stores.
+__device__ __forceinline__ void after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+template <typename... P, typename... A>
+cudaError_t launch_after(void (*kern)(P...), dim3 grid, int threads, cudaStream_t s, A... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, args...);
+}
+
 // ------------------------------------------------------------------ teams
 constexpr int kThreads = 256;
 constexpr int kMostLanes = 512;      // of a team that is a block
@@ -201,7 +219,7 @@ __device__ __forceinline__ void team_sum(float (&x)[N], int lanes) {
     }
   }
   if constexpr (LANES == kBlock) {
-    __shared__ float part[kMostLanes / 32][N];
+    __shared__ float part[32][N];
     const int warps = blockDim.x / 32;
     __syncthreads();
     if (threadIdx.x % 32 == 0) {
@@ -508,6 +526,7 @@ __device__ __forceinline__ void join_weights(const Norm& a, const float* partial
 }
 
 __global__ void __launch_bounds__(kJoinThreads) k_weights(Norm a, const float* partial, int64_t rows) {
+  after_previous();
   join_weights(a, partial, rows, blockIdx.x, blockIdx.y);
 }
 
@@ -679,8 +698,9 @@ __global__ void __launch_bounds__(kThreads, 3) k_slab(Norm a, Slab k) {
 template <typename T, int E>
 __global__ void __launch_bounds__(kThreads, 3) k_slab_back(Norm a, Slab k, float* partial) {
   extern __shared__ uint4 data[];
-  __shared__ float sums[2][E][kThreads];
+  __shared__ float sums[E][kThreads];
   __shared__ float2 from[kSlabRanks][kSlabGroups];
+  __shared__ float own[2][kSlabGroups];
   slab_arrive(k.ranks);
   const SlabThread<T, E> me(a, k);
   const int held = k.rows * k.cols;
@@ -715,43 +735,39 @@ __global__ void __launch_bounds__(kThreads, 3) k_slab_back(Norm a, Slab k, float
     add<E>(db, dz);
     fma<E>(dz, xh, dg, dg);
   }
-#pragma unroll
-  for (int e = 0; e < E; ++e) sums[0][e][threadIdx.x] = db[e], sums[1][e][threadIdx.x] = dg[e];
-  __syncthreads();
-  // each channel's sums over the rows of threads: to the first row's places, and out
+  // Each channel's sums over the rows of threads, to the first row's places and out, and each group's, weighted: dbeta's,
+  // then dgamma's (one array of sums leaves room for a third block an SM).
   const int64_t row = (int64_t)me.b * k.ranks + me.rank, rows = a.B * k.ranks;
-  const int c0 = me.tile * k.cols * E;
-  for (int i = threadIdx.x; i < 2 * E * k.cols; i += kThreads) {
-    const int e2 = (unsigned)i / (unsigned)k.cols, col = i - e2 * k.cols, e = e2 % E, which = e2 / E;
-    float v = 0.0f;
-    for (int r = 0; r < k.side; ++r) v += sums[which][e][r * k.cols + col];
-    sums[which][e][col] = v;
-    const int c = c0 + col * E + e;
-    if (partial && c < a.C) partial[(which * rows + row) * a.C + c] = v;
-  }
-  __syncthreads();
-  // and each group's, weighted
-  const int lane = threadIdx.x % 32;
-  for (int g = threadIdx.x / 32; g < k.groups; g += kThreads / 32) {
-    float2 v = make_float2(0.0f, 0.0f);
-    for (int i = lane; i < W; i += 32) {
-      const int col = g * k.wide + i / E, e = i % E;
-      const int c = c0 + col * E + e;
-      const float w = c < a.C ? (a.gamma ? __ldg(a.gamma + c) : 1.0f) : 0.0f;
-      v.x = fmaf(w, sums[0][e][col], v.x);
-      v.y = fmaf(w, sums[1][e][col], v.y);
-    }
+  const int c0 = me.tile * k.cols * E, lane = threadIdx.x % 32;
 #pragma unroll
-    for (int o = 16; o; o /= 2) {
-      v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
-      v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+  for (int which = 0; which < 2; ++which) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) sums[e][threadIdx.x] = which ? dg[e] : db[e];
+    __syncthreads();
+    for (int i = threadIdx.x; i < E * k.cols; i += kThreads) {
+      const int e = (unsigned)i / (unsigned)k.cols, col = i - e * k.cols;
+      float v = 0.0f;
+      for (int r = 0; r < k.side; ++r) v += sums[e][r * k.cols + col];
+      sums[e][col] = v;
+      const int c = c0 + col * E + e;
+      if (partial && c < a.C) partial[(which * rows + row) * a.C + c] = v;
     }
-    if (lane == 0) from[me.rank][g] = v;
+    __syncthreads();
+    for (int g = threadIdx.x / 32; g < k.groups; g += kThreads / 32) {
+      float v = 0.0f;
+      for (int i = lane; i < W; i += 32) {
+        const int col = g * k.wide + i / E, e = i % E, c = c0 + col * E + e;
+        v = fmaf(c < a.C ? (a.gamma ? __ldg(a.gamma + c) : 1.0f) : 0.0f, sums[e][col], v);
+      }
+#pragma unroll
+      for (int o = 16; o; o /= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
+      if (lane == 0) own[which][g] = v;
+    }
+    __syncthreads();
   }
-  __syncthreads();
-  const int mg = threadIdx.x;
-  const float2 own = mg < k.groups ? from[me.rank][mg] : make_float2(0.0f, 0.0f);
-  exchange(&from[me.rank][mg], own, mg < k.groups, k.ranks);
+  const bool joins = (int)threadIdx.x < k.groups;
+  const int mg = joins ? threadIdx.x : 0;
+  exchange(&from[me.rank][mg], make_float2(own[0][mg], own[1][mg]), joins, k.ranks);
   if (!me.on) return;
   float2 w = make_float2(0.0f, 0.0f);
   for (int r = 0; r < k.ranks; ++r) w.x += from[r][me.g].x, w.y += from[r][me.g].y;
@@ -775,7 +791,7 @@ __global__ void __launch_bounds__(kThreads, 3) k_slab_back(Norm a, Slab k, float
 // ------------------------------------------------------------------ chunks
 // Larger groups: a block takes `rows` positions of `cols` pieces of E channels, kThreads / cols rows side by side.
 struct Chunks {
-  int cols;             // pieces of a block, a power of two up to 32
+  int cols;             // pieces of a block, up to 64
   int rows;             // positions of a block
   int64_t count;        // chunks of an instance
 };
@@ -788,10 +804,10 @@ struct Place {
   __device__ Place(const Norm& a, const Chunks& k) {
     b = blockIdx.x / k.count;
     chunk = blockIdx.x - b * k.count;
-    c = (blockIdx.y * (int64_t)k.cols + threadIdx.x % k.cols) * E;
-    on = c < a.C;
     row = threadIdx.x / k.cols;
     rows = kThreads / k.cols;
+    c = (blockIdx.y * (int64_t)k.cols + threadIdx.x % k.cols) * E;
+    on = c < a.C && row < rows;
     s0 = chunk * k.rows;
     s1 = min(a.S, s0 + k.rows);
   }
@@ -809,7 +825,7 @@ __device__ __forceinline__ void join_rows(float (&x)[E], int cols) {
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       float s = 0.0f;
-      for (int i = threadIdx.x; i < kThreads; i += cols) s += part[e][i];
+      for (int i = threadIdx.x; i < kThreads / cols * cols; i += cols) s += part[e][i];
       x[e] = s;
     }
   }
@@ -851,7 +867,8 @@ __global__ void __launch_bounds__(kThreads) k_part(Norm a, Chunks k, float* part
 }
 
 // Mean and rstd of a group, a block each, from its channels' chunks.
-__global__ void __launch_bounds__(kThreads) k_stats(Norm a, Chunks k, const float* part) {
+__global__ void __launch_bounds__(kJoinThreads) k_stats(Norm a, Chunks k, const float* part) {
+  after_previous();
   const int64_t W = a.C / a.G, all = k.count * W;
   for (int64_t q = blockIdx.x; q < a.B * a.G; q += gridDim.x) {
     const int64_t b = q / a.G, c0 = q % a.G * W;
@@ -860,11 +877,11 @@ __global__ void __launch_bounds__(kThreads) k_stats(Norm a, Chunks k, const floa
     auto size = [&](int64_t chunk) { return (float)(min(a.S, (chunk + 1) * k.rows) - chunk * k.rows); };
     const float shift = m[0];
     float s[2] = {0.0f, 0.0f};
-    for (int64_t i = threadIdx.x; i < all; i += kThreads) s[0] += size(i / W) * (m[i / W * a.C + i % W] - shift);
+    for (int64_t i = threadIdx.x; i < all; i += blockDim.x) s[0] += size(i / W) * (m[i / W * a.C + i % W] - shift);
     team_sum<kBlock, 2>(s, 0);
     const float n = (float)a.S * (float)W, mean = shift + s[0] / n;
     s[0] = s[1] = 0.0f;
-    for (int64_t i = threadIdx.x; i < all; i += kThreads) {
+    for (int64_t i = threadIdx.x; i < all; i += blockDim.x) {
       const float d = m[i / W * a.C + i % W] - mean;
       s[0] += m2[i / W * a.C + i % W];
       s[1] = fmaf(size(i / W) * d, d, s[1]);
@@ -897,6 +914,7 @@ struct Weights {
 template <typename T, int E>
 __global__ void __launch_bounds__(kThreads) k_apply(Norm a, Chunks k) {
   const Place<E> me(a, k);
+  after_previous();
   if (!me.on) return;
   const Weights<E> w(a, me.b, me.c);
   const T* p = at<T>(a.x, me.b, me.s0 + me.row, me.c);
@@ -953,7 +971,8 @@ __global__ void __launch_bounds__(kThreads) k_part_back(Norm a, Chunks k, float*
 }
 
 // avg(w) and avg(w xh) of a group, a block each: avg[2][B * G].  The blocks after those sum dbeta and dgamma.
-__global__ void __launch_bounds__(kThreads) k_stats_back(Norm a, Chunks k, const float* part, float* avg, int64_t groups) {
+__global__ void __launch_bounds__(kJoinThreads) k_stats_back(Norm a, Chunks k, const float* part, float* avg, int64_t groups) {
+  after_previous();
   const int64_t rows = a.B * k.count;
   if (blockIdx.x >= groups) {
     join_weights(a, part, rows, (blockIdx.x - groups) / 2, (int)((blockIdx.x - groups) % 2));
@@ -965,7 +984,7 @@ __global__ void __launch_bounds__(kThreads) k_stats_back(Norm a, Chunks k, const
     const float* db = part + b * k.count * a.C + c0;
     const float* dg = db + rows * a.C;
     float s[2] = {0.0f, 0.0f};
-    for (int64_t i = threadIdx.x; i < all; i += kThreads) {
+    for (int64_t i = threadIdx.x; i < all; i += blockDim.x) {
       const float g = a.gamma ? a.gamma[c0 + i % W] : 1.0f;
       s[0] = fmaf(g, db[i / W * a.C + i % W], s[0]);
       s[1] = fmaf(g, dg[i / W * a.C + i % W], s[1]);
@@ -982,6 +1001,7 @@ __global__ void __launch_bounds__(kThreads) k_stats_back(Norm a, Chunks k, const
 template <typename T, int E>
 __global__ void __launch_bounds__(kThreads) k_apply_back(Norm a, Chunks k, const float* avg) {
   const Place<E> me(a, k);
+  after_previous();
   if (!me.on) return;
   const Weights<E> w(a, me.b, me.c);
   float m1[E], m2[E];
@@ -1085,7 +1105,7 @@ Plan make_plan(const net_norm* p, bool back) {
     return q;
   }
   // slabs: whole groups side by side, 64 bytes of a row at least, in as few blocks as leave three an SM (72 KB each,
-  // backward 16 of them for sums; then two, and clusters of 16).  Aligned pieces within a group alone.
+  // backward 8 of them for sums; then two, and clusters of 16).  Aligned pieces within a group alone.
   if (W % widest == 0 && fits(widest) && W / widest <= kThreads) {
     const int wide = (int)(W / widest);
     const int groups = (int)std::min<int64_t>(p->G, std::max(1, kSlabGroups / wide));
@@ -1095,8 +1115,8 @@ Plan make_plan(const net_norm* p, bool back) {
       const int64_t rows = std::max<int64_t>(1, bytes / row);
       return (p->S + rows - 1) / rows;
     };
-    int64_t ranks = ranks_for(back ? 56 * 1024 : 72 * 1024);
-    if (ranks > 8) ranks = ranks_for(back ? 92 * 1024 : 108 * 1024);
+    int64_t ranks = ranks_for(back ? 64 * 1024 : 72 * 1024);
+    if (ranks > 8) ranks = ranks_for(back ? 100 * 1024 : 108 * 1024);
     if (ranks <= kSlabRanks) {
       const int64_t tiles = (p->G + groups - 1) / groups;
       int r = pow2_at_least(ranks);
@@ -1112,12 +1132,14 @@ Plan make_plan(const net_norm* p, bool back) {
       if (q.slab) return q;
     }
   }
-  q.e = p->C % widest == 0 && fits(widest) ? widest : 1;
+  q.e = widest;
+  while (q.e > 1 && (p->C % q.e || !fits(q.e))) q.e = q.e > 2 ? 2 : 1;
   const int64_t cols = (p->C + q.e - 1) / q.e;
-  q.k.cols = std::min(32, pow2_at_least(cols));
-  const int64_t across = (cols + q.k.cols - 1) / q.k.cols;
+  const int64_t across = (cols + 63) / 64;
+  q.k.cols = (int)((cols + across - 1) / across);
   const int side = kThreads / q.k.cols;
-  int64_t want = std::max<int64_t>(1, (int64_t)sms * 8 / std::max<int64_t>(1, across * p->B));
+  // four blocks an SM, but no more chunks of an instance than its statistics are soon joined from
+  int64_t want = std::max<int64_t>(1, std::min<int64_t>(3 * sms, (int64_t)sms * 4 / std::max<int64_t>(1, across * p->B)));
   want = std::min(want, std::max<int64_t>(1, p->S / (side * 4)));
   int64_t per = (p->S + want - 1) / want;
   per = std::min<int64_t>(std::max<int64_t>(per, 1), 1 << 20);
@@ -1127,6 +1149,10 @@ Plan make_plan(const net_norm* p, bool back) {
   q.stats = std::min<int64_t>(p->B * p->G, 1 << 20);
   q.bytes = sizeof(float) * 2 * ((size_t)p->B * q.k.count * p->C + (back ? (size_t)p->B * p->G : 0));
   return q;
+}
+
+cudaError_t launch_weights(const Norm& a, const float* partial, int64_t rows, cudaStream_t s) {
+  return launch_after(k_weights, dim3((unsigned)((a.C + 31) / 32), 2), kJoinThreads, s, a, partial, rows);
 }
 
 template <typename T, int E, int SLOTS, int LANES>
@@ -1152,8 +1178,7 @@ cudaError_t launch_team(const Norm& a, const Plan& q, bool back, float* ws, cuda
   kern<<<q.grid, q.threads, smem, s>>>(a, q.t, weights ? ws : nullptr);
   e = cudaGetLastError();
   if (e == cudaSuccess && weights && q.grid.x > 1) {
-    k_weights<<<dim3((unsigned)((a.C + 31) / 32), 2), kJoinThreads, 0, s>>>(a, ws, q.grid.x);
-    e = cudaGetLastError();
+    return launch_weights(a, ws, q.grid.x, s);
   }
   return e;
 }
@@ -1196,25 +1221,26 @@ cudaError_t launch_slab(const Norm& a, const Plan& q, bool back, float* ws, cuda
   cfg.numAttrs = 1;
   if (back) e = cudaLaunchKernelEx(&cfg, k_slab_back<T, E>, a, q.sl, weights ? ws : (float*)nullptr);
   else e = cudaLaunchKernelEx(&cfg, k_slab<T, E>, a, q.sl);
-  if (e == cudaSuccess && weights)
-    k_weights<<<dim3((unsigned)((a.C + 31) / 32), 2), kJoinThreads, 0, s>>>(a, ws, a.B * q.sl.ranks);
-  return e == cudaSuccess ? cudaGetLastError() : e;
+  return e == cudaSuccess && weights ? launch_weights(a, ws, a.B * q.sl.ranks, s) : e;
 }
 
 template <typename T, int E>
 cudaError_t launch_chunks(const Norm& a, const Plan& q, bool back, float* ws, cudaStream_t s) {
+  cudaError_t e;
+  // threads that join a group: by what there is of it
+  const int join = q.k.count * (a.C / a.G) >= 1024 ? kJoinThreads : kThreads;
   if (!back) {
     k_part<T, E><<<q.grid, kThreads, 0, s>>>(a, q.k, ws);
-    k_stats<<<(unsigned)q.stats, kThreads, 0, s>>>(a, q.k, ws);
-    k_apply<T, E><<<q.grid, kThreads, 0, s>>>(a, q.k);
-    return cudaGetLastError();
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    e = launch_after(k_stats, dim3((unsigned)q.stats), join, s, a, q.k, (const float*)ws);
+    return e != cudaSuccess ? e : launch_after(k_apply<T, E>, q.grid, kThreads, s, a, q.k);
   }
   float* const avg = ws + 2 * a.B * q.k.count * a.C;
   const int64_t columns = a.dgamma || a.dbeta ? (a.C + 31) / 32 * 2 : 0;
   k_part_back<T, E><<<q.grid, kThreads, 0, s>>>(a, q.k, ws);
-  k_stats_back<<<(unsigned)(q.stats + columns), kThreads, 0, s>>>(a, q.k, ws, avg, q.stats);
-  k_apply_back<T, E><<<q.grid, kThreads, 0, s>>>(a, q.k, avg);
-  return cudaGetLastError();
+  if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  e = launch_after(k_stats_back, dim3((unsigned)(q.stats + columns)), join, s, a, q.k, (const float*)ws, avg, q.stats);
+  return e != cudaSuccess ? e : launch_after(k_apply_back<T, E>, q.grid, kThreads, s, a, q.k, (const float*)avg);
 }
 
 template <typename T>
@@ -1223,11 +1249,14 @@ cudaError_t launch(const Norm& a, const Plan& q, bool back, void* ws, cudaStream
   float* const w = static_cast<float*>(ws);
   if (a.B == 0 || a.S == 0) {
     if (!back && a.B) k_empty<<<(unsigned)((a.B * a.G + kThreads - 1) / kThreads), kThreads, 0, s>>>(a);
-    if (back && (a.dgamma || a.dbeta)) k_weights<<<dim3((unsigned)((a.C + 31) / 32), 2), kJoinThreads, 0, s>>>(a, nullptr, 0);
+    if (back && (a.dgamma || a.dbeta)) return launch_weights(a, nullptr, 0, s);
     return cudaGetLastError();
   }
   if (q.slab) return launch_slab<T>(a, q, back, w, s);
-  if (!q.team) return q.e > 1 ? launch_chunks<T, kWide>(a, q, back, w, s) : launch_chunks<T, 1>(a, q, back, w, s);
+  if (!q.team) {
+    if (q.e == kWide) return launch_chunks<T, kWide>(a, q, back, w, s);
+    return q.e == 2 ? launch_chunks<T, 2>(a, q, back, w, s) : launch_chunks<T, 1>(a, q, back, w, s);
+  }
   if (q.e == kWide) return launch_teams<T, kWide>(a, q, back, w, s);
   if (q.e == 2) return launch_teams<T, 2>(a, q, back, w, s);
   return launch_teams<T, 1>(a, q, back, w, s);
