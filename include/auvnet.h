@@ -90,6 +90,10 @@ typedef struct net_rows {
  * difference from the gradient of the unrounded recurrence (2^-9 of a state
  * for bf16, as much as v's own), and it saves a second array of states.
  * hT is not read.  dh0 = dhT is allowed.
+ *
+ * workspace: net_gate_scan_workspace_bytes(a, backward) bytes, 16-byte
+ * aligned (AUV_ERR_SIZE if there is less): 0 below 32 steps, and wherever the
+ * sequence need not be split into pieces.
  */
 typedef struct net_scan {
   uint32_t struct_size;           /* sizeof(net_scan): version guard          */
@@ -102,7 +106,10 @@ typedef struct net_scan {
   float* dh0;                     /* [N][D]                                   */
   const uint8_t* done;            /* [T][N]                                   */
   const uint8_t* done_prev;       /* [N]                                      */
+  void* workspace;
+  size_t workspace_bytes;
 } net_scan;
+size_t net_gate_scan_workspace_bytes(const net_scan* a, int backward);
 int net_gate_scan(const net_scan* a, void* stream);
 int net_gate_scan_backward(const net_scan* a, void* stream);
 

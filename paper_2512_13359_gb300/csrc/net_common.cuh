@@ -116,6 +116,25 @@ __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group 
 // Two-byte pieces (odd widths or strides of 16-bit types) have no asynchronous copy.
 template <typename T, int E> constexpr bool kAsync = sizeof(T) * E >= 4;
 
+// Kernels of one call follow each other closely: the next one's blocks are set up while the last of the one before run,
+// and wait here for its stores.
+__device__ __forceinline__ void after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+template <typename... P, typename... A>
+cudaError_t launch_after(void (*kern)(P...), dim3 grid, int threads, int smem, cudaStream_t s, A... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...);
+}
+
 // ---------------------------------------------------------------- host side
 int fail(int code, const char* fmt, ...);
 int cuda_fail(cudaError_t e, const char* what);

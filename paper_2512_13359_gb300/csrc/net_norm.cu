@@ -171,24 +171,6 @@ __device__ __forceinline__ void load_weights(const float* w, int64_t c, float no
   }
 }
 
-// Kernels of one call follow each other closely: the next one's blocks are set up while the last of the one before run,
-// and wait here for its stores.
-__device__ __forceinline__ void after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-
-template <typename... P, typename... A>
-cudaError_t launch_after(void (*kern)(P...), dim3 grid, int threads, cudaStream_t s, A... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3((unsigned)threads);
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kern, args...);
-}
-
 // ------------------------------------------------------------------ teams
 constexpr int kThreads = 256;
 constexpr int kMostLanes = 512;      // of a team that is a block
@@ -1152,7 +1134,7 @@ Plan make_plan(const net_norm* p, bool back) {
 }
 
 cudaError_t launch_weights(const Norm& a, const float* partial, int64_t rows, cudaStream_t s) {
-  return launch_after(k_weights, dim3((unsigned)((a.C + 31) / 32), 2), kJoinThreads, s, a, partial, rows);
+  return launch_after(k_weights, dim3((unsigned)((a.C + 31) / 32), 2), kJoinThreads, 0, s, a, partial, rows);
 }
 
 template <typename T, int E, int SLOTS, int LANES>
@@ -1232,15 +1214,15 @@ cudaError_t launch_chunks(const Norm& a, const Plan& q, bool back, float* ws, cu
   if (!back) {
     k_part<T, E><<<q.grid, kThreads, 0, s>>>(a, q.k, ws);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    e = launch_after(k_stats, dim3((unsigned)q.stats), join, s, a, q.k, (const float*)ws);
-    return e != cudaSuccess ? e : launch_after(k_apply<T, E>, q.grid, kThreads, s, a, q.k);
+    e = launch_after(k_stats, dim3((unsigned)q.stats), join, 0, s, a, q.k, (const float*)ws);
+    return e != cudaSuccess ? e : launch_after(k_apply<T, E>, q.grid, kThreads, 0, s, a, q.k);
   }
   float* const avg = ws + 2 * a.B * q.k.count * a.C;
   const int64_t columns = a.dgamma || a.dbeta ? (a.C + 31) / 32 * 2 : 0;
   k_part_back<T, E><<<q.grid, kThreads, 0, s>>>(a, q.k, ws);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
-  e = launch_after(k_stats_back, dim3((unsigned)(q.stats + columns)), join, s, a, q.k, (const float*)ws, avg, q.stats);
-  return e != cudaSuccess ? e : launch_after(k_apply_back<T, E>, q.grid, kThreads, s, a, q.k, (const float*)avg);
+  e = launch_after(k_stats_back, dim3((unsigned)(q.stats + columns)), join, 0, s, a, q.k, (const float*)ws, avg, q.stats);
+  return e != cudaSuccess ? e : launch_after(k_apply_back<T, E>, q.grid, kThreads, 0, s, a, q.k, (const float*)avg);
 }
 
 template <typename T>

@@ -13,17 +13,6 @@ namespace auv {
 namespace net {
 namespace {
 
-// An affine map h -> A h + B of one channel.  A piece with an episode end in it passes nothing on, whatever came
-// before (NaN times 0 included): its A is -0, and the sign is asked for; gates are never negative.
-struct Map {
-  float A, B;
-};
-__device__ __forceinline__ bool cuts(float A) { return __float_as_uint(A) >> 31; }
-__device__ __forceinline__ Map then(const Map& p, const Map& q) {   // p, then q
-  return cuts(q.A) ? q : Map{p.A * q.A, fmaf(q.A, p.B, q.B)};
-}
-__device__ __forceinline__ float apply(const Map& q, float h) { return cuts(q.A) ? q.B : fmaf(q.A, h, q.B); }
-
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));

@@ -8,7 +8,11 @@
 //  k_steps  one thread per E adjacent channels walks the steps.  Its inputs of the next 8 steps are on their way to
 //           shared memory (cp.async to slots of its own: no barrier), so few threads keep HBM busy.
 //  k_one    the same for a single step.
-//  k_pieces few channels, many steps: the steps are split too (net_pieces.cu).
+//  k_steps, k_join, k_steps: few channels, many steps: pieces of the sequence are folded to affine maps h -> A h + B,
+//           the maps joined to the states before the pieces, and the pieces walked from those.
+//  k_pieces few channels, fewer steps: both in one kernel, with the inputs read once (net_pieces.cu).
+#include <algorithm>
+
 #include "net_scan.cuh"
 
 namespace auv {
@@ -124,27 +128,44 @@ template <int E> constexpr int kAheadOf = E >= 4 ? 8 : 16;
 // make few warps, wait for each other's latency otherwise.
 template <int E> constexpr int kGroup = E == 4 ? 2 : 4;
 
-template <typename T, int E, bool BACK, bool MIXED>
-__global__ void __launch_bounds__(kStepThreads) k_steps(Scan a, int64_t width) {
+// A sequence in pieces of `rows` steps, blockIdx.y's each: the maps of the pieces' channels, A [pieces][m] and
+// B [pieces][m]; after k_join, B holds the states before the pieces.  One piece: rows = T, maps NULL.
+struct Split {
+  int rows;
+  int64_t m;
+  float* maps;
+};
+
+// SPLIT: in pieces; FOLD: only their maps.
+template <typename T, int E, bool BACK, bool MIXED, bool SPLIT, bool FOLD>
+__global__ void __launch_bounds__(kStepThreads) k_steps(Scan a, int64_t width, Split split) {
   using W = Raw<T, E>;
   using In = Inputs<T, BACK>;
   constexpr int K = In::kN, kAhead = kAsync<T, E> ? kAheadOf<E> : 8, kG = kAsync<T, E> ? kGroup<E> : kAhead;
+  constexpr int kHeld = FOLD ? 2 : K;                          // arrays read: folding f, and v or dy
+  constexpr int kX = FOLD && BACK ? 3 : 1;
   extern __shared__ uint4 smem[];
-  W* const ring = reinterpret_cast<W*>(smem) + threadIdx.x;    // slot (u, i) at (u * K + i) * kStepThreads
+  W* const ring = reinterpret_cast<W*>(smem) + threadIdx.x;    // slot (u, i) at (u * kHeld + i) * kStepThreads
   const int64_t m = blockIdx.x * (int64_t)kStepThreads + threadIdx.x, per = a.D / E;
   if (m >= a.N * per) return;
   const int64_t n = m / per, d = (m - n * per) * E;
   In in(a, n, d);
-  const int T_ = a.T;
-  static_assert(kAhead * E <= 32, "the flags of a round are one word");
-  [[maybe_unused]] W reg[kAhead][K];
-  auto fetch = [&](int u, int s) {      // the s-th step of the chain, in order
-    if (s < T_) {
+  // steps before the piece, and its own
+  const int skip = SPLIT ? blockIdx.y * split.rows : 0, steps = SPLIT ? min(split.rows, a.T - skip) : a.T;
+  if constexpr (SPLIT) {
 #pragma unroll
-      for (int i = 0; i < K; ++i) {
-        if (i != 2 || s < T_ - 1) {
-          if constexpr (kAsync<T, E>) copy_async<sizeof(W)>(ring + (u * K + i) * kStepThreads, in.p[i]);
-          else reg[u][i] = *reinterpret_cast<const W*>(in.p[i]);
+    for (int i = 0; i < K; ++i) in.p[i] += skip * in.by[i];
+  }
+  static_assert(kAhead * E <= 32, "the flags of a round are one word");
+  [[maybe_unused]] W reg[kAhead][kHeld];
+  auto fetch = [&](int u, int s) {      // the piece's s-th step in the chain's order, one after the other
+    if (s < steps) {
+#pragma unroll
+      for (int j = 0; j < kHeld; ++j) {
+        const int i = j == 1 ? kX : j;
+        if (i != 2 || skip + s < a.T - 1) {
+          if constexpr (kAsync<T, E>) copy_async<sizeof(W)>(ring + (u * kHeld + j) * kStepThreads, in.p[i]);
+          else reg[u][j] = *reinterpret_cast<const W*>(in.p[i]);
         }
         in.p[i] += in.by[i];
       }
@@ -152,7 +173,7 @@ __global__ void __launch_bounds__(kStepThreads) k_steps(Scan a, int64_t width) {
   };
   const bool flags = a.done || a.done_prev;
   const Owner<E, MIXED> owner(m * E, width);
-  auto flag_of = [&](int s) { return flags && s < T_ ? owner.load(a, BACK ? T_ - 1 - s : s) : 0u; };
+  auto flag_of = [&](int s) { return flags && s < steps ? owner.load(a, BACK ? a.T - 1 - skip - s : skip + s) : 0u; };
   uint32_t flag[kAhead];
 #pragma unroll
   for (int u = 0; u < kAhead; ++u) {
@@ -160,14 +181,25 @@ __global__ void __launch_bounds__(kStepThreads) k_steps(Scan a, int64_t width) {
     if (kAsync<T, E> && u % kG == kG - 1) copy_commit();
     flag[u] = flag_of(u);
   }
+  float* const maps = SPLIT ? split.maps + blockIdx.y * split.m + m * E : nullptr;
+  const int64_t to_b = SPLIT ? gridDim.y * split.m : 0;
   float h[E];
-  load_state<E>(BACK ? (a.dhT ? a.dhT + m * E : nullptr) : (a.h0 ? a.h0 + m * E : nullptr), h);
+  [[maybe_unused]] Map q[E];
+  if constexpr (FOLD) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) q[e] = {1.0f, 0.0f};
+  } else if constexpr (SPLIT) {
+    after_previous();
+    load_state<E>(maps + to_b, h);
+  } else {
+    load_state<E>(BACK ? (a.dhT ? a.dhT + m * E : nullptr) : (a.h0 ? a.h0 + m * E : nullptr), h);
+  }
   const float* const h0 = a.h0 ? a.h0 + m * E : nullptr;
   const net_rows &ro = BACK ? a.dv : a.y, &rz = BACK ? a.df : a.y;
-  T* y = const_cast<T*>(base<T>(ro, n, d)) + (BACK ? (T_ - 1) * ro.outer : 0);
-  T* z = BACK ? const_cast<T*>(base<T>(rz, n, d)) + (T_ - 1) * rz.outer : nullptr;
+  T* y = const_cast<T*>(base<T>(ro, n, d)) + (BACK ? a.T - 1 - skip : skip) * ro.outer;
+  T* z = BACK ? const_cast<T*>(base<T>(rz, n, d)) + (a.T - 1 - skip) * rz.outer : nullptr;
   const int64_t ys = BACK ? -ro.outer : ro.outer, zs = -rz.outer;
-  for (int s0 = 0; s0 < T_; s0 += kAhead) {
+  for (int s0 = 0; s0 < steps; s0 += kAhead) {
     uint32_t ends = 0;
     if (flags) {
 #pragma unroll
@@ -177,14 +209,14 @@ __global__ void __launch_bounds__(kStepThreads) k_steps(Scan a, int64_t width) {
     }
 #pragma unroll
     for (int u0 = 0; u0 < kAhead; u0 += kG) {
-      if (s0 + u0 >= T_) break;
-      W w[kG][K];
+      if (s0 + u0 >= steps) break;
+      W w[kG][kHeld];
       if constexpr (kAsync<T, E>) copy_wait<kAhead / kG - 1>();
 #pragma unroll
       for (int u = 0; u < kG; ++u)
 #pragma unroll
-        for (int i = 0; i < K; ++i) {
-          if constexpr (kAsync<T, E>) w[u][i] = ring[((u0 + u) * K + i) * kStepThreads];
+        for (int i = 0; i < kHeld; ++i) {
+          if constexpr (kAsync<T, E>) w[u][i] = ring[((u0 + u) * kHeld + i) * kStepThreads];
           else w[u][i] = reg[u][i];
         }
 #pragma unroll
@@ -201,53 +233,167 @@ __global__ void __launch_bounds__(kStepThreads) k_steps(Scan a, int64_t width) {
 #pragma unroll
       for (int u = 0; u < kG; ++u) {
         const int s = s0 + u0 + u;
-        if (s < T_) {
-          step<T, E, BACK>(ga[u], gb[u], w[u][1], w[u][BACK ? 2 : 0], w[u][BACK ? 3 : 0], s == T_ - 1, h0,
-                           ends >> ((u0 + u) * E), y, z, h);
-          y += ys;
-          if constexpr (BACK) z += zs;
+        const uint32_t end = ends >> ((u0 + u) * E);
+        if (s < steps) {
+          if constexpr (FOLD) {
+            float x[E];
+            unpack<T, E>(w[u][1], x);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+              const bool cut = end >> e & 1u;
+              if constexpr (BACK) q[e].B = cut ? 0.0f : ga[u][e] * (x[e] + q[e].B);
+              else q[e].B = fmaf(ga[u][e], cut ? 0.0f : q[e].B, gb[u][e] * x[e]);
+              q[e].A = cut ? -0.0f : q[e].A * ga[u][e];
+            }
+          } else {
+            step<T, E, BACK>(ga[u], gb[u], w[u][1], w[u][BACK ? 2 : 0], w[u][BACK ? 3 : 0], skip + s == a.T - 1, h0, end, y,
+                             z, h);
+            y += ys;
+            if constexpr (BACK) z += zs;
+          }
         }
       }
     }
   }
   if constexpr (kAsync<T, E>) copy_wait<0>();
-  float* const out = BACK ? a.dh0 : a.hT;
-  if (out) store_state<E>(out + m * E, h);
+  if constexpr (FOLD) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) h[e] = q[e].A;
+    store_state<E>(maps, h);
+#pragma unroll
+    for (int e = 0; e < E; ++e) h[e] = q[e].B;
+    store_state<E>(maps + to_b, h);
+  } else {
+    float* const out = BACK ? a.dh0 : a.hT;
+    if (out && skip + steps == a.T) store_state<E>(out + m * E, h);
+  }
 }
 
-template <typename T, int E, bool BACK, bool MIXED>
-cudaError_t launch_steps(const Scan& a, int64_t width, cudaStream_t s) {
+// The states before the pieces, in the place of B.  A block has 8 channels and all pieces: each of its 128 groups of 8
+// lanes some pieces, one after the other.
+constexpr int kJoinThreads = 1024, kJoinChannels = 8, kJoinGroups = kJoinThreads / kJoinChannels;
+__global__ void __launch_bounds__(kJoinThreads) k_join(int pieces, int64_t m, float* maps, const float* from) {
+  __shared__ Map warps[kJoinThreads / 32][kJoinChannels];
+  after_previous();
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, group = threadIdx.x / kJoinChannels;
+  const int k = threadIdx.x % kJoinChannels;
+  const int64_t c = blockIdx.x * (int64_t)kJoinChannels + k;
+  const bool live = c < m;
+  const int each = (pieces + kJoinGroups - 1) / kJoinGroups, p0 = min(pieces, group * each);
+  const float* const A = maps + p0 * m + c;
+  float* const B = maps + (pieces + (int64_t)p0) * m + c;
+  const int n = live ? min(pieces, p0 + each) - p0 : 0;
+  constexpr int kBatch = 8;             // maps loaded at a time
+  auto batches = [&](auto take) {
+    for (int p = 0; p < n; p += kBatch) {
+      Map r[kBatch];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i)
+        if (p + i < n) r[i] = {A[(p + i) * m], B[(p + i) * m]};
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i)
+        if (p + i < n) take(p + i, r[i]);
+    }
+  };
+  Map q = {1.0f, 0.0f};
+  batches([&](int, const Map& r) { q = then(q, r); });
+#pragma unroll
+  for (int o = kJoinChannels; o < 32; o *= 2) {
+    const Map r = {__shfl_up_sync(0xffffffffu, q.A, o), __shfl_up_sync(0xffffffffu, q.B, o)};
+    if (lane >= o) q = then(r, q);
+  }
+  if (lane >= 32 - kJoinChannels) warps[warp][k] = q;
+  q = {__shfl_up_sync(0xffffffffu, q.A, kJoinChannels), __shfl_up_sync(0xffffffffu, q.B, kJoinChannels)};
+  __syncthreads();
+  float h = live && from ? from[c] : 0.0f;
+  for (int w = 0; w < warp; ++w) h = apply(warps[w][k], h);
+  if (lane >= kJoinChannels) h = apply(q, h);
+  batches([&](int p, const Map& r) {
+    B[p * m] = h;
+    h = apply(r, h);
+  });
+}
+
+// How the steps are gone through, by what each way costs (measured, in ns):
+//  walked by a thread a channel or more: 100 a step forward, 190 backward, whatever the channels (up to HBM's pace);
+//  in blocks, or clusters of them where channels are few (net_pieces.cu): 3,300 to 4,600 for every round of blocks, of
+//    32 channels x 256 steps each (128 in fp32 and backward), that fit the SMs, two each (one backward in fp32; clusters
+//    fill less of the device).  512 steps of bf16 forward, walked and so: 32,768 channels 49 and 34 us, 131,072 channels
+//    87 and 121;
+//  in pieces whose maps are written, joined and walked from, where channels are few: 14,000, and their inputs twice, at
+//    6 TB/s.  65,536 steps of 256 bf16 channels: 4,960 us walked, 74 in clusters, 49 so; 8,192 of 500: 18.6 in
+//    clusters, 20 so.
+enum class Way { kWalk, kBlocks, kPieces };
+Way way_of(int T, int64_t m, int size, bool back) {
+  if (T < 32) return Way::kWalk;
+  const int64_t sms = sm_count(), tiles = (m + 31) / 32;
+  const bool clusters = tiles * 8 < sms, large = back && size == 4;
+  const int64_t rows = back || size == 4 ? 128 : 256;
+  const int64_t blocks = clusters ? std::min<int64_t>(128, (m + 15) / 16 * 8) : large ? sms : 2 * sms;
+  const double round = large ? (clusters ? 6600 : 3300) : back ? 3900 : size == 4 ? 3300 : 4600;
+  const double walk = (double)T * (back ? 190 : 100);
+  const double held = round * (double)((tiles * ((T + rows - 1) / rows) + blocks - 1) / blocks);
+  const double pieces = 14000.0 + (double)T * (double)m * size * (back ? 8 : 5) / 6000.0;
+  const bool split = clusters && pieces < held;
+  if (walk <= (split ? pieces : held)) return Way::kWalk;
+  return split ? Way::kPieces : Way::kBlocks;
+}
+
+// The pieces: for 1,024 threads an SM, of 32 steps at least.
+Split split_of(int T, int64_t m, float* ws) {
+  const int64_t threads = std::max<int64_t>(1, m / 4);
+  const int64_t want = std::max<int64_t>(1, std::min<int64_t>((int64_t)sm_count() * 1024 / threads, std::min(2048, T / 32)));
+  return {(int)((T + want - 1) / want), m, ws};
+}
+int pieces_of(const Split& s, int T) { return (T + s.rows - 1) / s.rows; }
+
+template <typename T, int E, bool BACK, bool MIXED, bool SPLIT, bool FOLD>
+cudaError_t launch_steps(const Scan& a, int64_t width, const Split& split, cudaStream_t s) {
   const int64_t blocks = (a.N * (a.D / E) + kStepThreads - 1) / kStepThreads;
   // slots: of a short sequence as many as it has steps, whole groups of them (a group is read whole)
   constexpr int kAhead = kAheadOf<E>, kG = kGroup<E>;
-  const int ahead = a.T < kAhead ? (a.T + kG - 1) / kG * kG : kAhead;
-  const int smem = kAsync<T, E> ? ahead * Inputs<T, BACK>::kN * kStepThreads * (int)sizeof(T) * E : 0;
-  const auto kern = k_steps<T, E, BACK, MIXED>;
+  const int ahead = split.rows < kAhead ? (split.rows + kG - 1) / kG * kG : kAhead;
+  const int held = FOLD ? 2 : Inputs<T, BACK>::kN;
+  const int smem = kAsync<T, E> ? ahead * held * kStepThreads * (int)sizeof(T) * E : 0;
+  const auto kern = k_steps<T, E, BACK, MIXED, SPLIT, FOLD>;
   if (smem > 48 * 1024) {
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
   }
-  kern<<<(unsigned)blocks, kStepThreads, smem, s>>>(a, width);
+  const dim3 grid((unsigned)blocks, (unsigned)pieces_of(split, a.T));
+  if (SPLIT && !FOLD) return launch_after(kern, grid, kStepThreads, smem, s, a, width, split);
+  kern<<<grid, kStepThreads, smem, s>>>(a, width, split);
   return cudaGetLastError();
 }
 
 template <typename T, int E, bool BACK, bool MIXED>
-cudaError_t launch_walk(const Scan& a, int64_t width, cudaStream_t s) {
+cudaError_t launch_walk(const Scan& a, int64_t width, const Split& split, cudaStream_t s) {
   if (a.T == 1) {
     k_one<T, E, BACK, MIXED><<<(unsigned)((a.N * (a.D / E) + 255) / 256), 256, 0, s>>>(a, width);
     return cudaGetLastError();
   }
-  if constexpr (E <= 4) return launch_steps<T, E, BACK, MIXED>(a, width, s);
-  else return cudaErrorInvalidValue;   // not asked for
+  if constexpr (E <= 4) {
+    if (split.maps) {
+      cudaError_t e = launch_steps<T, E, BACK, MIXED, true, true>(a, width, split, s);
+      if (e != cudaSuccess) return e;
+      e = launch_after(k_join, dim3((unsigned)((split.m + kJoinChannels - 1) / kJoinChannels)), kJoinThreads, 0, s,
+                       pieces_of(split, a.T), split.m,
+                       split.maps, BACK ? a.dhT : a.h0);
+      return e != cudaSuccess ? e : launch_steps<T, E, BACK, MIXED, true, false>(a, width, split, s);
+    }
+    return launch_steps<T, E, BACK, MIXED, false, false>(a, width, split, s);
+  } else {
+    return cudaErrorInvalidValue;   // not asked for
+  }
 }
 
 template <typename T, bool BACK, bool MIXED>
-cudaError_t launch_width(const Scan& a, int64_t width, int e, cudaStream_t s) {
+cudaError_t launch_width(const Scan& a, int64_t width, int e, const Split& split, cudaStream_t s) {
   if constexpr (sizeof(T) == 2)
-    if (e == 8) return launch_walk<T, 8, BACK, MIXED>(a, width, s);
-  if (e == 4) return launch_walk<T, 4, BACK, MIXED>(a, width, s);
-  if (e == 2) return launch_walk<T, 2, BACK, MIXED>(a, width, s);
-  return launch_walk<T, 1, BACK, false>(a, width, s);
+    if (e == 8) return launch_walk<T, 8, BACK, MIXED>(a, width, split, s);
+  if (e == 4) return launch_walk<T, 4, BACK, MIXED>(a, width, split, s);
+  if (e == 2) return launch_walk<T, 2, BACK, MIXED>(a, width, split, s);
+  return launch_walk<T, 1, BACK, false>(a, width, split, s);
 }
 
 // T = 0: the state passes as it is.
@@ -257,28 +403,22 @@ __global__ void k_none(int64_t m, const float* from, float* to) {
 }
 
 template <typename T, bool BACK>
-cudaError_t launch(const Scan& a, cudaStream_t s) {
+cudaError_t launch(const Scan& a, float* ws, cudaStream_t s) {
   const int64_t m = a.N * a.D, sms = sm_count();
   if (a.T == 0) {
     float* const to = BACK ? a.dh0 : a.hT;
     if (to) k_none<<<(unsigned)((m + 255) / 256), 256, 0, s>>>(m, BACK ? a.dhT : a.h0, to);
     return cudaGetLastError();
   }
-  // Walking the steps takes some 100 ns a step forward and 190 backward, whatever the channels (up to HBM's pace);
-  // splitting them 4 us for every round of pieces (32 channels x 256 steps, 128 backward in fp32) that the SMs' two
-  // blocks (one) take.  512 steps of bf16, forward: 32,768 channels 49 and 34 us, 131,072 channels 87 and 121.
-  if (a.T >= 32) {
-    constexpr bool kLarge = BACK && sizeof(T) == 4;
-    const int64_t rows = kLarge ? 128 : 256, blocks = kLarge ? sms : 2 * sms;
-    const int64_t rounds = ((m + 31) / 32 * ((a.T + rows - 1) / rows) + blocks - 1) / blocks;
-    if ((int64_t)a.T * (BACK ? 190 : 100) > 4000 * rounds) return launch_pieces<T>(a, BACK, s);
-  }
   // Channels of a thread: for one step as many as 16 bytes hold; over many steps four, since half as many bytes a
   // thread make twice the threads (4,096 envs x 256 channels x 128 steps of bf16: 127 us, 137 with eight), and two
   // where four would leave fewer than 160 threads an SM (512 steps, 65,536 channels: 55 us, 75 with four; 131,072: 99
   // and 86).
+  const Way way = way_of(a.T, m, sizeof(T), BACK);
+  if (way == Way::kBlocks) return launch_pieces<T>(a, BACK, s);
+  const Split split = way == Way::kPieces ? split_of(a.T, m, ws) : Split{a.T, m, nullptr};
   int most = 16 / (int)sizeof(T);
-  if (a.T > 1) most = m >= 4 * 160 * sms ? 4 : 2;
+  if (a.T > 1) most = split.maps || m >= 4 * 160 * sms ? 4 : 2;
   const net_rows* rows[] = {&a.f, &a.v, &a.y, &a.dy, &a.df, &a.dv};
   constexpr int kArrays = BACK ? 6 : 3;
   auto fits = [&](int e, int64_t n) {
@@ -292,13 +432,13 @@ cudaError_t launch(const Scan& a, cudaStream_t s) {
   for (int i = 0; i < kArrays; ++i) one_row = one_row && rows[i]->inner == a.D;
   flat.D = m, flat.N = 1;
   for (int e = most; e > 1; e /= 2) {
-    if (a.D % e == 0 && fits(e, a.N)) return launch_width<T, BACK, false>(a, a.D, e, s);
-    if (one_row && m % e == 0 && a.D >= e && fits(e, 1)) return launch_width<T, BACK, true>(flat, a.D, e, s);
+    if (a.D % e == 0 && fits(e, a.N)) return launch_width<T, BACK, false>(a, a.D, e, split, s);
+    if (one_row && m % e == 0 && a.D >= e && fits(e, 1)) return launch_width<T, BACK, true>(flat, a.D, e, split, s);
   }
-  return launch_width<T, BACK, false>(a, a.D, 1, s);
+  return launch_width<T, BACK, false>(a, a.D, 1, split, s);
 }
 
-int run(const net_scan* p, bool back, void* stream) {
+int check(const net_scan* p) {
   if (!p) return fail(AUV_ERR_INVALID, "argument block is NULL");
   if (p->struct_size != sizeof(net_scan))
     return fail(AUV_ERR_INVALID, "struct_size %u, expected %zu", p->struct_size, sizeof(net_scan));
@@ -307,10 +447,15 @@ int run(const net_scan* p, bool back, void* stream) {
   const int64_t most = (int64_t)1 << 37;   // channels of a call: blocks stay below 2^31
   if (p->N > most || p->D > most || (p->N && p->D > most / p->N) || p->T > INT32_MAX)
     return fail(AUV_ERR_UNSUPPORTED, "N * D past 2^37 or T past 2^31");
+  return AUV_OK;
+}
+
+int run(const net_scan* p, bool back, void* stream) {
+  int rc = check(p);
+  if (rc) return rc;
   const int64_t M = p->N * p->D;
   if (M == 0) return AUV_OK;
   const int z = type_size(p->dtype);
-  int rc;
   struct { const net_rows* r; const char* name; bool out, back; } rows[] = {
       {&p->f, "f", false, false}, {&p->v, "v", false, false}, {&p->y, "y", !back, false},
       {&p->dy, "dy", false, true}, {&p->df, "df", true, true}, {&p->dv, "dv", true, true}};
@@ -324,16 +469,22 @@ int run(const net_scan* p, bool back, void* stream) {
     if (q.p && q.used && (rc = need(q.p, q.name, q.align))) return rc;
   const Scan a = {(int)p->T, p->N, p->D, p->f, p->v, p->y, p->dy, p->df, p->dv, p->h0, p->hT, p->dhT, p->dh0, p->done,
                   p->done_prev, p->N};
+  const size_t bytes = net_gate_scan_workspace_bytes(p, back);
+  if (bytes) {
+    if (p->workspace_bytes < bytes) return fail(AUV_ERR_SIZE, "workspace of %zu bytes, %zu needed", p->workspace_bytes, bytes);
+    if ((rc = need(p->workspace, "workspace", 16))) return rc;
+  }
+  float* const ws = static_cast<float*>(p->workspace);
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaError_t e;
   if (back)
-    e = p->dtype == NET_FP32   ? launch<float, true>(a, s)
-        : p->dtype == NET_BF16 ? launch<__nv_bfloat16, true>(a, s)
-                               : launch<__half, true>(a, s);
+    e = p->dtype == NET_FP32   ? launch<float, true>(a, ws, s)
+        : p->dtype == NET_BF16 ? launch<__nv_bfloat16, true>(a, ws, s)
+                               : launch<__half, true>(a, ws, s);
   else
-    e = p->dtype == NET_FP32   ? launch<float, false>(a, s)
-        : p->dtype == NET_BF16 ? launch<__nv_bfloat16, false>(a, s)
-                               : launch<__half, false>(a, s);
+    e = p->dtype == NET_FP32   ? launch<float, false>(a, ws, s)
+        : p->dtype == NET_BF16 ? launch<__nv_bfloat16, false>(a, ws, s)
+                               : launch<__half, false>(a, ws, s);
   return e == cudaSuccess ? AUV_OK : cuda_fail(e, back ? "net_gate_scan_backward" : "net_gate_scan");
 }
 
@@ -342,6 +493,14 @@ int run(const net_scan* p, bool back, void* stream) {
 }  // namespace auv
 
 extern "C" {
+
+size_t net_gate_scan_workspace_bytes(const net_scan* a, int backward) {
+  using namespace auv::net;
+  if (!a || check(a) || !a->T || !a->N || !a->D) return 0;
+  const int64_t m = a->N * a->D;
+  if (way_of((int)a->T, m, type_size(a->dtype), backward) != Way::kPieces) return 0;
+  return sizeof(float) * 2 * (size_t)pieces_of(split_of((int)a->T, m, nullptr), (int)a->T) * (size_t)m;
+}
 
 int net_gate_scan(const net_scan* a, void* stream) { return auv::net::run(a, false, stream); }
 int net_gate_scan_backward(const net_scan* a, void* stream) { return auv::net::run(a, true, stream); }

@@ -46,6 +46,17 @@ struct Inputs {
   }
 };
 
+// An affine map h -> A h + B of one channel.  A piece with an episode end in it passes nothing on, whatever came
+// before (NaN times 0 included): its A is -0, and the sign is asked for; gates are never negative.
+struct Map {
+  float A, B;
+};
+__device__ __forceinline__ bool cuts(float A) { return __float_as_uint(A) >> 31; }
+__device__ __forceinline__ Map then(const Map& p, const Map& q) {   // p, then q
+  return cuts(q.A) ? q : Map{p.A * q.A, fmaf(q.A, p.B, q.B)};
+}
+__device__ __forceinline__ float apply(const Map& q, float h) { return cuts(q.A) ? q.B : fmaf(q.A, h, q.B); }
+
 // Few channels, many steps (net_pieces.cu); back: the gradients.
 constexpr int kPieceThreads = 256;
 template <typename T> cudaError_t launch_pieces(const Scan& a, bool back, cudaStream_t s);

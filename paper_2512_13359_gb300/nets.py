@@ -19,12 +19,12 @@ from .auvenv import AUV_ERR_INVALID, AUV_ERR_SIZE, AUV_OK, AuvError
 NET_DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 NET_ACT = {"none": 0, "relu": 1, "silu": 2, "tanh": 3}
 
-EXPORTED = ("net_gate_scan", "net_gate_scan_backward", "net_group_norm_workspace_bytes", "net_group_norm",
+EXPORTED = ("net_gate_scan_workspace_bytes", "net_gate_scan", "net_gate_scan_backward", "net_group_norm_workspace_bytes", "net_group_norm",
             "net_group_norm_backward", "net_dropout", "net_last_error")
 
 # The argument blocks, field by field as in the header (native alignment).
 _ROWS = "Pqq"
-_SCAN = struct.Struct("@II3q" + 6 * _ROWS + "6P")
+_SCAN = struct.Struct("@II3q" + 6 * _ROWS + "7PN")
 _NORM = struct.Struct("@IIIf4q" + 4 * _ROWS + "7PN")
 _DROP = struct.Struct("@4I3q" + 3 * _ROWS + "dQQ")
 _NO_ROWS = (0, 0, 0)
@@ -41,8 +41,9 @@ def lib():
                      "net_dropout"):
             getattr(L, name).argtypes = [C.c_char_p, C.c_void_p]
             getattr(L, name).restype = C.c_int
-        L.net_group_norm_workspace_bytes.argtypes = [C.c_char_p, C.c_int]
-        L.net_group_norm_workspace_bytes.restype = C.c_size_t
+        for name in ("net_gate_scan_workspace_bytes", "net_group_norm_workspace_bytes"):
+            getattr(L, name).argtypes = [C.c_char_p, C.c_int]
+            getattr(L, name).restype = C.c_size_t
         L.net_last_error.restype = C.c_char_p
         _lib = L
     return _lib
@@ -110,6 +111,17 @@ def _flags(t, name, shape, device):
     return _flat(t, name, shape, torch.bool if t is not None and t.dtype == torch.bool else torch.uint8, device)
 
 
+def _call_with_workspace(fn, size_of, backward, form, fields, device, stream, scratch):
+    """A call whose argument block ends in a workspace, allocated here if one is needed."""
+    need = size_of(form.pack(*fields, 0, 0), backward)
+    ws = 0
+    if need:
+        buf = torch.empty(need, dtype=torch.uint8, device=device)
+        scratch.append(buf)
+        ws = buf.data_ptr()
+    _call(fn, form.pack(*fields, ws, need), device, stream, scratch)
+
+
 def gate_scan(f, v, h0=None, *, done=None, done_prev=None, y=None, hT=None, stream=None):
     """Gated linear recurrence h[t] = a c[t] + (1 - a) v[t], a = sigmoid(f[t]), over f, v [T, N, D]; c[t] is h[t - 1], or
     0 where an episode ended before step t (done [T, N]: after the step; done_prev [N]: before step 0).  Returns
@@ -125,10 +137,11 @@ def gate_scan(f, v, h0=None, *, done=None, done_prev=None, y=None, hT=None, stre
     if hT is None:
         hT = torch.empty((N, D), dtype=f32, device=dev)
         scratch.append(hT)
-    args = _SCAN.pack(_SCAN.size, NET_DTYPE[f.dtype], T, N, D, *rf, *rv, *_rows(y, "y", f), *_NO_ROWS, *_NO_ROWS,
-                      *_NO_ROWS, _flat(h0, "h0", (N, D), f32, dev), _flat(hT, "hT", (N, D), f32, dev), 0, 0,
-                      _flags(done, "done", (T, N), dev), _flags(done_prev, "done_prev", (N,), dev))
-    _call(lib().net_gate_scan, args, dev, stream, scratch)
+    fields = (_SCAN.size, NET_DTYPE[f.dtype], T, N, D, *rf, *rv, *_rows(y, "y", f), *_NO_ROWS, *_NO_ROWS, *_NO_ROWS,
+              _flat(h0, "h0", (N, D), f32, dev), _flat(hT, "hT", (N, D), f32, dev), 0, 0,
+              _flags(done, "done", (T, N), dev), _flags(done_prev, "done_prev", (N,), dev))
+    L = lib()
+    _call_with_workspace(L.net_gate_scan, L.net_gate_scan_workspace_bytes, 0, _SCAN, fields, dev, stream, scratch)
     return y, hT
 
 
@@ -150,11 +163,12 @@ def gate_scan_backward(f, v, y, dy, h0=None, *, done=None, done_prev=None, dhT=N
     if dh0 is None:
         dh0 = torch.empty((N, D), dtype=f32, device=dev)
         scratch.append(dh0)
-    args = _SCAN.pack(_SCAN.size, NET_DTYPE[f.dtype], T, N, D, *rf, *rv, *ry, *rdy, *_rows(df, "df", f),
-                      *_rows(dv, "dv", f), _flat(h0, "h0", (N, D), f32, dev), 0,
-                      _flat(dhT, "dhT", (N, D), f32, dev), _flat(dh0, "dh0", (N, D), f32, dev),
-                      _flags(done, "done", (T, N), dev), _flags(done_prev, "done_prev", (N,), dev))
-    _call(lib().net_gate_scan_backward, args, dev, stream, scratch)
+    fields = (_SCAN.size, NET_DTYPE[f.dtype], T, N, D, *rf, *rv, *ry, *rdy, *_rows(df, "df", f), *_rows(dv, "dv", f),
+              _flat(h0, "h0", (N, D), f32, dev), 0, _flat(dhT, "dhT", (N, D), f32, dev),
+              _flat(dh0, "dh0", (N, D), f32, dev), _flags(done, "done", (T, N), dev),
+              _flags(done_prev, "done_prev", (N,), dev))
+    L = lib()
+    _call_with_workspace(L.net_gate_scan_backward, L.net_gate_scan_workspace_bytes, 1, _SCAN, fields, dev, stream, scratch)
     return df, dv, dh0
 
 
@@ -168,17 +182,6 @@ def _groups(groups):
     if not isinstance(groups, int) or groups < 1:
         _fail(AUV_ERR_INVALID, f"groups {groups!r} is no positive number")
     return groups
-
-
-def _norm(fn, backward, dev, head, ptrs, stream, scratch):
-    """Allocates the workspace and calls."""
-    need = lib().net_group_norm_workspace_bytes(_NORM.pack(*head, *ptrs, 0, 0), backward)
-    ws = 0
-    if need:
-        buf = torch.empty(need, dtype=torch.uint8, device=dev)
-        scratch.append(buf)
-        ws = buf.data_ptr()
-    _call(fn, _NORM.pack(*head, *ptrs, ws, need), dev, stream, scratch)
 
 
 def group_norm(x, groups, gamma=None, beta=None, *, eps=1e-5, act="none", y=None, mean=None, rstd=None, stream=None):
@@ -202,7 +205,8 @@ def group_norm(x, groups, gamma=None, beta=None, *, eps=1e-5, act="none", y=None
             *_NO_ROWS)
     ptrs = (_flat(gamma, "gamma", (Ch,), f32, dev), _flat(beta, "beta", (Ch,), f32, dev),
             _flat(mean, "mean", (B, groups), f32, dev), _flat(rstd, "rstd", (B, groups), f32, dev), 0, 0)
-    _norm(lib().net_group_norm, 0, dev, head, ptrs, stream, scratch)
+    L = lib()
+    _call_with_workspace(L.net_group_norm, L.net_group_norm_workspace_bytes, 0, _NORM, head + ptrs, dev, stream, scratch)
     return y, mean, rstd
 
 
@@ -228,7 +232,9 @@ def group_norm_backward(x, groups, gamma, beta, mean, rstd, dy, *, act="none", d
     ptrs = (_flat(gamma, "gamma", (Ch,), f32, dev), _flat(beta, "beta", (Ch,), f32, dev),
             _flat(mean, "mean", (B, groups), f32, dev), _flat(rstd, "rstd", (B, groups), f32, dev),
             _flat(dgamma, "dgamma", (Ch,), f32, dev), _flat(dbeta, "dbeta", (Ch,), f32, dev))
-    _norm(lib().net_group_norm_backward, 1, dev, head, ptrs, stream, scratch)
+    L = lib()
+    _call_with_workspace(L.net_group_norm_backward, L.net_group_norm_workspace_bytes, 1, _NORM, head + ptrs, dev, stream,
+                         scratch)
     return dx, dgamma, dbeta
 
 

@@ -29,7 +29,7 @@ def test_exports_what_the_header_declares(nets):
 
 def _blocks(nets):
     z = nets._NO_ROWS
-    scan = [nets._SCAN.size, 0, 1, 1, 1, *(6 * z), *(6 * (0,))]
+    scan = [nets._SCAN.size, 0, 1, 1, 1, *(6 * z), *(7 * (0,)), 0]
     norm = [nets._NORM.size, 0, 0, 1e-5, 1, 1, 4, 2, *(4 * z), *(7 * (0,)), 0]
     drop = [nets._DROP.size, 0, 0, 0, 1, 1, 1, *(3 * z), 0.5, 0, 0]
     return {"net_gate_scan": (nets._SCAN, scan), "net_gate_scan_backward": (nets._SCAN, scan),
@@ -67,6 +67,7 @@ def test_null_blocks_and_empty_calls(nets):
         fields[n] = 0                                            # no channels: nothing to read or write
         assert getattr(nets.lib(), fn)(form.pack(*fields), None) == 0
     assert nets.lib().net_group_norm_workspace_bytes(None, 0) == 0
+    assert nets.lib().net_gate_scan_workspace_bytes(None, 0) == 0
 
 
 def test_wrong_tensors_are_rejected(nets):
