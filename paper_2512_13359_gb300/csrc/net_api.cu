@@ -1,4 +1,5 @@
 // net_api.cu -- the network operators' error text and argument checks.
+#include <atomic>
 #include <cstdarg>
 
 #include "net_common.cuh"
@@ -55,10 +56,18 @@ int need_rows(const net_rows& r, const char* name, int64_t ni, int64_t nj, int64
 }
 
 int sm_count() {
+  static std::atomic<int> known[64];
   int dev = 0, n = 152;
   cudaGetDevice(&dev);
-  cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
-  return n > 0 ? n : 152;
+  if (dev < 0 || dev >= 64) return n;
+  const int k = known[dev].load(std::memory_order_relaxed);
+  if (k) return k;
+  if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) {
+    cudaGetLastError();
+    return 152;
+  }
+  known[dev].store(n, std::memory_order_relaxed);
+  return n;
 }
 
 }  // namespace net

@@ -53,73 +53,80 @@ def _fail(code, msg):
     raise AuvError(code, msg)
 
 
-def _call(fn, args, device, stream, scratch=()):
-    """One call with `device` current.  `scratch`: what was allocated here for it."""
-    current = torch.cuda.current_stream(device)
-    s = current if stream is None else stream
-    if stream is not None and stream.cuda_stream != current.cuda_stream:
-        # memory allocated here belongs to the current stream: order its earlier use before the
-        # call, and keep it from being handed out again until the call has run
-        if scratch:
-            s.wait_stream(current)
-        for t in scratch:
-            t.record_stream(s)
-    if device.index == torch.cuda.current_device():
-        rc = fn(args, s.cuda_stream)
+def _call(fn, args, index, stream, scratch):
+    """One call on device `index`.  `scratch`: what was allocated here for it."""
+    if stream is None:
+        handle = torch._C._cuda_getCurrentRawStream(index)
     else:
-        with torch.cuda.device(device):
-            rc = fn(args, s.cuda_stream)
+        handle = stream.cuda_stream
+        current = torch.cuda.current_stream(index)
+        if scratch and handle != current.cuda_stream:
+            # memory allocated here belongs to the current stream: order its earlier use before the
+            # call, and keep it from being handed out again until the call has run
+            stream.wait_stream(current)
+            for t in scratch:
+                t.record_stream(stream)
+    if index == torch.cuda.current_device():
+        rc = fn(args, handle)
+    else:
+        with torch.cuda.device(index):
+            rc = fn(args, handle)
     if rc != AUV_OK:
         raise AuvError(rc, lib().net_last_error().decode())
 
 
 def _activation(x, name):
-    """Checks of the tensor that sets shape, type and device of a call."""
+    """(shape, type, device) of the tensor that sets those of a call."""
     if not isinstance(x, torch.Tensor) or x.dim() != 3:
         _fail(AUV_ERR_INVALID, f"{name} is not a tensor of three axes")
     if x.dtype not in NET_DTYPE:
         _fail(AUV_ERR_INVALID, f"{name}: type {x.dtype} is none of float32, bfloat16, float16")
     if not x.is_cuda:
         _fail(AUV_ERR_SIZE, f"{name} is not device memory")
-    return _rows(x, name, x)
+    return x.shape, x.dtype, x.get_device()
 
 
 def _rows(t, name, like):
-    """(pointer, outer, inner) of an activation of the shape, type and device of `like`."""
-    if t is not like and (t.shape != like.shape or t.dtype != like.dtype or t.device != like.device):
+    """(pointer, outer, inner) of an activation of the (shape, type, device) `like`."""
+    shape, dtype, index = like
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != index:
         _fail(AUV_ERR_INVALID, f"{name}: {tuple(t.shape)} {t.dtype} on {t.device}, expected "
-                               f"{tuple(like.shape)} {like.dtype} on {like.device}")
+                               f"{tuple(shape)} {dtype} on device {index}")
     outer, inner, last = t.stride()
-    if last != 1 and t.shape[2] > 1:
+    if last != 1 and shape[2] > 1:
         _fail(AUV_ERR_SIZE, f"{name}: channels are not contiguous (stride {last})")
     return t.data_ptr(), outer, inner
 
 
-def _flat(t, name, shape, dtype, device):
+def _flat(t, name, shape, dtype, index):
     """Pointer of a contiguous array, 0 for None."""
     if t is None:
         return 0
-    if t.shape != shape or t.dtype != dtype or t.device != device:
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != index:
         _fail(AUV_ERR_INVALID, f"{name}: {tuple(t.shape)} {t.dtype} on {t.device}, expected "
-                               f"{tuple(shape)} {dtype} on {device}")
+                               f"{tuple(shape)} {dtype} on device {index}")
     if not t.is_contiguous():
         _fail(AUV_ERR_SIZE, f"{name} is not contiguous")
     return t.data_ptr()
 
 
-def _flags(t, name, shape, device):
-    return _flat(t, name, shape, torch.bool if t is not None and t.dtype == torch.bool else torch.uint8, device)
+def _flags(t, name, shape, index):
+    return _flat(t, name, shape, torch.bool if t is not None and t.dtype is torch.bool else torch.uint8, index)
 
 
-def _call_with_workspace(fn, size_of, backward, form, fields, device, stream, scratch):
+def _new(shape, dtype, index, scratch):
+    t = torch.empty(shape, dtype=dtype, device=index)
+    scratch.append(t)
+    return t
+
+
+def _call_with_workspace(fn, size_of, backward, form, fields, index, stream, scratch):
     """A call whose argument block ends in a workspace, allocated here if one is needed."""
-    need = size_of(form.pack(*fields, 0, 0), backward)
-    ws = 0
+    args = form.pack(*fields, 0, 0)
+    need = size_of(args, backward)
     if need:
-        buf = torch.empty(need, dtype=torch.uint8, device=device)
-        scratch.append(buf)
-        ws = buf.data_ptr()
-    _call(fn, form.pack(*fields, ws, need), device, stream, scratch)
+        args = form.pack(*fields, _new(need, torch.uint8, index, scratch).data_ptr(), need)
+    _call(fn, args, index, stream, scratch)
 
 
 def gate_scan(f, v, h0=None, *, done=None, done_prev=None, y=None, hT=None, stream=None):
@@ -127,21 +134,21 @@ def gate_scan(f, v, h0=None, *, done=None, done_prev=None, y=None, hT=None, stre
     0 where an episode ended before step t (done [T, N]: after the step; done_prev [N]: before step 0).  Returns
     (y [T, N, D], hT [N, D] fp32).  hT may be h0: a state updated in place."""
     scratch = []
-    rf = _activation(f, "f")
-    T, N, D = f.shape
-    dev, f32 = f.device, torch.float32
-    rv = _rows(v, "v", f)
+    like = shape, dtype, index = _activation(f, "f")
+    T, N, D = shape
+    f32 = torch.float32
     if y is None:
-        y = torch.empty((T, N, D), dtype=f.dtype, device=dev)
-        scratch.append(y)
+        y = _new(shape, dtype, index, scratch)
     if hT is None:
-        hT = torch.empty((N, D), dtype=f32, device=dev)
-        scratch.append(hT)
-    fields = (_SCAN.size, NET_DTYPE[f.dtype], T, N, D, *rf, *rv, *_rows(y, "y", f), *_NO_ROWS, *_NO_ROWS, *_NO_ROWS,
-              _flat(h0, "h0", (N, D), f32, dev), _flat(hT, "hT", (N, D), f32, dev), 0, 0,
-              _flags(done, "done", (T, N), dev), _flags(done_prev, "done_prev", (N,), dev))
+        hT = _new((N, D), f32, index, scratch)
+    fields = (_SCAN.size, NET_DTYPE[dtype], T, N, D, *_rows(f, "f", like), *_rows(v, "v", like), *_rows(y, "y", like),
+              *_NO_ROWS, *_NO_ROWS, *_NO_ROWS, _flat(h0, "h0", (N, D), f32, index), _flat(hT, "hT", (N, D), f32, index),
+              0, 0, _flags(done, "done", (T, N), index), _flags(done_prev, "done_prev", (N,), index))
     L = lib()
-    _call_with_workspace(L.net_gate_scan, L.net_gate_scan_workspace_bytes, 0, _SCAN, fields, dev, stream, scratch)
+    if T < 32:                        # short sequences need no workspace
+        _call(L.net_gate_scan, _SCAN.pack(*fields, 0, 0), index, stream, scratch)
+    else:
+        _call_with_workspace(L.net_gate_scan, L.net_gate_scan_workspace_bytes, 0, _SCAN, fields, index, stream, scratch)
     return y, hT
 
 
@@ -150,38 +157,35 @@ def gate_scan_backward(f, v, y, dy, h0=None, *, done=None, done_prev=None, dhT=N
     """Gradients (df, dv, dh0) of gate_scan from dy [T, N, D] and dhT [N, D] (None: zeros); y as gate_scan stored it,
     the other arguments as given to it."""
     scratch = []
-    rf = _activation(f, "f")
-    T, N, D = f.shape
-    dev, f32 = f.device, torch.float32
-    rv, ry, rdy = _rows(v, "v", f), _rows(y, "y", f), _rows(dy, "dy", f)
+    like = shape, dtype, index = _activation(f, "f")
+    T, N, D = shape
+    f32 = torch.float32
     if df is None:
-        df = torch.empty((T, N, D), dtype=f.dtype, device=dev)
-        scratch.append(df)
+        df = _new(shape, dtype, index, scratch)
     if dv is None:
-        dv = torch.empty((T, N, D), dtype=f.dtype, device=dev)
-        scratch.append(dv)
+        dv = _new(shape, dtype, index, scratch)
     if dh0 is None:
-        dh0 = torch.empty((N, D), dtype=f32, device=dev)
-        scratch.append(dh0)
-    fields = (_SCAN.size, NET_DTYPE[f.dtype], T, N, D, *rf, *rv, *ry, *rdy, *_rows(df, "df", f), *_rows(dv, "dv", f),
-              _flat(h0, "h0", (N, D), f32, dev), 0, _flat(dhT, "dhT", (N, D), f32, dev),
-              _flat(dh0, "dh0", (N, D), f32, dev), _flags(done, "done", (T, N), dev),
-              _flags(done_prev, "done_prev", (N,), dev))
+        dh0 = _new((N, D), f32, index, scratch)
+    fields = (_SCAN.size, NET_DTYPE[dtype], T, N, D, *_rows(f, "f", like), *_rows(v, "v", like), *_rows(y, "y", like),
+              *_rows(dy, "dy", like), *_rows(df, "df", like), *_rows(dv, "dv", like),
+              _flat(h0, "h0", (N, D), f32, index), 0, _flat(dhT, "dhT", (N, D), f32, index),
+              _flat(dh0, "dh0", (N, D), f32, index), _flags(done, "done", (T, N), index),
+              _flags(done_prev, "done_prev", (N,), index))
     L = lib()
-    _call_with_workspace(L.net_gate_scan_backward, L.net_gate_scan_workspace_bytes, 1, _SCAN, fields, dev, stream, scratch)
+    if T < 32:
+        _call(L.net_gate_scan_backward, _SCAN.pack(*fields, 0, 0), index, stream, scratch)
+    else:
+        _call_with_workspace(L.net_gate_scan_backward, L.net_gate_scan_workspace_bytes, 1, _SCAN, fields, index, stream,
+                             scratch)
     return df, dv, dh0
 
 
-def _act(act):
+def _norm_head(act, groups):
     if act not in NET_ACT:
         _fail(AUV_ERR_INVALID, f"act {act!r} is none of {', '.join(NET_ACT)}")
-    return NET_ACT[act]
-
-
-def _groups(groups):
     if not isinstance(groups, int) or groups < 1:
         _fail(AUV_ERR_INVALID, f"groups {groups!r} is no positive number")
-    return groups
+    return NET_ACT[act]
 
 
 def group_norm(x, groups, gamma=None, beta=None, *, eps=1e-5, act="none", y=None, mean=None, rstd=None, stream=None):
@@ -189,24 +193,21 @@ def group_norm(x, groups, gamma=None, beta=None, *, eps=1e-5, act="none", y=None
     channels over all S positions (groups = 1 and S = 1: layer norm).  act: "none", "relu", "silu" or "tanh".  Returns
     (y [B, S, C], mean [B, groups], rstd [B, groups])."""
     scratch = []
-    rx = _activation(x, "x")
-    B, S, Ch = x.shape
-    dev, f32 = x.device, torch.float32
+    like = shape, dtype, index = _activation(x, "x")
+    kind = _norm_head(act, groups)
+    B, S, Ch = shape
+    f32, stats = torch.float32, (B, groups)
     if y is None:
-        y = torch.empty((B, S, Ch), dtype=x.dtype, device=dev)
-        scratch.append(y)
+        y = _new(shape, dtype, index, scratch)
     if mean is None:
-        mean = torch.empty((B, _groups(groups)), dtype=f32, device=dev)
-        scratch.append(mean)
+        mean = _new(stats, f32, index, scratch)
     if rstd is None:
-        rstd = torch.empty((B, groups), dtype=f32, device=dev)
-        scratch.append(rstd)
-    head = (_NORM.size, NET_DTYPE[x.dtype], _act(act), eps, B, S, Ch, _groups(groups), *rx, *_rows(y, "y", x), *_NO_ROWS,
-            *_NO_ROWS)
-    ptrs = (_flat(gamma, "gamma", (Ch,), f32, dev), _flat(beta, "beta", (Ch,), f32, dev),
-            _flat(mean, "mean", (B, groups), f32, dev), _flat(rstd, "rstd", (B, groups), f32, dev), 0, 0)
+        rstd = _new(stats, f32, index, scratch)
+    fields = (_NORM.size, NET_DTYPE[dtype], kind, eps, B, S, Ch, groups, *_rows(x, "x", like), *_rows(y, "y", like),
+              *_NO_ROWS, *_NO_ROWS, _flat(gamma, "gamma", (Ch,), f32, index), _flat(beta, "beta", (Ch,), f32, index),
+              _flat(mean, "mean", stats, f32, index), _flat(rstd, "rstd", stats, f32, index), 0, 0)
     L = lib()
-    _call_with_workspace(L.net_group_norm, L.net_group_norm_workspace_bytes, 0, _NORM, head + ptrs, dev, stream, scratch)
+    _call_with_workspace(L.net_group_norm, L.net_group_norm_workspace_bytes, 0, _NORM, fields, index, stream, scratch)
     return y, mean, rstd
 
 
@@ -214,26 +215,23 @@ def group_norm_backward(x, groups, gamma, beta, mean, rstd, dy, *, act="none", d
                         stream=None):
     """Gradients (dx, dgamma, dbeta) of group_norm from dy [B, S, C]; mean and rstd as it returned them."""
     scratch = []
-    rx = _activation(x, "x")
-    B, S, Ch = x.shape
-    dev, f32 = x.device, torch.float32
-    rdy = _rows(dy, "dy", x)
+    like = shape, dtype, index = _activation(x, "x")
+    kind = _norm_head(act, groups)
+    B, S, Ch = shape
+    f32, stats = torch.float32, (B, groups)
     if dx is None:
-        dx = torch.empty((B, S, Ch), dtype=x.dtype, device=dev)
-        scratch.append(dx)
+        dx = _new(shape, dtype, index, scratch)
     if dgamma is None:
-        dgamma = torch.empty(Ch, dtype=f32, device=dev)
-        scratch.append(dgamma)
+        dgamma = _new((Ch,), f32, index, scratch)
     if dbeta is None:
-        dbeta = torch.empty(Ch, dtype=f32, device=dev)
-        scratch.append(dbeta)
-    head = (_NORM.size, NET_DTYPE[x.dtype], _act(act), 0.0, B, S, Ch, _groups(groups), *rx, *_NO_ROWS, *rdy,
-            *_rows(dx, "dx", x))
-    ptrs = (_flat(gamma, "gamma", (Ch,), f32, dev), _flat(beta, "beta", (Ch,), f32, dev),
-            _flat(mean, "mean", (B, groups), f32, dev), _flat(rstd, "rstd", (B, groups), f32, dev),
-            _flat(dgamma, "dgamma", (Ch,), f32, dev), _flat(dbeta, "dbeta", (Ch,), f32, dev))
+        dbeta = _new((Ch,), f32, index, scratch)
+    fields = (_NORM.size, NET_DTYPE[dtype], kind, 0.0, B, S, Ch, groups, *_rows(x, "x", like), *_NO_ROWS,
+              *_rows(dy, "dy", like), *_rows(dx, "dx", like), _flat(gamma, "gamma", (Ch,), f32, index),
+              _flat(beta, "beta", (Ch,), f32, index), _flat(mean, "mean", stats, f32, index),
+              _flat(rstd, "rstd", stats, f32, index), _flat(dgamma, "dgamma", (Ch,), f32, index),
+              _flat(dbeta, "dbeta", (Ch,), f32, index))
     L = lib()
-    _call_with_workspace(L.net_group_norm_backward, L.net_group_norm_workspace_bytes, 1, _NORM, head + ptrs, dev, stream,
+    _call_with_workspace(L.net_group_norm_backward, L.net_group_norm_workspace_bytes, 1, _NORM, fields, index, stream,
                          scratch)
     return dx, dgamma, dbeta
 
@@ -243,12 +241,11 @@ def dropout(x, p, seed, draw, *, residual=None, shared=False, y=None, stream=Non
     index, one for all T if shared.  The gradient by x is dropout(dy, p, seed, draw, shared=shared).  y may be x or
     residual."""
     scratch = []
-    rx = _activation(x, "x")
+    like = shape, dtype, index = _activation(x, "x")
     if y is None:
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        scratch.append(y)
-    rr = _NO_ROWS if residual is None else _rows(residual, "residual", x)
-    args = _DROP.pack(_DROP.size, NET_DTYPE[x.dtype], bool(shared), 0, *x.shape, *rx, *rr, *_rows(y, "y", x), p,
+        y = _new(shape, dtype, index, scratch)
+    args = _DROP.pack(_DROP.size, NET_DTYPE[dtype], bool(shared), 0, *shape, *_rows(x, "x", like),
+                      *(_NO_ROWS if residual is None else _rows(residual, "residual", like)), *_rows(y, "y", like), p,
                       seed & 0xFFFFFFFFFFFFFFFF, draw & 0xFFFFFFFFFFFFFFFF)
-    _call(lib().net_dropout, args, x.device, stream, scratch)
+    _call(lib().net_dropout, args, index, stream, scratch)
     return y
