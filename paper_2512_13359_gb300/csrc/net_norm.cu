@@ -171,6 +171,29 @@ __device__ __forceinline__ void load_weights(const float* w, int64_t c, float no
   }
 }
 
+// ------------------------------------------------------------------ clusters
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_arrive(int ranks) {
+  if (ranks > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  cluster_wait();
+}
+// The value at this block's address p in the shared memory of block `rank`.
+__device__ __forceinline__ float load_remote(const float* p, int rank) {
+  uint32_t there;
+  float v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(there) : "memory");
+  return v;
+}
+
 // ------------------------------------------------------------------ teams
 constexpr int kThreads = 256;
 constexpr int kMostLanes = 512;      // of a team that is a block
@@ -373,9 +396,10 @@ __global__ void __launch_bounds__(LANES == kBlock ? kMostLanes : kThreads) k_tea
   }
 }
 
-// partial: [2][gridDim.x][C], dbeta's and dgamma's sums by block (NULL: not wanted); of one block dbeta and dgamma.
+// weights: whether dbeta and dgamma are wanted.  Their sums by block go to partial [2][gridDim.x][C]; of few blocks, then
+// a cluster (ranks of them), they are joined here.
 template <typename T, int E, int SLOTS, int LANES>
-__global__ void __launch_bounds__(LANES == kBlock ? kMostLanes : kThreads) k_team_back(Norm a, Teams t, float* partial) {
+__global__ void __launch_bounds__(LANES == kBlock ? kMostLanes : kThreads) k_team_back(Norm a, Teams t, bool weights, int ranks, float* partial) {
   extern __shared__ uint4 smem[];
   const Lane<E, SLOTS> me(a, t);
   const float inv = 1.0f / (float)(a.S * (a.C / a.G));
@@ -450,7 +474,7 @@ __global__ void __launch_bounds__(LANES == kBlock ? kMostLanes : kThreads) k_tea
       pd[j] += dd;
     }
   }
-  if (!partial) return;
+  if (!weights) return;
   if constexpr (in.kRing) copy_wait<0>();
   __syncthreads();
   float* const sums = reinterpret_cast<float*>(smem);     // [2][teams of a block][lanes * SLOTS * E]
@@ -475,14 +499,31 @@ __global__ void __launch_bounds__(LANES == kBlock ? kMostLanes : kThreads) k_tea
         w += sums[all + (r * t.groups + i / width) * held + k];
       }
     const int64_t c = g * width + i % width;
-    if (gridDim.x == 1) {
-      if (a.dbeta) a.dbeta[c] = b;
-      if (a.dgamma) a.dgamma[c] = w;
+    if (ranks) {                   // kept in the first row's place, which no other thread reads
+      sums[i / width * held + i % width] = b;
+      sums[all + i / width * held + i % width] = w;
     } else {
       partial[blockIdx.x * a.C + c] = b;
       partial[((int64_t)gridDim.x + blockIdx.x) * a.C + c] = w;
     }
   }
+  if (!ranks) return;
+  cluster_sync();
+  if (blockIdx.x == 0) {
+    for (int i = threadIdx.x; i < t.groups * width; i += blockDim.x) {
+      const int64_t g = blockIdx.y * (int64_t)t.groups + i / width;
+      if (g >= a.G) break;
+      float b = 0.0f, w = 0.0f;
+      for (int r = 0; r < ranks; ++r) {
+        b += load_remote(sums + i / width * held + i % width, r);
+        w += load_remote(sums + all + i / width * held + i % width, r);
+      }
+      const int64_t c = g * width + i % width;
+      if (a.dbeta) a.dbeta[c] = b;
+      if (a.dgamma) a.dgamma[c] = w;
+    }
+  }
+  cluster_sync();                  // no block leaves before its sums are read
 }
 
 // dbeta and dgamma from [2][rows][C]: 32 columns of one a block, its warps over the rows.
@@ -521,18 +562,10 @@ struct Slab {
 constexpr int kSlabGroups = 4;             // of a slab at most
 constexpr int kSlabRanks = 16;
 
-__device__ __forceinline__ uint32_t slab_rank() {
-  uint32_t r;
-  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void slab_arrive(int ranks) {
-  if (ranks > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
-}
 // Stores v at this block's address p in the shared memory of every block of the cluster, all of which have started
-// (slab_arrive, a while ago), and waits for the others' stores.
+// (cluster_arrive, a while ago), and waits for the others' stores.
 __device__ __forceinline__ void exchange(float2* p, float2 v, bool mine, int ranks) {
-  if (ranks > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+  if (ranks > 1) cluster_wait();
   if (mine) {
     const uint32_t local = (uint32_t)__cvta_generic_to_shared(p);
     for (int r = 0; r < ranks; ++r) {
@@ -541,7 +574,7 @@ __device__ __forceinline__ void exchange(float2* p, float2 v, bool mine, int ran
       asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(v.x), "f"(v.y) : "memory");
     }
   }
-  if (ranks > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  if (ranks > 1) cluster_sync();
   else __syncthreads();
 }
 
@@ -551,7 +584,7 @@ struct SlabThread {
   int b, tile, c, s0, s1, n;   // instance, slab of it, first channel, the block's positions, the thread's pieces
   bool on;
   __device__ SlabThread(const Norm& a, const Slab& k) {
-    rank = (int)slab_rank();
+    rank = (int)cluster_rank();
     const unsigned q = blockIdx.x / (unsigned)k.ranks, i = q / (unsigned)k.tiles;
     b = (int)i;
     tile = (int)(q - i * k.tiles);
@@ -596,7 +629,7 @@ __global__ void __launch_bounds__(kThreads, 3) k_slab(Norm a, Slab k) {
   extern __shared__ uint4 data[];
   __shared__ float threads[2][kThreads], group[2][kSlabGroups];
   __shared__ float2 from[kSlabRanks][kSlabGroups], stats[kSlabGroups];   // mean, squared deviations; mean, rstd
-  slab_arrive(k.ranks);
+  cluster_arrive(k.ranks);
   const SlabThread<T, E> me(a, k);
   me.fetch(a.x, data, k);
   copy_commit();
@@ -683,7 +716,7 @@ __global__ void __launch_bounds__(kThreads, 3) k_slab_back(Norm a, Slab k, float
   __shared__ float sums[E][kThreads];
   __shared__ float2 from[kSlabRanks][kSlabGroups];
   __shared__ float own[2][kSlabGroups];
-  slab_arrive(k.ranks);
+  cluster_arrive(k.ranks);
   const SlabThread<T, E> me(a, k);
   const int held = k.rows * k.cols;
   me.fetch(a.x, data, k);
@@ -1027,6 +1060,7 @@ __global__ void k_empty(Norm a) {
 struct Plan {
   bool team;
   int e, slots, threads;
+  int join;             // blocks of a cluster that joins the weights' gradients, 0: none
   bool block;
   Teams t;
   dim3 grid;
@@ -1083,7 +1117,12 @@ Plan make_plan(const net_norm* p, bool back) {
     const int resident = back ? 512 : q.e == 8 && !q.block ? 1280 : 1024;
     const int64_t want = std::max<int64_t>(1, (int64_t)sms * (resident / q.threads) / gy);
     q.grid = dim3((unsigned)std::min(gx, want), (unsigned)gy);
-    if (back && (p->dgamma || p->dbeta)) q.bytes = sizeof(float) * 2 * q.grid.x * (size_t)p->C;
+    // Few instances: a cluster of up to eight blocks joins dgamma and dbeta itself.  That saves a launch and the
+    // workspace, 8 us of the host's 20 at 256 x 90, and costs some turns of the blocks.
+    if (back && (p->dgamma || p->dbeta)) {
+      if (gx <= 32) q.join = (int)std::min<int64_t>(gx, 8), q.grid.x = (unsigned)q.join;
+      else q.bytes = sizeof(float) * 2 * q.grid.x * (size_t)p->C;
+    }
     return q;
   }
   // slabs: whole groups side by side, 64 bytes of a row at least, in as few blocks as leave three an SM (72 KB each,
@@ -1137,6 +1176,22 @@ cudaError_t launch_weights(const Norm& a, const float* partial, int64_t rows, cu
   return launch_after(k_weights, dim3((unsigned)((a.C + 31) / 32), 2), kJoinThreads, 0, s, a, partial, rows);
 }
 
+template <typename... P, typename... A>
+cudaError_t launch_cluster(void (*kern)(P...), dim3 grid, int threads, int smem, int ranks, cudaStream_t s, A... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = ranks;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...);
+}
+
 template <typename T, int E, int SLOTS, int LANES>
 cudaError_t launch_team(const Norm& a, const Plan& q, bool back, float* ws, cudaStream_t s) {
   auto allow = [](const void* kern, int bytes) {
@@ -1157,12 +1212,10 @@ cudaError_t launch_team(const Norm& a, const Plan& q, bool back, float* ws, cuda
   const auto kern = k_team_back<T, E, SLOTS, LANES>;
   cudaError_t e = allow((const void*)kern, smem);
   if (e != cudaSuccess) return e;
-  kern<<<q.grid, q.threads, smem, s>>>(a, q.t, weights ? ws : nullptr);
+  if (q.join) return launch_cluster(kern, q.grid, q.threads, smem, q.join, s, a, q.t, weights, q.join, ws);
+  kern<<<q.grid, q.threads, smem, s>>>(a, q.t, weights, 0, ws);
   e = cudaGetLastError();
-  if (e == cudaSuccess && weights && q.grid.x > 1) {
-    return launch_weights(a, ws, q.grid.x, s);
-  }
-  return e;
+  return e == cudaSuccess && weights ? launch_weights(a, ws, q.grid.x, s) : e;
 }
 
 template <typename T, int E, int SLOTS>
@@ -1190,19 +1243,8 @@ cudaError_t launch_slab(const Norm& a, const Plan& q, bool back, float* ws, cuda
   if (e == cudaSuccess && q.sl.ranks > 8)
     e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = q.grid;
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = q.smem;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = q.sl.ranks;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  if (back) e = cudaLaunchKernelEx(&cfg, k_slab_back<T, E>, a, q.sl, weights ? ws : (float*)nullptr);
-  else e = cudaLaunchKernelEx(&cfg, k_slab<T, E>, a, q.sl);
+  e = back ? launch_cluster(k_slab_back<T, E>, q.grid, kThreads, q.smem, q.sl.ranks, s, a, q.sl, weights ? ws : (float*)nullptr)
+           : launch_cluster(k_slab<T, E>, q.grid, kThreads, q.smem, q.sl.ranks, s, a, q.sl);
   return e == cudaSuccess && weights ? launch_weights(a, ws, a.B * q.sl.ranks, s) : e;
 }
 
