@@ -131,7 +131,8 @@ int net_gate_scan_backward(const net_scan* a, void* stream);
  *   dx = rstd (w - avg(w) - xh avg(w xh)).
  *
  * workspace: net_group_norm_workspace_bytes(a, backward) bytes, 16-byte
- * aligned (AUV_ERR_SIZE if there is less; it may be 0 bytes).
+ * aligned (AUV_ERR_SIZE if there is less): 0 forward where a group has at most
+ * 2,048 values and there are at most 32,768 groups, and often otherwise.
  */
 typedef struct net_norm {
   uint32_t struct_size;           /* sizeof(net_norm): version guard          */

@@ -89,12 +89,18 @@ __device__ __forceinline__ void fill(float (&x)[E], float v) {
   for (int e = 0; e < E; ++e) x[e] = v;
 }
 
-// sigmoid alone: four instructions.  Where its exponential overflows it is 0.
-__device__ __forceinline__ float sigmoid(float u) {
-  float e, r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(u * -1.44269504088896341f));
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
-  return r;
+// sigmoid(u): three instructions a value, two of them the approximations'.  Where the exponential overflows it is 0.
+template <int E>
+__device__ __forceinline__ void sigmoid(const float (&u)[E], float (&s)[E]) {
+  float one[E];
+  fill<E>(one, 1.0f);
+  fill<E>(s, -1.44269504088896341f);
+  mul<E>(s, u);
+#pragma unroll
+  for (int e = 0; e < E; ++e) asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(s[e]) : "f"(s[e]));
+  add<E>(s, one);
+#pragma unroll
+  for (int e = 0; e < E; ++e) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s[e]) : "f"(s[e]));
 }
 
 // tanh: the difference of the gates is exact to 2^-22, which is enough ahead of a 16-bit store.
@@ -116,8 +122,9 @@ __device__ __forceinline__ void activate(uint32_t act, float (&u)[E]) {
 #pragma unroll
     for (int e = 0; e < E; ++e) asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(u[e]) : "f"(u[e]));
   } else if (act == NET_ACT_SILU) {
-#pragma unroll
-    for (int e = 0; e < E; ++e) u[e] *= sigmoid(u[e]);
+    float s[E];
+    sigmoid<E>(u, s);
+    mul<E>(u, s);
   } else if (act == NET_ACT_TANH) {
 #pragma unroll
     for (int e = 0; e < E; ++e) u[e] = tanh_of<T>(u[e]);
@@ -131,12 +138,13 @@ __device__ __forceinline__ void slope(uint32_t act, const float (&u)[E], float (
 #pragma unroll
     for (int e = 0; e < E; ++e) dy[e] = u[e] > 0.0f ? dy[e] : 0.0f;
   } else if (act == NET_ACT_SILU) {
-    float v[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) {      // s (1 + u (1 - s))
-      const float s = sigmoid(u[e]);
-      v[e] = fmaf(fmaf(-u[e], s, u[e]), s, s);
-    }
+    float s[E], v[E], one[E];
+    sigmoid<E>(u, s);
+    fill<E>(one, 1.0f);
+    fill<E>(v, -1.0f);
+    fma<E>(v, s, one, v);
+    mul<E>(v, u);
+    fma<E>(v, s, s, v);                // s (1 + u (1 - s))
     mul<E>(dy, v);
   } else if (act == NET_ACT_TANH) {
     float v[E];

@@ -207,7 +207,10 @@ def group_norm(x, groups, gamma=None, beta=None, *, eps=1e-5, act="none", y=None
               *_NO_ROWS, *_NO_ROWS, _flat(gamma, "gamma", (Ch,), f32, index), _flat(beta, "beta", (Ch,), f32, index),
               _flat(mean, "mean", stats, f32, index), _flat(rstd, "rstd", stats, f32, index), 0, 0)
     L = lib()
-    _call_with_workspace(L.net_group_norm, L.net_group_norm_workspace_bytes, 0, _NORM, fields, index, stream, scratch)
+    if S * Ch <= 2048 * groups <= 1 << 26:      # small groups need no workspace
+        _call(L.net_group_norm, _NORM.pack(*fields, 0, 0), index, stream, scratch)
+    else:
+        _call_with_workspace(L.net_group_norm, L.net_group_norm_workspace_bytes, 0, _NORM, fields, index, stream, scratch)
     return y, mean, rstd
 
 

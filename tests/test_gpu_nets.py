@@ -98,6 +98,12 @@ def test_recurrence_long(T, N, D, dt):
     _check_scan(T, N, D, dt, ends=0.0005, seed=7)
 
 
+@pytest.mark.parametrize("layout,T,N,D,dt", [("half", 30011, 1, 40, "bf16"), ("odd", 30011, 2, 33, "fp16"), ("swap", 20003, 2, 48, "fp32"),
+                                             ("pad", 25000, 3, 17, "fp32"), ("flat", 20003, 1, 250, "bf16"), ("flat", 16385, 4, 63, "fp16")])
+def test_recurrence_long_strides(layout, T, N, D, dt):
+    _check_scan(T, N, D, dt, layout, ends=0.0005, seed=12)
+
+
 @pytest.mark.parametrize("N,D,dt", [(40000, 256, "bf16"), (33333, 33, "fp16"), (70000, 64, "fp32")])
 def test_recurrence_wide(N, D, dt):
     _check_scan(3, N, D, dt, seed=8)
@@ -115,7 +121,7 @@ def test_recurrence_without_steps_or_envs():
     assert nets.gate_scan(z, z)[0].shape == (5, 0, 8)
 
 
-@pytest.mark.parametrize("T", [12, 900])
+@pytest.mark.parametrize("T", [12, 900, 60000])
 @pytest.mark.parametrize("dt", DT)
 def test_nothing_of_an_ended_episode_passes(T, dt):
     """Infinities and NaN in an ended episode's inputs and state: finite after its end, and the gradients before an end
@@ -404,7 +410,7 @@ def _buffers(torch, T, N, D, dtype, seed=1):
     return B
 
 
-@pytest.mark.parametrize("T,N,D", [(16, 64, 32), (2000, 2, 32), (3, 9000, 64), (2, 30000, 20)])
+@pytest.mark.parametrize("T,N,D", [(16, 64, 32), (2000, 2, 32), (3, 9000, 64), (2, 30000, 20), (40000, 1, 64)])
 @pytest.mark.parametrize("dt", ["fp32", "bf16"])
 def test_repeated_calls_other_streams_and_graphs_agree(T, N, D, dt):
     torch, nets, types = _t()
@@ -477,6 +483,21 @@ def test_refusals():
         with pytest.raises(AuvError) as e:
             bad()
         assert e.value.code == code, str(e.value)
+    L, z, r = nets.lib(), nets._NO_ROWS, (x.data_ptr(), 48, 8)
+    out, other = torch.empty_like(x), torch.empty_like(stats)
+    norm = (nets._NORM.size, 0, 0, 1e-5, 4, 6, 8, 2, *r, out.data_ptr(), 48, 8, *z, *z, 0, 0, stats.data_ptr(),
+            other.data_ptr(), 0, 0)
+    assert L.net_group_norm(nets._NORM.pack(*norm, 0, 0), 0) == 0
+    host = torch.zeros(4, 6, 8)
+    bad = (nets._NORM.size, 0, 0, 1e-5, 4, 6, 8, 2, host.data_ptr(), 48, 8, *norm[11:])
+    assert L.net_group_norm(nets._NORM.pack(*bad, 0, 0), 0) == AUV_ERR_SIZE and b"device memory" in L.net_last_error()
+    long = torch.zeros((40000, 1, 64), device="cuda")
+    q = (long.data_ptr(), 64, 64)
+    scan = (nets._SCAN.size, 0, 40000, 1, 64, *q, *q, *q, *z, *z, *z, *(6 * (0,)))
+    need = L.net_gate_scan_workspace_bytes(nets._SCAN.pack(*scan, 0, 0), 0)
+    assert need > 0
+    assert L.net_gate_scan(nets._SCAN.pack(*scan, 0, need), 0) == AUV_ERR_INVALID and b"workspace" in L.net_last_error()
+    assert L.net_gate_scan(nets._SCAN.pack(*scan, long.data_ptr(), need - 1), 0) == AUV_ERR_SIZE
     torch.cuda.synchronize()                     # nothing was launched that could have gone wrong
     y, hT = nets.gate_scan(x, x[:1].expand(4, 6, 8))                 # repeated inputs are fine
     assert torch.equal(y, nets.gate_scan(x, x[:1].expand(4, 6, 8).contiguous())[0])
