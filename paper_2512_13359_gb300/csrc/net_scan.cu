@@ -128,16 +128,18 @@ template <int E> constexpr int kAheadOf = E >= 4 ? 8 : 16;
 // make few warps, wait for each other's latency otherwise.
 template <int E> constexpr int kGroup = E == 4 ? 2 : 4;
 
-// A sequence in pieces of `rows` steps, blockIdx.y's each: the maps of the pieces' channels, A [pieces][m] and
-// B [pieces][m]; after k_join, B holds the states before the pieces.  One piece: rows = T, maps NULL.
+// A sequence in pieces of `rows` steps: the maps of the pieces' channels, A [pieces][m] and B [pieces][m]; after k_join, B
+// holds the states before the pieces.  A block takes adjacent pieces, `lanes` (a power of two) threads each.  One piece:
+// rows = T, maps NULL.
 struct Split {
-  int rows;
+  int rows, pieces, lanes;
   int64_t m;
   float* maps;
 };
 
-// SPLIT: in pieces; FOLD: only their maps.
-template <typename T, int E, bool BACK, bool MIXED, bool SPLIT, bool FOLD>
+// SPLIT: in pieces, one a block (1) or several of few channels (2: their steps are then in no uniform registers, which
+// takes 5 to 10 % longer where a piece fills the block).  FOLD: only their maps.
+template <typename T, int E, bool BACK, bool MIXED, int SPLIT, bool FOLD>
 __global__ void __launch_bounds__(kStepThreads) k_steps(Scan a, int64_t width, Split split) {
   using W = Raw<T, E>;
   using In = Inputs<T, BACK>;
@@ -146,12 +148,14 @@ __global__ void __launch_bounds__(kStepThreads) k_steps(Scan a, int64_t width, S
   constexpr int kX = FOLD && BACK ? 3 : 1;
   extern __shared__ uint4 smem[];
   W* const ring = reinterpret_cast<W*>(smem) + threadIdx.x;    // slot (u, i) at (u * kHeld + i) * kStepThreads
-  const int64_t m = blockIdx.x * (int64_t)kStepThreads + threadIdx.x, per = a.D / E;
-  if (m >= a.N * per) return;
+  const int lanes = SPLIT == 2 ? split.lanes : kStepThreads, lane = SPLIT == 2 ? threadIdx.x & (lanes - 1) : threadIdx.x;
+  const int piece = SPLIT == 2 ? blockIdx.y * (kStepThreads / lanes) + threadIdx.x / lanes : SPLIT ? blockIdx.y : 0;
+  const int64_t m = blockIdx.x * (int64_t)lanes + lane, per = a.D / E;
+  if (m >= a.N * per || (SPLIT == 2 && piece >= split.pieces)) return;
   const int64_t n = m / per, d = (m - n * per) * E;
   In in(a, n, d);
   // steps before the piece, and its own
-  const int skip = SPLIT ? blockIdx.y * split.rows : 0, steps = SPLIT ? min(split.rows, a.T - skip) : a.T;
+  const int skip = SPLIT ? piece * split.rows : 0, steps = SPLIT ? min(split.rows, a.T - skip) : a.T;
   if constexpr (SPLIT) {
 #pragma unroll
     for (int i = 0; i < K; ++i) in.p[i] += skip * in.by[i];
@@ -181,8 +185,8 @@ __global__ void __launch_bounds__(kStepThreads) k_steps(Scan a, int64_t width, S
     if (kAsync<T, E> && u % kG == kG - 1) copy_commit();
     flag[u] = flag_of(u);
   }
-  float* const maps = SPLIT ? split.maps + blockIdx.y * split.m + m * E : nullptr;
-  const int64_t to_b = SPLIT ? gridDim.y * split.m : 0;
+  float* const maps = SPLIT ? split.maps + piece * split.m + m * E : nullptr;
+  const int64_t to_b = SPLIT ? split.pieces * split.m : 0;
   float h[E];
   [[maybe_unused]] Map q[E];
   if constexpr (FOLD) {
@@ -338,13 +342,13 @@ Way way_of(int T, int64_t m, int size, bool back) {
 Split split_of(int T, int64_t m, float* ws) {
   const int64_t threads = std::max<int64_t>(1, m / 4);
   const int64_t want = std::max<int64_t>(1, std::min<int64_t>((int64_t)sm_count() * 1024 / threads, std::min(kMostPieces, T / 32)));
-  return {(int)((T + want - 1) / want), m, ws};
+  const int rows = (int)((T + want - 1) / want);
+  return {rows, (int)(((int64_t)T + rows - 1) / rows), kStepThreads, m, ws};
 }
-int pieces_of(const Split& s, int T) { return (int)(((int64_t)T + s.rows - 1) / s.rows); }
 
-template <typename T, int E, bool BACK, bool MIXED, bool SPLIT, bool FOLD>
+template <typename T, int E, bool BACK, bool MIXED, int SPLIT, bool FOLD>
 cudaError_t launch_steps(const Scan& a, int64_t width, const Split& split, cudaStream_t s) {
-  const int64_t blocks = (a.N * (a.D / E) + kStepThreads - 1) / kStepThreads;
+  const int64_t blocks = (a.N * (a.D / E) + split.lanes - 1) / split.lanes;
   // slots: of a short sequence as many as it has steps, whole groups of them (a group is read whole)
   constexpr int kAhead = kAheadOf<E>, kG = kGroup<E>;
   const int ahead = split.rows < kAhead ? (split.rows + kG - 1) / kG * kG : kAhead;
@@ -355,7 +359,8 @@ cudaError_t launch_steps(const Scan& a, int64_t width, const Split& split, cudaS
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
   }
-  const dim3 grid((unsigned)blocks, (unsigned)pieces_of(split, a.T));
+  const int side = kStepThreads / split.lanes;   // pieces of a block
+  const dim3 grid((unsigned)blocks, (unsigned)((split.pieces + side - 1) / side));
   if (SPLIT && !FOLD) return launch_after(kern, grid, kStepThreads, smem, s, a, width, split);
   kern<<<grid, kStepThreads, smem, s>>>(a, width, split);
   return cudaGetLastError();
@@ -368,15 +373,19 @@ cudaError_t launch_walk(const Scan& a, int64_t width, const Split& split, cudaSt
     return cudaGetLastError();
   }
   if constexpr (E <= 4) {
-    if (split.maps) {
-      cudaError_t e = launch_steps<T, E, BACK, MIXED, true, true>(a, width, split, s);
-      if (e != cudaSuccess) return e;
-      e = launch_after(k_join, dim3((unsigned)((split.m + kJoinChannels - 1) / kJoinChannels)), kJoinThreads, 0, s,
-                       pieces_of(split, a.T), split.m,
-                       split.maps, BACK ? a.dhT : a.h0);
-      return e != cudaSuccess ? e : launch_steps<T, E, BACK, MIXED, true, false>(a, width, split, s);
-    }
-    return launch_steps<T, E, BACK, MIXED, false, false>(a, width, split, s);
+    if (!split.maps) return launch_steps<T, E, BACK, MIXED, 0, false>(a, width, split, s);
+    Split p = split;
+    const int64_t threads = a.N * (a.D / E);
+    while (p.lanes > 8 && threads <= p.lanes / 2) p.lanes /= 2;
+    const bool whole = p.lanes == kStepThreads;
+    cudaError_t e = whole ? launch_steps<T, E, BACK, MIXED, 1, true>(a, width, p, s)
+                          : launch_steps<T, E, BACK, MIXED, 2, true>(a, width, p, s);
+    if (e != cudaSuccess) return e;
+    e = launch_after(k_join, dim3((unsigned)((p.m + kJoinChannels - 1) / kJoinChannels)), kJoinThreads, 0, s, p.pieces, p.m,
+                     p.maps, BACK ? a.dhT : a.h0);
+    if (e != cudaSuccess) return e;
+    return whole ? launch_steps<T, E, BACK, MIXED, 1, false>(a, width, p, s)
+                 : launch_steps<T, E, BACK, MIXED, 2, false>(a, width, p, s);
   } else {
     return cudaErrorInvalidValue;   // not asked for
   }
@@ -411,7 +420,7 @@ cudaError_t launch(const Scan& a, float* ws, cudaStream_t s) {
   // and 86).
   const Way way = way_of(a.T, m, sizeof(T), BACK);
   if (way == Way::kBlocks) return launch_pieces<T>(a, BACK, s);
-  const Split split = way == Way::kPieces ? split_of(a.T, m, ws) : Split{a.T, m, nullptr};
+  const Split split = way == Way::kPieces ? split_of(a.T, m, ws) : Split{a.T, 1, kStepThreads, m, nullptr};
   int most = 16 / (int)sizeof(T);
   if (a.T > 1) most = split.maps || m >= 4 * 160 * sms ? 4 : 2;
   const net_rows* rows[] = {&a.f, &a.v, &a.y, &a.dy, &a.df, &a.dv};
@@ -494,7 +503,7 @@ size_t net_gate_scan_workspace_bytes(const net_scan* a, int backward) {
   if (!a || check(a) || !a->T || !a->N || !a->D) return 0;
   const int64_t m = a->N * a->D;
   if (way_of((int)a->T, m, type_size(a->dtype), backward) != Way::kPieces) return 0;
-  return sizeof(float) * 2 * (size_t)pieces_of(split_of((int)a->T, m, nullptr), (int)a->T) * (size_t)m;
+  return sizeof(float) * 2 * (size_t)split_of((int)a->T, m, nullptr).pieces * (size_t)m;
 }
 
 int net_gate_scan(const net_scan* a, void* stream) { return auv::net::run(a, false, stream); }
