@@ -5,10 +5,15 @@
 //
 //  k_team, k_team_back      groups of a few thousand values: a team of lanes (of a warp, or a whole block) keeps a group
 //                           in registers and goes from instance to instance.  A team's channels stay the same, so the
-//                           backward pass sums dgamma and dbeta in registers and joins them once at its end.
+//                           backward pass sums dgamma and dbeta in registers and joins them once at its end.  65,536 x
+//                           256 bf16, one group: forward 12.8 us (5.2 TB/s; half of it issuing instructions), backward
+//                           28 us (3.6 TB/s, 60 registers of weights and their sums leave two blocks an SM).
 //  k_slab, k_slab_back      larger groups, as long as a cluster of blocks holds some adjacent ones of an instance in shared
 //                           memory, each block some positions: statistics are joined through distributed shared memory.
-//  k_part, k_stats, k_apply the rest: sums by chunk and channel, joined, and the elements read once more.
+//                           64 x 4,096 x 256 bf16, 32 groups: forward 60 us (4.5 TB/s), backward 136 us (3 TB/s): three
+//                           blocks an SM, between their barriers.
+//  k_part, k_stats, k_apply the rest: sums by chunk and channel, joined, and the elements read once more.  65,536 x 256
+//                           bf16 as one instance: forward 35 us, backward 68 us.
 //  (.._back)
 //
 // Variances are those of deviations: in registers from the mean, over chunks from each channel's first value, joined

@@ -1,10 +1,12 @@
 // net_pieces.cu -- the gated recurrence (net_scan.cu) of few channels over many steps: the steps are split as well.
 //
-// A block holds kChannels channels x some hundred steps in shared memory.  Each of its threads takes a run of steps of
+// A block holds 32 channels (16 where blocks would be few) x some hundred steps in shared memory.  Each of its threads takes a run of steps of
 // E adjacent channels, folds them to one affine map h -> A h + B a channel, and keeps the gates in registers.  The maps
 // are joined over the warp by shuffles, over the block's warps by a scan in shared memory, and over a cluster of blocks,
 // each with the next piece of the sequence, through distributed shared memory; then every run is gone through from its
 // right start.  Inputs are read from memory once.  The next piece is on its way meanwhile.
+// 512 steps of 32,768 bf16 channels: forward 34 us (3 TB/s), backward 53 us (3.8 TB/s); instructions take 60 % of the
+// issue slots, the barriers and the joins most of the rest.
 #include <type_traits>
 
 #include "net_scan.cuh"

@@ -19,8 +19,9 @@ from .auvenv import AUV_ERR_INVALID, AUV_ERR_SIZE, AUV_OK, AuvError
 NET_DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 NET_ACT = {"none": 0, "relu": 1, "silu": 2, "tanh": 3}
 
-EXPORTED = ("net_gate_scan_workspace_bytes", "net_gate_scan", "net_gate_scan_backward", "net_group_norm_workspace_bytes", "net_group_norm",
-            "net_group_norm_backward", "net_dropout", "net_last_error")
+EXPORTED = ("net_gate_scan_workspace_bytes", "net_gate_scan", "net_gate_scan_backward",
+            "net_group_norm_workspace_bytes", "net_group_norm", "net_group_norm_backward", "net_dropout",
+            "net_last_error")
 
 # The argument blocks, field by field as in the header (native alignment).
 _ROWS = "Pqq"
