@@ -572,7 +572,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_weights(Norm a, const float* p
 struct Slab {
   int cols, wide, groups, side, rows, ranks, tiles;
 };
-constexpr int kSlabGroups = 4;             // of a slab at most
+constexpr int kSlabGroups = 8;             // of a slab at most
 constexpr int kSlabRanks = 16;
 
 // Stores v at this block's address p in the shared memory of every block of the cluster, all of which have started
@@ -1138,32 +1138,36 @@ Plan make_plan(const net_norm* p, bool back) {
     }
     return q;
   }
-  // slabs: whole groups side by side, 64 bytes of a row at least, in as few blocks as leave three an SM (72 KB each,
-  // backward 8 of them for sums; then two, and clusters of 16).  Aligned pieces within a group alone.
+  // slabs: whole groups side by side, in as few blocks as leave three an SM (72 KB each, backward 8 of them for sums;
+  // then two, and clusters of 16).  128 bytes of a row at least where four blocks hold that (500 x 300 x 128 bf16: 22 us,
+  // 28 with 64 bytes), else 64 (64 x 4,096 x 256: 60 us, 64 with 128 bytes).  Aligned pieces within a group alone.
   if (W % widest == 0 && fits(widest) && W / widest <= kThreads) {
-    const int wide = (int)(W / widest);
-    const int groups = (int)std::min<int64_t>(p->G, std::max(1, kSlabGroups / wide));
-    const int cols = wide * groups, side = kThreads / cols, arrays = back ? 2 : 1;
-    const int64_t row = (int64_t)cols * 16 * arrays;
-    auto ranks_for = [&](int64_t bytes) {
-      const int64_t rows = std::max<int64_t>(1, bytes / row);
-      return (p->S + rows - 1) / rows;
-    };
-    int64_t ranks = ranks_for(back ? 64 * 1024 : 72 * 1024);
-    if (ranks > 8) ranks = ranks_for(back ? 100 * 1024 : 108 * 1024);
-    if (ranks <= kSlabRanks) {
+    const int wide = (int)(W / widest), arrays = back ? 2 : 1;
+    for (int least = kSlabGroups; least >= 4; least /= 2) {
+      const int groups = (int)std::min<int64_t>(p->G, std::max(1, least / wide));
+      const int cols = wide * groups, side = kThreads / cols;
+      const int64_t row = (int64_t)cols * 16 * arrays;
+      auto ranks_for = [&](int64_t bytes) {
+        const int64_t rows = std::max<int64_t>(1, bytes / row);
+        return (p->S + rows - 1) / rows;
+      };
+      int64_t ranks = ranks_for(back ? 64 * 1024 : 72 * 1024);
+      if (least > 4 && ranks > 4) continue;
+      if (ranks > 8) ranks = ranks_for(back ? 100 * 1024 : 108 * 1024);
+      if (ranks > kSlabRanks) break;
       const int64_t tiles = (p->G + groups - 1) / groups;
       int r = pow2_at_least(ranks);
       // more blocks where there are few
       while (r < 8 && p->B * tiles * r < sms && p->S >= 2 * r * side) r *= 2;
+      if (p->B * tiles * r > INT32_MAX) break;
       const int64_t rows = (p->S + r - 1) / r;
-      q.slab = p->B * tiles * r <= INT32_MAX;
+      q.slab = true;
       q.e = widest;
       q.sl = {cols, wide, groups, side, (int)rows, r, (int)tiles};
       q.grid = dim3((unsigned)(p->B * tiles * r));
       q.smem = (int)(rows * row);
       if (back && (p->dgamma || p->dbeta)) q.bytes = sizeof(float) * 2 * (size_t)(p->B * r) * p->C;
-      if (q.slab) return q;
+      return q;
     }
   }
   q.e = widest;
