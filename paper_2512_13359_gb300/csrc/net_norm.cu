@@ -108,15 +108,28 @@ __device__ __forceinline__ void sigmoid(const float (&u)[E], float (&s)[E]) {
   for (int e = 0; e < E; ++e) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s[e]) : "f"(s[e]));
 }
 
-// tanh: the difference of the gates is exact to 2^-22, which is enough ahead of a 16-bit store.
+// q = exp(-2 |u|) as 2^(-2 |u| log2 e), and r = 1 / (1 + q): tanh |u| = (1 - q) r.
+__device__ __forceinline__ void tanh_parts(float u, float& q, float& r) {
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(q) : "f"(fabsf(u) * -2.88539008177792681f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + q));
+}
+
+// tanh.  Ahead of a 16-bit store by its parts, whose difference is off by some 3 units of 2^-24 whatever u: 13 of them
+// relative to the result at |u| = 1/4, and below that Taylor's series to u^9 instead (what follows is 2^-26 of it there).
+// 65,536 x 256 bf16: 19.3 us, 17.1 without the series (and 1 % off at 1e-6), 19.6 with tanhf; 64 x 4,096 x 256 in 32
+// groups 73, 65 and 74.
 template <typename T>
 __device__ __forceinline__ float tanh_of(float u) {
   if constexpr (sizeof(T) == 4) {
     return tanhf(u);
   } else {
-    float s, r;
-    gates(2.0f * u, s, r);
-    return s - r;
+    float q, r;
+    tanh_parts(u, q, r);
+    const float w = u * u;
+    float p = fmaf(62.0f / 2835.0f, w, -17.0f / 315.0f);
+    p = fmaf(p, w, 2.0f / 15.0f);
+    p = fmaf(p, w, -1.0f / 3.0f);
+    return w < 0.0625f ? fmaf(u * w, p, u) : copysignf((1.0f - q) * r, u);
   }
 }
 
