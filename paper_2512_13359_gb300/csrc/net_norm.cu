@@ -168,8 +168,9 @@ __device__ __forceinline__ void slope(uint32_t act, const float (&u)[E], float (
     float v[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      const float t = tanh_of<T>(u[e]);
-      v[e] = fmaf(-t, t, 1.0f);
+      float q, r;
+      tanh_parts(u[e], q, r);
+      v[e] = 4.0f * q * r * r;         // 1 - tanh^2, which as a difference has no digits left where tanh saturates
     }
     mul<E>(dy, v);
   }

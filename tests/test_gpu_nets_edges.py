@@ -30,3 +30,40 @@ def test_tanh_keeps_its_precision_near_zero(B, S, C, G, off, dt):
     terms = ((np.abs(xg) + np.abs(_np(mean))[:, None, :, None]) * _np(rstd)[:, None, :, None]).reshape(B, S, C)
     E = _np(gamma) * R.U * (2 * terms + 4 * np.abs(xh)) + 16 * R.U * np.abs(np.tanh(u))
     _within(y, np.tanh(u), E, dt)
+
+
+@pytest.mark.parametrize("dt", ["fp32", "bf16"])
+@pytest.mark.parametrize("shift", [0.0, 4.0, -9.0, 20.0])
+@pytest.mark.parametrize("B,S,C,G,off", _shapes_of_every_way())
+def test_tanh_slope_keeps_its_precision(B, S, C, G, off, shift, dt):
+    """1 - tanh^2 where tanh saturates: 1.6e-16 at u = 20, of which a difference from 1 has no digit."""
+    torch, nets, types = _t()
+    g = torch.Generator(device="cuda").manual_seed(36)
+    x, dy = (torch.randn((B, S, C + off), device="cuda", generator=g).to(types[dt])[..., off:] for _ in range(2))
+    gamma = torch.rand(C, device="cuda", generator=g) * 0.3 + 0.1
+    beta = torch.randn(C, device="cuda", generator=g) * 0.1 + shift
+    _, mean, rstd = nets.group_norm(x, G, gamma, beta)
+    got = nets.group_norm_backward(x, G, gamma, beta, mean, rstd, dy, act="tanh")
+    U, ng, nb = R.U, _np(gamma), _np(beta)
+    xg, m, r = _np(x).reshape(B, S, G, C // G), _np(mean)[:, None, :, None], _np(rstd)[:, None, :, None]
+    xh = ((xg - m) * r).reshape(B, S, C)
+    Exh = (2 * U * (np.abs(xg) + np.abs(m)) * r).reshape(B, S, C) + U * np.abs(xh)
+    u = ng * xh + nb
+    Eu = ng * Exh + 3 * U * (np.abs(ng * xh) + np.abs(nb))
+    slope = 1 / np.cosh(u) ** 2
+    dz = _np(dy) * slope
+    # relative: of the slope by u, -2 tanh(u); its own, an exponential of 2 |u| (rounded: 2 |u|) and some ten roundings
+    Edz = np.abs(dz) * (2 * Eu + U * (4 * np.abs(u) + 32))
+    w, Ew = ng * dz, ng * (Edz + U * np.abs(dz))
+    split = lambda q: q.reshape(B, S, G, C // G)                   # noqa: E731
+    avg = lambda q: q.mean(axis=(1, 3), keepdims=True)             # noqa: E731
+    w, Ew, xs, Exs = split(w), split(Ew), split(xh), split(Exh)
+    k, kb = R._sum_error(S * (C // G)), R._sum_error(B * S)
+    m1, m2 = avg(w), avg(w * xs)
+    E1, E2 = avg(Ew) + k * avg(np.abs(w)), avg(Ew * np.abs(xs) + np.abs(w) * Exs) + k * avg(np.abs(w * xs))
+    dx = r * (w - m1 - xs * m2)
+    Edx = r * (Ew + E1 + np.abs(xs) * E2 + np.abs(m2) * Exs + 4 * U * (np.abs(w) + np.abs(m1) + np.abs(xs * m2)))
+    _within(got[0], dx.reshape(B, S, C), Edx.reshape(B, S, C), dt)
+    _within(got[1], (dz * xh).sum(axis=(0, 1)),
+            (Edz * np.abs(xh) + np.abs(dz) * Exh).sum(axis=(0, 1)) + kb * np.abs(dz * xh).sum(axis=(0, 1)))
+    _within(got[2], dz.sum(axis=(0, 1)), Edz.sum(axis=(0, 1)) + kb * np.abs(dz).sum(axis=(0, 1)))
