@@ -121,7 +121,9 @@ int net_gate_scan_backward(const net_scan* a, void* stream);
  *   xh = (x - mean) rstd,  rstd = 1 / sqrt(var + eps),
  *   y = act(gamma xh + beta),
  *
- * mean and rstd [B][G] are outputs.  gamma, beta [C]; NULL: ones, zeros.
+ * mean and rstd [B][G] are outputs.  gamma, beta [C]; NULL: ones, zeros.  Where
+ * the sum of squared deviations passes fp32's range (deviations of some 10^19
+ * and more), rstd is 0 and y = act(beta).
  *
  * net_group_norm_backward: dx, and dgamma, dbeta [C] (each NULL: not wanted)
  * from dy, and x, gamma, beta, mean, rstd as in the forward call.  With

@@ -267,11 +267,11 @@ __device__ __forceinline__ void team_sum(float (&x)[N], int lanes) {
   }
 }
 
-// 1 / sqrt(v): the approximation and a step of Newton's method.
+// 1 / sqrt(v): the approximation and a step of Newton's method; 0 for infinity, of which the step would make NaN.
 __device__ __forceinline__ float inverse_root(float v) {
   const float r = rsqrtf(v);
   const float q = fmaf(-v * r, r, 1.0f);
-  return v > 1e-30f ? fmaf(0.5f * r, q, r) : r;
+  return v > 1e-30f && v < INFINITY ? fmaf(0.5f * r, q, r) : r;
 }
 
 // What a lane of a team works on.

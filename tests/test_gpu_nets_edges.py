@@ -67,3 +67,21 @@ def test_tanh_slope_keeps_its_precision(B, S, C, G, off, shift, dt):
     _within(got[1], (dz * xh).sum(axis=(0, 1)),
             (Edz * np.abs(xh) + np.abs(dz) * Exh).sum(axis=(0, 1)) + kb * np.abs(dz * xh).sum(axis=(0, 1)))
     _within(got[2], dz.sum(axis=(0, 1)), Edz.sum(axis=(0, 1)) + kb * np.abs(dz).sum(axis=(0, 1)))
+
+
+@pytest.mark.parametrize("dt", ["fp32", "bf16"])
+@pytest.mark.parametrize("B,S,C,G,off", [(16, 1, 256, 1, 0), (3, 700, 24, 3, 1), (9, 40, 250, 1, 0), (200, 550, 80, 10, 0),
+                                         (3, 5000, 64, 2, 0), (3, 5000, 64, 2, 1), (1, 40000, 33, 3, 0)])
+def test_norm_of_values_whose_variance_overflows(B, S, C, G, off, dt):
+    """The sum of squares passes fp32: rstd is 0 and every value its beta, whichever way is taken."""
+    torch, nets, types = _t()
+    g = torch.Generator(device="cuda").manual_seed(34)
+    x = (torch.randn((B, S, C + off), device="cuda", generator=g) * 1e25).to(types[dt])[..., off:]
+    beta = torch.randn(C, device="cuda", generator=g)
+    dy = torch.randn((B, S, C), device="cuda", generator=g).to(types[dt])
+    y, mean, rstd = nets.group_norm(x, G, None, beta, act="tanh")
+    assert (rstd == 0).all() and torch.isfinite(mean).all()
+    assert torch.equal(y, y[:1, :1].expand_as(y))
+    _within(y[0, 0], np.tanh(_np(beta)), 16 * R.U * np.abs(np.tanh(_np(beta))), dt)
+    dx, dgamma, dbeta = nets.group_norm_backward(x, G, None, beta, mean, rstd, dy, act="tanh")
+    assert (dx == 0).all() and (dgamma == 0).all() and torch.isfinite(dbeta).all()
