@@ -71,7 +71,9 @@ typedef struct net_rows {
  * hT = h[T - 1].  An episode ended before step t where done[t - 1][n] is
  * nonzero (the rollout's array), before step 0 where done_prev[n] is: the
  * last step's flags of the call before.  Whatever the ended episode's state
- * held, infinities and NaN too, nothing of it passes.  In a rollout T = 1:
+ * held, infinities and NaN too, nothing of it passes.  Without an end a state
+ * that is infinite stays so until a gate is 0 in fp32 (f below -87), after
+ * which it is infinite or NaN.  In a rollout T = 1:
  * done_prev = the env's last flags, hT = h0 for a state updated in place.
  *
  * f, v, y (i = t, j = n) and done, done_prev, h0, hT; the others are not read.

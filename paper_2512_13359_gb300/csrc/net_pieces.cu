@@ -200,6 +200,8 @@ __global__ void __launch_bounds__(Shape<T, E, CH, BACK>::kThreads) k_pieces(Scan
 #pragma unroll
       for (int e = 0; e < E; ++e) mine[e].B *= last[e];
     }
+#pragma unroll
+    for (int e = 0; e < E; ++e) mine[e].A = positive(mine[e].A);
     if (ends) {
 #pragma unroll
       for (int e = 0; e < E; ++e) finite = finite && fabsf(mine[e].B) < INFINITY;

@@ -263,7 +263,7 @@ __global__ void __launch_bounds__(kStepThreads) k_steps(Scan a, int64_t width, S
   if constexpr (kAsync<T, E>) copy_wait<0>();
   if constexpr (FOLD) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) h[e] = q[e].A;
+    for (int e = 0; e < E; ++e) h[e] = positive(q[e].A);
     store_state<E>(maps, h);
 #pragma unroll
     for (int e = 0; e < E; ++e) h[e] = q[e].B;

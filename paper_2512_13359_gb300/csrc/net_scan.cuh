@@ -47,13 +47,16 @@ struct Inputs {
 };
 
 // An affine map h -> A h + B of one channel.  A piece with an episode end in it passes nothing on, whatever came
-// before (NaN times 0 included): its A is -0, and the sign is asked for; gates are never negative.
+// before (NaN times 0 included): its A is -0, and the sign is asked for; gates are never negative.  A product of gates
+// that would round to +0 is 2^-149 instead (`positive`), an error of the same size: what is infinite before a long piece
+// is so after it, as it is when the steps are walked, and not the NaN of 0 times infinity.
 struct Map {
   float A, B;
 };
 __device__ __forceinline__ bool cuts(float A) { return __float_as_uint(A) >> 31; }
+__device__ __forceinline__ float positive(float A) { return __uint_as_float(max(__float_as_uint(A), 1u)); }
 __device__ __forceinline__ Map then(const Map& p, const Map& q) {   // p, then q
-  return cuts(q.A) ? q : Map{p.A * q.A, fmaf(q.A, p.B, q.B)};
+  return cuts(q.A) ? q : Map{positive(p.A * q.A), fmaf(q.A, p.B, q.B)};
 }
 __device__ __forceinline__ float apply(const Map& q, float h) { return cuts(q.A) ? q.B : fmaf(q.A, h, q.B); }
 

@@ -85,3 +85,25 @@ def test_norm_of_values_whose_variance_overflows(B, S, C, G, off, dt):
     _within(y[0, 0], np.tanh(_np(beta)), 16 * R.U * np.abs(np.tanh(_np(beta))), dt)
     dx, dgamma, dbeta = nets.group_norm_backward(x, G, None, beta, mean, rstd, dy, act="tanh")
     assert (dx == 0).all() and (dgamma == 0).all() and torch.isfinite(dbeta).all()
+
+
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("T,N,D", [(12, 3, 40), (900, 3, 40), (600, 2, 3001), (5000, 2, 96), (60000, 2, 40)])
+def test_an_infinite_state_stays_infinite(T, N, D, dt):
+    """No end, no gate that is 0: what is infinite once is infinite from then on, however far."""
+    torch, nets, types = _t()
+    g = torch.Generator(device="cuda").manual_seed(24)
+    f = (torch.randn((T, N, D), device="cuda", generator=g) * 0.5 + 0.5).to(types[dt])
+    v, dy = (torch.randn((T, N, D), device="cuda", generator=g).to(types[dt]) for _ in range(2))
+    h0 = torch.randn((N, D), device="cuda", generator=g)
+    want = nets.gate_scan(f, v, h0)
+    v[3, 0, ::2] = float("inf")
+    h0[1, 1] = float("-inf")
+    y, hT = nets.gate_scan(f, v, h0)
+    assert (y[3:, 0, ::2] == float("inf")).all() and (hT[0, ::2] == float("inf")).all()
+    assert (y[:, 1, 1] == float("-inf")).all() and hT[1, 1] == float("-inf")
+    assert torch.equal(y[:, 0, 1::2], want[0][:, 0, 1::2]) and torch.equal(y[:, 1, 2:], want[0][:, 1, 2:])
+    dy[T - 4, 1, ::2] = float("inf")
+    _, dv, dh0 = nets.gate_scan_backward(f, v, want[0], dy, None)
+    assert (dv[:T - 3, 1, ::2] == float("inf")).all() and (dh0[1, ::2] == float("inf")).all()
+    assert torch.isfinite(dv[T - 3:]).all() and torch.isfinite(dv[:, 1, 1::2]).all() and torch.isfinite(dh0[0]).all()
