@@ -107,3 +107,20 @@ def test_an_infinite_state_stays_infinite(T, N, D, dt):
     _, dv, dh0 = nets.gate_scan_backward(f, v, want[0], dy, None)
     assert (dv[:T - 3, 1, ::2] == float("inf")).all() and (dh0[1, ::2] == float("inf")).all()
     assert torch.isfinite(dv[T - 3:]).all() and torch.isfinite(dv[:, 1, 1::2]).all() and torch.isfinite(dh0[0]).all()
+
+
+@pytest.mark.parametrize("first", [30.0, 1000.0])
+@pytest.mark.parametrize("B,S,C,G,dt", [(1, 65536, 8, 1, "fp32"), (1, 1 << 21, 4, 1, "fp32"), (1, 200000, 9, 3, "fp32"),
+                                        (2, 70000, 16, 1, "bf16"), (3, 2000, 32, 4, "fp32"), (40, 300, 64, 8, "fp32")])
+def test_norm_after_a_first_value_far_from_the_rest(B, S, C, G, dt, first):
+    """One row a thousand deviations off at the start: the statistics are as exact as elsewhere."""
+    torch, nets, types = _t()
+    g = torch.Generator(device="cuda").manual_seed(33)
+    x = torch.randn((B, S, C), device="cuda", generator=g)
+    x[:, 0] *= first
+    x = x.to(types[dt])
+    y, mean, rstd = nets.group_norm(x, G)
+    r = R.group_norm(_np(x), G, np.ones(C), np.zeros(C), 1e-5, "none")
+    _within(mean, r[1], r[4])
+    _within(rstd, r[2], r[5])
+    _within(y, r[0], r[3], dt)
