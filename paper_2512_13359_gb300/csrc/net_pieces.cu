@@ -383,19 +383,18 @@ cudaError_t launch_direction(Scan a, cudaStream_t s) {
   const net_rows* rows[] = {&a.f, &a.v, &a.y, &a.dy, &a.df, &a.dv};
   constexpr int kArrays = BACK ? 6 : 3, kUnit = 16 / (int)sizeof(T);
   const int64_t per = a.D;
-  bool flat = true, even = true, units = true, pairs = per % 2 == 0;
+  const Tiles t = tiles_of(a.N, a.D, rows, kArrays);
+  bool even = true, units = true, pairs = per % 2 == 0;
   for (int i = 0; i < kArrays; ++i) {
-    flat = flat && (a.N == 1 || rows[i]->inner == a.D);
     even = even && (a.T == 1 || rows[i]->outer % kUnit == 0);
     units = units && aligned(*rows[i], a.T, a.N, sizeof(T), kUnit);
     pairs = pairs && aligned(*rows[i], a.T, a.N, sizeof(T), 2);
   }
-  if (flat) a.D *= a.N, a.N = 1;
+  if (t.flat) a.D *= a.N, a.N = 1;
   const int sms = sm_count();
-  const int64_t wide = a.N * ((a.D + 31) / 32), narrow = a.N * ((a.D + 15) / 16);
   // Blocks of 16 channels where those of 32 would leave SMs without one; then blocks in clusters until they have one.
-  const bool half = pairs && wide * 8 < sms;
-  const int64_t tiles = half ? narrow : wide;
+  const bool half = pairs && t.wide * 8 < sms;
+  const int64_t tiles = half ? t.narrow : t.wide;
   int ranks = 1;
   while (ranks < 8 && tiles * ranks < sms) ranks *= 2;
   if (ranks == 8 && tiles * 16 <= 96) ranks = 16;

@@ -319,22 +319,23 @@ __global__ void __launch_bounds__(kJoinThreads) k_join(int pieces, int64_t m, fl
 //  in blocks, or clusters of them where channels are few (net_pieces.cu): 3,300 to 4,600 for every round of blocks, of
 //    32 channels x 256 steps each (128 in fp32 and backward), that fit the SMs, two each (one backward in fp32; clusters
 //    fill less of the device).  512 steps of bf16 forward, walked and so: 32,768 channels 49 and 34 us, 131,072 channels
-//    87 and 121;
+//    87 and 121.  Rows that do not follow each other make a tile of their own however narrow they are: 512 steps of
+//    4,096 envs x 8 channels as halves of one projection 51 and 103, 1,000 steps of 100 x 8 73 and 10;
 //  in pieces whose maps are written, joined and walked from, where channels are few: 14,000, and their inputs twice, at
 //    6 TB/s.  65,536 steps of 256 bf16 channels: 4,960 us walked, 74 in clusters, 49 so; 8,192 of 500: 18.6 in
-//    clusters, 20 so.
+//    clusters, 20 so; 8,192 of 64 envs x 1 fp32, halves of one projection: 532, 49 and 17.
 enum class Way { kWalk, kBlocks, kPieces };
-Way way_of(int T, int64_t m, int size, bool back) {
+Way way_of(int T, int64_t m, const Tiles& t, int size, bool back) {
   if (T < 32) return Way::kWalk;
-  const int64_t sms = sm_count(), tiles = (m + 31) / 32;
-  const bool clusters = tiles * 8 < sms, large = back && size == 4;
+  const int64_t sms = sm_count(), tiles = t.wide;
+  const bool clusters = tiles * 8 < sms, few = (m + 31) / 32 * 8 < sms, large = back && size == 4;
   const int64_t rows = back || size == 4 ? 128 : 256;
-  const int64_t blocks = clusters ? std::min<int64_t>(128, (m + 15) / 16 * 8) : large ? sms : 2 * sms;
+  const int64_t blocks = clusters ? std::min<int64_t>(128, t.narrow * 8) : large ? sms : 2 * sms;
   const double round = large ? (clusters ? 6600 : 3300) : back ? 3900 : size == 4 ? 3300 : 4600;
   const double walk = (double)T * (back ? 190 : 100);
   const double held = round * (double)((tiles * ((T + rows - 1) / rows) + blocks - 1) / blocks);
   const double pieces = 14000.0 + (double)T * (double)m * size * (back ? 8 : 5) / 6000.0;
-  const bool split = clusters && pieces < held;
+  const bool split = few && pieces < held;
   if (walk <= (split ? pieces : held)) return Way::kWalk;
   return split ? Way::kPieces : Way::kBlocks;
 }
@@ -419,13 +420,13 @@ cudaError_t launch(const Scan& a, float* ws, cudaStream_t s) {
   // thread make twice the threads (4,096 envs x 256 channels x 128 steps of bf16: 127 us, 137 with eight), and two
   // where four would leave fewer than 160 threads an SM (512 steps, 65,536 channels: 55 us, 75 with four; 131,072: 99
   // and 86).
-  const Way way = way_of(a.T, m, sizeof(T), BACK);
+  const net_rows* rows[] = {&a.f, &a.v, &a.y, &a.dy, &a.df, &a.dv};
+  constexpr int kArrays = BACK ? 6 : 3;
+  const Way way = way_of(a.T, m, tiles_of(a.N, a.D, rows, kArrays), sizeof(T), BACK);
   if (way == Way::kBlocks) return launch_pieces<T>(a, BACK, s);
   const Split split = way == Way::kPieces ? split_of(a.T, m, ws) : Split{a.T, 1, kStepThreads, m, nullptr};
   int most = 16 / (int)sizeof(T);
   if (a.T > 1) most = split.maps || m >= 4 * 160 * sms ? 4 : 2;
-  const net_rows* rows[] = {&a.f, &a.v, &a.y, &a.dy, &a.df, &a.dv};
-  constexpr int kArrays = BACK ? 6 : 3;
   auto fits = [&](int e, int64_t n) {
     for (int i = 0; i < kArrays; ++i)
       if (!aligned(*rows[i], a.T, n, sizeof(T), e)) return false;
@@ -503,7 +504,9 @@ size_t net_gate_scan_workspace_bytes(const net_scan* a, int backward) {
   using namespace auv::net;
   if (!a || check(a) || !a->T || !a->N || !a->D) return 0;
   const int64_t m = a->N * a->D;
-  if (way_of((int)a->T, m, type_size(a->dtype), backward) != Way::kPieces) return 0;
+  const net_rows* const rows[] = {&a->f, &a->v, &a->y, &a->dy, &a->df, &a->dv};
+  const Tiles t = tiles_of(a->N, a->D, rows, backward ? 6 : 3);
+  if (way_of((int)a->T, m, t, type_size(a->dtype), backward) != Way::kPieces) return 0;
   return sizeof(float) * 2 * (size_t)split_of((int)a->T, m, nullptr).pieces * (size_t)m;
 }
 

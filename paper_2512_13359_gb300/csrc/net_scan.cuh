@@ -60,6 +60,19 @@ __device__ __forceinline__ Map then(const Map& p, const Map& q) {   // p, then q
 }
 __device__ __forceinline__ float apply(const Map& q, float h) { return cuts(q.A) ? q.B : fmaf(q.A, h, q.B); }
 
+// The tiles of 32 and of 16 channels that k_pieces makes of a step.  Rows that follow each other in every array are one
+// row (flat); otherwise each env has tiles of its own, however few channels they hold.
+struct Tiles {
+  bool flat;
+  int64_t wide, narrow;
+};
+inline Tiles tiles_of(int64_t N, int64_t D, const net_rows* const* rows, int arrays) {
+  bool flat = true;
+  for (int i = 0; i < arrays; ++i) flat = flat && (N == 1 || rows[i]->inner == D);
+  if (flat) D *= N, N = 1;
+  return {flat, N * ((D + 31) / 32), N * ((D + 15) / 16)};
+}
+
 // Few channels, many steps (net_pieces.cu); back: the gradients.
 constexpr int kPieceThreads = 256;
 template <typename T> cudaError_t launch_pieces(const Scan& a, bool back, cudaStream_t s);

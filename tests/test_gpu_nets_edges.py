@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 import nets_ref as R
-from test_gpu_nets import DT, _np, _t, _within
+from test_gpu_nets import DT, _check_scan, _np, _t, _within
 
 pytestmark = pytest.mark.gpu
 
@@ -124,3 +124,10 @@ def test_norm_after_a_first_value_far_from_the_rest(B, S, C, G, dt, first):
     _within(mean, r[1], r[4])
     _within(rstd, r[2], r[5])
     _within(y, r[0], r[3], dt)
+
+
+@pytest.mark.parametrize("layout", ["half", "odd"])
+@pytest.mark.parametrize("T,N,D,dt", [(512, 300, 8, "bf16"), (300, 500, 1, "fp32"), (260, 400, 3, "fp16"), (200, 90, 40, "bf16"),
+                                      (8192, 64, 1, "fp32"), (9001, 20, 3, "bf16")])
+def test_recurrence_of_narrow_rows_apart(T, N, D, dt, layout):
+    _check_scan(T, N, D, dt, layout, ends=0.01, seed=23)
