@@ -31,8 +31,12 @@
  *    must not overlap (AUV_ERR_SIZE), and an output must not overlap another
  *    array of the call, except where a call says so.
  *  - Sizes of 0 are valid: nothing is read, sums over nothing are 0.
- *  - Reproducible: every sum has a fixed order, so a call repeated with the same
- *    inputs, sizes and strides gives the same bits.
+ *  - Reproducible: every sum has a fixed order, which follows from the sizes,
+ *    the strides and how the data pointers are aligned (up to 16 bytes): a call
+ *    repeated with the same of these and the same inputs gives the same bits.
+ *  - Workspaces: a query takes the argument block as the call will get it.
+ *    Where an array's data is still NULL, the answer serves any alignment and
+ *    any strides that it may come to have, and every output.
  */
 #ifndef AUVNET_H
 #define AUVNET_H
@@ -95,7 +99,8 @@ typedef struct net_rows {
  *
  * workspace: net_gate_scan_workspace_bytes(a, backward) bytes, 16-byte
  * aligned (AUV_ERR_SIZE if there is less): 0 below 32 steps, and wherever the
- * sequence need not be split into pieces.
+ * sequence need not be split into pieces; rows that follow each other in
+ * memory and rows that do not may differ in that.
  */
 typedef struct net_scan {
   uint32_t struct_size;           /* sizeof(net_scan): version guard          */
@@ -136,7 +141,8 @@ int net_gate_scan_backward(const net_scan* a, void* stream);
  *
  * workspace: net_group_norm_workspace_bytes(a, backward) bytes, 16-byte
  * aligned (AUV_ERR_SIZE if there is less): 0 forward where a group has at most
- * 2,048 values and there are at most 32,768 groups, and often otherwise.
+ * 2,048 values and there are at most 32,768 groups, and often otherwise; the
+ * alignment of rows and data, and whether dgamma or dbeta is wanted, count.
  */
 typedef struct net_norm {
   uint32_t struct_size;           /* sizeof(net_norm): version guard          */

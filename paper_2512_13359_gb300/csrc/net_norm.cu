@@ -1134,14 +1134,15 @@ int pow2_at_least(int64_t n) {
   return p;
 }
 
-// Sizes and strides alone: the same for the workspace and the call.
-Plan make_plan(const net_norm* p, bool back) {
+// By sizes, types, and the alignment of strides and data; pieces of up to `most_e` channels (the workspace's query asks
+// for every alignment that arrays may come to have).
+Plan make_plan(const net_norm* p, bool back, int most_e = 8) {
   Plan q = {};
   const int size = type_size(p->dtype), sms = sm_count();
   const int64_t W = p->C / p->G;
   const net_rows* rows[2][2] = {{&p->x, &p->y}, {&p->x, &p->dy}};
   auto fits = [&](int e) {
-    bool ok = true;
+    bool ok = e <= most_e;
     for (const net_rows* r : rows[back])
       ok = ok && (p->B <= 1 || r->outer % e == 0) && (p->S <= 1 || r->inner % e == 0) &&
            reinterpret_cast<uintptr_t>(r->data) % ((size_t)size * e) == 0;
@@ -1401,7 +1402,13 @@ extern "C" {
 size_t net_group_norm_workspace_bytes(const net_norm* a, int backward) {
   using namespace auv::net;
   if (!a || check(a, backward) || !a->B || !a->S || !a->C) return 0;
-  return make_plan(a, backward).bytes;
+  if (a->x.data && (backward ? a->dy.data && a->dx.data : a->y.data != nullptr)) return make_plan(a, backward).bytes;
+  net_norm any = *a;
+  any.x = any.y = any.dy = any.dx = net_rows{};
+  any.dgamma = any.dbeta = reinterpret_cast<float*>(16);      // wanted; not read here
+  size_t most = 0;
+  for (int e = 8; e; e /= 2) most = std::max(most, make_plan(&any, backward, e).bytes);
+  return most;
 }
 
 int net_group_norm(const net_norm* a, void* stream) { return auv::net::run(a, false, stream); }

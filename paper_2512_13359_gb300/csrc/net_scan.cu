@@ -505,8 +505,12 @@ size_t net_gate_scan_workspace_bytes(const net_scan* a, int backward) {
   if (!a || check(a) || !a->T || !a->N || !a->D) return 0;
   const int64_t m = a->N * a->D;
   const net_rows* const rows[] = {&a->f, &a->v, &a->y, &a->dy, &a->df, &a->dv};
-  const Tiles t = tiles_of(a->N, a->D, rows, backward ? 6 : 3);
-  if (way_of((int)a->T, m, t, type_size(a->dtype), backward) != Way::kPieces) return 0;
+  const int arrays = backward ? 6 : 3;
+  auto split = [&](const Tiles& t) { return way_of((int)a->T, m, t, type_size(a->dtype), backward) == Way::kPieces; };
+  bool there = true;
+  for (int i = 0; i < arrays; ++i) there = there && rows[i]->data;
+  if (!(there ? split(tiles_of(a->N, a->D, rows, arrays)) : split(tiles(a->N, a->D, true)) || split(tiles(a->N, a->D, false))))
+    return 0;
   return sizeof(float) * 2 * (size_t)split_of((int)a->T, m, nullptr).pieces * (size_t)m;
 }
 

@@ -66,11 +66,14 @@ struct Tiles {
   bool flat;
   int64_t wide, narrow;
 };
+inline Tiles tiles(int64_t N, int64_t D, bool flat) {
+  if (flat) D *= N, N = 1;
+  return {flat, N * ((D + 31) / 32), N * ((D + 15) / 16)};
+}
 inline Tiles tiles_of(int64_t N, int64_t D, const net_rows* const* rows, int arrays) {
   bool flat = true;
   for (int i = 0; i < arrays; ++i) flat = flat && (N == 1 || rows[i]->inner == D);
-  if (flat) D *= N, N = 1;
-  return {flat, N * ((D + 31) / 32), N * ((D + 15) / 16)};
+  return tiles(N, D, flat);
 }
 
 // Few channels, many steps (net_pieces.cu); back: the gradients.

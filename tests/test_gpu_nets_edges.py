@@ -131,3 +131,29 @@ def test_norm_after_a_first_value_far_from_the_rest(B, S, C, G, dt, first):
                                       (8192, 64, 1, "fp32"), (9001, 20, 3, "bf16")])
 def test_recurrence_of_narrow_rows_apart(T, N, D, dt, layout):
     _check_scan(T, N, D, dt, layout, ends=0.01, seed=23)
+
+
+@pytest.mark.parametrize("B,S,C,G", [(500, 300, 128, 1), (256, 1, 90, 9), (3, 5000, 64, 2), (70, 40, 48, 6)])
+def test_a_workspace_sized_before_the_arrays_serves_any_alignment(B, S, C, G):
+    torch, nets, types = _t()
+    L, F = nets.lib(), nets._NORM
+    n = B * S * C
+    x, dy = (torch.randn(n + 8, device="cuda").to(torch.bfloat16) for _ in range(2))
+    y, dx = (torch.empty(n + 8, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    mean, rstd = (torch.empty((B, G), device="cuda") for _ in range(2))
+    dg, db = (torch.empty(C, device="cuda") for _ in range(2))
+
+    def block(off, there=True):
+        at = lambda t: (t.data_ptr() + 2 * off if there else 0, S * C, C)      # noqa: E731
+        flat = [t.data_ptr() if there else 0 for t in (mean, rstd, dg, db)]
+        return (F.size, 1, 2, 1e-5, B, S, C, G, *at(x), *at(y), *at(dy), *at(dx), 0, 0, *flat)
+    need = [L.net_group_norm_workspace_bytes(F.pack(*block(0, False), 0, 0), back) for back in (0, 1)]
+    ws = torch.empty(max(need) + 16, dtype=torch.uint8, device="cuda")
+    for off in (0, 1, 2, 4, 7):
+        for back, fn in enumerate((L.net_group_norm, L.net_group_norm_backward)):
+            assert fn(F.pack(*block(off), ws.data_ptr(), need[back]), None) == 0, L.net_last_error()
+        xs, ds = (t[off:off + n].view(B, S, C) for t in (x, dy))
+        want = nets.group_norm(xs, G, act="silu")
+        assert torch.equal(y[off:off + n].view(B, S, C), want[0]) and torch.equal(rstd, want[2])
+        want = nets.group_norm_backward(xs, G, None, None, mean, rstd, ds, act="silu")
+        assert torch.equal(dx[off:off + n].view(B, S, C), want[0]) and torch.equal(dg, want[1]) and torch.equal(db, want[2])
