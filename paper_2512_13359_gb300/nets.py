@@ -9,6 +9,7 @@ place.  There is no CPU fallback.  Wrong arguments raise AuvError with the libra
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import struct
 
 import torch
@@ -90,6 +91,8 @@ def _activation(x, name):
 def _rows(t, name, like):
     """(pointer, outer, inner) of an activation of the (shape, type, device) `like`."""
     shape, dtype, index = like
+    if not isinstance(t, torch.Tensor):
+        _fail(AUV_ERR_INVALID, f"{name} is not a tensor")
     if t.shape != shape or t.dtype is not dtype or t.get_device() != index:
         _fail(AUV_ERR_INVALID, f"{name}: {tuple(t.shape)} {t.dtype} on {t.device}, expected "
                                f"{tuple(shape)} {dtype} on device {index}")
@@ -103,6 +106,8 @@ def _flat(t, name, shape, dtype, index):
     """Pointer of a contiguous array, 0 for None."""
     if t is None:
         return 0
+    if not isinstance(t, torch.Tensor):
+        _fail(AUV_ERR_INVALID, f"{name} is not a tensor")
     if t.shape != shape or t.dtype is not dtype or t.get_device() != index:
         _fail(AUV_ERR_INVALID, f"{name}: {tuple(t.shape)} {t.dtype} on {t.device}, expected "
                                f"{tuple(shape)} {dtype} on device {index}")
@@ -112,7 +117,7 @@ def _flat(t, name, shape, dtype, index):
 
 
 def _flags(t, name, shape, index):
-    return _flat(t, name, shape, torch.bool if t is not None and t.dtype is torch.bool else torch.uint8, index)
+    return _flat(t, name, shape, torch.bool if getattr(t, "dtype", None) is torch.bool else torch.uint8, index)
 
 
 def _new(shape, dtype, index, scratch):
@@ -121,12 +126,19 @@ def _new(shape, dtype, index, scratch):
     return t
 
 
+def _pack(form, *fields):
+    try:
+        return form.pack(*fields)
+    except (struct.error, OverflowError) as e:
+        _fail(AUV_ERR_INVALID, f"an argument is no number, or too large: {e}")
+
+
 def _call_with_workspace(fn, size_of, backward, form, fields, index, stream, scratch):
     """A call whose argument block ends in a workspace, allocated here if one is needed."""
-    args = form.pack(*fields, 0, 0)
+    args = _pack(form, *fields, 0, 0)
     need = size_of(args, backward)
     if need:
-        args = form.pack(*fields, _new(need, torch.uint8, index, scratch).data_ptr(), need)
+        args = _pack(form, *fields, _new(need, torch.uint8, index, scratch).data_ptr(), need)
     _call(fn, args, index, stream, scratch)
 
 
@@ -147,7 +159,7 @@ def gate_scan(f, v, h0=None, *, done=None, done_prev=None, y=None, hT=None, stre
               0, 0, _flags(done, "done", (T, N), index), _flags(done_prev, "done_prev", (N,), index))
     L = lib()
     if T < 32:                        # short sequences need no workspace
-        _call(L.net_gate_scan, _SCAN.pack(*fields, 0, 0), index, stream, scratch)
+        _call(L.net_gate_scan, _pack(_SCAN, *fields, 0, 0), index, stream, scratch)
     else:
         _call_with_workspace(L.net_gate_scan, L.net_gate_scan_workspace_bytes, 0, _SCAN, fields, index, stream, scratch)
     return y, hT
@@ -174,18 +186,20 @@ def gate_scan_backward(f, v, y, dy, h0=None, *, done=None, done_prev=None, dhT=N
               _flags(done_prev, "done_prev", (N,), index))
     L = lib()
     if T < 32:
-        _call(L.net_gate_scan_backward, _SCAN.pack(*fields, 0, 0), index, stream, scratch)
+        _call(L.net_gate_scan_backward, _pack(_SCAN, *fields, 0, 0), index, stream, scratch)
     else:
         _call_with_workspace(L.net_gate_scan_backward, L.net_gate_scan_workspace_bytes, 1, _SCAN, fields, index, stream,
                              scratch)
     return df, dv, dh0
 
 
-def _norm_head(act, groups):
-    if act not in NET_ACT:
+def _norm_head(act, groups, channels):
+    if not isinstance(act, str) or act not in NET_ACT:
         _fail(AUV_ERR_INVALID, f"act {act!r} is none of {', '.join(NET_ACT)}")
     if not isinstance(groups, int) or groups < 1:
         _fail(AUV_ERR_INVALID, f"groups {groups!r} is no positive number")
+    if channels % groups or groups > 1 << 31:
+        _fail(AUV_ERR_INVALID, f"{channels} channels are no multiple of {groups} groups")
     return NET_ACT[act]
 
 
@@ -195,8 +209,8 @@ def group_norm(x, groups, gamma=None, beta=None, *, eps=1e-5, act="none", y=None
     (y [B, S, C], mean [B, groups], rstd [B, groups])."""
     scratch = []
     like = shape, dtype, index = _activation(x, "x")
-    kind = _norm_head(act, groups)
     B, S, Ch = shape
+    kind = _norm_head(act, groups, Ch)
     f32, stats = torch.float32, (B, groups)
     if y is None:
         y = _new(shape, dtype, index, scratch)
@@ -209,7 +223,7 @@ def group_norm(x, groups, gamma=None, beta=None, *, eps=1e-5, act="none", y=None
               _flat(mean, "mean", stats, f32, index), _flat(rstd, "rstd", stats, f32, index), 0, 0)
     L = lib()
     if S * Ch <= 2048 * groups <= 1 << 26:      # small groups need no workspace
-        _call(L.net_group_norm, _NORM.pack(*fields, 0, 0), index, stream, scratch)
+        _call(L.net_group_norm, _pack(_NORM, *fields, 0, 0), index, stream, scratch)
     else:
         _call_with_workspace(L.net_group_norm, L.net_group_norm_workspace_bytes, 0, _NORM, fields, index, stream, scratch)
     return y, mean, rstd
@@ -220,8 +234,8 @@ def group_norm_backward(x, groups, gamma, beta, mean, rstd, dy, *, act="none", d
     """Gradients (dx, dgamma, dbeta) of group_norm from dy [B, S, C]; mean and rstd as it returned them."""
     scratch = []
     like = shape, dtype, index = _activation(x, "x")
-    kind = _norm_head(act, groups)
     B, S, Ch = shape
+    kind = _norm_head(act, groups, Ch)
     f32, stats = torch.float32, (B, groups)
     if dx is None:
         dx = _new(shape, dtype, index, scratch)
@@ -248,8 +262,12 @@ def dropout(x, p, seed, draw, *, residual=None, shared=False, y=None, stream=Non
     like = shape, dtype, index = _activation(x, "x")
     if y is None:
         y = _new(shape, dtype, index, scratch)
-    args = _DROP.pack(_DROP.size, NET_DTYPE[dtype], bool(shared), 0, *shape, *_rows(x, "x", like),
-                      *(_NO_ROWS if residual is None else _rows(residual, "residual", like)), *_rows(y, "y", like), p,
-                      seed & 0xFFFFFFFFFFFFFFFF, draw & 0xFFFFFFFFFFFFFFFF)
+    try:
+        seed, draw = operator.index(seed) & 0xFFFFFFFFFFFFFFFF, operator.index(draw) & 0xFFFFFFFFFFFFFFFF
+    except TypeError:
+        _fail(AUV_ERR_INVALID, f"seed {seed!r} or draw {draw!r} is no whole number")
+    args = _pack(_DROP, _DROP.size, NET_DTYPE[dtype], bool(shared), 0, *shape, *_rows(x, "x", like),
+                 *(_NO_ROWS if residual is None else _rows(residual, "residual", like)), *_rows(y, "y", like), p,
+                 seed, draw)
     _call(lib().net_dropout, args, index, stream, scratch)
     return y

@@ -157,3 +157,19 @@ def test_a_workspace_sized_before_the_arrays_serves_any_alignment(B, S, C, G):
         assert torch.equal(y[off:off + n].view(B, S, C), want[0]) and torch.equal(rstd, want[2])
         want = nets.group_norm_backward(xs, G, None, None, mean, rstd, ds, act="silu")
         assert torch.equal(dx[off:off + n].view(B, S, C), want[0]) and torch.equal(dg, want[1]) and torch.equal(db, want[2])
+
+
+def test_arguments_of_a_wrong_kind():
+    torch, nets, types = _t()
+    from paper_2512_13359_gb300.auvenv import AUV_ERR_INVALID, AuvError
+    x = torch.randn((4, 6, 8), device="cuda")
+    stats = torch.zeros((4, 2), device="cuda")
+    for bad in (lambda: nets.dropout(x, "0.5", 0, 0), lambda: nets.dropout(x, None, 0, 0),
+                lambda: nets.dropout(x, 0.5, 1.5, 0), lambda: nets.dropout(x, 0.5, 0, None),
+                lambda: nets.dropout(x, 0.5, 0, 0, residual=[1.0]), lambda: nets.group_norm(x, 2, eps="1"),
+                lambda: nets.group_norm(x, 1 << 70), lambda: nets.group_norm(x, 2, [1.0] * 8),
+                lambda: nets.group_norm(x, 2, y=3), lambda: nets.group_norm_backward(x, 2, None, None, stats, 1.0, x),
+                lambda: nets.gate_scan(x, 1.0), lambda: nets.gate_scan(x, x, h0=0.0), lambda: nets.gate_scan(x, x, done=[0])):
+        with pytest.raises(AuvError) as e:
+            bad()
+        assert e.value.code == AUV_ERR_INVALID, str(e.value)
