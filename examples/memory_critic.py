@@ -82,7 +82,7 @@ class MemoryCritic:
         g["v"] = self._gemm(1, d, rows, dv, 1, True, s["o"], d, True, torch.empty((1, d), device="cuda"), d)
         do = self._gemm(rows, d, 1, dv, 1, False, self.w["v"], d, True, torch.empty((rows, 1, d), device="cuda"), d)
         du, g["gamma"], g["beta"] = nets.group_norm_backward(s["u"].view(rows, 1, d), 1, self.w["gamma"], self.w["beta"],
-                                                             s["mean"], s["rstd"], do, act="relu", dx=do)
+                                                             s["mean"], s["rstd"], do, act="relu")
         dh = nets.dropout(du.view(T, N, d), self.p, self.seed, self.draw, shared=True, y=du.view(T, N, d))
         z, dz = s["z"], torch.empty_like(s["z"])
         nets.gate_scan_backward(z[..., :d], z[..., d:], s["h"], dh, s["state"], done=s["done"], done_prev=s["ended"],

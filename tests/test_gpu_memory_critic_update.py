@@ -1,0 +1,36 @@
+"""The updates of examples/memory_critic.py."""
+import os
+import sys
+
+import pytest
+
+from parity_util import need_gpu
+
+pytestmark = pytest.mark.gpu
+sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+
+
+def _inputs(torch, T=6, N=20, width=24):
+    import memory_critic as M
+    c = M.MemoryCritic(18, width, seed=5)
+    g = torch.Generator(device="cuda").manual_seed(9)
+    obs = torch.randn((T, N, 18), device="cuda", generator=g)
+    state = torch.zeros((N, width), device="cuda")
+    done = torch.zeros((T, N), dtype=torch.uint8, device="cuda")
+    return c, obs, torch.randn((T, N), device="cuda", generator=g), state, done, done[0]
+
+
+def test_outputs_overlap_no_other_array(monkeypatch):
+    torch = need_gpu()
+    from paper_2512_13359_gb300 import nets
+    c, obs, targets, state, done, ended = _inputs(torch)
+    seen = []
+    call = nets.group_norm_backward
+
+    def watch(x, groups, gamma, beta, mean, rstd, dy, **out):
+        ins = {t.data_ptr() for t in (x, gamma, beta, mean, rstd, dy) if t is not None}
+        seen.append(all(t.data_ptr() not in ins for t in out.values() if isinstance(t, torch.Tensor)))
+        return call(x, groups, gamma, beta, mean, rstd, dy, **out)
+    monkeypatch.setattr(nets, "group_norm_backward", watch)
+    c.update(obs, targets, state, done, ended)
+    assert seen and all(seen)
