@@ -34,7 +34,7 @@ class MemoryCritic:
     def __init__(self, obs_dim: int, width: int, p: float = 0.05, seed: int = 0, lr: float = 1e-2):
         g = torch.Generator(device="cuda").manual_seed(seed)
         self.obs_dim, self.width, self.p, self.seed, self.lr = obs_dim, width, p, seed, lr
-        self.draw = 0
+        self.draw = self.steps = 0           # masks drawn, updates made: a pass that only values draws a mask too
         self.w = dict(z=torch.randn(2 * width, obs_dim, device="cuda", generator=g) * obs_dim ** -0.5,
                       gamma=torch.ones(width, device="cuda"), beta=torch.zeros(width, device="cuda"),
                       v=torch.randn(1, width, device="cuda", generator=g) * width ** -0.5,
@@ -96,10 +96,11 @@ class MemoryCritic:
         values, s = self.forward(obs, state, done, ended)
         err = values - targets
         g = self.backward(err / err.numel(), s)
+        self.steps += 1
+        c1, c2 = 1 - 0.9 ** self.steps, 1 - 0.99 ** self.steps
         for k, w in self.w.items():
             self.m1[k].lerp_(g[k].view_as(w), 0.1)
             self.m2[k].lerp_(g[k].view_as(w) ** 2, 0.01)
-            c1, c2 = 1 - 0.9 ** self.draw, 1 - 0.99 ** self.draw
             w -= self.lr * (self.m1[k] / c1) / ((self.m2[k] / c2).sqrt() + 1e-8)
         return 0.5 * (err ** 2).mean(), s["hT"]
 

@@ -34,3 +34,18 @@ def test_outputs_overlap_no_other_array(monkeypatch):
     monkeypatch.setattr(nets, "group_norm_backward", watch)
     c.update(obs, targets, state, done, ended)
     assert seen and all(seen)
+
+
+def test_the_first_update_is_adams_first_step():
+    """Whatever was valued before: with both moments corrected for one step, m1 / sqrt(m2) is the gradient's sign and
+    each weight moves by the rate."""
+    torch = need_gpu()
+    c, obs, targets, state, done, ended = _inputs(torch)
+    for _ in range(3):
+        c.forward(obs, state, done, ended)
+    before = {k: w.clone() for k, w in c.w.items()}
+    c.update(obs, targets, state, done, ended)
+    for k, w in c.w.items():
+        # gradients are some 1e-2, of which 1e-8 in the denominator takes 1e-6, and weights of order 1 round to 1e-7
+        moved = (w - before[k]).abs().max()
+        assert abs(moved - c.lr) <= 1e-3 * c.lr, (k, float(moved))
