@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 import nets_ref as R
-from test_gpu_nets import DT, _check_scan, _np, _t, _within
+from test_gpu_nets import DT, _check_norm, _check_scan, _np, _t, _within
 
 pytestmark = pytest.mark.gpu
 
@@ -173,3 +173,36 @@ def test_arguments_of_a_wrong_kind():
         with pytest.raises(AuvError) as e:
             bad()
         assert e.value.code == AUV_ERR_INVALID, str(e.value)
+
+
+@pytest.mark.parametrize("T,N,D,dt,layout", [
+    (512, 1, 8192, "bf16", "flat"), (513, 5, 1031, "fp16", "odd"), (700, 40, 130, "fp32", "pad"), (1025, 3, 1700, "fp32", "flat"),
+    (3000, 2, 600, "bf16", "half"), (1500, 37, 18, "fp16", "flat")])
+def test_recurrence_in_rounds_of_blocks(T, N, D, dt, layout):
+    """More steps than the blocks, or clusters of them, hold at a time."""
+    _check_scan(T, N, D, dt, layout, ends=0.01, seed=21)
+
+
+@pytest.mark.parametrize("T,N,D,dt,layout", [
+    (45, 400, 256, "bf16", "flat"), (45, 400, 256, "fp32", "half"), (21, 3300, 30, "fp16", "flat"), (21, 3300, 30, "fp32", "flat"),
+    (17, 1000, 100, "bf16", "pad"), (33, 3001, 36, "fp16", "half")])
+def test_recurrence_of_many_channels_past_its_ring(T, N, D, dt, layout):
+    _check_scan(T, N, D, dt, layout, ends=0.1, seed=22)
+
+
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("B,S,C,G,layout", [
+    (2, 9000, 18, 2, "flat"), (2, 9000, 18, 2, "half"),       # pieces of two groups, two wide
+    (1, 20000, 24, 2, "pad"), (2, 6000, 12, 2, "flat"),       # and wider ones
+    (2, 5000, 8, 8, "flat"), (1, 7000, 24, 8, "flat"),        # of many groups
+    (1, 9000, 20, 1, "odd")])
+def test_norm_by_chunks_whose_pieces_share_groups(B, S, C, G, layout, dt):
+    _check_norm(B, S, C, G, dt, "silu", layout, seed=31)
+
+
+@pytest.mark.parametrize("B,S,C,G,dt", [
+    (200, 550, 80, 10, "bf16"), (200, 550, 80, 10, "fp32"),   # a last slab of fewer groups; a block an instance
+    (200, 80, 64, 1, "bf16"), (170, 250, 72, 3, "fp16"),      # one block in either direction
+    (3, 5000, 88, 11, "fp16"), (5, 900, 60, 5, "fp32")])      # fewer groups, in clusters
+def test_norm_slabs(B, S, C, G, dt):
+    _check_norm(B, S, C, G, dt, "silu", seed=32)
