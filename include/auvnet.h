@@ -21,8 +21,8 @@
  *  - Asynchrony: every call only enqueues work on `stream` (a cudaStream_t;
  *    NULL = the legacy default stream).  No call synchronises, allocates or
  *    keeps anything: calls can be captured in a CUDA graph.
- *  - Memory: every array is device memory of the current device (AUV_ERR_SIZE
- *    otherwise), owned by the caller.  Activations are fp32, bf16 or fp16 (all
+ *  - Memory: every array is device memory (AUV_ERR_SIZE otherwise) of the
+ *    current device (AUV_ERR_INVALID otherwise), owned by the caller.  Activations are fp32, bf16 or fp16 (all
  *    of a call the same); states, statistics, weights and their gradients are
  *    fp32, and so is all arithmetic: a 16-bit result is rounded once (to
  *    nearest even) when it is stored.

@@ -90,10 +90,10 @@ __device__ __forceinline__ void store(T* p, const float (&x)[E]) {
   *reinterpret_cast<Raw<T, E>*>(p) = pack<T, E>(x);
 }
 
-// sigmoid(x) and sigmoid(-x) from one exponential; both are right to a few
-// ulp, which 1 - sigmoid(x) is not where the gate is nearly shut.  Eight
-// instructions: the flush of what is below 2^-126 spares the scalings around
-// the two approximations.
+// sigmoid(x) and sigmoid(-x) from q = exp(-|x|), taken as 2^(-|x| log2 e): 1 / (1 + q) and q / (1 + q), neither of them
+// 1 - the other, which has no digits left where the gate is nearly shut.  The product with log2 e is rounded, so q, and
+// with it the smaller gate, is off by up to 2^-24 (|x| + 12) of itself; below 2^-126 it is 0.  The larger is right to a
+// few units of 2^-24.  Eight instructions.
 __device__ __forceinline__ void gates(float x, float& a, float& b) {
   float e, r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fabsf(x) * -1.44269504088896341f));

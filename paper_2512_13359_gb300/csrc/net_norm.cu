@@ -7,14 +7,15 @@
 //                           in registers and goes from instance to instance.  A team's channels stay the same, so the
 //                           backward pass sums dgamma and dbeta in registers and joins them once at its end.  65,536 x
 //                           256 bf16, one group: forward 12.8 us (5.2 TB/s; half of it issuing instructions), backward
-//                           28 us (3.6 TB/s, 60 registers of weights and their sums leave two blocks an SM).
+//                           28 us (3.6 TB/s; it waits for loads: 60 registers of weights and their sums leave two blocks
+//                           an SM, 16 warps).
 //  k_slab, k_slab_back      larger groups, as long as a cluster of blocks holds some adjacent ones of an instance in shared
 //                           memory, each block some positions: statistics are joined through distributed shared memory.
-//                           64 x 4,096 x 256 bf16, 32 groups: forward 60 us (4.5 TB/s), backward 136 us (3 TB/s): three
-//                           blocks an SM, between their barriers.
+//                           64 x 4,096 x 256 bf16, 32 groups: forward 60 us (4.5 TB/s), backward 136 us (3 TB/s): a block
+//                           loads, joins and stores in turn, and three an SM cover that by half (issue slots 50 %).
 //  k_part, k_stats, k_apply the rest: sums by chunk and channel, joined, and the elements read once more.  65,536 x 256
-//                           bf16 as one instance: forward 35 us, backward 68 us.
-//  (.._back)
+//  (.._back)                bf16 as one instance of 8 groups: forward 35 us, backward 63 us; as one group, whose chunks a
+//                           single block joins, 108 and 100.
 //
 // Variances are those of deviations: in registers from the mean, else of up to 32 values from the first of them, joined
 // by the distances of the means (Chan et al.).  All sums have a fixed order.
@@ -94,7 +95,8 @@ __device__ __forceinline__ void fill(float (&x)[E], float v) {
   for (int e = 0; e < E; ++e) x[e] = v;
 }
 
-// sigmoid(u): three instructions a value, two of them the approximations'.  Where the exponential overflows it is 0.
+// sigmoid(u) = 1 / (1 + 2^(-u log2 e)): three instructions a value, two of them the approximations'.  As with the gates,
+// the rounded product makes it 2^-24 (|u| + 12) of itself off where it is small; where the exponential overflows it is 0.
 template <int E>
 __device__ __forceinline__ void sigmoid(const float (&u)[E], float (&s)[E]) {
   float one[E];

@@ -5,6 +5,12 @@
 from a counter, never stored) launch the library's CUDA kernels on the current (or given) stream and return without
 waiting.  Outputs are allocated unless they are given; a raw state or gradient buffer given as an output is written in
 place.  There is no CPU fallback.  Wrong arguments raise AuvError with the library's code and reason.
+
+Gradients are calls of their own: tensors that require gradients are taken as they are, and outputs carry no graph.
+
+A given stream is the caller's to order, as with every call of the package: behind what made the inputs, and ahead of what
+uses the outputs.  A call that allocates also makes it wait for the current stream, whose memory the allocations are; one
+whose outputs are all given may not, so nothing should rest on that.
 """
 from __future__ import annotations
 
