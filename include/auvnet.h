@@ -13,6 +13,12 @@
  *  - net_dropout: dropout whose mask is drawn where it is used and never
  *    stored, optionally added to a residual; the backward pass is the same
  *    call on the gradient.
+ *  - net_causal_conv and net_select_scan: a memory with many states a channel,
+ *    whose decays and inputs are chosen by the input (a selective state space
+ *    layer), and the short convolution in front of it; both with the rollout's
+ *    episode ends, their backward passes and, with T = 1, their single steps.
+ *  - net_orthogonalise: weight matrices' updates with their singular values
+ *    moved towards 1 by Newton-Schulz products.
  *
  * Conventions
  *  - Return value: AUV_OK (0) or a negative AUV_ERR_* code (auvenv.h);
@@ -184,6 +190,158 @@ typedef struct net_drop {
   uint64_t seed, draw;
 } net_drop;
 int net_dropout(const net_drop* a, void* stream);
+
+/*
+ * net_causal_conv: for every env n and channel d, along the steps t
+ *
+ *   y[t] = act(b + sum over k < K of w[k] x[t - (K - 1) + k]),
+ *
+ * with x[-j] = state[K - 1 - j], and in the place of rows behind an episode end
+ * zeros: what an ended episode's rows held, infinities and NaN too, passes
+ * nothing on.  new_state: the last K - 1 rows of (state, x), zeros where an
+ * episode has ended ahead of the last step; the next call's state, together
+ * with its done_prev.  done, done_prev as in net_gate_scan.  state and
+ * new_state are of the activations' type; new_state may be state.  bias,
+ * state, new_state, done, done_prev may be NULL: zeros, zeros, not wanted, no
+ * ends.  act: NET_ACT_NONE or NET_ACT_SILU.  K <= 8 (AUV_ERR_UNSUPPORTED).
+ *
+ * net_causal_conv_backward: dx, dw, dbias and dstate (each of the last three
+ * unless NULL) from dy, dnew_state (NULL: zeros) and what the forward call had.
+ * With p the sums in front of act and dp = dy act'(p),
+ *
+ *   dx[s] = sum over j of w[K - 1 - j] dp[s + j], j < K, of the steps s + j
+ *           that see row s, + dnew_state where row s is left in the state,
+ *   dw[k] = sum of dp[t] x[t - (K - 1) + k],   dbias = sum of dp,
+ *
+ * dstate as dx, for the rows ahead of the first.
+ *
+ * workspace: net_causal_conv_workspace_bytes(a, backward) bytes, 16-byte
+ * aligned: 0 forward, and backward where neither dw nor dbias is wanted.
+ */
+typedef struct net_conv {
+  uint32_t struct_size;           /* sizeof(net_conv): version guard          */
+  uint32_t dtype;                 /* NET_*: type of x, y, dy, dx, the states  */
+  uint32_t act;                   /* NET_ACT_NONE or NET_ACT_SILU             */
+  uint32_t reserved;              /* 0                                        */
+  int64_t T, N, D, K;             /* steps, envs, channels, taps              */
+  net_rows x, y, dy, dx;          /* [T][N][D]                                */
+  const float *w, *bias;          /* [K][D], [D]                              */
+  const void* state;              /* [K - 1][N][D]                            */
+  void* new_state;                /* [K - 1][N][D]                            */
+  const void* dnew_state;         /* [K - 1][N][D]                            */
+  void* dstate;                   /* [K - 1][N][D]                            */
+  float *dw, *dbias;              /* [K][D], [D]                              */
+  const uint8_t* done;            /* [T][N]                                   */
+  const uint8_t* done_prev;       /* [N]                                      */
+  void* workspace;
+  size_t workspace_bytes;
+} net_conv;
+size_t net_causal_conv_workspace_bytes(const net_conv* a, int backward);
+int net_causal_conv(const net_conv* a, void* stream);
+int net_causal_conv_backward(const net_conv* a, void* stream);
+
+/*
+ * net_select_scan: a state space layer whose step sizes, inputs and outputs are
+ * functions of the input.  For every env n, channel d with S states, and g the
+ * group of D / G channels that d is in, along the steps t
+ *
+ *   e = softplus(dt[t] + dt_bias),
+ *   h[t][s] = exp(e A[d][s]) c[t][s] + e B[t][g][s] x[t],
+ *   y[t] = (sum over s of C[t][g][s] h[t][s] + skip x[t]) silu(gate[t]),
+ *
+ * c[t] = 0 where an episode ended before step t (done, done_prev as in
+ * net_gate_scan), else h[t - 1]; h[-1] = h0, hT = h[T - 1].  Nothing of an
+ * ended episode's state passes.  A state that has become infinite is infinite
+ * or NaN until its episode ends.  In a rollout T = 1, done_prev = the env's
+ * last flags and hT = h0 for states updated in place.
+ *
+ * B and C have rows of G S channels.  h0, hT and kept are fp32.  kept
+ * [(T + 15) / 16][N][D][S]: h before steps 0, 16, 32, ..., from which the
+ * backward pass starts again.  gate.data, skip, dt_bias, h0, done, done_prev
+ * may be NULL: no gate, zeros, zeros, zeros, no ends; hT, kept: not wanted.
+ * S <= 128 (AUV_ERR_UNSUPPORTED).
+ *
+ * net_select_scan_backward: gradients from dy, dhT (NULL: zeros), kept as the
+ * forward call wrote it, and the other arguments of that call (h0 is kept's
+ * first state).  With p = dy silu(gate), f the gradient of h[t], G' = that of
+ * c[t + 1] (dhT after the last step), and sums over the s of a channel, the d
+ * of a group, or all t and n, as the output's indices say,
+ *
+ *   f = C p + G',   dC = sum p h,   dB = sum e x f,   dA = sum f a c e,
+ *   dx = skip p + e sum B f,   de = sum f (a c A + B x),   dskip = sum p x,
+ *   ddt = de sigmoid(dt + dt_bias),   ddt_bias = sum ddt,
+ *   dgate = dy silu'(gate) (y in front of the gate),
+ *   gradient of c[t] = a f, or 0 where an episode ended before step t;
+ *   dh0 that of c[0],
+ *
+ * a = exp(e A).  dA, dskip, ddt_bias, dgate.data, dh0 may be NULL: not wanted;
+ * dgate has no use without a gate.  dh0 = dhT is allowed.
+ *
+ * workspace: net_select_scan_workspace_bytes(a, backward) bytes, 16-byte
+ * aligned; forward 0 unless envs and channels are few and steps many.
+ */
+typedef struct net_select {
+  uint32_t struct_size;           /* sizeof(net_select): version guard        */
+  uint32_t dtype;                 /* NET_*: type of the rows                  */
+  int64_t T, N, D, S, G;          /* steps, envs, channels, states, groups    */
+  net_rows x, dt, gate, y;        /* [T][N][D]                                */
+  net_rows B, C;                  /* [T][N][G S]                              */
+  net_rows dy, dx, ddt, dgate;    /* [T][N][D]                                */
+  net_rows dB, dC;                /* [T][N][G S]                              */
+  const float* A;                 /* [D][S]                                   */
+  const float *skip, *dt_bias;    /* [D]                                      */
+  const float* h0;                /* [N][D][S]                                */
+  float* hT;                      /* [N][D][S]                                */
+  float* kept;                    /* [(T + 15) / 16][N][D][S]                 */
+  const float* dhT;               /* [N][D][S]                                */
+  float* dh0;                     /* [N][D][S]                                */
+  float* dA;                      /* [D][S]                                   */
+  float *dskip, *ddt_bias;        /* [D]                                      */
+  const uint8_t* done;            /* [T][N]                                   */
+  const uint8_t* done_prev;       /* [N]                                      */
+  void* workspace;
+  size_t workspace_bytes;
+} net_select;
+size_t net_select_scan_workspace_bytes(const net_select* a, int backward);
+int net_select_scan(const net_select* a, void* stream);
+int net_select_scan_backward(const net_select* a, void* stream);
+
+/*
+ * net_orthogonalise: y = p(p(...(x / (|x| + eps)))), `steps` times, of each of
+ * the L matrices x [M][N] (i = the matrix, j = the row), |x| its Frobenius
+ * norm, with
+ *
+ *   p(x) = a x + (b P + c P P) x,   P = x x^T,
+ *
+ * which takes each singular value v to a v + b v^3 + c v^5 and leaves the
+ * singular vectors: with coef (a, b, c) = (3.4445, -4.775, 2.0315) and five
+ * steps an update's singular values come to lie about 1.  Where M > N the
+ * products are x (b P + c P P) with P = x^T x, the same polynomial.  Norms are
+ * taken in range whatever the scale of x.  steps = 0: y = x / (|x| + eps).
+ *
+ * The products are taken of two fp16 pieces of every value (22 bits) with sums
+ * in fp32, so the coefficients have to keep what is between them in fp16's
+ * range: from v in [0, 1] no singular value may come above 8, nor
+ * |a| + |b| v^2 + |c| v^4 above 1000 (AUV_ERR_UNSUPPORTED; the usual ones reach 1.3 and 15).
+ *
+ * workspace: net_orthogonalise_workspace_bytes(a) bytes, 256-byte aligned.  Its
+ * first 32-bit word is AUV_OK after the call has run, or AUV_ERR_TIMEOUT where
+ * a wait inside a kernel gave up (2 s); y then holds NaN.
+ */
+typedef struct net_ortho {
+  uint32_t struct_size;           /* sizeof(net_ortho): version guard         */
+  uint32_t dtype;                 /* NET_*: type of x and y                   */
+  uint32_t steps;                 /* <= 64                                    */
+  float eps;                      /* >= 0                                     */
+  float coef[3];
+  uint32_t reserved;              /* 0                                        */
+  int64_t L, M, N;
+  net_rows x, y;                  /* [L][M][N]                                */
+  void* workspace;
+  size_t workspace_bytes;
+} net_ortho;
+size_t net_orthogonalise_workspace_bytes(const net_ortho* a);
+int net_orthogonalise(const net_ortho* a, void* stream);
 
 const char* net_last_error(void);
 

@@ -17,7 +17,8 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libauvenv.so")
 SOURCES = ["api.cu", "ppo_api.cu", "rbuf.cu", "shac.cu", "k_env.cu", "k_paper.cu", "k_fp32.cu", "k_ppo.cu",
            "k_adjoint.cu", "k_bf16.cu", "k_gemm.cu", "k_tf32.cu", "noalloc.cu", "probes.cu",
-           "net_api.cu", "net_scan.cu", "net_pieces.cu", "net_norm.cu", "net_drop.cu"]
+           "net_api.cu", "net_scan.cu", "net_pieces.cu", "net_norm.cu", "net_drop.cu",
+           "net_conv.cu", "net_select.cu", "net_select_back.cu", "net_ortho.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",
               "-I", CSRC, "-I", INCLUDE]

@@ -1,0 +1,352 @@
+// net_select.cu -- selective state space scan along a trajectory (auvnet.h, net_select_scan): forward, entry points.
+//
+// Per channel and state a chain h = a c + u B with a = exp(e A), u = e x: S exponentials and 4 S products and sums a value
+// of x, against 8 to 16 bytes of it, so with S = 16 the multi-function unit, the fp32 pipe and HBM are all near their
+// limits.  k_select walks the steps with the states in registers (layout: net_select.cuh), B and C of 16 steps staged in
+// shared memory by each warp for itself.  Sequences of few channels are cut into pieces: each is walked from 0 for its
+// final state and the sum of its step sizes (the product of its decays is exp(A sum)), those are joined to the states
+// before the pieces (k_select_join), and the pieces are walked from these.
+#include <algorithm>
+
+#include "net_select.cuh"
+
+namespace auv {
+namespace net {
+namespace {
+
+constexpr int kWarps = 4;
+constexpr int kHalf = 8;        // steps whose inputs are loaded together
+
+// FOLD: only the piece's final state from 0, and the sum of its step sizes (-1 where an episode ends in it: nothing
+// passes through).
+template <typename T, typename L, bool FOLD>
+__global__ void __launch_bounds__(32 * kWarps) k_select(Select a) {
+  constexpr int SP = L::SP, LS = L::LS, CC = L::CC, SW = L::SW;
+  __shared__ __align__(16) float rows[kWarps][FOLD ? 1 : 2][kKeep * SW];
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  int64_t id = blockIdx.x * (int64_t)kWarps + warp;
+  const int64_t envs_groups = a.N * a.G;
+  if (id >= envs_groups * a.tiles * a.pieces) return;
+  const int tile = (int)(id % a.tiles);
+  id /= a.tiles;
+  const int g = (int)(id % a.G);
+  id /= a.G;
+  const int64_t n = id % a.N;
+  const int piece = (int)(id / a.N);
+  float* const Bs = rows[warp][0];
+  float* const Cs = rows[warp][FOLD ? 0 : 1];
+
+  const int q = lane % LS, s0 = q * SP;
+  const int first = tile * L::CW + lane / LS * CC;            // in the group
+  const int own = first + q % CC;
+  const bool live = own < a.per, writes = live && q < CC;
+  const int64_t d = (int64_t)g * a.per + own;                 // own channel
+  int64_t at[CC], at_weight[CC];
+  bool there[CC];
+#pragma unroll
+  for (int c = 0; c < CC; ++c) {
+    at_weight[c] = (int64_t)g * a.per + first + c;
+    at[c] = n * a.D + at_weight[c];
+    there[c] = first + c < a.per;
+  }
+  const int t0 = piece * a.piece, t1 = min(a.T, t0 + a.piece);
+  const int64_t states = a.N * a.D * a.S;
+  F2 h[CC][SP / 2], A2[CC][SP / 2];
+  if constexpr (!FOLD) {
+    if (a.pieces > 1) {
+      after_previous();
+      load_states<SP, CC>(a.maps + piece * states, at, there, s0, a.S, h);
+    } else {
+      load_states<SP, CC>(a.h0, at, there, s0, a.S, h);
+    }
+  } else {
+#pragma unroll
+    for (int c = 0; c < CC; ++c)
+#pragma unroll
+      for (int i = 0; i < SP / 2; ++i) h[c][i] = pair(0.0f, 0.0f);
+  }
+  load_states<SP, CC>(a.A, at_weight, there, s0, a.S, A2);
+#pragma unroll
+  for (int c = 0; c < CC; ++c)
+#pragma unroll
+    for (int i = 0; i < SP / 2; ++i) A2[c][i] = A2[c][i] * pair(kLog2e, kLog2e);
+  const float bias = live && a.dt_bias ? a.dt_bias[d] : 0.0f, skip = live && a.skip ? a.skip[d] : 0.0f;
+  float sum = 0.0f;
+  bool cut = false;
+
+  for (int ts = t0; ts < t1; ts += kKeep) {
+    const int steps = min(kKeep, t1 - ts);
+    const uint32_t ends = ends_of(a, ts, n, lane);
+    stage<T, SW>(a, a.B, ts, steps, n, g, lane, Bs);
+    if constexpr (!FOLD) {
+      stage<T, SW>(a, a.C, ts, steps, n, g, lane, Cs);
+      if (a.kept) store_states<SP, CC>(a.kept + ts / kKeep * states, at, there, s0, a.S, h);
+    }
+    __syncwarp();
+#pragma unroll 1
+    for (int k0 = 0; k0 < steps; k0 += kHalf) {
+      T rx[kHalf], rdt[kHalf], rgate[kHalf];
+#pragma unroll
+      for (int k = 0; k < kHalf; ++k) {
+        from_float(0.0f, rx[k]);
+        rdt[k] = rgate[k] = rx[k];
+        if (live && k0 + k < steps) {
+          const int t = ts + k0 + k;
+          rx[k] = *row_at<T>(a.x, t, n, d);
+          rdt[k] = *row_at<T>(a.dt, t, n, d);
+          if (!FOLD && a.gate.data) rgate[k] = *row_at<T>(a.gate, t, n, d);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kHalf; ++k) {
+        if (k0 + k >= steps) break;
+        const float x = to_float(rx[k]);
+        const float e = live ? softplus(to_float(rdt[k]) + bias) : 0.0f;
+        float es[CC], us[CC];
+        to_lanes<LS, CC>(e, es);
+        to_lanes<LS, CC>(e * x, us);
+        F2 B[SP / 2], C[SP / 2];
+        load_pairs<SP>(Bs + (k0 + k) * SW + s0, B);
+        if constexpr (!FOLD) load_pairs<SP>(Cs + (k0 + k) * SW + s0, C);
+        if (ends >> (k0 + k) & 1u) {
+#pragma unroll
+          for (int c = 0; c < CC; ++c)
+#pragma unroll
+            for (int i = 0; i < SP / 2; ++i) h[c][i] = pair(0.0f, 0.0f);
+          cut = true;
+        }
+        float y[CC];
+#pragma unroll
+        for (int c = 0; c < CC; ++c) {
+          const F2 e2 = pair(es[c], es[c]), u2 = pair(us[c], us[c]);
+          F2 acc = pair(0.0f, 0.0f);
+#pragma unroll
+          for (int i = 0; i < SP / 2; ++i) {
+            h[c][i] = fma2(ex2(e2 * A2[c][i]), h[c][i], u2 * B[i]);
+            if constexpr (!FOLD) acc = fma2(C[i], h[c][i], acc);
+          }
+          y[c] = total(acc);
+        }
+        if constexpr (FOLD) {
+          sum += e;
+        } else {
+          float p = fmaf(skip, x, over_states<LS, CC>(y, lane));
+          if (a.gate.data) {
+            const float z = to_float(rgate[k]);
+            float s, o;
+            gates(z, s, o);
+            p *= z * s;
+          }
+          if (writes) from_float(p, *const_cast<T*>(row_at<T>(a.y, ts + k0 + k, n, d)));
+        }
+      }
+    }
+    __syncwarp();
+  }
+  if constexpr (FOLD) {
+    store_states<SP, CC>(a.maps + piece * states, at, there, s0, a.S, h);
+    if (writes) a.sums[(int64_t)piece * a.N * a.D + n * a.D + d] = cut ? -1.0f : sum;
+  } else {
+    if (a.hT && t1 == a.T) store_states<SP, CC>(a.hT, at, there, s0, a.S, h);
+  }
+}
+
+// The states before the pieces (backward: their gradients behind the pieces), in the place of the pieces' own: a thread
+// per state.  The product of a piece's decays is kept from 0: an infinite state does not become NaN by a long piece.
+constexpr int kJoin = 128, kJoinAhead = 8;
+__global__ void __launch_bounds__(kJoin) k_select_join(Select a, bool back) {
+  after_previous();
+  const int64_t m = a.N * a.D * a.S, i = blockIdx.x * (int64_t)kJoin + threadIdx.x;
+  if (i >= m) return;
+  const int64_t nd = i / a.S;
+  const float A2 = a.A[nd % a.D * a.S + i % a.S] * kLog2e;
+  const float* const from = back ? a.dhT : a.h0;
+  float h = from ? from[i] : 0.0f;
+  const int64_t by = back ? -1 : 1;
+  int64_t p = back ? a.pieces - 1 : 0;
+  for (int left = a.pieces; left > 0; left -= kJoinAhead) {
+    float sum[kJoinAhead], own[kJoinAhead];
+#pragma unroll
+    for (int k = 0; k < kJoinAhead; ++k)
+      if (k < left) {
+        sum[k] = a.sums[(p + k * by) * a.N * a.D + nd];
+        own[k] = a.maps[(p + k * by) * m + i];
+      }
+#pragma unroll
+    for (int k = 0; k < kJoinAhead; ++k)
+      if (k < left) {
+        a.maps[(p + k * by) * m + i] = h;
+        h = sum[k] < 0.0f ? own[k] : fmaf(fmaxf(ex2(A2 * sum[k]), 1.17549435e-38f), h, own[k]);
+      }
+    p += kJoinAhead * by;
+  }
+}
+
+// T = 0: the states pass as they are.
+__global__ void k_select_none(int64_t m, const float* from, float* to) {
+  const int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x;
+  if (i < m) to[i] = from ? from[i] : 0.0f;
+}
+
+template <typename T, typename L, bool FOLD>
+cudaError_t launch_walk(const Select& a, cudaStream_t s) {
+  const int64_t warps = a.N * a.G * a.tiles * a.pieces;
+  const dim3 grid((unsigned)((warps + kWarps - 1) / kWarps));
+  if (!FOLD && a.pieces > 1) return launch_after(k_select<T, L, FOLD>, grid, 32 * kWarps, 0, s, a);
+  k_select<T, L, FOLD><<<grid, 32 * kWarps, 0, s>>>(a);
+  return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t launch(const Select& a, cudaStream_t s) {
+  return with_lanes(a.S, [&](auto l) {
+    using L = decltype(l);
+    if (a.pieces > 1) {
+      cudaError_t e = launch_walk<T, L, true>(a, s);
+      if (e == cudaSuccess) e = launch_select_join(a, false, s);
+      if (e != cudaSuccess) return e;
+    }
+    return launch_walk<T, L, false>(a, s);
+  });
+}
+
+int check(const net_select* p) {
+  if (!p) return fail(AUV_ERR_INVALID, "argument block is NULL");
+  if (p->struct_size != sizeof(net_select))
+    return fail(AUV_ERR_INVALID, "struct_size %u, expected %zu", p->struct_size, sizeof(net_select));
+  if (p->dtype > NET_FP16) return fail(AUV_ERR_INVALID, "dtype %u unknown", p->dtype);
+  if (p->T < 0 || p->N < 0 || p->D < 0) return fail(AUV_ERR_INVALID, "negative size");
+  if (p->S < 1 || p->G < 1) return fail(AUV_ERR_INVALID, "S or G < 1");
+  if (p->D % p->G) return fail(AUV_ERR_INVALID, "D is no multiple of G");
+  if (p->S > kMostStates) return fail(AUV_ERR_UNSUPPORTED, "S past %d", kMostStates);
+  const int64_t most = (int64_t)1 << 32;
+  if (p->N > most || p->D > (1 << 20) || p->G > (1 << 20) || p->N * std::max<int64_t>(p->D, p->G) > most || p->T > (1 << 30))
+    return fail(AUV_ERR_UNSUPPORTED, "N * D or N * G past 2^32, D or G past 2^20, or T past 2^30");
+  return AUV_OK;
+}
+
+Select of(const net_select* p, bool back) {
+  Select a = {};
+  a.T = (int)p->T, a.S = (int)p->S, a.G = (int)p->G, a.per = (int)(p->D / p->G), a.N = p->N, a.D = p->D;
+  a.x = p->x, a.dt = p->dt, a.gate = p->gate, a.y = p->y, a.B = p->B, a.C = p->C, a.dy = p->dy, a.dx = p->dx;
+  a.ddt = p->ddt, a.dgate = p->dgate, a.dB = p->dB, a.dC = p->dC;
+  a.A = p->A, a.skip = p->skip, a.dt_bias = p->dt_bias, a.h0 = p->h0, a.hT = p->hT, a.kept = p->kept, a.dhT = p->dhT;
+  a.dh0 = p->dh0, a.dA = p->dA, a.dskip = p->dskip, a.ddt_bias = p->ddt_bias, a.done = p->done, a.done_prev = p->done_prev;
+  a.tiles = (a.per + lanes_channels(a.S) - 1) / lanes_channels(a.S);
+  select_pieces(a, back);
+  return a;
+}
+
+// The workspace's parts, each on a 16-byte boundary, and its size.
+size_t lay_out(Select& a, bool back, char* at) {
+  size_t n = 0;
+  auto part = [&](int64_t floats) {
+    float* const p = reinterpret_cast<float*>(at + n);
+    n += ((size_t)floats * 4 + 15) / 16 * 16;
+    return floats ? p : nullptr;
+  };
+  const bool split = a.pieces > 1;
+  a.sums = part(split ? a.pieces * a.N * a.D : 0);
+  a.maps = part(split ? a.pieces * a.N * a.D * a.S : 0);
+  if (back) {
+    int64_t blocks;
+    int rows;
+    const int64_t slots = select_slots(a, &blocks, &rows);
+    a.weights = part(slots * a.D * (a.S + 2));
+    a.parts = part(blocks > 1 ? blocks * a.T * a.N * a.G * 2 * a.S : 0);
+  }
+  return n;
+}
+
+int run(const net_select* p, bool back, void* stream) {
+  int rc = check(p);
+  if (rc) return rc;
+  if (p->D == 0 || (p->N == 0 && !back)) return AUV_OK;
+  const int z = type_size(p->dtype);
+  const bool gate = p->gate.data != nullptr;
+  const int64_t GS = p->G * p->S;
+  struct { const net_rows* r; const char* name; bool out, used; int64_t k; } rows[] = {
+      {&p->x, "x", false, true, p->D},        {&p->dt, "dt", false, true, p->D},   {&p->gate, "gate", false, gate, p->D},
+      {&p->B, "B", false, true, GS},          {&p->C, "C", false, true, GS},       {&p->y, "y", true, !back, p->D},
+      {&p->dy, "dy", false, back, p->D},      {&p->dx, "dx", true, back, p->D},    {&p->ddt, "ddt", true, back, p->D},
+      {&p->dgate, "dgate", true, back && gate && p->dgate.data, p->D},
+      {&p->dB, "dB", true, back, GS},         {&p->dC, "dC", true, back, GS}};
+  if (p->T && p->N)
+    for (const auto& q : rows)
+      if (q.used && (rc = need_rows(*q.r, q.name, p->T, p->N, q.k, z, q.out))) return rc;
+  if ((rc = need(p->A, "A", 4))) return rc;
+  if (back && p->T && p->N && (rc = need(p->kept, "kept", 4))) return rc;
+  struct { const void* p; const char* name; bool used; } flat[] = {
+      {p->skip, "skip", true}, {p->dt_bias, "dt_bias", true}, {p->h0, "h0", !back}, {p->hT, "hT", !back}, {p->kept, "kept", !back},
+      {p->dhT, "dhT", back}, {p->dh0, "dh0", back}, {p->dA, "dA", back}, {p->dskip, "dskip", back}, {p->ddt_bias, "ddt_bias", back}};
+  for (const auto& q : flat)
+    if (q.p && q.used && (rc = need(q.p, q.name, 4))) return rc;
+  if (p->done && (rc = need(p->done, "done", 1))) return rc;
+  if (p->done_prev && (rc = need(p->done_prev, "done_prev", 1))) return rc;
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (p->T == 0 || p->N == 0) {
+    const int64_t m = p->N * p->D * p->S;
+    auto fill = [&](int64_t k, const float* from, float* to) {
+      if (to && k) k_select_none<<<(unsigned)((k + 255) / 256), 256, 0, s>>>(k, from, to);
+    };
+    if (back) {
+      fill(m, p->dhT, p->dh0);
+      fill(p->D * p->S, nullptr, p->dA);
+      fill(p->D, nullptr, p->dskip);
+      fill(p->D, nullptr, p->ddt_bias);
+    } else {
+      fill(m, p->h0, p->hT);
+    }
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? AUV_OK : cuda_fail(e, "net_select_scan");
+  }
+  Select a = of(p, back);
+  const size_t bytes = lay_out(a, back, static_cast<char*>(p->workspace));
+  if (bytes) {
+    if (p->workspace_bytes < bytes) return fail(AUV_ERR_SIZE, "workspace of %zu bytes, %zu needed", p->workspace_bytes, bytes);
+    if ((rc = need(p->workspace, "workspace", 16))) return rc;
+  }
+  cudaError_t e;
+  if (back) {
+    if (!gate) a.dgate.data = nullptr;
+    e = p->dtype == NET_FP32   ? launch_select_back<float>(a, a.pieces > 1, s)
+        : p->dtype == NET_BF16 ? launch_select_back<__nv_bfloat16>(a, a.pieces > 1, s)
+                               : launch_select_back<__half>(a, a.pieces > 1, s);
+  } else {
+    e = p->dtype == NET_FP32 ? launch<float>(a, s) : p->dtype == NET_BF16 ? launch<__nv_bfloat16>(a, s) : launch<__half>(a, s);
+  }
+  return e == cudaSuccess ? AUV_OK : cuda_fail(e, back ? "net_select_scan_backward" : "net_select_scan");
+}
+
+}  // namespace
+
+void select_pieces(Select& a, bool back) {
+  const int64_t warps = a.N * a.G * a.tiles, want = (int64_t)sm_count() * (back ? 8 : 16);
+  int64_t pieces = std::min(want / std::max<int64_t>(1, warps), (int64_t)a.T / 64);
+  if (pieces < 2) pieces = 1;
+  const int64_t piece = pieces == 1 ? a.T : ((a.T + pieces - 1) / pieces + kKeep - 1) / kKeep * kKeep;
+  a.piece = (int)std::max<int64_t>(1, piece);
+  a.pieces = a.T ? (a.T + a.piece - 1) / a.piece : 1;
+}
+
+cudaError_t launch_select_join(const Select& a, bool back, cudaStream_t s) {
+  const int64_t m = a.N * a.D * a.S;
+  return launch_after(k_select_join, dim3((unsigned)((m + kJoin - 1) / kJoin)), kJoin, 0, s, a, back);
+}
+
+}  // namespace net
+}  // namespace auv
+
+extern "C" {
+
+size_t net_select_scan_workspace_bytes(const net_select* p, int backward) {
+  using namespace auv::net;
+  if (!p || check(p) || !p->T || !p->N || !p->D) return 0;
+  Select a = of(p, backward);
+  return lay_out(a, backward, nullptr);
+}
+
+int net_select_scan(const net_select* a, void* stream) { return auv::net::run(a, false, stream); }
+int net_select_scan_backward(const net_select* a, void* stream) { return auv::net::run(a, true, stream); }
+
+}  // extern "C"

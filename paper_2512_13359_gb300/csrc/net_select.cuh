@@ -1,0 +1,221 @@
+// net_select.cuh -- what the kernels of the selective scan (net_select.cu, net_select_back.cu) share.
+//
+// Layout.  A warp has adjacent channels of one env n and group g, whose states all read the same B[t] and C[t].  LS lanes
+// share CC channels: each of them holds SP of their S states (padded to LS * SP; what is padded has A = B = C = 0), of all
+// CC channels, in pairs for the packed fp32 instructions.  Sums over states go over LS lanes, those over channels (dB, dC)
+// over the others.  What is computed per channel and step, ahead of the states, is each lane's own for one channel.
+#pragma once
+
+#include "net_common.cuh"
+
+namespace auv {
+namespace net {
+
+constexpr int kKeep = 16;       // steps from one kept state to the next
+constexpr int kMostStates = 128;
+
+struct Select {
+  int T, S, G, per;             // per: channels of a group
+  int piece, pieces;            // steps of a piece of the sequence, multiples of kKeep
+  int tiles;                    // warps that a group's channels take
+  int64_t N, D;
+  net_rows x, dt, gate, y, B, C, dy, dx, ddt, dgate, dB, dC;
+  const float *A, *skip, *dt_bias, *h0;
+  float *hT, *kept;
+  const float* dhT;
+  float *dh0, *dA, *dskip, *ddt_bias;
+  const uint8_t *done, *done_prev;
+  float *sums, *maps;           // pieces: [pieces][N][D] sums of step sizes, [pieces][N][D][S] states
+  float *weights;               // backward: [slots][D][S + 2] sums of weight gradients
+  float *parts;                 // backward, groups of several blocks: [blocks][T][N][G][2][S] sums of dB and dC
+};
+
+// ---- pairs of fp32 ----
+struct F2 {
+  uint64_t v;
+};
+__device__ __forceinline__ F2 pair(float lo, float hi) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void split(F2 a, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(a.v)); }
+__device__ __forceinline__ F2 operator*(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ float total(F2 a) {
+  float lo, hi;
+  split(a, lo, hi);
+  return lo + hi;
+}
+__device__ __forceinline__ float ex2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ F2 ex2(F2 a) {
+  float lo, hi;
+  split(a, lo, hi);
+  return pair(ex2(lo), ex2(hi));
+}
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+
+// softplus(v) = max(v, 0) + log(1 + q), q = exp(-|v|), and sigmoid(v) = 1 / (1 + q) or q / (1 + q).  log(1 + q) = 2 atanh(z)
+// with z = q / (2 + q) <= 1/3: z times a polynomial in z^2 fitted on [0, 1/9] (Chebyshev, 8e-9 relative), so that a small
+// step keeps its digits; off by a few units of 2^-24, and q by 2^-24 |v|.
+__device__ __forceinline__ float softplus(float v, float* sigmoid = nullptr) {
+  const float q = ex2(fabsf(v) * -kLog2e);
+  const float z = __fdividef(q, 2.0f + q), w = z * z;
+  float p = fmaf(w, 0.2815778f, 0.27965158f);
+  p = fmaf(w, p, 0.40024596f);
+  p = fmaf(w, p, 0.6666632f);
+  p = fmaf(w, p, 2.0f);
+  if (sigmoid) {
+    const float r = __fdividef(1.0f, 1.0f + q);
+    *sigmoid = v >= 0.0f ? r : q * r;
+  }
+  return fmaf(z, p, fmaxf(v, 0.0f));
+}
+
+// Sums over the lanes that share channels, of CC values a lane (one per channel): afterwards v[0] is that of the lane's own
+// channel, q % CC.
+template <int LS, int CC>
+__device__ __forceinline__ float over_states(const float (&v)[CC], int lane) {
+  float r = v[0];
+  int bit = 1;
+  if constexpr (CC == 2) {
+    const bool up = lane & 1;
+    r = (up ? v[1] : v[0]) + __shfl_xor_sync(0xffffffffu, up ? v[0] : v[1], 1);
+    bit = 2;
+  }
+#pragma unroll
+  for (; bit < LS; bit *= 2) r += __shfl_xor_sync(0xffffffffu, r, bit);
+  return r;
+}
+
+// A value of the lane's own channel to the lanes that share it: r[c] is channel c's.
+template <int LS, int CC>
+__device__ __forceinline__ void to_lanes(float own, float (&r)[CC]) {
+#pragma unroll
+  for (int c = 0; c < CC; ++c) r[c] = LS == 1 ? own : __shfl_sync(0xffffffffu, own, c, LS);
+}
+
+template <typename T>
+__device__ __forceinline__ const T* row_at(const net_rows& r, int64_t t, int64_t n, int64_t k) {
+  return reinterpret_cast<const T*>(r.data) + t * r.outer + n * r.inner + k;
+}
+__device__ __forceinline__ bool ended(const Select& a, int t, int64_t n) {
+  const uint8_t* p = t ? a.done : a.done_prev;
+  return p && p[(t ? (t - 1) * a.N : 0) + n];
+}
+// Bit i: an episode ended before step t + i, of the 16 from t on.
+__device__ __forceinline__ uint32_t ends_of(const Select& a, int t, int64_t n, int lane) {
+  if (!a.done && !a.done_prev) return 0u;
+  return __ballot_sync(0xffffffffu, lane < kKeep && t + lane < a.T && ended(a, t + lane, n));
+}
+
+// SP states of CC channels from s0 of an [.][S] array: pairs, zeros past S and for channels that are not there.
+template <int SP, int CC>
+__device__ __forceinline__ void load_states(const float* p, const int64_t (&at)[CC], const bool (&there)[CC], int s0, int S,
+                                            F2 (&h)[CC][SP / 2]) {
+  const bool vec = S % 4 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0;
+#pragma unroll
+  for (int c = 0; c < CC; ++c) {
+    const float* q = p + at[c] * S + s0;
+#pragma unroll
+    for (int i = 0; i < SP; i += 4) {
+      float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (p && there[c]) {
+        if (vec) {
+          if (s0 + i < S) {
+            const float4 w = *reinterpret_cast<const float4*>(q + i);
+            v[0] = w.x, v[1] = w.y, v[2] = w.z, v[3] = w.w;
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (s0 + i + k < S) v[k] = q[i + k];
+        }
+      }
+      h[c][i / 2] = pair(v[0], v[1]);
+      h[c][i / 2 + 1] = pair(v[2], v[3]);
+    }
+  }
+}
+template <int SP, int CC>
+__device__ __forceinline__ void store_states(float* p, const int64_t (&at)[CC], const bool (&there)[CC], int s0, int S,
+                                             const F2 (&h)[CC][SP / 2]) {
+  const bool vec = S % 4 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0;
+#pragma unroll
+  for (int c = 0; c < CC; ++c) {
+    if (!there[c]) continue;
+    float* q = p + at[c] * S + s0;
+#pragma unroll
+    for (int i = 0; i < SP; i += 4) {
+      float v[4];
+      split(h[c][i / 2], v[0], v[1]);
+      split(h[c][i / 2 + 1], v[2], v[3]);
+      if (vec) {
+        if (s0 + i < S) *reinterpret_cast<float4*>(q + i) = make_float4(v[0], v[1], v[2], v[3]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (s0 + i + k < S) q[i + k] = v[k];
+      }
+    }
+  }
+}
+
+// The rows of B or C of up to 16 steps from t on, into [16][SW] fp32, zeros past S.
+template <typename T, int SW>
+__device__ __forceinline__ void stage(const Select& a, const net_rows& r, int t, int steps, int64_t n, int g, int lane, float* to) {
+  for (int i = lane; i < kKeep * SW; i += 32) {
+    const int k = i / SW, s = i % SW;
+    to[i] = k < steps && s < a.S ? to_float(*row_at<T>(r, t + k, n, (int64_t)g * a.S + s)) : 0.0f;
+  }
+}
+
+// SP values of a staged row as pairs.
+template <int SP>
+__device__ __forceinline__ void load_pairs(const float* p, F2 (&v)[SP / 2]) {
+#pragma unroll
+  for (int i = 0; i < SP; i += 4) {
+    const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(p + i);
+    v[i / 2].v = w.x;
+    v[i / 2 + 1].v = w.y;
+  }
+}
+
+// How S states are laid over lanes.
+template <int SP_, int LS_, int CC_> struct Lanes {
+  static constexpr int SP = SP_, LS = LS_, CC = CC_;
+  static constexpr int SW = SP * LS;          // states, padded
+  static constexpr int CW = 32 / LS * CC;     // channels of a warp
+};
+template <typename F>
+cudaError_t with_lanes(int S, F f) {
+  if (S <= 4) return f(Lanes<4, 1, 1>());
+  if (S <= 8) return f(Lanes<8, 1, 1>());
+  if (S <= 16) return f(Lanes<8, 2, 2>());
+  if (S <= 32) return f(Lanes<8, 4, 2>());
+  if (S <= 64) return f(Lanes<8, 8, 2>());
+  return f(Lanes<8, 16, 2>());
+}
+inline int lanes_channels(int S) { return S <= 16 ? 32 : S <= 32 ? 16 : S <= 64 ? 8 : 4; }
+
+// The states before the pieces from the pieces' maps, in the maps' place (net_select.cu).
+cudaError_t launch_select_join(const Select& a, bool back, cudaStream_t s);
+template <typename T> cudaError_t launch_select_back(const Select& a, bool split, cudaStream_t s);
+// Pieces and steps of a piece for warps that each walk T steps.
+void select_pieces(Select& a, bool back);
+int64_t select_slots(const Select& a, int64_t* blocks, int* rows);
+
+}  // namespace net
+}  // namespace auv

@@ -1,8 +1,10 @@
 """Network operators (include/auvnet.h) on torch tensors: argument marshalling only.
 
 ``gate_scan`` and ``gate_scan_backward`` (gated linear recurrence along a trajectory, with the rollout's episode ends),
-``group_norm`` and ``group_norm_backward`` (group norm with an activation, channels last) and ``dropout`` (mask drawn
-from a counter, never stored) launch the library's CUDA kernels on the current (or given) stream and return without
+``group_norm`` and ``group_norm_backward`` (group norm with an activation, channels last), ``dropout`` (mask drawn
+from a counter, never stored), ``causal_conv`` and ``select_scan`` with their gradients (a memory with many states a
+channel and the short convolution in front of it, with the rollout's episode ends) and ``orthogonalise`` (updates of weight
+matrices by Newton-Schulz products) launch the library's CUDA kernels on the current (or given) stream and return without
 waiting.  Outputs are allocated unless they are given; a raw state or gradient buffer given as an output is written in
 place.  There is no CPU fallback.  Wrong arguments raise AuvError with the library's code and reason.
 
@@ -27,13 +29,18 @@ NET_ACT = {"none": 0, "relu": 1, "silu": 2, "tanh": 3}
 
 EXPORTED = ("net_gate_scan_workspace_bytes", "net_gate_scan", "net_gate_scan_backward",
             "net_group_norm_workspace_bytes", "net_group_norm", "net_group_norm_backward", "net_dropout",
-            "net_last_error")
+            "net_causal_conv_workspace_bytes", "net_causal_conv", "net_causal_conv_backward",
+            "net_select_scan_workspace_bytes", "net_select_scan", "net_select_scan_backward",
+            "net_orthogonalise_workspace_bytes", "net_orthogonalise", "net_last_error")
 
 # The argument blocks, field by field as in the header (native alignment).
 _ROWS = "Pqq"
 _SCAN = struct.Struct("@II3q" + 6 * _ROWS + "7PN")
 _NORM = struct.Struct("@IIIf4q" + 4 * _ROWS + "7PN")
 _DROP = struct.Struct("@4I3q" + 3 * _ROWS + "dQQ")
+_CONV = struct.Struct("@4I4q" + 4 * _ROWS + "11PN")
+_SELECT = struct.Struct("@II5q" + 12 * _ROWS + "14PN")
+_ORTHO = struct.Struct("@3I4fI3q" + 2 * _ROWS + "PN")
 _NO_ROWS = (0, 0, 0)
 
 _lib = None
@@ -45,12 +52,16 @@ def lib():
     if _lib is None:
         L = auvenv.lib()
         for name in ("net_gate_scan", "net_gate_scan_backward", "net_group_norm", "net_group_norm_backward",
-                     "net_dropout"):
+                     "net_dropout", "net_causal_conv", "net_causal_conv_backward", "net_select_scan",
+                     "net_select_scan_backward", "net_orthogonalise"):
             getattr(L, name).argtypes = [C.c_char_p, C.c_void_p]
             getattr(L, name).restype = C.c_int
-        for name in ("net_gate_scan_workspace_bytes", "net_group_norm_workspace_bytes"):
+        for name in ("net_gate_scan_workspace_bytes", "net_group_norm_workspace_bytes", "net_causal_conv_workspace_bytes",
+                     "net_select_scan_workspace_bytes"):
             getattr(L, name).argtypes = [C.c_char_p, C.c_int]
             getattr(L, name).restype = C.c_size_t
+        L.net_orthogonalise_workspace_bytes.argtypes = [C.c_char_p]
+        L.net_orthogonalise_workspace_bytes.restype = C.c_size_t
         L.net_last_error.restype = C.c_char_p
         _lib = L
     return _lib
@@ -287,4 +298,183 @@ def dropout(x, p, seed, draw, *, residual=None, shared=False, y=None, stream=Non
     except (*_NO_NUMBER, TypeError) as e:
         _no_number(e)
     _call(lib().net_dropout, args, index, stream, scratch)
+    return y
+
+
+def _call_packed(fn, form, fields, index, stream, scratch):
+    try:
+        args = form.pack(*fields, 0, 0)
+    except _NO_NUMBER as e:
+        _no_number(e)
+    _call(fn, args, index, stream, scratch)
+
+
+def _conv_head(x, w, act):
+    shape, dtype, index = like = _activation(x, "x")
+    if act not in ("none", "silu"):
+        _fail(AUV_ERR_INVALID, f"act {act!r} is neither none nor silu")
+    if not isinstance(w, torch.Tensor) or w.dim() != 2 or w.shape[0] < 1:
+        _fail(AUV_ERR_INVALID, "w is not a tensor [K, D]")
+    return like, w.shape[0]
+
+
+def causal_conv(x, w, bias=None, state=None, *, done=None, done_prev=None, act="none", y=None, new_state=None, stream=None):
+    """Short causal convolution y[t] = act(bias + sum over k < K of w[k] x[t - (K - 1) + k]) of each channel of x [T, N, D];
+    w [K, D] and bias [D] fp32, K <= 8, act "none" or "silu".  state [K - 1, N, D] (of x's type): the rows ahead of x; rows
+    behind an episode end count as zeros (done [T, N]: ends after the step; done_prev [N]: before step 0).  Returns
+    (y [T, N, D], new_state [K - 1, N, D], the state of the next call).  new_state may be state."""
+    scratch = []
+    like, K = _conv_head(x, w, act)
+    shape, dtype, index = like
+    T, N, D = shape
+    states = (K - 1, N, D)
+    if y is None:
+        y = _new(shape, dtype, index, scratch)
+    if new_state is None:
+        new_state = _new(states, dtype, index, scratch)
+    fields = (_CONV.size, NET_DTYPE[dtype], NET_ACT[act], 0, T, N, D, K, *_rows(x, "x", like), *_rows(y, "y", like), *_NO_ROWS,
+              *_NO_ROWS, _flat(w, "w", (K, D), torch.float32, index), _flat(bias, "bias", (D,), torch.float32, index),
+              _flat(state, "state", states, dtype, index), _flat(new_state, "new_state", states, dtype, index), 0, 0, 0, 0,
+              _flags(done, "done", (T, N), index), _flags(done_prev, "done_prev", (N,), index))
+    _call_packed(lib().net_causal_conv, _CONV, fields, index, stream, scratch)
+    return y, new_state
+
+
+def causal_conv_backward(x, w, bias, dy, state=None, *, done=None, done_prev=None, act="none", dnew_state=None, dx=None,
+                         dw=None, dbias=None, dstate=None, stream=None):
+    """Gradients (dx, dw, dbias, dstate) of causal_conv from dy [T, N, D] and dnew_state [K - 1, N, D] (None: zeros); the
+    other arguments as given to it."""
+    scratch = []
+    like, K = _conv_head(x, w, act)
+    shape, dtype, index = like
+    T, N, D = shape
+    states, f32 = (K - 1, N, D), torch.float32
+    if dx is None:
+        dx = _new(shape, dtype, index, scratch)
+    if dw is None:
+        dw = _new((K, D), f32, index, scratch)
+    if dbias is None:
+        dbias = _new((D,), f32, index, scratch)
+    if dstate is None:
+        dstate = _new(states, dtype, index, scratch)
+    fields = (_CONV.size, NET_DTYPE[dtype], NET_ACT[act], 0, T, N, D, K, *_rows(x, "x", like), *_NO_ROWS, *_rows(dy, "dy", like),
+              *_rows(dx, "dx", like), _flat(w, "w", (K, D), f32, index), _flat(bias, "bias", (D,), f32, index),
+              _flat(state, "state", states, dtype, index), 0, _flat(dnew_state, "dnew_state", states, dtype, index),
+              _flat(dstate, "dstate", states, dtype, index), _flat(dw, "dw", (K, D), f32, index),
+              _flat(dbias, "dbias", (D,), f32, index), _flags(done, "done", (T, N), index),
+              _flags(done_prev, "done_prev", (N,), index))
+    L = lib()
+    _call_with_workspace(L.net_causal_conv_backward, L.net_causal_conv_workspace_bytes, 1, _CONV, fields, index, stream, scratch)
+    return dx, dw, dbias, dstate
+
+
+KEPT = 16             # steps from one kept state of select_scan to the next
+
+
+def _select_head(x, A, B):
+    """(like x, like B, states a channel, groups)."""
+    shape, dtype, index = like = _activation(x, "x")
+    if not isinstance(A, torch.Tensor) or A.dim() != 2 or A.shape[1] < 1:
+        _fail(AUV_ERR_INVALID, "A is not a tensor [D, S]")
+    if not isinstance(B, torch.Tensor) or B.dim() != 3:
+        _fail(AUV_ERR_INVALID, "B is not a tensor of three axes")
+    S, wide = A.shape[1], B.shape[2]
+    if wide < S or wide % S or shape[2] % (wide // S):
+        _fail(AUV_ERR_INVALID, f"B has {wide} channels: not {S} states times a number of groups that {shape[2]} channels divide into")
+    return like, (torch.Size((shape[0], shape[1], wide)), dtype, index), S, wide // S
+
+
+def select_scan(x, dt, A, B, C, *, skip=None, dt_bias=None, gate=None, h0=None, done=None, done_prev=None, y=None, hT=None,
+                kept=None, stream=None):
+    """Selective state space scan over x, dt [T, N, D]: with e = softplus(dt + dt_bias), for each of a channel's S states
+    h[t] = exp(e A) c[t] + e B[t] x[t], y[t] = (sum of C[t] h[t] + skip x[t]) silu(gate[t]); c[t] is h[t - 1], or 0 where an
+    episode ended before step t (done [T, N]: after the step; done_prev [N]: before step 0).  A [D, S], skip, dt_bias [D],
+    h0 [N, D, S] fp32; B, C [T, N, G S], each of G groups of D / G channels with its own.  Returns (y [T, N, D],
+    hT [N, D, S] fp32, kept).  kept: None, or True or a buffer [(T + 15) // 16, N, D, S] fp32 for the states before steps 0,
+    16, 32, ... that select_scan_backward needs.  hT may be h0: states updated in place."""
+    scratch = []
+    like, rows, S, G = _select_head(x, A, B)
+    shape, dtype, index = like
+    T, N, D = shape
+    f32, states = torch.float32, (N, D, S)
+    if y is None:
+        y = _new(shape, dtype, index, scratch)
+    if hT is None:
+        hT = _new(states, f32, index, scratch)
+    kept_shape = ((T + KEPT - 1) // KEPT, *states)
+    if kept is True:
+        kept = _new(kept_shape, f32, index, scratch)
+    fields = (_SELECT.size, NET_DTYPE[dtype], T, N, D, S, G, *_rows(x, "x", like), *_rows(dt, "dt", like),
+              *(_NO_ROWS if gate is None else _rows(gate, "gate", like)), *_rows(y, "y", like), *_rows(B, "B", rows),
+              *_rows(C, "C", rows), *(6 * _NO_ROWS), _flat(A, "A", (D, S), f32, index), _flat(skip, "skip", (D,), f32, index),
+              _flat(dt_bias, "dt_bias", (D,), f32, index), _flat(h0, "h0", states, f32, index),
+              _flat(hT, "hT", states, f32, index), _flat(kept, "kept", kept_shape, f32, index), 0, 0, 0, 0, 0,
+              _flags(done, "done", (T, N), index), _flags(done_prev, "done_prev", (N,), index))
+    L = lib()
+    if T < 128:                       # short sequences need no workspace
+        _call_packed(L.net_select_scan, _SELECT, fields, index, stream, scratch)
+    else:
+        _call_with_workspace(L.net_select_scan, L.net_select_scan_workspace_bytes, 0, _SELECT, fields, index, stream, scratch)
+    return y, hT, kept
+
+
+def select_scan_backward(x, dt, A, B, C, kept, dy, *, skip=None, dt_bias=None, gate=None, done=None, done_prev=None, dhT=None,
+                         dx=None, ddt=None, dA=None, dB=None, dC=None, dskip=None, ddt_bias=None, dgate=None, dh0=None,
+                         stream=None):
+    """Gradients (dx, ddt, dA, dB, dC, dskip, ddt_bias, dgate, dh0) of select_scan from dy [T, N, D] and dhT [N, D, S]
+    (None: zeros); kept as it returned it, the other arguments as given to it.  dgate is None without a gate."""
+    scratch = []
+    like, rows, S, G = _select_head(x, A, B)
+    shape, dtype, index = like
+    T, N, D = shape
+    f32, states = torch.float32, (N, D, S)
+    dx = _new(shape, dtype, index, scratch) if dx is None else dx
+    ddt = _new(shape, dtype, index, scratch) if ddt is None else ddt
+    dB = _new(rows[0], dtype, index, scratch) if dB is None else dB
+    dC = _new(rows[0], dtype, index, scratch) if dC is None else dC
+    dA = _new((D, S), f32, index, scratch) if dA is None else dA
+    dskip = _new((D,), f32, index, scratch) if dskip is None else dskip
+    ddt_bias = _new((D,), f32, index, scratch) if ddt_bias is None else ddt_bias
+    dh0 = _new(states, f32, index, scratch) if dh0 is None else dh0
+    if gate is None:
+        if dgate is not None:
+            _fail(AUV_ERR_INVALID, "dgate without a gate")
+    elif dgate is None:
+        dgate = _new(shape, dtype, index, scratch)
+    if kept is None:
+        _fail(AUV_ERR_INVALID, "kept is None: the forward call has to keep its states")
+    fields = (_SELECT.size, NET_DTYPE[dtype], T, N, D, S, G, *_rows(x, "x", like), *_rows(dt, "dt", like),
+              *(_NO_ROWS if gate is None else _rows(gate, "gate", like)), *_NO_ROWS, *_rows(B, "B", rows), *_rows(C, "C", rows),
+              *_rows(dy, "dy", like), *_rows(dx, "dx", like), *_rows(ddt, "ddt", like),
+              *(_NO_ROWS if gate is None else _rows(dgate, "dgate", like)), *_rows(dB, "dB", rows), *_rows(dC, "dC", rows),
+              _flat(A, "A", (D, S), f32, index), _flat(skip, "skip", (D,), f32, index),
+              _flat(dt_bias, "dt_bias", (D,), f32, index), 0, 0,
+              _flat(kept, "kept", ((T + KEPT - 1) // KEPT, *states), f32, index), _flat(dhT, "dhT", states, f32, index),
+              _flat(dh0, "dh0", states, f32, index), _flat(dA, "dA", (D, S), f32, index),
+              _flat(dskip, "dskip", (D,), f32, index), _flat(ddt_bias, "ddt_bias", (D,), f32, index),
+              _flags(done, "done", (T, N), index), _flags(done_prev, "done_prev", (N,), index))
+    L = lib()
+    _call_with_workspace(L.net_select_scan_backward, L.net_select_scan_workspace_bytes, 1, _SELECT, fields, index, stream, scratch)
+    return dx, ddt, dA, dB, dC, dskip, ddt_bias, dgate, dh0
+
+
+def orthogonalise(x, steps=5, *, coef=(3.4445, -4.775, 2.0315), eps=1e-7, y=None, stream=None):
+    """Each of the matrices x [L, M, N] with its singular values v, over their norm, taken `steps` times through
+    a v + b v^3 + c v^5 (coef): with the usual coefficients and five steps they come to lie about 1, and the singular
+    vectors stay.  Returns y [L, M, N] of x's type."""
+    scratch = []
+    shape, dtype, index = like = _activation(x, "x")
+    if y is None:
+        y = _new(shape, dtype, index, scratch)
+    try:
+        a, b, c = coef
+        fields = (_ORTHO.size, NET_DTYPE[dtype], steps, eps, a, b, c, 0, *shape, *_rows(x, "x", like), *_rows(y, "y", like))
+        args = _ORTHO.pack(*fields, 0, 0)
+    except (*_NO_NUMBER, TypeError, ValueError) as e:
+        _no_number(e)
+    L = lib()
+    need = L.net_orthogonalise_workspace_bytes(args)
+    if need:
+        args = _ORTHO.pack(*fields, _new(need, torch.uint8, index, scratch).data_ptr(), need)
+    _call(L.net_orthogonalise, args, index, stream, scratch)
     return y
