@@ -8,10 +8,14 @@
 // into one fp32 accumulator; lo lo, 2^-22 of the product, is left out.  Scaled by powers of two the pieces' range holds
 // every value to 2^-34 of the largest that can occur (the coefficients are checked for that).
 //
-// One block computes a 128 x 128 or 128 x 256 tile: a producer thread streams 128-byte-swizzled tiles of both pieces of
-// both operands into a ring with TMA, one thread issues tcgen05.mma into tensor memory, and eight warps read the sums back,
-// split them into pieces again and store them; of the symmetric products the tiles on and below the diagonal, stored on
-// both sides of it.  The products of a call follow each other by programmatic launches.
+// All products of a call are one cooperative launch, a block an SM, with barriers over all blocks between the products.
+// Of a 128 x 128 or 128 x 256 tile a producer thread streams 128-byte-swizzled tiles of both pieces of both operands into a
+// ring with TMA, one thread issues tcgen05.mma into tensor memory, and eight warps read the sums back, split them into
+// pieces again and store them; of the symmetric products the tiles on and below the diagonal, stored on both sides of it.
+//
+// The tensor core cuts what it adds to an accumulator (each addition loses up to 2^-23 of it, always towards 0), which over
+// K = 4096 came to 9e-5 of the result.  So a sum runs over 64 of K there, small products first, and those sums are added in
+// registers, rounded to nearest, while the next 64 run into the other half of tensor memory.
 #include <cuda.h>
 
 #include <algorithm>
@@ -31,18 +35,6 @@ constexpr uint64_t kWaitLimitNs = 2000000000ull;
 
 enum Kind { kP, kQ, kX, kLast };
 
-struct Product {
-  int rows, cols, K, L;       // of the result; contraction; matrices
-  int kind, tiles_n;
-  float b, c, a;              // kQ
-  __half* out;                // pieces [2][L][rows][ld]
-  const __half* prev;         // kQ: P
-  int ld;
-  net_rows y;                 // kLast
-  int dtype;
-  int* error;
-};
-
 // ---- sums of squares ----
 // Of x, and of x times 2^64 and 2^-64: one of the three is in range wherever the largest |x| is.
 constexpr float kUp = 18446744073709551616.0f, kDown = 1.0f / 18446744073709551616.0f;
@@ -52,7 +44,7 @@ template <typename T>
 __global__ void __launch_bounds__(kNormThreads) k_squares(net_rows x, int64_t M, int64_t N, float* partial, int* error) {
   __shared__ float part[3][kNormThreads / 32];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *error = AUV_OK;
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) error[0] = AUV_OK, error[1] = 0;     // and the barriers' count
   const T* const p = reinterpret_cast<const T*>(x.data) + blockIdx.y * x.outer;
   float s0 = 0.0f, s1 = 0.0f, s2 = 0.0f;
   const int64_t all = M * N, step = gridDim.x * (int64_t)kNormThreads;
@@ -173,24 +165,48 @@ __device__ __forceinline__ void wait_landed(uint64_t* b, uint32_t phase) {
   }
 }
 
+// One of a step's products: result rows x cols, contraction K; which operands run along M or N.
+struct Product {
+  int kind, rows, cols, K;
+  bool a_mn, b_mn;
+};
+
+struct Steps {
+  CUtensorMap x_rows[2], x_cols[2], p, q;   // boxes of 128 rows; x_cols: of 64
+  int L, M, N, s, steps, ldx, lds;          // s: the shorter side
+  bool wide;                                // M <= N
+  float a, b, c;
+  __half *x[2], *P, *Q;                     // pieces [2][L][rows][ld]
+  net_rows y;
+  int dtype;
+  int* error;
+  unsigned* arrived;                        // blocks at the barriers between products
+};
+
 template <int BN>
 struct Tile {
   static constexpr int kStages = BN > 128 ? 2 : 3;
   static constexpr uint32_t kA = kBM * 128, kB = BN * 128;      // one piece of a stage
   static constexpr uint32_t kStage = 2 * (kA + kB);
-  static constexpr uint32_t kSmem = kStages * kStage + 256 + 1024;
+  static constexpr uint32_t kTurn = 8 * 32 * 33 * 4;            // a 32 x 32 block a storing warp
+  static constexpr uint32_t kSmem = kStages * kStage + kTurn + 256 + 1024;
 };
 struct Bars {
-  uint64_t full[3], empty[3], sums;
+  uint64_t full[3], empty[3], sums[2], taken[2], drained;
   uint32_t tmem;
   int abort;
 };
-constexpr int kEpilogue = 8, kProducer = 8, kIssuer = 9, kThreads = 320;
+// Two warpgroups that store, and one with the producer and the issuer.  Registers: at launch 384 threads x 168 = 64,512;
+// the storing warps, with up to 128 sums a thread, take 216, the others keep 64: 256 x 216 + 128 x 64 = 63,488.
+constexpr int kStorers = 8, kProducer = 8, kIssuer = 9, kThreads = 384;
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 216;"); }
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 64;"); }
 
 // 32 scaled values of row r from column c on, as pieces (whole 16-byte stores; a row's padding may be written).
-__device__ __forceinline__ void store_pieces(const Product& p, int64_t l, int r, int c, const float (&v)[32], bool mirror) {
-  const int64_t each = (int64_t)p.L * p.rows * p.ld;
-  __half* const hi = p.out + (l * p.rows + r) * (int64_t)p.ld + c;
+__device__ __forceinline__ void store_pieces(__half* out, int L, int rows, int cols, int ld, int l, int r, int c, const float* v,
+                                             bool mirror) {
+  const int64_t each = (int64_t)L * rows * ld;
+  __half* const hi = out + ((int64_t)l * rows + r) * ld + c;
   uint32_t h[16], o[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
@@ -200,195 +216,308 @@ __device__ __forceinline__ void store_pieces(const Product& p, int64_t l, int r,
     h[i] = *reinterpret_cast<const uint32_t*>(&w);
     o[i] = *reinterpret_cast<const uint32_t*>(&z);
   }
-  if (r < p.rows) {
+  if (r >= rows) return;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (c + 8 * i < p.cols) {
-        *reinterpret_cast<uint4*>(hi + 8 * i) = make_uint4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]);
-        *reinterpret_cast<uint4*>(hi + each + 8 * i) = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
-      }
-    if (mirror) {                        // the lanes' rows are next to each other
-      uint16_t* const to = reinterpret_cast<uint16_t*>(p.out) + (l * p.rows + c) * (int64_t)p.ld + r;
-#pragma unroll
-      for (int i = 0; i < 32; ++i)
-        if (c + i < p.cols) {
-          to[i * (int64_t)p.ld] = (uint16_t)(i & 1 ? h[i / 2] >> 16 : h[i / 2]);
-          to[i * (int64_t)p.ld + each] = (uint16_t)(i & 1 ? o[i / 2] >> 16 : o[i / 2]);
-        }
+  for (int i = 0; i < 4; ++i)
+    if (c + 8 * i < cols) {
+      *reinterpret_cast<uint4*>(hi + 8 * i) = make_uint4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]);
+      *reinterpret_cast<uint4*>(hi + each + 8 * i) = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
     }
+  if (mirror) {                              // the lanes' rows are next to each other
+    uint16_t* const to = reinterpret_cast<uint16_t*>(out) + ((int64_t)l * rows + c) * ld + r;
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if (c + i < cols) {
+        to[i * (int64_t)ld] = (uint16_t)(i & 1 ? h[i / 2] >> 16 : h[i / 2]);
+        to[i * (int64_t)ld + each] = (uint16_t)(i & 1 ? o[i / 2] >> 16 : o[i / 2]);
+      }
   }
 }
 
-template <bool A_MN, bool B_MN, int BN>
-__global__ void __launch_bounds__(kThreads, 1)
-k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, Product p) {
+template <typename T>
+__device__ __forceinline__ void store_turned(const Steps& a, int l, int r0, int col, const float* v, float* turn, int lane) {
+#pragma unroll
+  for (int i = 0; i < 32; ++i) turn[lane * 33 + i] = v[i] * (1.0f / (kScaleQ * kScaleX));
+  __syncwarp();
+  if (col + lane < a.N) {
+    T* p = reinterpret_cast<T*>(a.y.data) + l * a.y.outer + r0 * a.y.inner + col + lane;
+#pragma unroll 8
+    for (int i = 0; i < 32; ++i, p += a.y.inner)
+      if (r0 + i < a.M) from_float(turn[i * 33 + lane], *p);
+  }
+  __syncwarp();
+}
+
+// Tiles of a product: number, and the t-th of a matrix.  Of symmetric results those that reach the diagonal or lie below it.
+template <int BN>
+__device__ __forceinline__ int tiles_of(const Product& p) {
+  const int tm = (p.rows + kBM - 1) / kBM;
+  if (p.kind != kP && p.kind != kQ) return tm * ((p.cols + BN - 1) / BN);
+  if (BN == kBM) return tm * (tm + 1) / 2;
+  const int half = tm / 2;                       // 1, 1, 2, 2, 3, 3, ...
+  return half * (half + 1) + (tm & 1 ? half + 1 : 0);
+}
+template <int BN>
+__device__ __forceinline__ void tile_at(const Product& p, int t, int& ti, int& tj) {
+  if (p.kind != kP && p.kind != kQ) {
+    // neighbours in groups of 8 tile rows: they read the same columns of B at about the same time
+    const int tm = (p.rows + kBM - 1) / kBM, tn = (p.cols + BN - 1) / BN, group = t / (8 * tn), first = group * 8;
+    const int high = min(8, tm - first), in = t - group * 8 * tn;
+    ti = first + in % high, tj = in / high;
+    return;
+  }
+  // row ti's first tile is number ti (ti + 1) / 2, or about ti^2 / 4 of the wider ones
+  auto start = [](int i) { return BN == kBM ? i * (i + 1) / 2 : (i / 2) * (i / 2 + 1) + (i & 1 ? i / 2 + 1 : 0); };
+  ti = (int)sqrtf((BN == kBM ? 2.0f : 4.0f) * t);
+  while (start(ti) > t) --ti;
+  while (start(ti + 1) <= t) ++ti;
+  tj = t - start(ti);
+}
+
+// Every block has arrived `round` times, and what they stored is seen.  Bounded.
+__device__ __forceinline__ void all_blocks(const Steps& a, unsigned round, volatile int* abort) {
+  asm volatile("fence.proxy.async;" ::: "memory");
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(a.arrived) : "memory");
+    const uint64_t t0 = tc::global_timer_ns();
+    for (unsigned it = 1;; ++it) {
+      unsigned v;
+      asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(a.arrived) : "memory");
+      if (v >= round * gridDim.x) break;
+      if ((it & 63u) == 0 && tc::global_timer_ns() - t0 > kWaitLimitNs) {
+        *abort = 1;
+        break;
+      }
+    }
+  }
+  __syncthreads();
+  asm volatile("fence.proxy.async;" ::: "memory");
+}
+
+template <int BN>
+__global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant__ Steps a) {
   using TL = Tile<BN>;
+  constexpr int kCols = BN / 2;              // of a storing warp's row
   extern __shared__ uint8_t smem_raw[];
   uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023u) & ~(uintptr_t)1023u);
-  Bars* const bar = reinterpret_cast<Bars*>(smem + TL::kStages * TL::kStage);
+  Bars* const bar = reinterpret_cast<Bars*>(smem + TL::kStages * TL::kStage + TL::kTurn);
   volatile int* const abort = &bar->abort;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
-  int ti, tj;
-  if (p.kind == kP || p.kind == kQ) {    // tiles on and below the diagonal
-    const int t = blockIdx.x;
-    ti = (int)((sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
-    while (ti * (ti + 1) / 2 > t) --ti;
-    while ((ti + 1) * (ti + 2) / 2 <= t) ++ti;
-    tj = t - ti * (ti + 1) / 2;
-  } else {
-    ti = blockIdx.x / p.tiles_n, tj = blockIdx.x % p.tiles_n;
-  }
-  const int m0 = ti * kBM, n0 = tj * BN, l = blockIdx.y;
-  const int chunks = (p.K + kBK - 1) / kBK;
   if (tid == 0) {
     for (int s = 0; s < TL::kStages; ++s) {
       tc::mbar_init(&bar->full[s], 1);
       tc::mbar_init(&bar->empty[s], 1);
     }
-    tc::mbar_init(&bar->sums, 1);
+    for (int b = 0; b < 2; ++b) {
+      tc::mbar_init(&bar->sums[b], 1);
+      tc::mbar_init(&bar->taken[b], kStorers);
+    }
+    tc::mbar_init(&bar->drained, 1);
     bar->abort = 0;
     tc::mbar_fence_init();
   }
   if (warp == kIssuer) {
-    tc::tmem_alloc(&bar->tmem, BN);
+    tc::tmem_alloc(&bar->tmem, 2 * BN);
     tc::tmem_relinquish();
   }
   tc::tc_fence_before();
   __syncthreads();
   tc::tc_fence_after();
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  after_previous();
   const uint32_t tmem = bar->tmem;
-
-  if (warp == kProducer) {
-    if (lane == 0) {
-      int c = 0;
-      for (; c < chunks; ++c) {
-        const int s = c % TL::kStages;
-        if (c >= TL::kStages && !tc::mbar_wait(&bar->empty[s], (uint32_t)(c / TL::kStages - 1) & 1u, abort, kWaitLimitNs)) break;
-        tc::mbar_arrive_expect_tx(&bar->full[s], TL::kStage);
-        uint8_t* to = smem + s * TL::kStage;
-        const int k = c * kBK;
-#pragma unroll
-        for (int piece = 0; piece < 2; ++piece) {
-          const int z = l + piece * p.L;
-          if (A_MN) {
-            tma_load_3d(to, &map_a, m0, k, z, &bar->full[s]);
-            tma_load_3d(to + 8192, &map_a, m0 + 64, k, z, &bar->full[s]);
-          } else {
-            tma_load_3d(to, &map_a, k, m0, z, &bar->full[s]);
-          }
-          to += TL::kA;
-        }
-#pragma unroll
-        for (int piece = 0; piece < 2; ++piece) {
-          const int z = l + piece * p.L;
-#pragma unroll
-          for (int j = 0; j < BN; j += B_MN ? 64 : 128) {
-            if (B_MN) tma_load_3d(to + j * 128, &map_b, n0 + j, k, z, &bar->full[s]);
-            else tma_load_3d(to + j * 128, &map_b, k, n0 + j, z, &bar->full[s]);
-          }
-          to += TL::kB;
-        }
+  // The blocks' products and tiles, the same for every role: do(p, A, B, chunks, l, m0, n0, in).
+  uint32_t chunk = 0;                        // of this block, over all tiles and products: each role counts its own
+  auto all_tiles = [&](auto&& work) {
+    for (int k = 0; k < a.steps * 3; ++k) {
+      const int in = k / 3 & 1;                // which of the two X is read
+      const bool last = k / 3 + 1 == a.steps;
+      Product p;
+      const CUtensorMap *A, *B;
+      if (k % 3 == 0) {
+        p = {kP, a.s, a.s, a.wide ? a.N : a.M, !a.wide, !a.wide};
+        A = B = a.wide ? &a.x_rows[in] : &a.x_cols[in];
+      } else if (k % 3 == 1) {
+        p = {kQ, a.s, a.s, a.s, false, false};
+        A = B = &a.p;
+      } else {
+        p = {last ? kLast : kX, a.M, a.N, a.s, false, a.wide};
+        A = a.wide ? &a.q : &a.x_rows[in];
+        B = a.wide ? &a.x_cols[in] : &a.q;
       }
-      if (*abort)                        // the copies still in flight
-        for (int s = 0; s < TL::kStages; ++s) {
-          const int fills = c / TL::kStages + (s < c % TL::kStages ? 1 : 0);
-          if (fills > 0) wait_landed(&bar->full[s], (uint32_t)(fills - 1) & 1u);
-        }
-    }
-    __syncwarp();
-  } else if (warp == kIssuer) {
-    if (lane == 0) {
-      constexpr uint32_t kId = idesc_f16(A_MN, B_MN, kBM, BN);
-      for (int c = 0; c < chunks; ++c) {
-        const int s = c % TL::kStages;
-        if (!tc::mbar_wait(&bar->full[s], (uint32_t)(c / TL::kStages) & 1u, abort, kWaitLimitNs)) break;
-        tc::tc_fence_after();
-        const uint32_t a0 = tc::smem_u32(smem + s * TL::kStage), b0 = a0 + 2 * TL::kA;
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-          // 16 of K: 32 bytes along a row, or 16 rows of 128 bytes
-          const uint32_t da = A_MN ? kk * 2048 : kk * 32, db = B_MN ? kk * 2048 : kk * 32;
-          const uint32_t la = A_MN ? 8192 : 16, lb = B_MN ? 8192 : 16;
-          const uint64_t ah = tile_desc(a0 + da, la, 1024), al = tile_desc(a0 + TL::kA + da, la, 1024);
-          const uint64_t bh = tile_desc(b0 + db, lb, 1024), bl = tile_desc(b0 + TL::kB + db, lb, 1024);
-          tc::mma_ss(tmem, al, bh, kId, c > 0 || kk > 0);
-          tc::mma_ss(tmem, ah, bl, kId, 1u);
-          tc::mma_ss(tmem, ah, bh, kId, 1u);
-        }
-        tc::mma_commit(&bar->empty[s]);
+      const int chunks = (p.K + kBK - 1) / kBK, each = tiles_of<BN>(p);
+      const int64_t all = (int64_t)each * a.L;
+      for (int64_t t = blockIdx.x; t < all; t += gridDim.x) {
+        if (*abort) break;
+        int ti, tj;
+        const int l = (int)(t / each);
+        tile_at<BN>(p, (int)(t % each), ti, tj);
+        const int m0 = ti * kBM, n0 = tj * BN;
+        work(p, A, B, chunks, l, m0, n0, in);
       }
-      tc::mma_commit(&bar->sums);
-      wait_landed(&bar->sums, 0);        // tensor memory is freed below
+      if (k + 1 < a.steps * 3) all_blocks(a, (unsigned)k + 1, abort);
+      if (*abort) break;                       // seen by all: behind a barrier, or at the end
     }
-    __syncwarp();
-  } else {
-    const bool ok = tc::mbar_wait(&bar->sums, 0, abort, kWaitLimitNs);
-    tc::tc_fence_after();
-    const int row = m0 + warp % 4 * 32 + lane;
-    const uint32_t from = tmem + ((uint32_t)(warp % 4 * 32) << 16);
-    float* const turn = reinterpret_cast<float*>(smem) + warp * 32 * 33;   // the ring is done with
+  };
+  if (warp < kStorers) {
+    more_registers();
+    all_tiles([&](const Product& p, const CUtensorMap*, const CUtensorMap*, int chunks, int l, int m0, int n0, int in) {
+        float acc[kCols];
+#pragma unroll
+        for (int i = 0; i < kCols; ++i) acc[i] = 0.0f;
+        bool ok = true;
+        const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16, half = warp / 4 * kCols;
 #pragma unroll 1
-    for (int j = warp / 4 * 32; j < BN; j += 64) {
-      const int col = n0 + j;
-      if (col >= p.cols) break;
-      uint32_t acc[32];
-      tc::tmem_ld32(from + j, acc);
-      tc::tmem_ld_wait(acc);
-      float v[32];
+        for (int c = 0; c < chunks; ++c, ++chunk) {
+          const uint32_t buf = chunk & 1u;
+          ok = ok && tc::mbar_wait(&bar->sums[buf], chunk / 2 & 1u, abort, kWaitLimitNs);
+          if (!__all_sync(0xffffffffu, ok)) ok = false;
+          tc::tc_fence_after();
+          if (ok) {
 #pragma unroll
-      for (int i = 0; i < 32; ++i) v[i] = ok ? __uint_as_float(acc[i]) : __uint_as_float(0x7fc00000u);
-      if (p.kind == kP) {
+            for (int j = 0; j < kCols; j += 32) {
+              uint32_t r[32];
+              tc::tmem_ld32(tmem + lanes + buf * BN + half + j, r);
+              tc::tmem_ld_wait(r);
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] *= kScaleP / (kScaleX * kScaleX);
-        store_pieces(p, l, row, col, v, ti != tj);
-      } else if (p.kind == kQ) {
-        const float fc = p.c * (kScaleQ / (kScaleP * kScaleP)), fb = p.b * (kScaleQ / kScaleP);
-        const int64_t each = (int64_t)p.L * p.rows * p.ld;
-        const __half* const prev = p.prev + ((int64_t)l * p.rows + row) * p.ld + col;
-#pragma unroll
-        for (int i = 0; i < 32; i += 8) {
-          uint4 h = make_uint4(0, 0, 0, 0), o = h;
-          if (row < p.rows && col + i < p.cols) {
-            h = *reinterpret_cast<const uint4*>(prev + i);
-            o = *reinterpret_cast<const uint4*>(prev + each + i);
+              for (int i = 0; i < 32; ++i) acc[j + i] += __uint_as_float(r[i]);
+            }
           }
-          float hf[8], of[8];
-          unpack<__half, 8>(h, hf);
-          unpack<__half, 8>(o, of);
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            v[i + e] = fmaf(fc, v[i + e], fmaf(fb, hf[e], fb * of[e])) + (col + i + e == row ? p.a * kScaleQ : 0.0f);
+          tc::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive(&bar->taken[buf]);
         }
-        store_pieces(p, l, row, col, v, ti != tj);
-      } else if (p.kind == kX) {
+        const int r0 = m0 + warp % 4 * 32, row = r0 + lane;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] *= 1.0f / kScaleQ;
-        store_pieces(p, l, row, col, v, false);
-      } else {                           // y's rows start anywhere: turned, the warp stores a row's values together
+        for (int j = 0; j < kCols; j += 32) {
+          const int col = n0 + (int)half + j;
+          float* const v = acc + j;
+          if (!ok) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) turn[lane * 33 + i] = v[i] * (1.0f / (kScaleQ * kScaleX));
-        __syncwarp();
-        const int r0 = m0 + warp % 4 * 32;
-        if (col + lane < p.cols)
-          for (int i = 0; i < 32 && r0 + i < p.rows; ++i) {
-            const float w = turn[i * 33 + lane];
-            const int64_t at = l * p.y.outer + (r0 + i) * p.y.inner + col + lane;
-            if (p.dtype == NET_FP32) reinterpret_cast<float*>(p.y.data)[at] = w;
-            else if (p.dtype == NET_BF16) from_float(w, reinterpret_cast<__nv_bfloat16*>(p.y.data)[at]);
-            else from_float(w, reinterpret_cast<__half*>(p.y.data)[at]);
+            for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(0x7fc00000u);
+          }
+          if (r0 < p.rows && col < p.cols && (p.kind >= kX || col <= r0)) {
+            if (p.kind == kP) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) v[i] *= kScaleP / (kScaleX * kScaleX);
+              store_pieces(a.P, a.L, p.rows, p.cols, a.lds, l, row, col, v, col < r0);
+            } else if (p.kind == kQ) {
+              const float fc = a.c * (kScaleQ / (kScaleP * kScaleP)), fb = a.b * (kScaleQ / kScaleP);
+              const int64_t pieces = (int64_t)a.L * a.s * a.lds;
+              const __half* const prev = a.P + ((int64_t)l * a.s + row) * a.lds + col;
+#pragma unroll
+              for (int i = 0; i < 32; i += 8) {
+                uint4 h = make_uint4(0, 0, 0, 0), o = h;
+                if (row < p.rows && col + i < p.cols) {
+                  h = *reinterpret_cast<const uint4*>(prev + i);
+                  o = *reinterpret_cast<const uint4*>(prev + pieces + i);
+                }
+                float hf[8], of[8];
+                unpack<__half, 8>(h, hf);
+                unpack<__half, 8>(o, of);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                  v[i + e] = fmaf(fc, v[i + e], fmaf(fb, hf[e], fb * of[e])) + (col + i + e == row ? a.a * kScaleQ : 0.0f);
+              }
+              store_pieces(a.Q, a.L, p.rows, p.cols, a.lds, l, row, col, v, col < r0);
+            } else if (p.kind == kX) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) v[i] *= 1.0f / kScaleQ;
+              store_pieces(a.x[in ^ 1], a.L, p.rows, p.cols, a.ldx, l, row, col, v, false);
+            } else {                         // y's rows start anywhere: turned, the warp stores a row's values together
+              float* const turn = reinterpret_cast<float*>(smem + TL::kStages * TL::kStage) + warp * 32 * 33;
+              if (a.dtype == NET_FP32) store_turned<float>(a, l, r0, col, v, turn, lane);
+              else if (a.dtype == NET_BF16) store_turned<__nv_bfloat16>(a, l, r0, col, v, turn, lane);
+              else store_turned<__half>(a, l, r0, col, v, turn, lane);
+            }
+          }
+        }
+    });
+  } else {
+    fewer_registers();
+    if (warp == kProducer) {
+      all_tiles([&](const Product& p, const CUtensorMap* A, const CUtensorMap* B, int chunks, int l, int m0, int n0, int) {
+        if (lane == 0)
+          for (int c = 0; c < chunks; ++c, ++chunk) {
+            const uint32_t s = chunk % TL::kStages, use = chunk / TL::kStages;
+            if (use && !tc::mbar_wait(&bar->empty[s], (use - 1) & 1u, abort, kWaitLimitNs)) break;
+            tc::mbar_arrive_expect_tx(&bar->full[s], TL::kStage);
+            uint8_t* to = smem + s * TL::kStage;
+            const int kk = c * kBK;
+#pragma unroll
+            for (int piece = 0; piece < 2; ++piece) {
+              const int z = l + piece * a.L;
+              if (p.a_mn) {
+                tma_load_3d(to, A, m0, kk, z, &bar->full[s]);
+                tma_load_3d(to + 8192, A, m0 + 64, kk, z, &bar->full[s]);
+              } else {
+                tma_load_3d(to, A, kk, m0, z, &bar->full[s]);
+              }
+              to += TL::kA;
+            }
+#pragma unroll
+            for (int piece = 0; piece < 2; ++piece) {
+              const int z = l + piece * a.L;
+              if (p.b_mn) {
+#pragma unroll
+                for (int j = 0; j < BN; j += 64) tma_load_3d(to + j * 128, B, n0 + j, kk, z, &bar->full[s]);
+              } else {
+#pragma unroll
+                for (int j = 0; j < BN; j += 128) tma_load_3d(to + j * 128, B, kk, n0 + j, z, &bar->full[s]);
+              }
+              to += TL::kB;
+            }
           }
         __syncwarp();
-      }
+      });
+    } else {
+      all_tiles([&](const Product& p, const CUtensorMap*, const CUtensorMap*, int chunks, int, int, int, int) {
+        if (warp != kIssuer) return;
+        if (lane == 0) {
+          const uint32_t id = idesc_f16(p.a_mn, p.b_mn, kBM, BN);
+          // 16 of K: 32 bytes along a row, or 16 rows of 128 bytes
+          const uint32_t da = p.a_mn ? 2048 : 32, db = p.b_mn ? 2048 : 32, la = p.a_mn ? 8192 : 16, lb = p.b_mn ? 8192 : 16;
+          for (int c = 0; c < chunks; ++c, ++chunk) {
+            const uint32_t s = chunk % TL::kStages, buf = chunk & 1u, to = tmem + buf * BN;
+            if (chunk >= 2 && !tc::mbar_wait(&bar->taken[buf], (chunk / 2 - 1) & 1u, abort, kWaitLimitNs)) break;
+            if (!tc::mbar_wait(&bar->full[s], chunk / TL::kStages & 1u, abort, kWaitLimitNs)) break;
+            tc::tc_fence_after();
+            const uint32_t a0 = tc::smem_u32(smem + s * TL::kStage), b0 = a0 + 2 * TL::kA;
+            // the small products first: what the sum of the large ones is rounded by does not grow with them
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+              const uint64_t ah = tile_desc(a0 + kk * da, la, 1024), al = tile_desc(a0 + TL::kA + kk * da, la, 1024);
+              const uint64_t bh = tile_desc(b0 + kk * db, lb, 1024), bl = tile_desc(b0 + TL::kB + kk * db, lb, 1024);
+              tc::mma_ss(to, al, bh, id, kk > 0);
+              tc::mma_ss(to, ah, bl, id, 1u);
+            }
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk)
+              tc::mma_ss(to, tile_desc(a0 + kk * da, la, 1024), tile_desc(b0 + kk * db, lb, 1024), id, 1u);
+            tc::mma_commit(&bar->empty[s]);
+            tc::mma_commit(&bar->sums[buf]);
+          }
+        }
+        __syncwarp();
+      });
     }
   }
+  // on the way out after a wait that gave up: nothing may land when the block has left
+  if (warp == kIssuer && lane == 0) {
+    tc::mma_commit(&bar->drained);
+    wait_landed(&bar->drained, 0);
+  }
+  if (warp == kProducer && lane == 0 && *abort)
+    for (uint32_t s = 0; s < TL::kStages; ++s) {
+      const uint32_t fills = chunk / TL::kStages + (s < chunk % TL::kStages ? 1 : 0);
+      if (fills) wait_landed(&bar->full[s], (fills - 1) & 1u);
+    }
   tc::tc_fence_before();
   __syncthreads();
-  if (tid == 0 && bar->abort) *p.error = AUV_ERR_TIMEOUT;
+  if (tid == 0 && bar->abort) *a.error = AUV_ERR_TIMEOUT;
   if (warp == kIssuer) {
     tc::tc_fence_after();
-    tc::tmem_dealloc(tmem, BN);
+    tc::tmem_dealloc(tmem, 2 * BN);
   }
 }
 
@@ -484,15 +613,25 @@ int check(const net_ortho* p) {
   return AUV_OK;
 }
 
-template <bool A_MN, bool B_MN, int BN>
-cudaError_t launch_product(const CUtensorMap& A, const CUtensorMap& B, Product& p, cudaStream_t s) {
-  const auto kern = k_product<A_MN, B_MN, BN>;
+template <int BN>
+cudaError_t launch_products(const Steps& a, cudaStream_t s) {
+  const auto kern = k_products<BN>;
+  static_assert(Tile<BN>::kSmem <= 227 * 1024, "shared memory of a block");
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Tile<BN>::kSmem);
   if (e != cudaSuccess) return e;
-  const int64_t tm = (p.rows + kBM - 1) / kBM;
-  p.tiles_n = (p.cols + BN - 1) / BN;
-  const int64_t tiles = p.kind == kP || p.kind == kQ ? tm * (tm + 1) / 2 : tm * p.tiles_n;
-  return launch_after(kern, dim3((unsigned)tiles, (unsigned)p.L), kThreads, Tile<BN>::kSmem, s, A, B, p);
+  // the blocks wait for each other: all of them, one an SM, or none; no more than the largest product has tiles
+  const int64_t tiles = (int64_t)((a.M + kBM - 1) / kBM) * ((a.N + BN - 1) / BN) * a.L;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)std::min<int64_t>(sm_count(), std::max<int64_t>(1, tiles)));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = Tile<BN>::kSmem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeCooperative;
+  attr[0].val.cooperative = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, a);
 }
 
 template <typename T>
@@ -511,34 +650,22 @@ cudaError_t launch(const net_ortho* a, const Space& z, cudaStream_t s) {
                         (int64_t)0, a->y);
   e = launch_after(k_scaled<T, true>, grid, kNormThreads, 0, s, a->x, a->M, a->N, a->L, partial, z.blocks, a->eps, x[0], z.ldx, a->y);
   if (e != cudaSuccess) return e;
-  const bool wide = a->M <= a->N;
-  CUtensorMap rows[2], cols[2], pm, qm;            // of x, read by rows and along columns
-  bool ok = make_map(&pm, P, z.s, z.s, z.lds, a->L, kBM) && make_map(&qm, Q, z.s, z.s, z.lds, a->L, kBM);
+  Steps p = {};
+  p.L = (int)a->L, p.M = (int)a->M, p.N = (int)a->N, p.s = (int)z.s, p.steps = (int)a->steps, p.ldx = (int)z.ldx, p.lds = (int)z.lds;
+  p.wide = a->M <= a->N;
+  p.a = a->coef[0], p.b = a->coef[1], p.c = a->coef[2];
+  p.x[0] = x[0], p.x[1] = x[1], p.P = P, p.Q = Q;
+  p.y = a->y, p.dtype = (int)a->dtype;
+  p.error = reinterpret_cast<int*>(ws), p.arrived = reinterpret_cast<unsigned*>(ws) + 1;
+  bool ok = make_map(&p.p, P, z.s, z.s, z.lds, a->L, kBM) && make_map(&p.q, Q, z.s, z.s, z.lds, a->L, kBM);
   for (int i = 0; i < 2 && ok; ++i) {
     const __half* const at = x[a->steps > 1 ? i : 0];
-    ok = make_map(&rows[i], at, a->N, a->M, z.ldx, a->L, kBM) && make_map(&cols[i], at, a->N, a->M, z.ldx, a->L, kBK);
+    ok = make_map(&p.x_rows[i], at, a->N, a->M, z.ldx, a->L, kBM) && make_map(&p.x_cols[i], at, a->N, a->M, z.ldx, a->L, kBK);
   }
   if (!ok) return cudaErrorInvalidValue;
-  Product p = {};
-  p.L = (int)a->L;
-  p.a = a->coef[0], p.b = a->coef[1], p.c = a->coef[2];
-  p.error = reinterpret_cast<int*>(ws);
-  p.y = a->y, p.dtype = (int)a->dtype;
-  for (uint32_t k = 0; k < a->steps; ++k) {
-    const int i = k & 1;
-    p.kind = kP, p.rows = p.cols = (int)z.s, p.K = (int)std::max(a->M, a->N), p.out = P, p.ld = (int)z.lds;
-    e = wide ? launch_product<false, false, 128>(rows[i], rows[i], p, s) : launch_product<true, true, 128>(cols[i], cols[i], p, s);
-    if (e != cudaSuccess) return e;
-    p.kind = kQ, p.K = (int)z.s, p.out = Q, p.prev = P;
-    if ((e = launch_product<false, false, 128>(pm, pm, p, s)) != cudaSuccess) return e;
-    p.kind = k + 1 == a->steps ? kLast : kX, p.rows = (int)a->M, p.cols = (int)a->N, p.out = x[i ^ 1], p.ld = (int)z.ldx;
-    // wide tiles where they still fill the device
-    const bool large = ((a->M + 127) / 128) * ((a->N + 255) / 256) * a->L >= sm_count();
-    if (wide) e = large ? launch_product<false, true, 256>(qm, cols[i], p, s) : launch_product<false, true, 128>(qm, cols[i], p, s);
-    else e = large ? launch_product<false, false, 256>(rows[i], qm, p, s) : launch_product<false, false, 128>(rows[i], qm, p, s);
-    if (e != cudaSuccess) return e;
-  }
-  return cudaSuccess;
+  // wide tiles, which read less of shared memory for a product, where they still fill the device
+  const int64_t large = ((a->M + 127) / 128) * ((a->N + 255) / 256) * a->L;
+  return large >= sm_count() ? launch_products<256>(p, s) : launch_products<128>(p, s);
 }
 
 int run(const net_ortho* p, void* stream) {

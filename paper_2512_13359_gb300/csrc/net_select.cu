@@ -20,7 +20,7 @@ constexpr int kHalf = 8;        // steps whose inputs are loaded together
 // FOLD: only the piece's final state from 0, and the sum of its step sizes (-1 where an episode ends in it: nothing
 // passes through).
 template <typename T, typename L, bool FOLD>
-__global__ void __launch_bounds__(32 * kWarps) k_select(Select a) {
+__global__ void __launch_bounds__(32 * kWarps, L::SP == 8 ? 4 : 6) k_select(Select a) {
   constexpr int SP = L::SP, LS = L::LS, CC = L::CC, SW = L::SW;
   __shared__ __align__(16) float rows[kWarps][FOLD ? 1 : 2][kKeep * SW];
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
@@ -73,6 +73,11 @@ __global__ void __launch_bounds__(32 * kWarps) k_select(Select a) {
   const float bias = live && a.dt_bias ? a.dt_bias[d] : 0.0f, skip = live && a.skip ? a.skip[d] : 0.0f;
   float sum = 0.0f;
   bool cut = false;
+  const bool gated = !FOLD && a.gate.data;
+  const T* px = row_at<T>(a.x, t0, n, d);
+  const T* pdt = row_at<T>(a.dt, t0, n, d);
+  const T* pgate = gated ? row_at<T>(a.gate, t0, n, d) : px;
+  T* py = FOLD ? nullptr : const_cast<T*>(row_at<T>(a.y, t0, n, d));
 
   for (int ts = t0; ts < t1; ts += kKeep) {
     const int steps = min(kKeep, t1 - ts);
@@ -91,11 +96,12 @@ __global__ void __launch_bounds__(32 * kWarps) k_select(Select a) {
         from_float(0.0f, rx[k]);
         rdt[k] = rgate[k] = rx[k];
         if (live && k0 + k < steps) {
-          const int t = ts + k0 + k;
-          rx[k] = *row_at<T>(a.x, t, n, d);
-          rdt[k] = *row_at<T>(a.dt, t, n, d);
-          if (!FOLD && a.gate.data) rgate[k] = *row_at<T>(a.gate, t, n, d);
+          rx[k] = *px;
+          rdt[k] = *pdt;
+          if (gated) rgate[k] = *pgate;
         }
+        px += a.x.outer, pdt += a.dt.outer;
+        if (gated) pgate += a.gate.outer;
       }
 #pragma unroll
       for (int k = 0; k < kHalf; ++k) {
@@ -131,13 +137,14 @@ __global__ void __launch_bounds__(32 * kWarps) k_select(Select a) {
           sum += e;
         } else {
           float p = fmaf(skip, x, over_states<LS, CC>(y, lane));
-          if (a.gate.data) {
+          if (gated) {
             const float z = to_float(rgate[k]);
             float s, o;
             gates(z, s, o);
             p *= z * s;
           }
-          if (writes) from_float(p, *const_cast<T*>(row_at<T>(a.y, ts + k0 + k, n, d)));
+          if (writes) from_float(p, *py);
+          py += a.y.outer;
         }
       }
     }

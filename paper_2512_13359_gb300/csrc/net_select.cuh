@@ -176,9 +176,16 @@ __device__ __forceinline__ void store_states(float* p, const int64_t (&at)[CC], 
 // The rows of B or C of up to 16 steps from t on, into [16][SW] fp32, zeros past S.
 template <typename T, int SW>
 __device__ __forceinline__ void stage(const Select& a, const net_rows& r, int t, int steps, int64_t n, int g, int lane, float* to) {
-  for (int i = lane; i < kKeep * SW; i += 32) {
-    const int k = i / SW, s = i % SW;
-    to[i] = k < steps && s < a.S ? to_float(*row_at<T>(r, t + k, n, (int64_t)g * a.S + s)) : 0.0f;
+  constexpr int kSide = SW < 32 ? SW : 32, kRows = 32 / kSide;        // a lane's state stays, its rows are kRows apart
+  const int s = lane % kSide, k = lane / kSide;
+  const T* p = row_at<T>(r, t + k, n, (int64_t)g * a.S + s);
+  const int64_t by = kRows * r.outer;
+#pragma unroll
+  for (int j = 0; j < kKeep / kRows; ++j) {
+#pragma unroll
+    for (int i = 0; i < SW / kSide; ++i)
+      to[(k + j * kRows) * SW + s + i * 32] = k + j * kRows < steps && s + i * 32 < a.S ? to_float(p[i * 32]) : 0.0f;
+    p += by;
   }
 }
 
