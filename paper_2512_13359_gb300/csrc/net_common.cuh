@@ -103,6 +103,48 @@ __device__ __forceinline__ void gates(float x, float& a, float& b) {
   b = x >= 0.0f ? q : r;
 }
 
+// ---- pairs of fp32, an instruction for two (the pipe takes as long as for one after the other) ----
+struct F2 {
+  uint64_t v;
+};
+__device__ __forceinline__ F2 pair(float lo, float hi) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void split(F2 a, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(a.v)); }
+__device__ __forceinline__ F2 operator*(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 operator+(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ float ex2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+constexpr float kLog2e = 1.44269504088896341f;
+// sigmoid of both, as 1 / (1 + exp(-u)): off by 2^-24 (|u| + 6) of itself; 0 below -88.
+__device__ __forceinline__ F2 sigmoid2(F2 u) {
+  float lo, hi;
+  split(u * pair(-kLog2e, -kLog2e), lo, hi);
+  split(pair(ex2(lo), ex2(hi)) + pair(1.0f, 1.0f), lo, hi);
+  float a, b;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(lo));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(b) : "f"(hi));
+  return pair(a, b);
+}
+
 template <int BYTES>
 __device__ __forceinline__ void copy_async(void* dst, const void* src) {
   const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);

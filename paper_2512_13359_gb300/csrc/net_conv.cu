@@ -31,22 +31,32 @@ template <typename T>
 __device__ __forceinline__ const T* row_of(const net_rows& r, int64_t n, int64_t d) {
   return reinterpret_cast<const T*>(r.data) + n * r.inner + d;
 }
-__device__ __forceinline__ bool ended(const Conv& a, int t, int64_t n) {
+// The flag of the end before step t.  Loaded long before it is asked for: nothing may wait for the load in between.
+__device__ __forceinline__ uint8_t flag_at(const Conv& a, int t, int64_t n) {
   const uint8_t* p = t ? a.done : a.done_prev;
-  return p && p[(t ? (t - 1) * a.N : 0) + n];
+  return p ? p[(t ? (t - 1) * a.N : 0) + n] : (uint8_t)0;
 }
+__device__ __forceinline__ bool ended(const Conv& a, int t, int64_t n) { return flag_at(a, t, n) != 0; }
 
-// silu and its slope s (1 + u sigmoid(-u)).
-__device__ __forceinline__ float silu(float u) {
-  float s, o;
-  gates(u, s, o);
-  return u * s;
+// E channels as pairs (of one channel: with a zero beside it).
+template <typename T, int E>
+__device__ __forceinline__ void to_pairs(const Raw<T, E>& w, F2 (&v)[(E + 1) / 2]) {
+  float x[E];
+  unpack<T, E>(w, x);
+#pragma unroll
+  for (int i = 0; i < (E + 1) / 2; ++i) v[i] = pair(x[2 * i], 2 * i + 1 < E ? x[(2 * i + 1) % E] : 0.0f);
 }
-__device__ __forceinline__ float silu_slope(float u) {
-  float s, o;
-  gates(u, s, o);
-  return s * fmaf(u, o, 1.0f);
+template <typename T, int E>
+__device__ __forceinline__ Raw<T, E> from_pairs(const F2 (&v)[(E + 1) / 2]) {
+  float x[E + 1];
+#pragma unroll
+  for (int i = 0; i < (E + 1) / 2; ++i) split(v[i], x[2 * i], x[2 * i + 1]);
+  float y[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) y[e] = x[e];
+  return pack<T, E>(y);
 }
+__device__ __forceinline__ F2 zeros() { return pair(0.0f, 0.0f); }
 
 // The last K - 1 rows of the sequence, zeros where an episode has ended since.  By the thread that read the old state,
 // row i from row i + T or from x, first to last: new_state may be state.
@@ -76,26 +86,31 @@ __device__ void store_window(const Conv& a, int64_t n, int64_t d) {
   }
 }
 
+// The weights, w[j] of the row j steps back.
 template <int E, int K>
-__device__ __forceinline__ void load_taps(const Conv& a, int64_t d, float (&w)[K][E], float (&b)[E]) {
+__device__ __forceinline__ void load_taps(const Conv& a, int64_t d, F2 (&w)[K][(E + 1) / 2], F2 (&b)[(E + 1) / 2]) {
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
+  for (int i = 0; i < (E + 1) / 2; ++i) {
 #pragma unroll
-    for (int j = 0; j < K; ++j) w[j][e] = a.w[(K - 1 - j) * a.D + d + e];    // of the row j steps back
-    b[e] = a.bias ? a.bias[d + e] : 0.0f;
+    for (int j = 0; j < K; ++j) {
+      const float* const p = a.w + (K - 1 - j) * a.D + d + 2 * i;
+      w[j][i] = pair(p[0], 2 * i + 1 < E ? p[1] : 0.0f);
+    }
+    b[i] = a.bias ? pair(a.bias[d + 2 * i], 2 * i + 1 < E ? a.bias[d + 2 * i + 1] : 0.0f) : zeros();
   }
 }
 
 // The K - 1 rows ahead of step t0, win[j - 1] the one j steps back, zeros where an episode has ended since.
 template <typename T, int E, int K>
-__device__ __forceinline__ void load_window(const Conv& a, int t0, int64_t n, int64_t d, float (&win)[K][E]) {
+__device__ __forceinline__ void load_window(const Conv& a, int t0, int64_t n, int64_t d, F2 (&win)[K][(E + 1) / 2]) {
 #pragma unroll
   for (int j = 1; j < K; ++j) {
     const int s = t0 - j;
-#pragma unroll
-    for (int e = 0; e < E; ++e) win[j - 1][e] = 0.0f;
-    if (s >= 0) load<T, E>(row_of<T>(a.x, n, d) + s * a.x.outer, win[j - 1]);
-    else if (a.state) load<T, E>(reinterpret_cast<const T*>(a.state) + (s + K - 1) * a.N * a.D + n * a.D + d, win[j - 1]);
+    Raw<T, E> w = {};
+    if (s >= 0) w = *reinterpret_cast<const Raw<T, E>*>(row_of<T>(a.x, n, d) + s * a.x.outer);
+    else if (a.state)
+      w = *reinterpret_cast<const Raw<T, E>*>(reinterpret_cast<const T*>(a.state) + (s + K - 1) * a.N * a.D + n * a.D + d);
+    to_pairs<T, E>(w, win[j - 1]);
   }
   bool gone = false;                                 // ends between the rows (that before t0 is the walk's)
 #pragma unroll
@@ -104,35 +119,37 @@ __device__ __forceinline__ void load_window(const Conv& a, int t0, int64_t n, in
     if (next >= 0) gone = gone || ended(a, next, n);
     if (gone) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) win[j - 1][e] = 0.0f;
+      for (int i = 0; i < (E + 1) / 2; ++i) win[j - 1][i] = zeros();
     }
   }
 }
 
-constexpr int kForward = 256;
-constexpr int kBatch = 8;
+constexpr int kForward = 128;
 
+// A batch of steps' inputs is on its way while one is computed.
 template <typename T, int E, int K>
-__global__ void __launch_bounds__(kForward) k_conv(Conv a, bool act) {
+__global__ void __launch_bounds__(kForward, 4) k_conv(Conv a, bool act) {
+  constexpr int P = (E + 1) / 2, kBatch = E == 8 ? 4 : 8;
   const int64_t m = blockIdx.x * (int64_t)kForward + threadIdx.x, per = a.D / E;
   if (m >= a.N * per) return;
   const int64_t n = m / per, d = (m - n * per) * E;
   const int t0 = blockIdx.y * a.chunk, t1 = min(a.T, t0 + a.chunk);
   using W = Raw<T, E>;
-  float w[K][E], b[E], win[K][E];
+  F2 w[K][P], b[P], win[K][P];
   const T* x = row_of<T>(a.x, n, d) + t0 * a.x.outer;
   T* y = const_cast<T*>(row_of<T>(a.y, n, d)) + t0 * a.y.outer;
+  const bool flagged = K > 1 && (a.done || a.done_prev);
   W next[kBatch];
-  uint32_t flags = 0;
+  uint8_t next_flag[kBatch];
   auto fetch = [&](int t) {
-    flags = 0;
 #pragma unroll
     for (int u = 0; u < kBatch; ++u)
       if (t + u < t1) {
         next[u] = *reinterpret_cast<const W*>(x);
         x += a.x.outer;
-        if (K > 1 && ended(a, t + u, n)) flags |= 1u << u;
       }
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) next_flag[u] = flagged && t + u < t1 ? flag_at(a, t + u, n) : (uint8_t)0;
   };
   fetch(t0);
   load_taps<E, K>(a, d, w, b);
@@ -140,33 +157,36 @@ __global__ void __launch_bounds__(kForward) k_conv(Conv a, bool act) {
   if (blockIdx.y == 0 && a.new_state) store_window<T, E, K>(a, n, d);
   for (int t = t0; t < t1; t += kBatch) {
     W raw[kBatch];
-    const uint32_t ends = flags;
+    uint32_t ends = 0;
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u) raw[u] = next[u];
+    for (int u = 0; u < kBatch; ++u) {
+      raw[u] = next[u];
+      ends |= (next_flag[u] ? 1u : 0u) << u;
+    }
     fetch(t + kBatch);
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
       if (t + u >= t1) break;
-      float r[E], p[E];
-      unpack<T, E>(raw[u], r);
+      F2 r[P], p[P];
+      to_pairs<T, E>(raw[u], r);
       if (ends >> u & 1u) {
 #pragma unroll
         for (int j = 0; j < K; ++j)
 #pragma unroll
-          for (int e = 0; e < E; ++e) win[j][e] = 0.0f;
+          for (int i = 0; i < P; ++i) win[j][i] = zeros();
       }
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        p[e] = b[e];
+      for (int i = 0; i < P; ++i) {
+        p[i] = b[i];
 #pragma unroll
-        for (int j = K - 1; j > 0; --j) p[e] = fmaf(w[j][e], win[j - 1][e], p[e]);
-        p[e] = fmaf(w[0][e], r[e], p[e]);
+        for (int j = K - 1; j > 0; --j) p[i] = fma2(w[j][i], win[j - 1][i], p[i]);
+        p[i] = fma2(w[0][i], r[i], p[i]);
 #pragma unroll
-        for (int j = K - 1; j > 0; --j) win[j][e] = win[j - 1][e];
-        win[0][e] = r[e];
-        if (act) p[e] = silu(p[e]);
+        for (int j = K - 1; j > 0; --j) win[j][i] = win[j - 1][i];
+        win[0][i] = r[i];
+        if (act) p[i] = p[i] * sigmoid2(p[i]);
       }
-      store<T, E>(y, p);
+      *reinterpret_cast<W*>(y) = from_pairs<T, E>(p);
       y += a.y.outer;
     }
   }
@@ -175,56 +195,138 @@ __global__ void __launch_bounds__(kForward) k_conv(Conv a, bool act) {
 // Backward.  With p the sums and dp = dy act'(p): dx[s] = sum_j w_j dp[s + j] over the steps s + j that see row s, so a row
 // is done K - 1 steps after its own, or ahead of the step before which its episode ended.  The weights' gradients are
 // summed in registers over all chunks of a thread, over the block's threads of the same channels, and over the blocks by
-// k_conv_sums, each in a fixed order.
+// k_conv_sums, each in a fixed order.  Inputs come by cp.async to slots of the thread's own, three batches of four steps
+// ahead; a batch without an end, inside the chunk, is gone through without a question about its rows.
 constexpr int kBackward = 128;
+constexpr int kBack = 4, kRing = 4;                   // steps of a batch, batches in shared memory
 
 template <typename T, int E, int K>
 __global__ void __launch_bounds__(kBackward) k_conv_back(Conv a, bool act, int side) {
+  constexpr int P = (E + 1) / 2;
+  using W = Raw<T, E>;
+  constexpr bool kCopied = kAsync<T, E>;
+  extern __shared__ uint4 smem[];
   __shared__ float part[kBackward][E];
+  W* const ring = reinterpret_cast<W*>(smem) + threadIdx.x;       // slot (step, array) at (step % 16 * 2 + array) * kBackward
   const int lane = threadIdx.x % side, slot = threadIdx.x / side, slots = kBackward / side;
   const int64_t d = (blockIdx.x * (int64_t)side + lane) * E;
   const bool live = d < a.D;
-  using W = Raw<T, E>;
-  float w[K][E], b[E], dw[K][E], db[E];
+  F2 w[K][P], b[P], dw[K][P], db[P];
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    db[e] = 0.0f;
+  for (int i = 0; i < P; ++i) {
+    db[i] = zeros();
 #pragma unroll
-    for (int j = 0; j < K; ++j) dw[j][e] = 0.0f;
+    for (int j = 0; j < K; ++j) dw[j][i] = zeros();
   }
   if (live) load_taps<E, K>(a, d, w, b);
   const int64_t m = a.N * a.D, items = live ? a.N * a.chunks : 0;
+  const bool flagged = K > 1 && (a.done || a.done_prev);
   for (int64_t item = blockIdx.y * (int64_t)slots + slot; item < items; item += gridDim.y * (int64_t)slots) {
     const int64_t n = item % a.N;
     const int t0 = (int)(item / a.N) * a.chunk, t1 = min(a.T, t0 + a.chunk), last = min(a.T, t1 + K - 1);
-    float win[K][E], acc[K][E];
+    const T* const x = row_of<T>(a.x, n, d);
+    const T* const dy = row_of<T>(a.dy, n, d);
+    T* const dx = const_cast<T*>(row_of<T>(a.dx, n, d));
+    const T* px = x + t0 * a.x.outer;
+    const T* pdy = dy + t0 * a.dy.outer;
+    auto copy = [&](int t) {
+      if constexpr (kCopied) {
+#pragma unroll
+        for (int u = 0; u < kBack; ++u) {
+          if (t + u < last) {
+            W* const to = ring + (t - t0 + u) % (kBack * kRing) * 2 * kBackward;
+            copy_async<sizeof(W)>(to, px);
+            copy_async<sizeof(W)>(to + kBackward, pdy);
+          }
+          px += a.x.outer, pdy += a.dy.outer;
+        }
+        copy_commit();
+      }
+    };
+    uint8_t next_flag[kBack];
+    auto fetch_flags = [&](int t) {
+#pragma unroll
+      for (int u = 0; u < kBack; ++u) next_flag[u] = flagged && t + u < last ? flag_at(a, t + u, n) : (uint8_t)0;
+    };
+#pragma unroll
+    for (int i = 0; i < kRing - 1; ++i) copy(t0 + i * kBack);
+    fetch_flags(t0);
+    F2 win[K][P], acc[K][P];
     load_window<T, E, K>(a, t0, n, d, win);
 #pragma unroll
     for (int j = 0; j < K; ++j)
 #pragma unroll
-      for (int e = 0; e < E; ++e) acc[j][e] = 0.0f;
-    const T* const x = row_of<T>(a.x, n, d);
-    const T* const dy = row_of<T>(a.dy, n, d);
-    T* const dx = const_cast<T*>(row_of<T>(a.dx, n, d));
+      for (int i = 0; i < P; ++i) acc[j][i] = zeros();
     // rows that may still gain: of the sequence's own chunk, and ahead of the first step the state's
     int pending = t0 ? 0 : K - 1;
-    auto put = [&](int s, float (&v)[E]) {
-      if (s >= t0 && s < t1) store<T, E>(dx + s * a.dx.outer, v);
+    auto put = [&](int s, F2 (&v)[P]) {
+      if (s >= t0 && s < t1) *reinterpret_cast<W*>(dx + s * a.dx.outer) = from_pairs<T, E>(v);
       else if (s < 0 && t0 == 0 && a.dstate)
-        store<T, E>(reinterpret_cast<T*>(a.dstate) + (s + K - 1) * m + n * a.D + d, v);
+        *reinterpret_cast<W*>(reinterpret_cast<T*>(a.dstate) + (s + K - 1) * m + n * a.D + d) = from_pairs<T, E>(v);
     };
-    for (int tb = t0; tb < last; tb += kBatch) {
-      W rx[kBatch], rdy[kBatch];
-      uint32_t flags = 0;
+    auto step = [&](const W& rx, const W& rdy, bool counts) {
+      F2 r[P], dp[P];
+      to_pairs<T, E>(rx, r);
+      to_pairs<T, E>(rdy, dp);
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u)
-        if (tb + u < last) {
-          rx[u] = *reinterpret_cast<const W*>(x + (tb + u) * a.x.outer);
-          rdy[u] = *reinterpret_cast<const W*>(dy + (tb + u) * a.dy.outer);
-          if (K > 1 && ended(a, tb + u, n)) flags |= 1u << u;
+      for (int i = 0; i < P; ++i) {
+        if (act) {
+          F2 p = b[i];
+#pragma unroll
+          for (int j = K - 1; j > 0; --j) p = fma2(w[j][i], win[j - 1][i], p);
+          p = fma2(w[0][i], r[i], p);
+          // s (1 + p (1 - s)): p - p s is off by 2^-24 p, of a slope near 1 where p is large
+          const F2 s = sigmoid2(p), q = fma2(p * pair(-1.0f, -1.0f), s, p);
+          dp[i] = dp[i] * fma2(s, q, s);
+        }
+        if (counts) {
+          db[i] = db[i] + dp[i];
+          dw[0][i] = fma2(dp[i], r[i], dw[0][i]);
+#pragma unroll
+          for (int j = 1; j < K; ++j) dw[j][i] = fma2(dp[i], win[j - 1][i], dw[j][i]);
         }
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
+        for (int j = K - 1; j > 0; --j) {
+          acc[j][i] = fma2(w[j][i], dp[i], acc[j - 1][i]);
+          win[j][i] = win[j - 1][i];
+        }
+        acc[0][i] = w[0][i] * dp[i];
+        win[0][i] = r[i];
+      }
+    };
+    T* pdx = dx + (int64_t)(t0 - K + 1) * a.dx.outer;             // of the row that a step completes
+#pragma unroll 1
+    for (int tb = t0; tb < last; tb += kBack, pdx += kBack * a.dx.outer) {
+      uint32_t flags = 0;
+#pragma unroll
+      for (int u = 0; u < kBack; ++u) flags |= (next_flag[u] ? 1u : 0u) << u;
+      fetch_flags(tb + kBack);
+      W* const from = ring + (tb - t0) % (kBack * kRing) * 2 * kBackward;
+      W rx[kBack], rdy[kBack];
+      if constexpr (kCopied) {
+        copy_wait<kRing - 2>();
+#pragma unroll
+        for (int u = 0; u < kBack; ++u) rx[u] = from[u * 2 * kBackward], rdy[u] = from[(u * 2 + 1) * kBackward];
+        copy(tb + (kRing - 1) * kBack);
+      } else {
+#pragma unroll
+        for (int u = 0; u < kBack; ++u)
+          if (tb + u < last) {
+            rx[u] = *reinterpret_cast<const W*>(px);
+            rdy[u] = *reinterpret_cast<const W*>(pdy);
+            px += a.x.outer, pdy += a.dy.outer;
+          }
+      }
+      if (!flags && pending == K - 1 && tb - (K - 1) >= t0 && tb + kBack <= t1) {
+#pragma unroll
+        for (int u = 0; u < kBack; ++u) {
+          step(rx[u], rdy[u], true);
+          *reinterpret_cast<W*>(pdx + u * a.dx.outer) = from_pairs<T, E>(acc[K - 1]);
+        }
+        continue;
+      }
+#pragma unroll
+      for (int u = 0; u < kBack; ++u) {
         const int t = tb + u;
         if (t >= last) break;
         if (flags >> u & 1u) {
@@ -232,48 +334,25 @@ __global__ void __launch_bounds__(kBackward) k_conv_back(Conv a, bool act, int s
           for (int j = 1; j < K; ++j) {
             if (j <= pending) put(t - j, acc[j - 1]);
 #pragma unroll
-            for (int e = 0; e < E; ++e) win[j - 1][e] = 0.0f;
+            for (int i = 0; i < P; ++i) win[j - 1][i] = zeros();
           }
           pending = 0;
         }
-        float r[E], dp[E];
-        unpack<T, E>(rx[u], r);
-        unpack<T, E>(rdy[u], dp);
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          if (act) {
-            float p = b[e];
-#pragma unroll
-            for (int j = K - 1; j > 0; --j) p = fmaf(w[j][e], win[j - 1][e], p);
-            dp[e] *= silu_slope(fmaf(w[0][e], r[e], p));
-          }
-          if (t < t1) {
-            db[e] += dp[e];
-            dw[0][e] = fmaf(dp[e], r[e], dw[0][e]);
-#pragma unroll
-            for (int j = 1; j < K; ++j) dw[j][e] = fmaf(dp[e], win[j - 1][e], dw[j][e]);
-          }
-#pragma unroll
-          for (int j = K - 1; j > 0; --j) {
-            acc[j][e] = fmaf(w[j][e], dp[e], acc[j - 1][e]);
-            win[j][e] = win[j - 1][e];
-          }
-          acc[0][e] = w[0][e] * dp[e];
-          win[0][e] = r[e];
-        }
+        step(rx[u], rdy[u], t < t1);
         if (pending == K - 1) put(t - (K - 1), acc[K - 1]);
         else ++pending;
       }
     }
+    if constexpr (kCopied) copy_wait<0>();
     if (last == a.T) {                                // what is left passes into the state after the last step
 #pragma unroll
       for (int j = 1; j < K; ++j) {
         if (j > pending) break;
         if (a.dnew_state) {
-          float g[E];
-          load<T, E>(reinterpret_cast<const T*>(a.dnew_state) + (K - 1 - j) * m + n * a.D + d, g);
+          F2 g[P];
+          to_pairs<T, E>(*reinterpret_cast<const W*>(reinterpret_cast<const T*>(a.dnew_state) + (K - 1 - j) * m + n * a.D + d), g);
 #pragma unroll
-          for (int e = 0; e < E; ++e) acc[j - 1][e] += g[e];
+          for (int i = 0; i < P; ++i) acc[j - 1][i] = acc[j - 1][i] + g[i];
         }
         put(a.T - j, acc[j - 1]);
       }
@@ -283,12 +362,15 @@ __global__ void __launch_bounds__(kBackward) k_conv_back(Conv a, bool act, int s
   float* const out = a.partial + blockIdx.y * (K + 1) * a.D;
   for (int k = 0; k <= K; ++k) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      float v = db[e];
+    for (int i = 0; i < P; ++i) {
+      F2 q = db[i];
 #pragma unroll
       for (int j = 0; j < K; ++j)
-        if (k == K - 1 - j) v = dw[j][e];
-      part[threadIdx.x][e] = v;
+        if (k == K - 1 - j) q = dw[j][i];
+      float lo, hi;
+      split(q, lo, hi);
+      part[threadIdx.x][2 * i] = lo;
+      if (2 * i + 1 < E) part[threadIdx.x][(2 * i + 1) % E] = hi;
     }
     __syncthreads();
     if (slot == 0 && live) {
@@ -367,17 +449,19 @@ BackPlan back_plan(int64_t T, int64_t N, int64_t D, int e) {
   return p;
 }
 
-// Channels of a thread: four where every access of four is aligned.
+// Channels of a thread, as many as every access can be aligned to: forward 16 bytes, with few taps and enough channels,
+// else four, two or one.
 int width_of(const net_conv* a, bool back) {
   const int z = type_size(a->dtype);
-  if (a->D % 4) return 1;
   const net_rows* rows[] = {&a->x, back ? &a->dy : &a->y, back ? &a->dx : &a->x};
-  for (const net_rows* r : rows)
-    if (!aligned(*r, a->T, a->N, z, 4)) return 1;
   const void* flat[] = {a->state, back ? a->dnew_state : a->new_state, back ? a->dstate : nullptr};
-  for (const void* p : flat)
-    if (reinterpret_cast<uintptr_t>(p) % ((size_t)z * 4)) return 1;
-  return 4;
+  for (int e = !back && z == 2 && a->K <= 4 && a->N * a->D >= (int64_t)sm_count() * 8192 ? 8 : 4; e > 1; e /= 2) {
+    bool fits = a->D % e == 0;
+    for (const net_rows* r : rows) fits = fits && aligned(*r, a->T, a->N, z, e);
+    for (const void* p : flat) fits = fits && reinterpret_cast<uintptr_t>(p) % ((size_t)z * e) == 0;
+    if (fits) return e;
+  }
+  return 1;
 }
 
 template <typename T, int E, int K>
@@ -389,15 +473,22 @@ cudaError_t launch_taps(Conv& a, bool back, bool act, float* dw, float* dbias, c
     k_conv<T, E, K><<<dim3((unsigned)((threads + kForward - 1) / kForward), (unsigned)a.chunks), kForward, 0, s>>>(a, act);
     return cudaGetLastError();
   }
+  if constexpr (E > 4) return cudaErrorInvalidValue;   // not asked for
+  else {
   const BackPlan p = back_plan(a.T, a.N, a.D, E);
   a.chunk = p.chunk, a.chunks = p.chunks;
   if (!dw && !dbias) a.partial = nullptr;
-  k_conv_back<T, E, K><<<dim3((unsigned)p.tiles, (unsigned)p.blocks), kBackward, 0, s>>>(a, act, p.side);
-  cudaError_t e = cudaGetLastError();
+  const auto kern = k_conv_back<T, E, K>;
+  const int smem = kAsync<T, E> ? kBack * kRing * 2 * kBackward * (int)sizeof(T) * E : 0;
+  cudaError_t e = smem > 40 * 1024 ? cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) : cudaSuccess;
+  if (e != cudaSuccess) return e;
+  kern<<<dim3((unsigned)p.tiles, (unsigned)p.blocks), kBackward, smem, s>>>(a, act, p.side);
+  e = cudaGetLastError();
   if (e != cudaSuccess || !a.partial) return e;
   const int64_t cols = (K + 1) * a.D;
   return launch_after(k_conv_sums, dim3((unsigned)((cols + 31) / 32)), 1024, 0, s, a.partial, (int)p.blocks, cols, K * a.D, dw,
                       dbias);
+  }
 }
 
 template <typename T, int E>
@@ -407,11 +498,16 @@ cudaError_t launch_width(Conv& a, int K, bool back, bool act, float* dw, float* 
     case 2: return launch_taps<T, E, 2>(a, back, act, dw, dbias, s);
     case 3: return launch_taps<T, E, 3>(a, back, act, dw, dbias, s);
     case 4: return launch_taps<T, E, 4>(a, back, act, dw, dbias, s);
-    case 5: return launch_taps<T, E, 5>(a, back, act, dw, dbias, s);
-    case 6: return launch_taps<T, E, 6>(a, back, act, dw, dbias, s);
-    case 7: return launch_taps<T, E, 7>(a, back, act, dw, dbias, s);
-    default: return launch_taps<T, E, 8>(a, back, act, dw, dbias, s);
   }
+  if constexpr (E <= 4) {
+    switch (K) {
+      case 5: return launch_taps<T, E, 5>(a, back, act, dw, dbias, s);
+      case 6: return launch_taps<T, E, 6>(a, back, act, dw, dbias, s);
+      case 7: return launch_taps<T, E, 7>(a, back, act, dw, dbias, s);
+      case 8: return launch_taps<T, E, 8>(a, back, act, dw, dbias, s);
+    }
+  }
+  return cudaErrorInvalidValue;   // not asked for
 }
 
 template <typename T>
@@ -427,8 +523,13 @@ cudaError_t launch(Conv& a, const net_conv* p, bool back, cudaStream_t s) {
     if (back && p->dbias) k_conv_zero<<<(unsigned)((a.D + 255) / 256), 256, 0, s>>>(a.D, p->dbias);
     return cudaGetLastError();
   }
-  if (width_of(p, back) == 4) return launch_width<T, 4>(a, (int)p->K, back, act, p->dw, p->dbias, s);
-  return launch_width<T, 1>(a, (int)p->K, back, act, p->dw, p->dbias, s);
+  switch (width_of(p, back)) {
+    case 8:
+      if constexpr (sizeof(T) == 2) return launch_width<T, 8>(a, (int)p->K, back, act, p->dw, p->dbias, s);
+    case 4: return launch_width<T, 4>(a, (int)p->K, back, act, p->dw, p->dbias, s);
+    case 2: return launch_width<T, 2>(a, (int)p->K, back, act, p->dw, p->dbias, s);
+    default: return launch_width<T, 1>(a, (int)p->K, back, act, p->dw, p->dbias, s);
+  }
 }
 
 int check(const net_conv* p) {
@@ -491,8 +592,9 @@ size_t net_causal_conv_workspace_bytes(const net_conv* a, int backward) {
   using namespace auv::net;
   if (!a || check(a) || !backward || !a->T || !a->N || !a->D || !(a->dw || a->dbias)) return 0;
   // whatever the alignment of arrays that are not there yet
-  const int64_t wide = back_plan(a->T, a->N, a->D, 4).blocks, narrow = back_plan(a->T, a->N, a->D, 1).blocks;
-  return sizeof(float) * (size_t)std::max(wide, narrow) * (size_t)((a->K + 1) * a->D);
+  int64_t most = 0;
+  for (int e = 1; e <= 4; e *= 2) most = std::max(most, back_plan(a->T, a->N, a->D, e).blocks);
+  return sizeof(float) * (size_t)most * (size_t)((a->K + 1) * a->D);
 }
 
 int net_causal_conv(const net_conv* a, void* stream) { return auv::net::run(a, false, stream); }

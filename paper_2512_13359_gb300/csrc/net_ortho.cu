@@ -197,55 +197,80 @@ struct Bars {
   int abort;
 };
 // Two warpgroups that store, and one with the producer and the issuer.  Registers: at launch 384 threads x 168 = 64,512;
-// the storing warps, with up to 128 sums a thread, take 216, the others keep 64: 256 x 216 + 128 x 64 = 63,488.
+// the storing warps, with up to 128 sums a thread, take 224, the others keep 56: 256 x 224 + 128 x 56 = 64,512.
 constexpr int kStorers = 8, kProducer = 8, kIssuer = 9, kThreads = 384;
-__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 216;"); }
-__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 64;"); }
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 224;"); }
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 56;"); }
 
-// 32 scaled values of row r from column c on, as pieces (whole 16-byte stores; a row's padding may be written).
-__device__ __forceinline__ void store_pieces(__half* out, int L, int rows, int cols, int ld, int l, int r, int c, const float* v,
-                                             bool mirror) {
-  const int64_t each = (int64_t)L * rows * ld;
-  __half* const hi = out + ((int64_t)l * rows + r) * ld + c;
-  uint32_t h[16], o[16];
+// A warp's 32 x 32 block of sums, a row a lane, is turned through shared memory so that four lanes have a row's 32 columns
+// (64 bytes of a piece) and an access eight rows; a thread storing its own row took 2.1 us a 128 x 128 tile, and 4 to 5 us
+// more where the block is also stored on the other side of the diagonal, a value at a time.
+
+// Eight scaled values as pieces (a row's padding may be written).
+__device__ __forceinline__ void store_pieces(__half* hi, int64_t to_lo, const float (&v)[8]) {
+  uint32_t h[4], o[4];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
+  for (int i = 0; i < 4; ++i) {
     const __half2 w = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
     const float2 f = __half22float2(w);
     const __half2 z = __floats2half2_rn(v[2 * i] - f.x, v[2 * i + 1] - f.y);
     h[i] = *reinterpret_cast<const uint32_t*>(&w);
     o[i] = *reinterpret_cast<const uint32_t*>(&z);
   }
-  if (r >= rows) return;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (c + 8 * i < cols) {
-      *reinterpret_cast<uint4*>(hi + 8 * i) = make_uint4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]);
-      *reinterpret_cast<uint4*>(hi + each + 8 * i) = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+  *reinterpret_cast<uint4*>(hi) = make_uint4(h[0], h[1], h[2], h[3]);
+  *reinterpret_cast<uint4*>(hi + to_lo) = make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+// The block at (r0, c0) of a product that goes on as pieces, or with `other` its mirror image, from turn[row * 33 + column].
+template <int AHEAD>
+__device__ __forceinline__ void store_block(const Steps& a, const Product& p, __half* out, int ld, int l, int r0, int c0, bool other,
+                                            const float* turn, int lane) {
+  const int64_t to_lo = (int64_t)a.L * p.rows * ld, at = (int64_t)l * p.rows * ld;
+  const int q = lane % 4 * 8, c = (other ? r0 : c0) + q;
+  const float scale = p.kind == kP ? kScaleP / (kScaleX * kScaleX) : p.kind == kX ? 1.0f / kScaleQ : a.c * (kScaleQ / (kScaleP * kScaleP));
+  const float fb = a.b * (kScaleQ / kScaleP);
+  uint4 ph[AHEAD], po[AHEAD];                // P's values, on their way ahead of the stores
+  auto fetch = [&](int i) {
+    const int r = (other ? c0 : r0) + i * 8 + lane / 4;
+    ph[i % AHEAD] = po[i % AHEAD] = make_uint4(0, 0, 0, 0);
+    if (r < p.rows && c < p.cols) {
+      const __half* const from = a.P + at + (int64_t)r * ld + c;
+      ph[i % AHEAD] = *reinterpret_cast<const uint4*>(from);
+      po[i % AHEAD] = *reinterpret_cast<const uint4*>(from + to_lo);
     }
-  if (mirror) {                              // the lanes' rows are next to each other
-    uint16_t* const to = reinterpret_cast<uint16_t*>(out) + ((int64_t)l * rows + c) * ld + r;
+  };
 #pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if (c + i < cols) {
-        to[i * (int64_t)ld] = (uint16_t)(i & 1 ? h[i / 2] >> 16 : h[i / 2]);
-        to[i * (int64_t)ld + each] = (uint16_t)(i & 1 ? o[i / 2] >> 16 : o[i / 2]);
+  for (int i = 0; i < 4; ++i) {
+    if (p.kind == kQ && i % AHEAD == 0) {
+#pragma unroll
+      for (int k = i; k < i + AHEAD; ++k) fetch(k);
+    }
+    const int k = i * 8 + lane / 4, r = (other ? c0 : r0) + k;
+    if (r < p.rows && c < p.cols) {
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = turn[other ? (q + e) * 33 + k : k * 33 + q + e] * scale;
+      const int64_t here = at + (int64_t)r * ld + c;
+      if (p.kind == kQ) {
+        float h[8], o[8];
+        unpack<__half, 8>(ph[i % AHEAD], h);
+        unpack<__half, 8>(po[i % AHEAD], o);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += fmaf(fb, h[e], fb * o[e]) + (c + e == r ? a.a * kScaleQ : 0.0f);
       }
+      store_pieces(out + here, to_lo, v);
+    }
   }
 }
 
+// The block at (r0, c0) of the last product: y's rows start anywhere, the warp stores a row's values together.
 template <typename T>
-__device__ __forceinline__ void store_turned(const Steps& a, int l, int r0, int col, const float* v, float* turn, int lane) {
-#pragma unroll
-  for (int i = 0; i < 32; ++i) turn[lane * 33 + i] = v[i] * (1.0f / (kScaleQ * kScaleX));
-  __syncwarp();
-  if (col + lane < a.N) {
-    T* p = reinterpret_cast<T*>(a.y.data) + l * a.y.outer + r0 * a.y.inner + col + lane;
+__device__ __forceinline__ void store_last(const Steps& a, int l, int r0, int c0, const float* turn, int lane) {
+  if (c0 + lane >= a.N) return;
+  T* p = reinterpret_cast<T*>(a.y.data) + l * a.y.outer + r0 * a.y.inner + c0 + lane;
 #pragma unroll 8
-    for (int i = 0; i < 32; ++i, p += a.y.inner)
-      if (r0 + i < a.M) from_float(turn[i * 33 + lane], *p);
-  }
-  __syncwarp();
+  for (int i = 0; i < 32; ++i, p += a.y.inner)
+    if (r0 + i < a.M) from_float(turn[i * 33 + lane] * (1.0f / (kScaleQ * kScaleX)), *p);
 }
 
 // Tiles of a product: number, and the t-th of a matrix.  Of symmetric results those that reach the diagonal or lie below it.
@@ -274,12 +299,12 @@ __device__ __forceinline__ void tile_at(const Product& p, int t, int& ti, int& t
   tj = t - start(ti);
 }
 
-// Every block has arrived `round` times, and what they stored is seen.  Bounded.
+// Every block has arrived `round` times, and what they stored is seen, by TMA too.  Bounded.
 __device__ __forceinline__ void all_blocks(const Steps& a, unsigned round, volatile int* abort) {
-  asm volatile("fence.proxy.async;" ::: "memory");
-  __threadfence();
+  asm volatile("fence.proxy.async.global;" ::: "memory");
   __syncthreads();
   if (threadIdx.x == 0) {
+    __threadfence();
     asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(a.arrived) : "memory");
     const uint64_t t0 = tc::global_timer_ns();
     for (unsigned it = 1;; ++it) {
@@ -293,7 +318,7 @@ __device__ __forceinline__ void all_blocks(const Steps& a, unsigned round, volat
     }
   }
   __syncthreads();
-  asm volatile("fence.proxy.async;" ::: "memory");
+  asm volatile("fence.proxy.async.global;" ::: "memory");
 }
 
 template <int BN>
@@ -317,6 +342,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant_
     tc::mbar_init(&bar->drained, 1);
     bar->abort = 0;
     tc::mbar_fence_init();
+  }
+  if (warp == kProducer && lane < 6) {
+    const CUtensorMap* const maps[6] = {&a.x_rows[0], &a.x_rows[1], &a.x_cols[0], &a.x_cols[1], &a.p, &a.q};
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(maps[lane])) : "memory");
   }
   if (warp == kIssuer) {
     tc::tmem_alloc(&bar->tmem, 2 * BN);
@@ -387,7 +416,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant_
           __syncwarp();
           if (lane == 0) tc::mbar_arrive(&bar->taken[buf]);
         }
-        const int r0 = m0 + warp % 4 * 32, row = r0 + lane;
+        const int r0 = m0 + warp % 4 * 32;
+        float* const turn = reinterpret_cast<float*>(smem + TL::kStages * TL::kStage) + warp * 32 * 33;
 #pragma unroll
         for (int j = 0; j < kCols; j += 32) {
           const int col = n0 + (int)half + j;
@@ -397,39 +427,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant_
             for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(0x7fc00000u);
           }
           if (r0 < p.rows && col < p.cols && (p.kind >= kX || col <= r0)) {
-            if (p.kind == kP) {
 #pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] *= kScaleP / (kScaleX * kScaleX);
-              store_pieces(a.P, a.L, p.rows, p.cols, a.lds, l, row, col, v, col < r0);
-            } else if (p.kind == kQ) {
-              const float fc = a.c * (kScaleQ / (kScaleP * kScaleP)), fb = a.b * (kScaleQ / kScaleP);
-              const int64_t pieces = (int64_t)a.L * a.s * a.lds;
-              const __half* const prev = a.P + ((int64_t)l * a.s + row) * a.lds + col;
-#pragma unroll
-              for (int i = 0; i < 32; i += 8) {
-                uint4 h = make_uint4(0, 0, 0, 0), o = h;
-                if (row < p.rows && col + i < p.cols) {
-                  h = *reinterpret_cast<const uint4*>(prev + i);
-                  o = *reinterpret_cast<const uint4*>(prev + pieces + i);
-                }
-                float hf[8], of[8];
-                unpack<__half, 8>(h, hf);
-                unpack<__half, 8>(o, of);
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                  v[i + e] = fmaf(fc, v[i + e], fmaf(fb, hf[e], fb * of[e])) + (col + i + e == row ? a.a * kScaleQ : 0.0f);
-              }
-              store_pieces(a.Q, a.L, p.rows, p.cols, a.lds, l, row, col, v, col < r0);
-            } else if (p.kind == kX) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] *= 1.0f / kScaleQ;
-              store_pieces(a.x[in ^ 1], a.L, p.rows, p.cols, a.ldx, l, row, col, v, false);
-            } else {                         // y's rows start anywhere: turned, the warp stores a row's values together
-              float* const turn = reinterpret_cast<float*>(smem + TL::kStages * TL::kStage) + warp * 32 * 33;
-              if (a.dtype == NET_FP32) store_turned<float>(a, l, r0, col, v, turn, lane);
-              else if (a.dtype == NET_BF16) store_turned<__nv_bfloat16>(a, l, r0, col, v, turn, lane);
-              else store_turned<__half>(a, l, r0, col, v, turn, lane);
+            for (int i = 0; i < 32; ++i) turn[lane * 33 + i] = v[i];
+            __syncwarp();
+            if (p.kind == kLast) {
+              if (a.dtype == NET_FP32) store_last<float>(a, l, r0, col, turn, lane);
+              else if (a.dtype == NET_BF16) store_last<__nv_bfloat16>(a, l, r0, col, turn, lane);
+              else store_last<__half>(a, l, r0, col, turn, lane);
+            } else {
+              __half* const out = p.kind == kP ? a.P : p.kind == kQ ? a.Q : a.x[in ^ 1];
+              const int ld = p.kind == kX ? a.ldx : a.lds;
+              store_block<BN == 128 ? 4 : 1>(a, p, out, ld, l, r0, col, false, turn, lane);
+              if (p.kind != kX && col < r0) store_block<BN == 128 ? 4 : 1>(a, p, out, ld, l, r0, col, true, turn, lane);
             }
+            __syncwarp();
           }
         }
     });

@@ -15,14 +15,15 @@ namespace net {
 namespace {
 
 constexpr int kWarps = 4;
-constexpr int kHalf = 8;        // steps whose inputs are loaded together
+constexpr int kBatch = 4;       // steps whose inputs are on their way while as many are computed
 
 // FOLD: only the piece's final state from 0, and the sum of its step sizes (-1 where an episode ends in it: nothing
 // passes through).
 template <typename T, typename L, bool FOLD>
 __global__ void __launch_bounds__(32 * kWarps, L::SP == 8 ? 4 : 6) k_select(Select a) {
   constexpr int SP = L::SP, LS = L::LS, CC = L::CC, SW = L::SW;
-  __shared__ __align__(16) float rows[kWarps][FOLD ? 1 : 2][kKeep * SW];
+  using In = Staged<T, SW, kBatch>;
+  __shared__ __align__(16) float rows[kWarps][FOLD ? 1 : 2][kBatch * SW];
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   int64_t id = blockIdx.x * (int64_t)kWarps + warp;
   const int64_t envs_groups = a.N * a.G;
@@ -45,12 +46,49 @@ __global__ void __launch_bounds__(32 * kWarps, L::SP == 8 ? 4 : 6) k_select(Sele
   bool there[CC];
 #pragma unroll
   for (int c = 0; c < CC; ++c) {
-    at_weight[c] = (int64_t)g * a.per + first + c;
+    const int k = first + (q % CC ^ c);
+    at_weight[c] = (int64_t)g * a.per + k;
     at[c] = n * a.D + at_weight[c];
-    there[c] = first + c < a.per;
+    there[c] = k < a.per;
   }
   const int t0 = piece * a.piece, t1 = min(a.T, t0 + a.piece);
   const int64_t states = a.N * a.D * a.S;
+  const bool gated = !FOLD && a.gate.data, flagged = a.done || a.done_prev;
+  const T* px = row_at<T>(a.x, t0, n, d);
+  const T* pdt = row_at<T>(a.dt, t0, n, d);
+  const T* pgate = gated ? row_at<T>(a.gate, t0, n, d) : px;
+  T* py = FOLD ? nullptr : const_cast<T*>(row_at<T>(a.y, t0, n, d));
+  const int64_t in_row = (int64_t)g * a.S + lane % In::kSide;
+  const T* pB = row_at<T>(a.B, t0 + lane / In::kSide, n, in_row);
+  const T* pC = row_at<T>(a.C, t0 + lane / In::kSide, n, in_row);
+  T rx[kBatch], rdt[kBatch], rgate[kBatch];
+  In rB, rC;
+  uint8_t rend = 0;
+  auto fetch = [&](int t) {
+    const int steps = t1 - t;
+    if (steps <= 0) return;
+    rend = flagged && lane < min(kBatch, steps) ? flag_at(a, t + lane, n) : (uint8_t)0;
+    rB.load(pB, a.B.outer, steps, a.S, lane);
+    pB += kBatch * a.B.outer;
+    if constexpr (!FOLD) {
+      rC.load(pC, a.C.outer, steps, a.S, lane);
+      pC += kBatch * a.C.outer;
+    }
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      from_float(0.0f, rx[k]);
+      rdt[k] = rgate[k] = rx[k];
+      if (live && k < steps) {
+        rx[k] = *px;
+        rdt[k] = *pdt;
+        if (gated) rgate[k] = *pgate;
+      }
+      px += a.x.outer, pdt += a.dt.outer;
+      if (gated) pgate += a.gate.outer;
+    }
+  };
+  fetch(t0);
+
   F2 h[CC][SP / 2], A2[CC][SP / 2];
   if constexpr (!FOLD) {
     if (a.pieces > 1) {
@@ -73,82 +111,68 @@ __global__ void __launch_bounds__(32 * kWarps, L::SP == 8 ? 4 : 6) k_select(Sele
   const float bias = live && a.dt_bias ? a.dt_bias[d] : 0.0f, skip = live && a.skip ? a.skip[d] : 0.0f;
   float sum = 0.0f;
   bool cut = false;
-  const bool gated = !FOLD && a.gate.data;
-  const T* px = row_at<T>(a.x, t0, n, d);
-  const T* pdt = row_at<T>(a.dt, t0, n, d);
-  const T* pgate = gated ? row_at<T>(a.gate, t0, n, d) : px;
-  T* py = FOLD ? nullptr : const_cast<T*>(row_at<T>(a.y, t0, n, d));
 
-  for (int ts = t0; ts < t1; ts += kKeep) {
-    const int steps = min(kKeep, t1 - ts);
-    const uint32_t ends = ends_of(a, ts, n, lane);
-    stage<T, SW>(a, a.B, ts, steps, n, g, lane, Bs);
-    if constexpr (!FOLD) {
-      stage<T, SW>(a, a.C, ts, steps, n, g, lane, Cs);
-      if (a.kept) store_states<SP, CC>(a.kept + ts / kKeep * states, at, there, s0, a.S, h);
-    }
-    __syncwarp();
 #pragma unroll 1
-    for (int k0 = 0; k0 < steps; k0 += kHalf) {
-      T rx[kHalf], rdt[kHalf], rgate[kHalf];
+  for (int ts = t0; ts < t1; ts += kBatch) {
+    const int steps = t1 - ts;
+    __syncwarp();                                             // the last batch's rows are read
+    rB.put(Bs, lane);
+    if constexpr (!FOLD) rC.put(Cs, lane);
+    const uint32_t ends = flagged ? __ballot_sync(0xffffffffu, rend != 0) : 0u;
+    float x[kBatch], e[kBatch];
+    [[maybe_unused]] float z[kBatch];
 #pragma unroll
-      for (int k = 0; k < kHalf; ++k) {
-        from_float(0.0f, rx[k]);
-        rdt[k] = rgate[k] = rx[k];
-        if (live && k0 + k < steps) {
-          rx[k] = *px;
-          rdt[k] = *pdt;
-          if (gated) rgate[k] = *pgate;
-        }
-        px += a.x.outer, pdt += a.dt.outer;
-        if (gated) pgate += a.gate.outer;
-      }
-#pragma unroll
-      for (int k = 0; k < kHalf; ++k) {
-        if (k0 + k >= steps) break;
-        const float x = to_float(rx[k]);
-        const float e = live ? softplus(to_float(rdt[k]) + bias) : 0.0f;
-        float es[CC], us[CC];
-        to_lanes<LS, CC>(e, es);
-        to_lanes<LS, CC>(e * x, us);
-        F2 B[SP / 2], C[SP / 2];
-        load_pairs<SP>(Bs + (k0 + k) * SW + s0, B);
-        if constexpr (!FOLD) load_pairs<SP>(Cs + (k0 + k) * SW + s0, C);
-        if (ends >> (k0 + k) & 1u) {
-#pragma unroll
-          for (int c = 0; c < CC; ++c)
-#pragma unroll
-            for (int i = 0; i < SP / 2; ++i) h[c][i] = pair(0.0f, 0.0f);
-          cut = true;
-        }
-        float y[CC];
-#pragma unroll
-        for (int c = 0; c < CC; ++c) {
-          const F2 e2 = pair(es[c], es[c]), u2 = pair(us[c], us[c]);
-          F2 acc = pair(0.0f, 0.0f);
-#pragma unroll
-          for (int i = 0; i < SP / 2; ++i) {
-            h[c][i] = fma2(ex2(e2 * A2[c][i]), h[c][i], u2 * B[i]);
-            if constexpr (!FOLD) acc = fma2(C[i], h[c][i], acc);
-          }
-          y[c] = total(acc);
-        }
-        if constexpr (FOLD) {
-          sum += e;
-        } else {
-          float p = fmaf(skip, x, over_states<LS, CC>(y, lane));
-          if (gated) {
-            const float z = to_float(rgate[k]);
-            float s, o;
-            gates(z, s, o);
-            p *= z * s;
-          }
-          if (writes) from_float(p, *py);
-          py += a.y.outer;
-        }
+    for (int k = 0; k < kBatch; ++k) {
+      x[k] = to_float(rx[k]);
+      e[k] = live ? softplus(to_float(rdt[k]) + bias) : 0.0f;
+      if (gated) {
+        const float v = to_float(rgate[k]);
+        float s, o;
+        gates(v, s, o);
+        z[k] = v * s;
       }
     }
+    fetch(ts + kBatch);
+    if constexpr (!FOLD)
+      if (a.kept && ts % kKeep == 0) store_states<SP, CC>(a.kept + ts / kKeep * states, at, there, s0, a.S, h);
     __syncwarp();
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      if (k >= steps) break;
+      float es[CC], us[CC];
+      to_lanes<CC>(e[k], es);
+      to_lanes<CC>(e[k] * x[k], us);
+      F2 B[SP / 2], C[SP / 2];
+      load_pairs<SP>(Bs + k * SW + s0, B);
+      if constexpr (!FOLD) load_pairs<SP>(Cs + k * SW + s0, C);
+      if (ends >> k & 1u) {
+#pragma unroll
+        for (int c = 0; c < CC; ++c)
+#pragma unroll
+          for (int i = 0; i < SP / 2; ++i) h[c][i] = pair(0.0f, 0.0f);
+        cut = true;
+      }
+      float y[CC];
+#pragma unroll
+      for (int c = 0; c < CC; ++c) {
+        const F2 e2 = pair(es[c], es[c]), u2 = pair(us[c], us[c]);
+        F2 acc = pair(0.0f, 0.0f);
+#pragma unroll
+        for (int i = 0; i < SP / 2; ++i) {
+          h[c][i] = fma2(ex2(e2 * A2[c][i]), h[c][i], u2 * B[i]);
+          if constexpr (!FOLD) acc = i ? fma2(C[i], h[c][i], acc) : C[i] * h[c][i];
+        }
+        y[c] = total(acc);
+      }
+      if constexpr (FOLD) {
+        sum += e[k];
+      } else {
+        float p = fmaf(skip, x[k], over_states<LS, CC>(y));
+        if (gated) p *= z[k];
+        if (writes) from_float(p, *py);
+        py += a.y.outer;
+      }
+    }
   }
   if constexpr (FOLD) {
     store_states<SP, CC>(a.maps + piece * states, at, there, s0, a.S, h);

@@ -30,42 +30,17 @@ struct Select {
   float *parts;                 // backward, groups of several blocks: [blocks][T][N][G][2][S] sums of dB and dC
 };
 
-// ---- pairs of fp32 ----
-struct F2 {
-  uint64_t v;
-};
-__device__ __forceinline__ F2 pair(float lo, float hi) {
-  F2 r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
-  return r;
-}
-__device__ __forceinline__ void split(F2 a, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(a.v)); }
-__device__ __forceinline__ F2 operator*(F2 a, F2 b) {
-  F2 r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
-}
-__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
-  F2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-  return r;
-}
 __device__ __forceinline__ float total(F2 a) {
   float lo, hi;
   split(a, lo, hi);
   return lo + hi;
-}
-__device__ __forceinline__ float ex2(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
 }
 __device__ __forceinline__ F2 ex2(F2 a) {
   float lo, hi;
   split(a, lo, hi);
   return pair(ex2(lo), ex2(hi));
 }
-constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+constexpr float kLn2 = 0.693147180559945309f;
 
 // softplus(v) = max(v, 0) + log(1 + q), q = exp(-|v|), and sigmoid(v) = 1 / (1 + q) or q / (1 + q).  log(1 + q) = 2 atanh(z)
 // with z = q / (2 + q) <= 1/3: z times a polynomial in z^2 fitted on [0, 1/9] (Chebyshev, 8e-9 relative), so that a small
@@ -84,15 +59,13 @@ __device__ __forceinline__ float softplus(float v, float* sigmoid = nullptr) {
   return fmaf(z, p, fmaxf(v, 0.0f));
 }
 
-// Sums over the lanes that share channels, of CC values a lane (one per channel): afterwards v[0] is that of the lane's own
-// channel, q % CC.
+// Sums over the lanes that share channels, of CC values a lane (one per channel, its own first): that of its own channel.
 template <int LS, int CC>
-__device__ __forceinline__ float over_states(const float (&v)[CC], int lane) {
+__device__ __forceinline__ float over_states(const float (&v)[CC]) {
   float r = v[0];
   int bit = 1;
   if constexpr (CC == 2) {
-    const bool up = lane & 1;
-    r = (up ? v[1] : v[0]) + __shfl_xor_sync(0xffffffffu, up ? v[0] : v[1], 1);
+    r += __shfl_xor_sync(0xffffffffu, v[1], 1);
     bit = 2;
   }
 #pragma unroll
@@ -100,21 +73,23 @@ __device__ __forceinline__ float over_states(const float (&v)[CC], int lane) {
   return r;
 }
 
-// A value of the lane's own channel to the lanes that share it: r[c] is channel c's.
-template <int LS, int CC>
+// A value of the lane's own channel to the lanes that share it: r[c] is that of the lane's c-th channel, its own first.
+template <int CC>
 __device__ __forceinline__ void to_lanes(float own, float (&r)[CC]) {
-#pragma unroll
-  for (int c = 0; c < CC; ++c) r[c] = LS == 1 ? own : __shfl_sync(0xffffffffu, own, c, LS);
+  r[0] = own;
+  if constexpr (CC == 2) r[1] = __shfl_xor_sync(0xffffffffu, own, 1);
 }
 
 template <typename T>
 __device__ __forceinline__ const T* row_at(const net_rows& r, int64_t t, int64_t n, int64_t k) {
   return reinterpret_cast<const T*>(r.data) + t * r.outer + n * r.inner + k;
 }
-__device__ __forceinline__ bool ended(const Select& a, int t, int64_t n) {
+// The flag of the end before step t.
+__device__ __forceinline__ uint8_t flag_at(const Select& a, int t, int64_t n) {
   const uint8_t* p = t ? a.done : a.done_prev;
-  return p && p[(t ? (t - 1) * a.N : 0) + n];
+  return p ? p[(t ? (t - 1) * a.N : 0) + n] : (uint8_t)0;
 }
+__device__ __forceinline__ bool ended(const Select& a, int t, int64_t n) { return flag_at(a, t, n) != 0; }
 // Bit i: an episode ended before step t + i, of the 16 from t on.
 __device__ __forceinline__ uint32_t ends_of(const Select& a, int t, int64_t n, int lane) {
   if (!a.done && !a.done_prev) return 0u;
@@ -188,6 +163,35 @@ __device__ __forceinline__ void stage(const Select& a, const net_rows& r, int t,
     p += by;
   }
 }
+
+// The same for STEPS steps, in two parts: the loads, of a lane's values, and their way into shared memory.
+template <typename T, int SW, int STEPS>
+struct Staged {
+  static constexpr int kSide = SW < 32 ? SW : 32, kRows = 32 / kSide;
+  static constexpr int kDown = (STEPS + kRows - 1) / kRows, kAcross = SW / kSide;
+  T v[kDown][kAcross];
+  __device__ __forceinline__ void load(const T* p, int64_t by, int steps, int S, int lane) {   // p: the lane's first value
+    const int s = lane % kSide, k = lane / kSide;
+#pragma unroll
+    for (int j = 0; j < kDown; ++j) {
+#pragma unroll
+      for (int i = 0; i < kAcross; ++i) {
+        from_float(0.0f, v[j][i]);
+        if (k + j * kRows < steps && s + i * 32 < S) v[j][i] = p[i * 32];
+      }
+      p += kRows * by;
+    }
+  }
+  __device__ __forceinline__ void put(float* to, int lane) const {
+    const int s = lane % kSide, k = lane / kSide;
+#pragma unroll
+    for (int j = 0; j < kDown; ++j)
+      if (STEPS % kRows == 0 || k + j * kRows < STEPS) {
+#pragma unroll
+        for (int i = 0; i < kAcross; ++i) to[(k + j * kRows) * SW + s + i * 32] = to_float(v[j][i]);
+      }
+  }
+};
 
 // SP values of a staged row as pairs.
 template <int SP>

@@ -91,8 +91,9 @@ __global__ void __launch_bounds__(32 * kBackWarps<L>, 1) k_select_back(Select a,
   bool there[CC];
 #pragma unroll
   for (int c = 0; c < CC; ++c) {
-    at_weight[c] = (int64_t)g * a.per + first + c;
-    there[c] = first + c < a.per;
+    const int k = first + (q % CC ^ c);
+    at_weight[c] = (int64_t)g * a.per + k;
+    there[c] = k < a.per;
   }
   if (a.pieces > 1) after_previous();
   F2 A2[CC][kP], dA[CC][kP];
@@ -167,7 +168,7 @@ __global__ void __launch_bounds__(32 * kBackWarps<L>, 1) k_select_back(Select a,
         auto channels = [&](int k, float (&e)[CC], float (&u)[CC], float (&p)[CC]) {
 #pragma unroll
           for (int c = 0; c < CC; ++c) {
-            const float4 w = m.own[k][lane / LS * LS + c];
+            const float4 w = m.own[k][lane ^ c];
             e[c] = w.x, u[c] = w.x * w.y, p[c] = w.z;
           }
         };
@@ -239,7 +240,7 @@ __global__ void __launch_bounds__(32 * kBackWarps<L>, 1) k_select_back(Select a,
                 }
                 yc[c] = total(acc);
               }
-              y[k] = over_states<LS, CC>(yc, lane);
+              y[k] = over_states<LS, CC>(yc);
 #pragma unroll
               for (int i = 0; i < kP; ++i) split(sC[i], dC[2 * i], dC[2 * i + 1]);
               put_sums<SP, LS>(dC, lane, &m.sums[i0][1][s0]);
@@ -271,7 +272,7 @@ __global__ void __launch_bounds__(32 * kBackWarps<L>, 1) k_select_back(Select a,
                 by_B[c] = total(accB);
                 by_A[c] = total(accA);
               }
-              const float sumB = over_states<LS, CC>(by_B, lane), sumA = over_states<LS, CC>(by_A, lane) * kLn2;
+              const float sumB = over_states<LS, CC>(by_B), sumA = over_states<LS, CC>(by_A) * kLn2;
 #pragma unroll
               for (int i = 0; i < kP; ++i) split(sB[i], dB[2 * i], dB[2 * i + 1]);
               put_sums<SP, LS>(dB, lane, &m.sums[i0][0][s0]);
@@ -341,9 +342,10 @@ __global__ void __launch_bounds__(32 * kFoldWarps) k_select_fold_back(Select a) 
   bool there[CC];
 #pragma unroll
   for (int c = 0; c < CC; ++c) {
-    at_weight[c] = (int64_t)g * a.per + first + c;
+    const int k = first + (q % CC ^ c);
+    at_weight[c] = (int64_t)g * a.per + k;
     at[c] = n * a.D + at_weight[c];
-    there[c] = first + c < a.per;
+    there[c] = k < a.per;
   }
   const int t0 = piece * a.piece, t1 = min(a.T, t0 + a.piece);
   F2 G[CC][SP / 2], A2[CC][SP / 2];
@@ -389,8 +391,8 @@ __global__ void __launch_bounds__(32 * kFoldWarps) k_select_fold_back(Select a) 
             p *= z * s;
           }
           float es[CC], ps[CC];
-          to_lanes<LS, CC>(e, es);
-          to_lanes<LS, CC>(p, ps);
+          to_lanes<CC>(e, es);
+          to_lanes<CC>(p, ps);
           F2 C[SP / 2];
           load_pairs<SP>(Cs + (k0 + k) * SW + s0, C);
           const bool end = ends >> (k0 + k) & 1u;
