@@ -19,7 +19,7 @@ namespace {
 constexpr int kSub = 4;         // steps held in registers
 
 // Warps of a block: shared memory grows with the padded states.
-template <typename L> constexpr int kBackWarps = L::SW <= 32 ? 8 : L::SW <= 64 ? 4 : 2;
+constexpr int back_warps(int padded) { return padded <= 16 ? 8 : padded <= 64 ? 4 : 2; }
 
 // A warp's shared memory.
 template <typename L> struct Back {
@@ -27,63 +27,136 @@ template <typename L> struct Back {
   float4 own[kKeep][32];                        // e, x, p, dy silu'(gate) of the lane's own channel
   float slope[kKeep][32];                       // sigmoid(dt + dt_bias)
   float4 start[kKeep / kSub][L::CC * L::SP / 4][32];   // the lane's states before steps 0, 4, 8, 12
-  float sums[kKeep][2][L::SW];                  // dB and dC over the warp's channels
+  float sums[2][kKeep][2][L::SW];               // dB and dC over the warp's channels; of this segment and the last
 };
 
-// Sums over the lanes with the same q of SP values: at each level a lane gives half of its values away.  Returns how many
-// are left, the sums of values base, base + 1, ...; lanes whose bits in `same` are not 0 hold what another one holds too.
-template <int SP, int LS>
-__device__ __forceinline__ void over_channels(float (&v)[SP], int lane, int& base, int& same) {
-  base = same = 0;
-  int n = SP;
+// The order of a lane's pairs of states.  Sums over channels go over the lanes with the same q; at each level a lane keeps
+// half of its values and gives half away.  Lanes that keep the upper half of the pairs have them first: what a lane keeps
+// and gives then sits in the same registers everywhere, and nothing is selected.
+template <typename L>
+__device__ __forceinline__ int pair_order(int lane) {
+  int order = 0;
+  int bit = 16;
 #pragma unroll
-  for (int bit = 16; bit >= LS; bit /= 2) {
-    if (n > 1) {
+  for (int n = L::SP / 4; n >= 1 && bit >= L::LS; n /= 2, bit /= 2) order |= lane & bit ? n : 0;
+  return order;
+}
+__device__ __forceinline__ F2 other(F2 v, int bit) {
+  float lo, hi;
+  split(v, lo, hi);
+  return pair(__shfl_xor_sync(0xffffffffu, lo, bit), __shfl_xor_sync(0xffffffffu, hi, bit));
+}
+// The sums of v over the warp's channels, to [SW] (to: the lane's states of it).
+template <typename L>
+__device__ __forceinline__ void put_sums(F2 (&v)[L::SP / 2], int lane, int order, float* to) {
+  constexpr int P = L::SP / 2, LS = L::LS;
+  int n = P, bit = 16;
+#pragma unroll
+  for (int k = 0; k < 5; ++k)
+    if (n > 1 && bit >= LS) {
       n /= 2;
-      const bool up = lane & bit;
 #pragma unroll
-      for (int i = 0; i < SP / 2; ++i)
-        if (i < n) {
-          const float give = up ? v[i] : v[i + n];
-          v[i] = (up ? v[i + n] : v[i]) + __shfl_xor_sync(0xffffffffu, give, bit);
-        }
-      base += up ? n : 0;
-    } else {
-      v[0] += __shfl_xor_sync(0xffffffffu, v[0], bit);
-      same |= bit;
+      for (int i = 0; i < P / 2; ++i)
+        if (i < n) v[i] = v[i] + other(v[i + n], bit);
+      bit /= 2;
     }
-  }
-}
-template <int SP, int LS> constexpr int left_over() {
-  int n = SP;
-  for (int bit = 16; bit >= LS; bit /= 2) n = n > 1 ? n / 2 : 1;
-  return n;
-}
-template <int SP, int LS>
-__device__ __forceinline__ void put_sums(float (&v)[SP], int lane, float* to) {
-  int base, same;
-  over_channels<SP, LS>(v, lane, base, same);
-  if (!(lane & same)) {
+  if (n > 1 || bit < LS) {                      // lanes ran out: pairs are left
 #pragma unroll
-    for (int i = 0; i < left_over<SP, LS>(); ++i) to[base + i] = v[i];
+    for (int i = 0; i < P; ++i)
+      if (i < n) {
+        float2 w;
+        split(v[i], w.x, w.y);
+        *reinterpret_cast<float2*>(to + 2 * (i ^ order)) = w;
+      }
+    return;
   }
+  float lo, hi;
+  split(v[0], lo, hi);
+  const bool up = lane & bit;
+  float r = (up ? hi : lo) + __shfl_xor_sync(0xffffffffu, up ? lo : hi, bit);
+  const int odd = up;
+  int same = 0;
+  bit /= 2;
+#pragma unroll
+  for (int k = 0; k < 5; ++k)
+    if (bit >= LS) {
+      r += __shfl_xor_sync(0xffffffffu, r, bit);
+      same |= bit;
+      bit /= 2;
+    }
+  if (!(lane & same)) to[2 * order + odd] = r;
 }
 
-// rows: (env, group) pairs a block walks side by side, kBackWarps / rows warps each.
+// SP states of CC channels in the lane's order.
+template <int SP, int CC>
+__device__ __forceinline__ void load_ordered(const float* p, const int64_t (&at)[CC], const bool (&there)[CC], int s0, int order,
+                                             int S, F2 (&h)[CC][SP / 2]) {
+  const bool vec = S % 2 == 0 && reinterpret_cast<uintptr_t>(p) % 8 == 0;
+#pragma unroll
+  for (int c = 0; c < CC; ++c)
+#pragma unroll
+    for (int i = 0; i < SP / 2; ++i) {
+      const int s = s0 + 2 * (i ^ order);
+      const float* const q = p + at[c] * S + s;
+      float2 w = make_float2(0.0f, 0.0f);
+      if (p && there[c] && s < S) {
+        if (vec) w = *reinterpret_cast<const float2*>(q);
+        else w = make_float2(q[0], s + 1 < S ? q[1] : 0.0f);
+      }
+      h[c][i] = pair(w.x, w.y);
+    }
+}
+template <int SP, int CC>
+__device__ __forceinline__ void store_ordered(float* p, const int64_t (&at)[CC], const bool (&there)[CC], int s0, int order, int S,
+                                              const F2 (&h)[CC][SP / 2]) {
+  const bool vec = S % 2 == 0 && reinterpret_cast<uintptr_t>(p) % 8 == 0;
+#pragma unroll
+  for (int c = 0; c < CC; ++c)
+#pragma unroll
+    for (int i = 0; i < SP / 2; ++i) {
+      const int s = s0 + 2 * (i ^ order);
+      float* const q = p + at[c] * S + s;
+      float2 w;
+      split(h[c][i], w.x, w.y);
+      if (there[c] && s < S) {
+        if (vec) {
+          *reinterpret_cast<float2*>(q) = w;
+        } else {
+          q[0] = w.x;
+          if (s + 1 < S) q[1] = w.y;
+        }
+      }
+    }
+}
+template <int P>
+__device__ __forceinline__ void load_pairs(const float* row, int order, F2 (&v)[P]) {   // row: at the lane's states
+#pragma unroll
+  for (int i = 0; i < P; ++i) v[i].v = *reinterpret_cast<const uint64_t*>(row + 2 * (i ^ order));
+}
+template <int CC, int P>
+__device__ __forceinline__ void clear(F2 (&h)[CC][P]) {
+#pragma unroll
+  for (int c = 0; c < CC; ++c)
+#pragma unroll
+    for (int i = 0; i < P; ++i) h[c][i] = pair(0.0f, 0.0f);
+}
+__device__ __forceinline__ void prefetch(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+
+// rows: (env, group) pairs a block walks side by side, back_warps / rows warps each.
 template <typename T, typename L>
-__global__ void __launch_bounds__(32 * kBackWarps<L>, 1) k_select_back(Select a, int rows) {
-  constexpr int SP = L::SP, LS = L::LS, CC = L::CC, SW = L::SW, kP = SP / 2;
+__global__ void __launch_bounds__(32 * back_warps(L::SW), 1) k_select_back(Select a, int rows) {
+  constexpr int SP = L::SP, LS = L::LS, CC = L::CC, SW = L::SW, P = SP / 2;
   extern __shared__ __align__(16) uint8_t smem[];
   Back<L>* const all = reinterpret_cast<Back<L>*>(smem);
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   Back<L>& m = all[warp];
-  const int side = kBackWarps<L> / rows;                     // warps of a row
+  const int side = back_warps(SW) / rows;                    // warps of a row
   const int row = warp / side;
   const int blocks = (a.tiles + side - 1) / side;             // blocks along a group's channels
   const int g = blockIdx.x / blocks, block = blockIdx.x % blocks;
   const int tile = block * side + warp % side;
 
-  const int q = lane % LS, s0 = q * SP;
+  const int q = lane % LS, s0 = q * SP, order = pair_order<L>(lane);
   const int first = tile * L::CW + lane / LS * CC, own = first + q % CC;
   const bool live = own < a.per, writes = live && q < CC;
   const int64_t d = (int64_t)g * a.per + own;
@@ -96,44 +169,44 @@ __global__ void __launch_bounds__(32 * kBackWarps<L>, 1) k_select_back(Select a,
     there[c] = k < a.per;
   }
   if (a.pieces > 1) after_previous();
-  F2 A2[CC][kP], dA[CC][kP];
-  load_states<SP, CC>(a.A, at_weight, there, s0, a.S, A2);
+  F2 A2[CC][P], dA[CC][P];
+  load_ordered<SP, CC>(a.A, at_weight, there, s0, order, a.S, A2);
 #pragma unroll
   for (int c = 0; c < CC; ++c)
 #pragma unroll
-    for (int i = 0; i < kP; ++i) {
-      A2[c][i] = A2[c][i] * pair(kLog2e, kLog2e);
-      dA[c][i] = pair(0.0f, 0.0f);
-    }
+    for (int i = 0; i < P; ++i) A2[c][i] = A2[c][i] * pair(kLog2e, kLog2e);
+  clear(dA);
   const float bias = live && a.dt_bias ? a.dt_bias[d] : 0.0f, skip = live && a.skip ? a.skip[d] : 0.0f;
   float dskip = 0.0f, dbias = 0.0f;
+  const bool gated = a.gate.data, gate_out = a.dgate.data;
   const int64_t states = a.N * a.D * a.S, items = a.N * a.pieces;
+  int buf = 0;
   // every warp of a block makes the same number of rounds: the block's barriers are in them
   for (int64_t item0 = blockIdx.y * (int64_t)rows; item0 < items; item0 += gridDim.y * (int64_t)rows) {
-    const int64_t item = min(item0 + row, items - 1);
     const bool real = item0 + row < items;
+    const int64_t item = real ? item0 + row : 0;
     const int64_t n = item % a.N;
     const int piece = (int)(item / a.N);
-    const int t0 = piece * a.piece, t1 = min(a.T, t0 + a.piece);
+    const int t0 = piece * a.piece, t1 = real ? min(a.T, t0 + a.piece) : t0;
     const int segments = (min(a.T, a.piece) + kKeep - 1) / kKeep;       // of the longest piece
     int64_t at[CC];
-    bool put[CC];
 #pragma unroll
-    for (int c = 0; c < CC; ++c) {
-      at[c] = n * a.D + at_weight[c];
-      put[c] = there[c] && real;
-    }
-    F2 G[CC][kP];
-    load_states<SP, CC>(a.pieces > 1 ? a.maps + piece * states : a.dhT, at, there, s0, a.S, G);
+    for (int c = 0; c < CC; ++c) at[c] = n * a.D + at_weight[c];
+    F2 G[CC][P];
+    load_ordered<SP, CC>(a.pieces > 1 ? a.maps + piece * states : a.dhT, at, there, s0, order, a.S, G);
 
-    for (int seg = segments - 1; seg >= 0; --seg) {
+    for (int seg = segments - 1; seg >= 0; --seg, buf ^= 1) {
       const int ts = t0 + seg * kKeep, steps = min(kKeep, t1 - ts);
       if (steps > 0) {
-        const uint32_t ends = ends_of(a, ts, n, lane);
+        const uint8_t rend = (a.done || a.done_prev) && lane < steps ? flag_at(a, ts + lane, n) : (uint8_t)0;
+        F2 h[CC][P];
+        load_ordered<SP, CC>(a.kept + ts / kKeep * states, at, there, s0, order, a.S, h);
         stage<T, SW>(a, a.B, ts, steps, n, g, lane, m.B[0]);
         stage<T, SW>(a, a.C, ts, steps, n, g, lane, m.C[0]);
-        F2 h[CC][kP];
-        load_states<SP, CC>(a.kept + ts / kKeep * states, at, there, s0, a.S, h);
+        const T* px = row_at<T>(a.x, ts, n, d);
+        const T* pdt = row_at<T>(a.dt, ts, n, d);
+        const T* pdy = row_at<T>(a.dy, ts, n, d);
+        const T* pgate = gated ? row_at<T>(a.gate, ts, n, d) : px;
 #pragma unroll 1
         for (int k0 = 0; k0 < steps; k0 += 8) {
           T rx[8], rdt[8], rgate[8], rdy[8];
@@ -142,18 +215,19 @@ __global__ void __launch_bounds__(32 * kBackWarps<L>, 1) k_select_back(Select a,
             from_float(0.0f, rx[k]);
             rdt[k] = rgate[k] = rdy[k] = rx[k];
             if (live && k0 + k < steps) {
-              const int t = ts + k0 + k;
-              rx[k] = *row_at<T>(a.x, t, n, d);
-              rdt[k] = *row_at<T>(a.dt, t, n, d);
-              rdy[k] = *row_at<T>(a.dy, t, n, d);
-              if (a.gate.data) rgate[k] = *row_at<T>(a.gate, t, n, d);
+              rx[k] = *px;
+              rdt[k] = *pdt;
+              rdy[k] = *pdy;
+              if (gated) rgate[k] = *pgate;
             }
+            px += a.x.outer, pdt += a.dt.outer, pdy += a.dy.outer;
+            if (gated) pgate += a.gate.outer;
           }
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
             float slope, p = to_float(rdy[k]), qy = 0.0f;
             const float e = softplus(to_float(rdt[k]) + bias, &slope);
-            if (a.gate.data) {
+            if (gated) {
               const float z = to_float(rgate[k]);
               float s, o;
               gates(z, s, o);
@@ -164,13 +238,24 @@ __global__ void __launch_bounds__(32 * kBackWarps<L>, 1) k_select_back(Select a,
             m.slope[k0 + k][lane] = slope;
           }
         }
+        if (ts > t0 && live) {                          // the next segment's rows, on their way to L2
+          const int t = ts - kKeep + lane % kKeep;
+          if (lane < kKeep) {
+            prefetch(row_at<T>(a.x, t, n, d));
+            prefetch(row_at<T>(a.dy, t, n, d));
+          } else {
+            prefetch(row_at<T>(a.dt, t, n, d));
+            if (gated) prefetch(row_at<T>(a.gate, t, n, d));
+          }
+          prefetch(a.kept + (ts / kKeep - 1) * states + at[0] * a.S);
+        }
+        const uint32_t ends = __ballot_sync(0xffffffffu, rend != 0);
         __syncwarp();
         auto channels = [&](int k, float (&e)[CC], float (&u)[CC], float (&p)[CC]) {
-#pragma unroll
-          for (int c = 0; c < CC; ++c) {
-            const float4 w = m.own[k][lane ^ c];
-            e[c] = w.x, u[c] = w.x * w.y, p[c] = w.z;
-          }
+          const float4 w = m.own[k][lane];
+          to_lanes<CC>(w.x, e);
+          to_lanes<CC>(w.x * w.y, u);
+          to_lanes<CC>(w.z, p);
         };
         const int subs = (steps + kSub - 1) / kSub;
 #pragma unroll 1
@@ -178,7 +263,7 @@ __global__ void __launch_bounds__(32 * kBackWarps<L>, 1) k_select_back(Select a,
 #pragma unroll
           for (int c = 0; c < CC; ++c)
 #pragma unroll
-            for (int i = 0; i < kP; i += 2) {
+            for (int i = 0; i < P; i += 2) {
               float4 w;
               split(h[c][i], w.x, w.y);
               split(h[c][i + 1], w.z, w.w);
@@ -188,29 +273,33 @@ __global__ void __launch_bounds__(32 * kBackWarps<L>, 1) k_select_back(Select a,
 #pragma unroll
             for (int k = 0; k < kSub; ++k) {
               const int i0 = sub * kSub + k;
-              float e[CC], u[CC], p[CC];
-              channels(i0, e, u, p);
-              F2 B[kP];
-              load_pairs<SP>(m.B[i0] + s0, B);
-              const bool end = ends >> i0 & 1u;
+              const float4 own4 = m.own[i0][lane];
+              float e[CC], u[CC];
+              to_lanes<CC>(own4.x, e);
+              to_lanes<CC>(own4.x * own4.y, u);
+              F2 B[P];
+              load_pairs(m.B[i0] + s0, order, B);
+              if (ends >> i0 & 1u) clear(h);
 #pragma unroll
               for (int c = 0; c < CC; ++c) {
                 const F2 e2 = pair(e[c], e[c]), u2 = pair(u[c], u[c]);
 #pragma unroll
-                for (int i = 0; i < kP; ++i)
-                  h[c][i] = fma2(ex2(e2 * A2[c][i]), end ? pair(0.0f, 0.0f) : h[c][i], u2 * B[i]);
+                for (int i = 0; i < P; ++i) h[c][i] = fma2(ex2(e2 * A2[c][i]), h[c][i], u2 * B[i]);
               }
             }
           }
         }
+        T* pdx = const_cast<T*>(row_at<T>(a.dx, ts + subs * kSub, n, d));
+        T* pddt = const_cast<T*>(row_at<T>(a.ddt, ts + subs * kSub, n, d));
+        T* pdgate = gate_out ? const_cast<T*>(row_at<T>(a.dgate, ts + subs * kSub, n, d)) : pdx;
 #pragma unroll 1
         for (int sub = subs - 1; sub >= 0; --sub) {
-          F2 decay[kSub][CC][kP], passed[kSub][CC][kP];
+          F2 decay[kSub][CC][P], passed[kSub][CC][P];
           float y[kSub];
 #pragma unroll
           for (int c = 0; c < CC; ++c)
 #pragma unroll
-            for (int i = 0; i < kP; i += 2) {
+            for (int i = 0; i < P; i += 2) {
               const float4 w = m.start[sub][(c * SP + 2 * i) / 4][lane];
               h[c][i] = pair(w.x, w.y);
               h[c][i + 1] = pair(w.z, w.w);
@@ -220,97 +309,93 @@ __global__ void __launch_bounds__(32 * kBackWarps<L>, 1) k_select_back(Select a,
             const int i0 = sub * kSub + k;
             y[k] = 0.0f;
             if (i0 < steps) {
-              float e[CC], u[CC], p[CC], yc[CC], dC[SP];
+              float e[CC], u[CC], p[CC], yc[CC];
               channels(i0, e, u, p);
-              F2 B[kP], C[kP], sC[kP];
-              load_pairs<SP>(m.B[i0] + s0, B);
-              load_pairs<SP>(m.C[i0] + s0, C);
-              const bool end = ends >> i0 & 1u;
+              F2 B[P], C[P], sC[P];
+              load_pairs(m.B[i0] + s0, order, B);
+              load_pairs(m.C[i0] + s0, order, C);
+              if (ends >> i0 & 1u) clear(h);
 #pragma unroll
               for (int c = 0; c < CC; ++c) {
                 const F2 e2 = pair(e[c], e[c]), u2 = pair(u[c], u[c]), p2 = pair(p[c], p[c]);
-                F2 acc = pair(0.0f, 0.0f);
+                F2 acc;
 #pragma unroll
-                for (int i = 0; i < kP; ++i) {
+                for (int i = 0; i < P; ++i) {
                   decay[k][c][i] = ex2(e2 * A2[c][i]);
-                  passed[k][c][i] = end ? pair(0.0f, 0.0f) : decay[k][c][i] * h[c][i];
+                  passed[k][c][i] = decay[k][c][i] * h[c][i];
                   h[c][i] = fma2(u2, B[i], passed[k][c][i]);
-                  acc = fma2(C[i], h[c][i], acc);
+                  acc = i ? fma2(C[i], h[c][i], acc) : C[i] * h[c][i];
                   sC[i] = c ? fma2(p2, h[c][i], sC[i]) : p2 * h[c][i];
                 }
                 yc[c] = total(acc);
               }
               y[k] = over_states<LS, CC>(yc);
-#pragma unroll
-              for (int i = 0; i < kP; ++i) split(sC[i], dC[2 * i], dC[2 * i + 1]);
-              put_sums<SP, LS>(dC, lane, &m.sums[i0][1][s0]);
+              put_sums<L>(sC, lane, order, &m.sums[buf][i0][1][s0]);
             }
           }
 #pragma unroll
           for (int k = kSub - 1; k >= 0; --k) {
             const int i0 = sub * kSub + k;
+            pdx -= a.dx.outer, pddt -= a.ddt.outer;
+            if (gate_out) pdgate -= a.dgate.outer;
             if (i0 < steps) {
-              float e[CC], u[CC], p[CC], by_B[CC], by_A[CC], dB[SP];
+              float e[CC], u[CC], p[CC], by_B[CC], by_A[CC];
               channels(i0, e, u, p);
-              F2 B[kP], C[kP], sB[kP];
-              load_pairs<SP>(m.B[i0] + s0, B);
-              load_pairs<SP>(m.C[i0] + s0, C);
-              const bool end = ends >> i0 & 1u;
+              F2 B[P], C[P], sB[P];
+              load_pairs(m.B[i0] + s0, order, B);
+              load_pairs(m.C[i0] + s0, order, C);
 #pragma unroll
               for (int c = 0; c < CC; ++c) {
                 const F2 e2 = pair(e[c], e[c]), u2 = pair(u[c], u[c]), p2 = pair(p[c], p[c]);
-                F2 accB = pair(0.0f, 0.0f), accA = accB;
+                F2 accB, accA;
 #pragma unroll
-                for (int i = 0; i < kP; ++i) {
+                for (int i = 0; i < P; ++i) {
                   const F2 f = fma2(p2, C[i], G[c][i]), w = f * passed[k][c][i];
-                  accB = fma2(f, B[i], accB);
-                  accA = fma2(w, A2[c][i], accA);
+                  accB = i ? fma2(f, B[i], accB) : f * B[i];
+                  accA = i ? fma2(w, A2[c][i], accA) : w * A2[c][i];
                   sB[i] = c ? fma2(u2, f, sB[i]) : u2 * f;
-                  dA[c][i] = fma2(w, real ? e2 : pair(0.0f, 0.0f), dA[c][i]);
-                  G[c][i] = end ? pair(0.0f, 0.0f) : decay[k][c][i] * f;
+                  dA[c][i] = fma2(w, e2, dA[c][i]);
+                  G[c][i] = decay[k][c][i] * f;
                 }
                 by_B[c] = total(accB);
                 by_A[c] = total(accA);
               }
+              if (ends >> i0 & 1u) clear(G);
               const float sumB = over_states<LS, CC>(by_B), sumA = over_states<LS, CC>(by_A) * kLn2;
-#pragma unroll
-              for (int i = 0; i < kP; ++i) split(sB[i], dB[2 * i], dB[2 * i + 1]);
-              put_sums<SP, LS>(dB, lane, &m.sums[i0][0][s0]);
+              put_sums<L>(sB, lane, order, &m.sums[buf][i0][0][s0]);
               const float4 w = m.own[i0][lane];
               const float du = fmaf(w.y, sumB, sumA) * m.slope[i0][lane];
-              if (writes && real) {
-                const int t = ts + i0;
-                from_float(fmaf(w.x, sumB, skip * w.z), *const_cast<T*>(row_at<T>(a.dx, t, n, d)));
-                from_float(du, *const_cast<T*>(row_at<T>(a.ddt, t, n, d)));
-                if (a.dgate.data) from_float(w.w * fmaf(skip, w.y, y[k]), *const_cast<T*>(row_at<T>(a.dgate, t, n, d)));
-                dskip = fmaf(w.z, w.y, dskip);
-                dbias += du;
+              if (writes) {
+                from_float(fmaf(w.x, sumB, skip * w.z), *pdx);
+                from_float(du, *pddt);
+                if (gate_out) from_float(w.w * fmaf(skip, w.y, y[k]), *pdgate);
               }
+              dskip = fmaf(w.z, w.y, dskip);
+              dbias += du;
             }
           }
         }
       }
       __syncthreads();
-      // dB and dC of the segment over the row's warps, in their order
-      if (steps > 0 && real) {
+      // dB and dC of the segment over the row's warps, in their order; the next barrier is ahead of their next change
+      if (steps > 0) {
         const int threads = 32 * side, me = threadIdx.x % threads;
         const Back<L>* const from = all + row * side;
         const int live_warps = min(side, a.tiles - block * side);
         for (int i = me; i < steps * 2 * a.S; i += threads) {
           const int k = i / (2 * a.S), j = i % (2 * a.S), which = j >= a.S, s = which ? j - a.S : j, t = ts + k;
           float v = 0.0f;
-          for (int w = 0; w < live_warps; ++w) v += from[w].sums[k][which][s];
+          for (int w = 0; w < live_warps; ++w) v += from[w].sums[buf][k][which][s];
           if (blocks > 1) a.parts[((((int64_t)block * a.T + t) * a.N + n) * a.G + g) * 2 * a.S + j] = v;
           else from_float(v, *const_cast<T*>(row_at<T>(which ? a.dC : a.dB, t, n, (int64_t)g * a.S + s)));
         }
       }
-      __syncthreads();
     }
-    if (a.dh0 && piece == 0) store_states<SP, CC>(a.dh0, at, put, s0, a.S, G);
+    if (a.dh0 && piece == 0 && real) store_ordered<SP, CC>(a.dh0, at, there, s0, order, a.S, G);
   }
   if (a.weights) {
     float* const to = a.weights + (blockIdx.y * (int64_t)rows + row) * a.D * (a.S + 2);
-    store_states<SP, CC>(to, at_weight, there, s0, a.S, dA);
+    store_ordered<SP, CC>(to, at_weight, there, s0, order, a.S, dA);
     if (writes) {
       to[a.D * a.S + d] = dskip;
       to[a.D * (a.S + 1) + d] = dbias;
@@ -457,13 +542,13 @@ __global__ void __launch_bounds__(256) k_select_rows(Select a, int64_t blocks) {
 
 // How many partial sums of the weight gradients there are; *blocks: along a group's channels; *rows: of a block.
 int64_t select_slots(const Select& a, int64_t* blocks, int* rows) {
-  const int warps = a.S <= 32 ? 8 : a.S <= 64 ? 4 : 2;
+  const int warps = back_warps(a.S);
   int side = 1;
   while (side < a.tiles && side < warps) side *= 2;
   *rows = warps / side;
   *blocks = (a.tiles + side - 1) / side;
   const int64_t items = (a.N * a.pieces + *rows - 1) / *rows;
-  const int64_t most = std::max<int64_t>(1, (int64_t)sm_count() * (8 / warps) / (*blocks * a.G));
+  const int64_t most = std::max<int64_t>(1, (int64_t)sm_count() / (*blocks * a.G));
   // as many rounds as the fullest slot makes, spread evenly
   const int64_t rounds = (items + most - 1) / most;
   return std::min<int64_t>((items + rounds - 1) / rounds, 65535) * *rows;
@@ -483,12 +568,12 @@ cudaError_t launch_select_back(const Select& a, bool split, cudaStream_t s) {
       if ((e = cudaGetLastError()) != cudaSuccess || (e = launch_select_join(a, true, s)) != cudaSuccess) return e;
     }
     const auto kern = k_select_back<T, L>;
-    const int smem = (int)sizeof(Back<L>) * kBackWarps<L>;
-    static_assert(sizeof(Back<L>) * kBackWarps<L> <= 227 * 1024, "shared memory of a block");
+    const int smem = (int)sizeof(Back<L>) * back_warps(L::SW);
+    static_assert(sizeof(Back<L>) * back_warps(L::SW) <= 227 * 1024, "shared memory of a block");
     if ((e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess) return e;
     const dim3 grid((unsigned)(blocks * a.G), (unsigned)(slots / rows));
-    if (split) return launch_after(kern, grid, 32 * kBackWarps<L>, smem, s, a, rows);
-    kern<<<grid, 32 * kBackWarps<L>, smem, s>>>(a, rows);
+    if (split) return launch_after(kern, grid, 32 * back_warps(L::SW), smem, s, a, rows);
+    kern<<<grid, 32 * back_warps(L::SW), smem, s>>>(a, rows);
     return cudaGetLastError();
   });
   if (e != cudaSuccess) return e;
