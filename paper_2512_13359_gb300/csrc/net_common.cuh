@@ -90,6 +90,22 @@ __device__ __forceinline__ void store(T* p, const float (&x)[E]) {
   *reinterpret_cast<Raw<T, E>*>(p) = pack<T, E>(x);
 }
 
+// One value, where `on`, without a branch.
+template <typename T>
+__device__ __forceinline__ void store_if(bool on, T* p, float v) {
+  if constexpr (sizeof(T) == 4) {
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t@q st.global.b32 [%0], %1;\n\t}" ::"l"(p), "r"(__float_as_uint(v)),
+                 "r"((int)on)
+                 : "memory");
+  } else {
+    T t;
+    from_float(v, t);
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t@q st.global.b16 [%0], %1;\n\t}" ::"l"(p),
+                 "h"(*reinterpret_cast<const uint16_t*>(&t)), "r"((int)on)
+                 : "memory");
+  }
+}
+
 // sigmoid(x) and sigmoid(-x) from q = exp(-|x|), taken as 2^(-|x| log2 e): 1 / (1 + q) and q / (1 + q), neither of them
 // 1 - the other, which has no digits left where the gate is nearly shut.  The product with log2 e is rounded, so q, and
 // with it the smaller gate, is off by up to 2^-24 (|x| + 12) of itself; below 2^-126 it is 0.  The larger is right to a

@@ -142,12 +142,15 @@ __global__ void __launch_bounds__(kForward, 4) k_conv(Conv a, bool act) {
   W next[kBatch];
   uint8_t next_flag[kBatch];
   auto fetch = [&](int t) {
+    if (t + kBatch <= t1) {
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u)
-      if (t + u < t1) {
-        next[u] = *reinterpret_cast<const W*>(x);
-        x += a.x.outer;
-      }
+      for (int u = 0; u < kBatch; ++u) next[u] = *reinterpret_cast<const W*>(x + u * a.x.outer);
+    } else {
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u)
+        if (t + u < t1) next[u] = *reinterpret_cast<const W*>(x + u * a.x.outer);
+    }
+    x += kBatch * a.x.outer;
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) next_flag[u] = flagged && t + u < t1 ? flag_at(a, t + u, n) : (uint8_t)0;
   };
@@ -155,6 +158,7 @@ __global__ void __launch_bounds__(kForward, 4) k_conv(Conv a, bool act) {
   load_taps<E, K>(a, d, w, b);
   load_window<T, E, K>(a, t0, n, d, win);
   if (blockIdx.y == 0 && a.new_state) store_window<T, E, K>(a, n, d);
+#pragma unroll 1
   for (int t = t0; t < t1; t += kBatch) {
     W raw[kBatch];
     uint32_t ends = 0;
@@ -164,31 +168,37 @@ __global__ void __launch_bounds__(kForward, 4) k_conv(Conv a, bool act) {
       ends |= (next_flag[u] ? 1u : 0u) << u;
     }
     fetch(t + kBatch);
+    // PLAIN: a whole batch without an end: no questions
+    auto walk = [&](auto plain) {
+      constexpr bool kPlain = decltype(plain)::value;
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u) {
-      if (t + u >= t1) break;
-      F2 r[P], p[P];
-      to_pairs<T, E>(raw[u], r);
-      if (ends >> u & 1u) {
+      for (int u = 0; u < kBatch; ++u) {
+        if (!kPlain && t + u >= t1) break;
+        F2 r[P], p[P];
+        to_pairs<T, E>(raw[u], r);
+        if (!kPlain && (ends >> u & 1u)) {
 #pragma unroll
-        for (int j = 0; j < K; ++j)
+          for (int j = 0; j < K; ++j)
 #pragma unroll
-          for (int i = 0; i < P; ++i) win[j][i] = zeros();
+            for (int i = 0; i < P; ++i) win[j][i] = zeros();
+        }
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+          p[i] = b[i];
+#pragma unroll
+          for (int j = K - 1; j > 0; --j) p[i] = fma2(w[j][i], win[j - 1][i], p[i]);
+          p[i] = fma2(w[0][i], r[i], p[i]);
+#pragma unroll
+          for (int j = K - 1; j > 0; --j) win[j][i] = win[j - 1][i];
+          win[0][i] = r[i];
+          if (act) p[i] = p[i] * sigmoid2(p[i]);
+        }
+        *reinterpret_cast<W*>(y + u * a.y.outer) = from_pairs<T, E>(p);
       }
-#pragma unroll
-      for (int i = 0; i < P; ++i) {
-        p[i] = b[i];
-#pragma unroll
-        for (int j = K - 1; j > 0; --j) p[i] = fma2(w[j][i], win[j - 1][i], p[i]);
-        p[i] = fma2(w[0][i], r[i], p[i]);
-#pragma unroll
-        for (int j = K - 1; j > 0; --j) win[j][i] = win[j - 1][i];
-        win[0][i] = r[i];
-        if (act) p[i] = p[i] * sigmoid2(p[i]);
-      }
-      *reinterpret_cast<W*>(y) = from_pairs<T, E>(p);
-      y += a.y.outer;
-    }
+    };
+    if (t + kBatch <= t1 && !ends) walk(std::true_type());
+    else walk(std::false_type());
+    y += kBatch * a.y.outer;
   }
 }
 

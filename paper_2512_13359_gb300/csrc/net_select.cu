@@ -64,28 +64,34 @@ __global__ void __launch_bounds__(32 * kWarps, L::SP == 8 ? 4 : 6) k_select(Sele
   T rx[kBatch], rdt[kBatch], rgate[kBatch];
   In rB, rC;
   uint8_t rend = 0;
+  const bool all_live = __all_sync(0xffffffffu, live);
   auto fetch = [&](int t) {
     const int steps = t1 - t;
     if (steps <= 0) return;
     rend = flagged && lane < min(kBatch, steps) ? flag_at(a, t + lane, n) : (uint8_t)0;
     rB.load(pB, a.B.outer, steps, a.S, lane);
-    pB += kBatch * a.B.outer;
-    if constexpr (!FOLD) {
-      rC.load(pC, a.C.outer, steps, a.S, lane);
-      pC += kBatch * a.C.outer;
-    }
+    if constexpr (!FOLD) rC.load(pC, a.C.outer, steps, a.S, lane);
+    if (all_live && steps >= kBatch) {
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-      from_float(0.0f, rx[k]);
-      rdt[k] = rgate[k] = rx[k];
-      if (live && k < steps) {
-        rx[k] = *px;
-        rdt[k] = *pdt;
-        if (gated) rgate[k] = *pgate;
+      for (int k = 0; k < kBatch; ++k) rx[k] = px[k * a.x.outer], rdt[k] = pdt[k * a.dt.outer];
+      if (gated) {
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) rgate[k] = pgate[k * a.gate.outer];
       }
-      px += a.x.outer, pdt += a.dt.outer;
-      if (gated) pgate += a.gate.outer;
+    } else {
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        from_float(0.0f, rx[k]);
+        rdt[k] = rgate[k] = rx[k];
+        if (live && k < steps) {
+          rx[k] = px[k * a.x.outer], rdt[k] = pdt[k * a.dt.outer];
+          if (gated) rgate[k] = pgate[k * a.gate.outer];
+        }
+      }
     }
+    px += kBatch * a.x.outer, pdt += kBatch * a.dt.outer, pB += kBatch * a.B.outer;
+    if (gated) pgate += kBatch * a.gate.outer;
+    if constexpr (!FOLD) pC += kBatch * a.C.outer;
   };
   fetch(t0);
 
@@ -119,13 +125,16 @@ __global__ void __launch_bounds__(32 * kWarps, L::SP == 8 ? 4 : 6) k_select(Sele
     rB.put(Bs, lane);
     if constexpr (!FOLD) rC.put(Cs, lane);
     const uint32_t ends = flagged ? __ballot_sync(0xffffffffu, rend != 0) : 0u;
-    float x[kBatch], e[kBatch];
-    [[maybe_unused]] float z[kBatch];
+    float x[kBatch], e[kBatch], z[kBatch];
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
       x[k] = to_float(rx[k]);
-      e[k] = live ? softplus(to_float(rdt[k]) + bias) : 0.0f;
-      if (gated) {
+      e[k] = softplus(to_float(rdt[k]) + bias);
+      z[k] = 1.0f;
+    }
+    if (gated) {
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
         const float v = to_float(rgate[k]);
         float s, o;
         gates(v, s, o);
@@ -136,43 +145,44 @@ __global__ void __launch_bounds__(32 * kWarps, L::SP == 8 ? 4 : 6) k_select(Sele
     if constexpr (!FOLD)
       if (a.kept && ts % kKeep == 0) store_states<SP, CC>(a.kept + ts / kKeep * states, at, there, s0, a.S, h);
     __syncwarp();
+    // PLAIN: four steps there are, and no end among them; straight through, which took 1.3 times as long with the questions
+    auto walk = [&](auto plain) {
+      constexpr bool kPlain = decltype(plain)::value;
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-      if (k >= steps) break;
-      float es[CC], us[CC];
-      to_lanes<CC>(e[k], es);
-      to_lanes<CC>(e[k] * x[k], us);
-      F2 B[SP / 2], C[SP / 2];
-      load_pairs<SP>(Bs + k * SW + s0, B);
-      if constexpr (!FOLD) load_pairs<SP>(Cs + k * SW + s0, C);
-      if (ends >> k & 1u) {
+      for (int k = 0; k < kBatch; ++k) {
+        if (!kPlain && k >= steps) break;
+        float es[CC], us[CC];
+        to_lanes<CC>(e[k], es);
+        to_lanes<CC>(e[k] * x[k], us);
+        F2 B[SP / 2], C[SP / 2];
+        load_pairs<SP>(Bs + k * SW + s0, B);
+        if constexpr (!FOLD) load_pairs<SP>(Cs + k * SW + s0, C);
+        if (!kPlain && (ends >> k & 1u)) {
 #pragma unroll
-        for (int c = 0; c < CC; ++c)
+          for (int c = 0; c < CC; ++c)
 #pragma unroll
-          for (int i = 0; i < SP / 2; ++i) h[c][i] = pair(0.0f, 0.0f);
-        cut = true;
-      }
-      float y[CC];
-#pragma unroll
-      for (int c = 0; c < CC; ++c) {
-        const F2 e2 = pair(es[c], es[c]), u2 = pair(us[c], us[c]);
-        F2 acc = pair(0.0f, 0.0f);
-#pragma unroll
-        for (int i = 0; i < SP / 2; ++i) {
-          h[c][i] = fma2(ex2(e2 * A2[c][i]), h[c][i], u2 * B[i]);
-          if constexpr (!FOLD) acc = i ? fma2(C[i], h[c][i], acc) : C[i] * h[c][i];
+            for (int i = 0; i < SP / 2; ++i) h[c][i] = pair(0.0f, 0.0f);
+          cut = true;
         }
-        y[c] = total(acc);
+        float y[CC];
+#pragma unroll
+        for (int c = 0; c < CC; ++c) {
+          const F2 e2 = pair(es[c], es[c]), u2 = pair(us[c], us[c]);
+          F2 acc = pair(0.0f, 0.0f);
+#pragma unroll
+          for (int i = 0; i < SP / 2; ++i) {
+            h[c][i] = fma2(ex2(e2 * A2[c][i]), h[c][i], u2 * B[i]);
+            if constexpr (!FOLD) acc = i ? fma2(C[i], h[c][i], acc) : C[i] * h[c][i];
+          }
+          y[c] = total(acc);
+        }
+        if constexpr (FOLD) sum += e[k];
+        else store_if(writes, py + k * a.y.outer, fmaf(skip, x[k], over_states<LS, CC>(y)) * z[k]);
       }
-      if constexpr (FOLD) {
-        sum += e[k];
-      } else {
-        float p = fmaf(skip, x[k], over_states<LS, CC>(y));
-        if (gated) p *= z[k];
-        if (writes) from_float(p, *py);
-        py += a.y.outer;
-      }
-    }
+    };
+    if (steps >= kBatch && !ends) walk(std::true_type());
+    else walk(std::false_type());
+    py += kBatch * a.y.outer;
   }
   if constexpr (FOLD) {
     store_states<SP, CC>(a.maps + piece * states, at, there, s0, a.S, h);
