@@ -211,7 +211,7 @@ constexpr int kBackward = 128;
 constexpr int kBack = 4, kRing = 4;                   // steps of a batch, batches in shared memory
 
 template <typename T, int E, int K>
-__global__ void __launch_bounds__(kBackward) k_conv_back(Conv a, bool act, int side) {
+__global__ void __launch_bounds__(kBackward, K <= 4 ? 4 : 2) k_conv_back(Conv a, bool act, int side) {
   constexpr int P = (E + 1) / 2;
   using W = Raw<T, E>;
   constexpr bool kCopied = kAsync<T, E>;

@@ -223,6 +223,112 @@ __global__ void __launch_bounds__(kJoin) k_select_join(Select a, bool back) {
   }
 }
 
+// One step, as in a rollout: the states are read, changed and written, so few registers and no staging; a warp takes its
+// channels of one env after the other, A in registers.  wide: B's and C's values of a lane are aligned vectors.
+template <typename T, int SP>
+__device__ __forceinline__ void load_row(const T* p, bool wide, int s0, int S, F2 (&v)[SP / 2]) {
+  float x[SP];
+  if (wide) {
+    constexpr int E = SP * sizeof(T) > 16 ? 16 / sizeof(T) : SP;
+#pragma unroll
+    for (int i = 0; i < SP; i += E) {
+      float y[E];
+      load<T, E>(p + i, y);
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[i + e] = y[e];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < SP; ++i) x[i] = s0 + i < S ? to_float(p[i]) : 0.0f;
+  }
+#pragma unroll
+  for (int i = 0; i < SP / 2; ++i) v[i] = pair(x[2 * i], x[2 * i + 1]);
+}
+
+constexpr int kOneWarps = 8;
+template <typename T, typename L>
+__global__ void __launch_bounds__(32 * kOneWarps, 3) k_select_one(Select a, bool wide) {
+  constexpr int SP = L::SP, LS = L::LS, CC = L::CC, P = SP / 2;
+  const int lane = threadIdx.x % 32;
+  const int64_t id = blockIdx.x * (int64_t)kOneWarps + threadIdx.x / 32, side = (int64_t)a.G * a.tiles;
+  const int64_t envs = gridDim.x * (int64_t)kOneWarps / side;           // walked side by side
+  int64_t n = id / side;
+  if (n >= min(envs, a.N)) return;
+  const int g = (int)(id % side / a.tiles), tile = (int)(id % a.tiles);
+  const int q = lane % LS, s0 = q * SP;
+  const int first = tile * L::CW + lane / LS * CC, own = first + q % CC;
+  const bool live = own < a.per, writes = live && q < CC;
+  const int64_t d = (int64_t)g * a.per + own;
+  int64_t at_weight[CC];
+  bool there[CC];
+#pragma unroll
+  for (int c = 0; c < CC; ++c) {
+    const int k = first + (q % CC ^ c);
+    at_weight[c] = (int64_t)g * a.per + k;
+    there[c] = k < a.per;
+  }
+  F2 A2[CC][P];
+  load_states<SP, CC>(a.A, at_weight, there, s0, a.S, A2);
+  const float bias = live && a.dt_bias ? a.dt_bias[d] : 0.0f, skip = live && a.skip ? a.skip[d] : 0.0f;
+#pragma unroll
+  for (int c = 0; c < CC; ++c)
+#pragma unroll
+    for (int i = 0; i < P; ++i) A2[c][i] = A2[c][i] * pair(kLog2e, kLog2e);
+  for (; n < a.N; n += envs) {
+    int64_t at[CC];
+    bool from[CC];
+    const uint8_t end = a.done_prev ? a.done_prev[n] : (uint8_t)0;
+#pragma unroll
+    for (int c = 0; c < CC; ++c) {
+      at[c] = n * a.D + at_weight[c];
+      from[c] = there[c];
+    }
+    F2 h[CC][P], B[P], C[P];
+    load_states<SP, CC>(a.h0, at, from, s0, a.S, h);
+    T rx, rdt, rgate;
+    from_float(0.0f, rx);
+    rdt = rgate = rx;
+    if (live) {
+      rx = *row_at<T>(a.x, 0, n, d);
+      rdt = *row_at<T>(a.dt, 0, n, d);
+      if (a.gate.data) rgate = *row_at<T>(a.gate, 0, n, d);
+    }
+    load_row<T, SP>(row_at<T>(a.B, 0, n, (int64_t)g * a.S + s0), wide, s0, a.S, B);
+    load_row<T, SP>(row_at<T>(a.C, 0, n, (int64_t)g * a.S + s0), wide, s0, a.S, C);
+    if (a.kept) store_states<SP, CC>(a.kept, at, there, s0, a.S, h);
+    const float x = to_float(rx), e = live ? softplus(to_float(rdt) + bias) : 0.0f;
+    float es[CC], us[CC], y[CC];
+    to_lanes<CC>(e, es);
+    to_lanes<CC>(e * x, us);
+    if (end) {
+#pragma unroll
+      for (int c = 0; c < CC; ++c)
+#pragma unroll
+        for (int i = 0; i < P; ++i) h[c][i] = pair(0.0f, 0.0f);
+    }
+#pragma unroll
+    for (int c = 0; c < CC; ++c) {
+      const F2 e2 = pair(es[c], es[c]), u2 = pair(us[c], us[c]);
+      F2 acc;
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        h[c][i] = fma2(ex2(e2 * A2[c][i]), h[c][i], u2 * B[i]);
+        acc = i ? fma2(C[i], h[c][i], acc) : C[i] * h[c][i];
+      }
+      y[c] = total(acc);
+    }
+    if (a.hT) store_states<SP, CC>(a.hT, at, there, s0, a.S, h);
+    float p = fmaf(skip, x, over_states<LS, CC>(y));
+    if (a.gate.data) {
+      const float z = to_float(rgate);
+      float s, o;
+      gates(z, s, o);
+      p *= z * s;
+    }
+    store_if(writes, const_cast<T*>(row_at<T>(a.y, 0, n, d)), p);
+  }
+}
+
 // T = 0: the states pass as they are.
 __global__ void k_select_none(int64_t m, const float* from, float* to) {
   const int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x;
@@ -242,6 +348,19 @@ template <typename T>
 cudaError_t launch(const Select& a, cudaStream_t s) {
   return with_lanes(a.S, [&](auto l) {
     using L = decltype(l);
+    if (a.T == 1) {
+      const int z = sizeof(T);
+      const int64_t side = (int64_t)a.G * a.tiles;
+      const net_rows* rows[] = {&a.B, &a.C};
+      bool wide = a.S % L::SP == 0;
+      for (const net_rows* r : rows) wide = wide && aligned(*r, 1, a.N, z, std::min(L::SP, 16 / z));
+      // a warp takes two to four envs where there are enough: fewer leave A's load unused, more leave warps out
+      const int64_t blocks = (side * a.N + kOneWarps - 1) / kOneWarps, few = (int64_t)sm_count() * 3;
+      const int64_t turns = std::max<int64_t>(1, std::min<int64_t>(4, blocks / (4 * few)));
+      const int64_t envs = (a.N + turns - 1) / turns;
+      k_select_one<T, L><<<(unsigned)((envs * side + kOneWarps - 1) / kOneWarps), 32 * kOneWarps, 0, s>>>(a, wide);
+      return cudaGetLastError();
+    }
     if (a.pieces > 1) {
       cudaError_t e = launch_walk<T, L, true>(a, s);
       if (e == cudaSuccess) e = launch_select_join(a, false, s);

@@ -96,53 +96,62 @@ __device__ __forceinline__ uint32_t ends_of(const Select& a, int t, int64_t n, i
   return __ballot_sync(0xffffffffu, lane < kKeep && t + lane < a.T && ended(a, t + lane, n));
 }
 
-// SP states of CC channels from s0 of an [.][S] array: pairs, zeros past S and for channels that are not there.
+// SP states of CC channels from s0 of an [.][S] array: pairs, zeros past S and for channels that are not there.  Whole
+// sectors of 32 bytes a thread where S and the array allow them.
+template <int SP>
+__device__ __forceinline__ bool whole_sectors(const float* p, int S) {
+  return S % SP == 0 && reinterpret_cast<uintptr_t>(p) % (4 * SP) == 0;
+}
 template <int SP, int CC>
 __device__ __forceinline__ void load_states(const float* p, const int64_t (&at)[CC], const bool (&there)[CC], int s0, int S,
                                             F2 (&h)[CC][SP / 2]) {
-  const bool vec = S % 4 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0;
+  const bool vec = whole_sectors<SP>(p, S);
 #pragma unroll
   for (int c = 0; c < CC; ++c) {
     const float* q = p + at[c] * S + s0;
 #pragma unroll
-    for (int i = 0; i < SP; i += 4) {
-      float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-      if (p && there[c]) {
-        if (vec) {
-          if (s0 + i < S) {
-            const float4 w = *reinterpret_cast<const float4*>(q + i);
-            v[0] = w.x, v[1] = w.y, v[2] = w.z, v[3] = w.w;
-          }
-        } else {
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (s0 + i + k < S) v[k] = q[i + k];
-        }
+    for (int i = 0; i < SP / 2; ++i) h[c][i] = pair(0.0f, 0.0f);
+    if (!p || !there[c] || s0 >= S) continue;
+    if (vec) {
+      if constexpr (SP == 8) {
+        asm volatile("ld.global.v4.b64 {%0, %1, %2, %3}, [%4];"
+                     : "=l"(h[c][0].v), "=l"(h[c][1].v), "=l"(h[c][2].v), "=l"(h[c][3].v)
+                     : "l"(q)
+                     : "memory");
+      } else {
+        const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(q);
+        h[c][0].v = w.x, h[c][1].v = w.y;
       }
-      h[c][i / 2] = pair(v[0], v[1]);
-      h[c][i / 2 + 1] = pair(v[2], v[3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < SP / 2; ++i)
+        h[c][i] = pair(s0 + 2 * i < S ? q[2 * i] : 0.0f, s0 + 2 * i + 1 < S ? q[2 * i + 1] : 0.0f);
     }
   }
 }
 template <int SP, int CC>
 __device__ __forceinline__ void store_states(float* p, const int64_t (&at)[CC], const bool (&there)[CC], int s0, int S,
                                              const F2 (&h)[CC][SP / 2]) {
-  const bool vec = S % 4 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0;
+  const bool vec = whole_sectors<SP>(p, S);
 #pragma unroll
   for (int c = 0; c < CC; ++c) {
-    if (!there[c]) continue;
     float* q = p + at[c] * S + s0;
-#pragma unroll
-    for (int i = 0; i < SP; i += 4) {
-      float v[4];
-      split(h[c][i / 2], v[0], v[1]);
-      split(h[c][i / 2 + 1], v[2], v[3]);
-      if (vec) {
-        if (s0 + i < S) *reinterpret_cast<float4*>(q + i) = make_float4(v[0], v[1], v[2], v[3]);
+    if (!there[c] || s0 >= S) continue;
+    if (vec) {
+      if constexpr (SP == 8) {
+        asm volatile("st.global.v4.b64 [%0], {%1, %2, %3, %4};" ::"l"(q), "l"(h[c][0].v), "l"(h[c][1].v), "l"(h[c][2].v),
+                     "l"(h[c][3].v)
+                     : "memory");
       } else {
+        *reinterpret_cast<ulonglong2*>(q) = make_ulonglong2(h[c][0].v, h[c][1].v);
+      }
+    } else {
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (s0 + i + k < S) q[i + k] = v[k];
+      for (int i = 0; i < SP / 2; ++i) {
+        float lo, hi;
+        split(h[c][i], lo, hi);
+        if (s0 + 2 * i < S) q[2 * i] = lo;
+        if (s0 + 2 * i + 1 < S) q[2 * i + 1] = hi;
       }
     }
   }
