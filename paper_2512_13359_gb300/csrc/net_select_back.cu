@@ -16,18 +16,21 @@ namespace auv {
 namespace net {
 namespace {
 
-constexpr int kSub = 4;         // steps held in registers
+// Steps whose a and a c are held in registers (four: 176 registers of them, and spills), and from one kept start to the next.
+constexpr int kHeld = 2, kSub = 4;
 
 // Warps of a block: shared memory grows with the padded states.
 constexpr int back_warps(int padded) { return padded <= 16 ? 8 : padded <= 64 ? 4 : 2; }
 
-// A warp's shared memory.
+// A warp's shared memory.  What multiplies pairs of states is there twice: copies in registers took a twelfth of all
+// instructions.
 template <typename L> struct Back {
   float B[kKeep][L::SW], C[kKeep][L::SW];
-  float4 own[kKeep][32];                        // e, x, p, dy silu'(gate) of the lane's own channel
+  float4 eu[kKeep][32];                         // e, e, e x, e x of the lane's own channel
+  float2 pp[kKeep][32], xq[kKeep][32];          // p, p; x, dy silu'(gate)
   float slope[kKeep][32];                       // sigmoid(dt + dt_bias)
-  float4 start[kKeep / kSub][L::CC * L::SP / 4][32];   // the lane's states before steps 0, 4, 8, 12
-  float sums[2][kKeep][2][L::SW];               // dB and dC over the warp's channels; of this segment and the last
+  float4 start[kKeep / kSub - 1][L::CC * L::SP / 4][32];   // the lane's states before steps 4, 8, 12
+  float sums[kKeep][2][L::SW];                  // dB and dC over the warp's channels
 };
 
 // The order of a lane's pairs of states.  Sums over channels go over the lanes with the same q; at each level a lane keeps
@@ -140,6 +143,20 @@ __device__ __forceinline__ void clear(F2 (&h)[CC][P]) {
 #pragma unroll
     for (int i = 0; i < P; ++i) h[c][i] = pair(0.0f, 0.0f);
 }
+// One value, where `on`, without a branch.
+template <typename T>
+__device__ __forceinline__ void store_if(bool on, T* p, float v) {
+  T t;
+  from_float(v, t);
+  if constexpr (sizeof(T) == 4)
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t@q st.global.b32 [%0], %1;\n\t}" ::"l"(p), "r"(__float_as_uint(v)),
+                 "r"((int)on)
+                 : "memory");
+  else
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t@q st.global.b16 [%0], %1;\n\t}" ::"l"(p),
+                 "h"(*reinterpret_cast<const uint16_t*>(&t)), "r"((int)on)
+                 : "memory");
+}
 __device__ __forceinline__ void prefetch(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
 // rows: (env, group) pairs a block walks side by side, back_warps / rows warps each.
@@ -180,7 +197,6 @@ __global__ void __launch_bounds__(32 * back_warps(L::SW), 1) k_select_back(Selec
   float dskip = 0.0f, dbias = 0.0f;
   const bool gated = a.gate.data, gate_out = a.dgate.data;
   const int64_t states = a.N * a.D * a.S, items = a.N * a.pieces;
-  int buf = 0;
   // every warp of a block makes the same number of rounds: the block's barriers are in them
   for (int64_t item0 = blockIdx.y * (int64_t)rows; item0 < items; item0 += gridDim.y * (int64_t)rows) {
     const bool real = item0 + row < items;
@@ -195,7 +211,7 @@ __global__ void __launch_bounds__(32 * back_warps(L::SW), 1) k_select_back(Selec
     F2 G[CC][P];
     load_ordered<SP, CC>(a.pieces > 1 ? a.maps + piece * states : a.dhT, at, there, s0, order, a.S, G);
 
-    for (int seg = segments - 1; seg >= 0; --seg, buf ^= 1) {
+    for (int seg = segments - 1; seg >= 0; --seg) {
       const int ts = t0 + seg * kKeep, steps = min(kKeep, t1 - ts);
       if (steps > 0) {
         const uint8_t rend = (a.done || a.done_prev) && lane < steps ? flag_at(a, ts + lane, n) : (uint8_t)0;
@@ -234,7 +250,10 @@ __global__ void __launch_bounds__(32 * back_warps(L::SW), 1) k_select_back(Selec
               qy = p * (s * fmaf(z, o, 1.0f));
               p *= z * s;
             }
-            m.own[k0 + k][lane] = make_float4(live ? e : 0.0f, to_float(rx[k]), p, qy);
+            const float x = to_float(rx[k]), u = e * x;
+            m.eu[k0 + k][lane] = live ? make_float4(e, e, u, u) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            m.pp[k0 + k][lane] = make_float2(p, p);
+            m.xq[k0 + k][lane] = make_float2(x, qy);
             m.slope[k0 + k][lane] = slope;
           }
         }
@@ -251,15 +270,123 @@ __global__ void __launch_bounds__(32 * back_warps(L::SW), 1) k_select_back(Selec
         }
         const uint32_t ends = __ballot_sync(0xffffffffu, rend != 0);
         __syncwarp();
-        auto channels = [&](int k, float (&e)[CC], float (&u)[CC], float (&p)[CC]) {
-          const float4 w = m.own[k][lane];
-          to_lanes<CC>(w.x, e);
-          to_lanes<CC>(w.x * w.y, u);
-          to_lanes<CC>(w.z, p);
+        // e, e x and p of step k, for both states of a pair
+        auto inputs = [&](int k, F2 (&e)[CC], F2 (&u)[CC]) {
+#pragma unroll
+          for (int c = 0; c < CC; ++c) {
+            const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(&m.eu[k][lane ^ c]);
+            e[c].v = w.x, u[c].v = w.y;
+          }
+        };
+        auto weights = [&](int k, F2 (&p)[CC]) {
+#pragma unroll
+          for (int c = 0; c < CC; ++c) p[c].v = *reinterpret_cast<const uint64_t*>(&m.pp[k][lane ^ c]);
         };
         const int subs = (steps + kSub - 1) / kSub;
+        // COUNT steps forward: the states behind them.  plain: no end is among them (and, below, all of them are there).
+        auto ahead = [&](auto plain, auto count, int first_step) {
+          constexpr bool kPlain = decltype(plain)::value;
+#pragma unroll
+          for (int k = 0; k < decltype(count)::value; ++k) {
+            const int i0 = first_step + k;
+            F2 e[CC], u[CC], B[P];
+            inputs(i0, e, u);
+            load_pairs(m.B[i0] + s0, order, B);
+            if (!kPlain && (ends >> i0 & 1u)) clear(h);
+#pragma unroll
+            for (int c = 0; c < CC; ++c)
+#pragma unroll
+              for (int i = 0; i < P; ++i) h[c][i] = fma2(ex2(e[c] * A2[c][i]), h[c][i], u[c] * B[i]);
+          }
+        };
+        T* pdx = const_cast<T*>(row_at<T>(a.dx, ts + subs * kSub, n, d));
+        T* pddt = const_cast<T*>(row_at<T>(a.ddt, ts + subs * kSub, n, d));
+        T* pdgate = gate_out ? const_cast<T*>(row_at<T>(a.dgate, ts + subs * kSub, n, d)) : pdx;
+        // kHeld steps forward from the states h, and back.
+        auto through = [&](auto plain, int first_step) {
+          constexpr bool kPlain = decltype(plain)::value;
+          F2 decay[kHeld][CC][P], passed[kHeld][CC][P];
+          float y[kHeld];
+#pragma unroll
+          for (int k = 0; k < kHeld; ++k) {
+            const int i0 = first_step + k;
+            y[k] = 0.0f;
+            if (kPlain || i0 < steps) {
+              float yc[CC];
+              F2 e[CC], u[CC], p[CC], B[P], C[P], sC[P];
+              inputs(i0, e, u);
+              weights(i0, p);
+              load_pairs(m.B[i0] + s0, order, B);
+              load_pairs(m.C[i0] + s0, order, C);
+              if (!kPlain && (ends >> i0 & 1u)) clear(h);
+#pragma unroll
+              for (int c = 0; c < CC; ++c) {
+                F2 acc;
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                  decay[k][c][i] = ex2(e[c] * A2[c][i]);
+                  passed[k][c][i] = decay[k][c][i] * h[c][i];
+                  h[c][i] = fma2(u[c], B[i], passed[k][c][i]);
+                  acc = i ? fma2(C[i], h[c][i], acc) : C[i] * h[c][i];
+                  sC[i] = c ? fma2(p[c], h[c][i], sC[i]) : p[c] * h[c][i];
+                }
+                yc[c] = total(acc);
+              }
+              y[k] = over_states<LS, CC>(yc);
+              put_sums<L>(sC, lane, order, &m.sums[i0][1][s0]);
+            }
+          }
+#pragma unroll
+          for (int k = kHeld - 1; k >= 0; --k) {
+            const int i0 = first_step + k;
+            pdx -= a.dx.outer, pddt -= a.ddt.outer;
+            if (gate_out) pdgate -= a.dgate.outer;
+            if (kPlain || i0 < steps) {
+              float by_B[CC], by_A[CC];
+              F2 e[CC], u[CC], p[CC], B[P], C[P], sB[P];
+              inputs(i0, e, u);
+              weights(i0, p);
+              load_pairs(m.B[i0] + s0, order, B);
+              load_pairs(m.C[i0] + s0, order, C);
+#pragma unroll
+              for (int c = 0; c < CC; ++c) {
+                F2 accB, accA;
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                  const F2 f = fma2(p[c], C[i], G[c][i]), w = f * passed[k][c][i];
+                  accB = i ? fma2(f, B[i], accB) : f * B[i];
+                  accA = i ? fma2(w, A2[c][i], accA) : w * A2[c][i];
+                  sB[i] = c ? fma2(u[c], f, sB[i]) : u[c] * f;
+                  dA[c][i] = fma2(w, e[c], dA[c][i]);
+                  G[c][i] = decay[k][c][i] * f;
+                }
+                by_B[c] = total(accB);
+                by_A[c] = total(accA);
+              }
+              if (!kPlain && (ends >> i0 & 1u)) clear(G);
+              const float sumB = over_states<LS, CC>(by_B), sumA = over_states<LS, CC>(by_A) * kLn2;
+              put_sums<L>(sB, lane, order, &m.sums[i0][0][s0]);
+              float e1, p1, copy;
+              split(e[0], e1, copy);
+              split(p[0], p1, copy);
+              const float2 w = m.xq[i0][lane];
+              const float du = fmaf(w.x, sumB, sumA) * m.slope[i0][lane];
+              store_if(writes, pdx, fmaf(e1, sumB, skip * p1));
+              store_if(writes, pddt, du);
+              if (gate_out) store_if(writes, pdgate, w.y * fmaf(skip, w.x, y[k]));
+              dskip = fmaf(p1, w.x, dskip);
+              dbias += du;
+            }
+          }
+        };
+        const auto plain = std::true_type();
+        const auto any = std::false_type();
+        const auto two = std::integral_constant<int, kHeld>();
+        const auto four = std::integral_constant<int, kSub>();
 #pragma unroll 1
-        for (int sub = 0; sub < subs; ++sub) {            // the states before every 4th step
+        for (int sub = 0; sub + 1 < subs; ++sub) {        // the states before every 4th step but the first
+          if (ends >> (sub * kSub) & 15u) ahead(any, four, sub * kSub);
+          else ahead(plain, four, sub * kSub);
 #pragma unroll
           for (int c = 0; c < CC; ++c)
 #pragma unroll
@@ -269,115 +396,33 @@ __global__ void __launch_bounds__(32 * back_warps(L::SW), 1) k_select_back(Selec
               split(h[c][i + 1], w.z, w.w);
               m.start[sub][(c * SP + 2 * i) / 4][lane] = w;
             }
-          if (sub + 1 < subs) {
-#pragma unroll
-            for (int k = 0; k < kSub; ++k) {
-              const int i0 = sub * kSub + k;
-              const float4 own4 = m.own[i0][lane];
-              float e[CC], u[CC];
-              to_lanes<CC>(own4.x, e);
-              to_lanes<CC>(own4.x * own4.y, u);
-              F2 B[P];
-              load_pairs(m.B[i0] + s0, order, B);
-              if (ends >> i0 & 1u) clear(h);
-#pragma unroll
-              for (int c = 0; c < CC; ++c) {
-                const F2 e2 = pair(e[c], e[c]), u2 = pair(u[c], u[c]);
-#pragma unroll
-                for (int i = 0; i < P; ++i) h[c][i] = fma2(ex2(e2 * A2[c][i]), h[c][i], u2 * B[i]);
-              }
-            }
-          }
         }
-        T* pdx = const_cast<T*>(row_at<T>(a.dx, ts + subs * kSub, n, d));
-        T* pddt = const_cast<T*>(row_at<T>(a.ddt, ts + subs * kSub, n, d));
-        T* pdgate = gate_out ? const_cast<T*>(row_at<T>(a.dgate, ts + subs * kSub, n, d)) : pdx;
 #pragma unroll 1
-        for (int sub = subs - 1; sub >= 0; --sub) {
-          F2 decay[kSub][CC][P], passed[kSub][CC][P];
-          float y[kSub];
+        for (int half = subs * 2 - 1; half >= 0; --half) {
+          const int sub = half / 2, at0 = half * kHeld;
+          if (sub) {
 #pragma unroll
-          for (int c = 0; c < CC; ++c)
+            for (int c = 0; c < CC; ++c)
 #pragma unroll
-            for (int i = 0; i < P; i += 2) {
-              const float4 w = m.start[sub][(c * SP + 2 * i) / 4][lane];
-              h[c][i] = pair(w.x, w.y);
-              h[c][i + 1] = pair(w.z, w.w);
-            }
-#pragma unroll
-          for (int k = 0; k < kSub; ++k) {
-            const int i0 = sub * kSub + k;
-            y[k] = 0.0f;
-            if (i0 < steps) {
-              float e[CC], u[CC], p[CC], yc[CC];
-              channels(i0, e, u, p);
-              F2 B[P], C[P], sC[P];
-              load_pairs(m.B[i0] + s0, order, B);
-              load_pairs(m.C[i0] + s0, order, C);
-              if (ends >> i0 & 1u) clear(h);
-#pragma unroll
-              for (int c = 0; c < CC; ++c) {
-                const F2 e2 = pair(e[c], e[c]), u2 = pair(u[c], u[c]), p2 = pair(p[c], p[c]);
-                F2 acc;
-#pragma unroll
-                for (int i = 0; i < P; ++i) {
-                  decay[k][c][i] = ex2(e2 * A2[c][i]);
-                  passed[k][c][i] = decay[k][c][i] * h[c][i];
-                  h[c][i] = fma2(u2, B[i], passed[k][c][i]);
-                  acc = i ? fma2(C[i], h[c][i], acc) : C[i] * h[c][i];
-                  sC[i] = c ? fma2(p2, h[c][i], sC[i]) : p2 * h[c][i];
-                }
-                yc[c] = total(acc);
+              for (int i = 0; i < P; i += 2) {
+                const float4 w = m.start[sub - 1][(c * SP + 2 * i) / 4][lane];
+                h[c][i] = pair(w.x, w.y);
+                h[c][i + 1] = pair(w.z, w.w);
               }
-              y[k] = over_states<LS, CC>(yc);
-              put_sums<L>(sC, lane, order, &m.sums[buf][i0][1][s0]);
-            }
+          } else {
+            load_ordered<SP, CC>(a.kept + ts / kKeep * states, at, there, s0, order, a.S, h);
           }
-#pragma unroll
-          for (int k = kSub - 1; k >= 0; --k) {
-            const int i0 = sub * kSub + k;
-            pdx -= a.dx.outer, pddt -= a.ddt.outer;
-            if (gate_out) pdgate -= a.dgate.outer;
-            if (i0 < steps) {
-              float e[CC], u[CC], p[CC], by_B[CC], by_A[CC];
-              channels(i0, e, u, p);
-              F2 B[P], C[P], sB[P];
-              load_pairs(m.B[i0] + s0, order, B);
-              load_pairs(m.C[i0] + s0, order, C);
-#pragma unroll
-              for (int c = 0; c < CC; ++c) {
-                const F2 e2 = pair(e[c], e[c]), u2 = pair(u[c], u[c]), p2 = pair(p[c], p[c]);
-                F2 accB, accA;
-#pragma unroll
-                for (int i = 0; i < P; ++i) {
-                  const F2 f = fma2(p2, C[i], G[c][i]), w = f * passed[k][c][i];
-                  accB = i ? fma2(f, B[i], accB) : f * B[i];
-                  accA = i ? fma2(w, A2[c][i], accA) : w * A2[c][i];
-                  sB[i] = c ? fma2(u2, f, sB[i]) : u2 * f;
-                  dA[c][i] = fma2(w, e2, dA[c][i]);
-                  G[c][i] = decay[k][c][i] * f;
-                }
-                by_B[c] = total(accB);
-                by_A[c] = total(accA);
-              }
-              if (ends >> i0 & 1u) clear(G);
-              const float sumB = over_states<LS, CC>(by_B), sumA = over_states<LS, CC>(by_A) * kLn2;
-              put_sums<L>(sB, lane, order, &m.sums[buf][i0][0][s0]);
-              const float4 w = m.own[i0][lane];
-              const float du = fmaf(w.y, sumB, sumA) * m.slope[i0][lane];
-              if (writes) {
-                from_float(fmaf(w.x, sumB, skip * w.z), *pdx);
-                from_float(du, *pddt);
-                if (gate_out) from_float(w.w * fmaf(skip, w.y, y[k]), *pdgate);
-              }
-              dskip = fmaf(w.z, w.y, dskip);
-              dbias += du;
-            }
+          if ((ends >> (sub * kSub) & 15u) || at0 + kHeld > steps) {
+            if (half & 1) ahead(any, two, at0 - kHeld);
+            through(any, at0);
+          } else {
+            if (half & 1) ahead(plain, two, at0 - kHeld);
+            through(plain, at0);
           }
         }
       }
       __syncthreads();
-      // dB and dC of the segment over the row's warps, in their order; the next barrier is ahead of their next change
+      // dB and dC of the segment over the row's warps, in their order
       if (steps > 0) {
         const int threads = 32 * side, me = threadIdx.x % threads;
         const Back<L>* const from = all + row * side;
@@ -385,11 +430,12 @@ __global__ void __launch_bounds__(32 * back_warps(L::SW), 1) k_select_back(Selec
         for (int i = me; i < steps * 2 * a.S; i += threads) {
           const int k = i / (2 * a.S), j = i % (2 * a.S), which = j >= a.S, s = which ? j - a.S : j, t = ts + k;
           float v = 0.0f;
-          for (int w = 0; w < live_warps; ++w) v += from[w].sums[buf][k][which][s];
+          for (int w = 0; w < live_warps; ++w) v += from[w].sums[k][which][s];
           if (blocks > 1) a.parts[((((int64_t)block * a.T + t) * a.N + n) * a.G + g) * 2 * a.S + j] = v;
           else from_float(v, *const_cast<T*>(row_at<T>(which ? a.dC : a.dB, t, n, (int64_t)g * a.S + s)));
         }
       }
+      __syncthreads();
     }
     if (a.dh0 && piece == 0 && real) store_ordered<SP, CC>(a.dh0, at, there, s0, order, a.S, G);
   }
