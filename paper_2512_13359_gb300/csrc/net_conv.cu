@@ -141,6 +141,7 @@ __global__ void __launch_bounds__(kForward, 4) k_conv(Conv a, bool act) {
   const bool flagged = K > 1 && (a.done || a.done_prev);
   W next[kBatch];
   uint8_t next_flag[kBatch];
+  const uint8_t* done = a.done + ((int64_t)t0 - 1) * a.N + n;       // of the end before a batch's first step; not read for step 0
   auto fetch = [&](int t) {
     if (t + kBatch <= t1) {
 #pragma unroll
@@ -151,9 +152,19 @@ __global__ void __launch_bounds__(kForward, 4) k_conv(Conv a, bool act) {
         if (t + u < t1) next[u] = *reinterpret_cast<const W*>(x + u * a.x.outer);
     }
     x += kBatch * a.x.outer;
+    if (flagged) {
+      if (t > 0 && t + kBatch <= t1 && a.done) {
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u) next_flag[u] = flagged && t + u < t1 ? flag_at(a, t + u, n) : (uint8_t)0;
+        for (int u = 0; u < kBatch; ++u) next_flag[u] = done[u * a.N];
+      } else {
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) next_flag[u] = t + u < t1 ? flag_at(a, t + u, n) : (uint8_t)0;
+      }
+      done += kBatch * a.N;
+    }
   };
+#pragma unroll
+  for (int u = 0; u < kBatch; ++u) next_flag[u] = 0;
   fetch(t0);
   load_taps<E, K>(a, d, w, b);
   load_window<T, E, K>(a, t0, n, d, win);
@@ -241,22 +252,39 @@ __global__ void __launch_bounds__(kBackward, K <= 4 ? 4 : 2) k_conv_back(Conv a,
     const T* pdy = dy + t0 * a.dy.outer;
     auto copy = [&](int t) {
       if constexpr (kCopied) {
+        W* const to = ring + (t - t0) % (kBack * kRing) * 2 * kBackward;
+        if (t + kBack <= last) {
 #pragma unroll
-        for (int u = 0; u < kBack; ++u) {
-          if (t + u < last) {
-            W* const to = ring + (t - t0 + u) % (kBack * kRing) * 2 * kBackward;
-            copy_async<sizeof(W)>(to, px);
-            copy_async<sizeof(W)>(to + kBackward, pdy);
+          for (int u = 0; u < kBack; ++u) {
+            copy_async<sizeof(W)>(to + u * 2 * kBackward, px + u * a.x.outer);
+            copy_async<sizeof(W)>(to + (u * 2 + 1) * kBackward, pdy + u * a.dy.outer);
           }
-          px += a.x.outer, pdy += a.dy.outer;
+        } else {
+#pragma unroll
+          for (int u = 0; u < kBack; ++u)
+            if (t + u < last) {
+              copy_async<sizeof(W)>(to + u * 2 * kBackward, px + u * a.x.outer);
+              copy_async<sizeof(W)>(to + (u * 2 + 1) * kBackward, pdy + u * a.dy.outer);
+            }
         }
+        px += kBack * a.x.outer, pdy += kBack * a.dy.outer;
         copy_commit();
       }
     };
     uint8_t next_flag[kBack];
-    auto fetch_flags = [&](int t) {
+    const uint8_t* done = a.done + ((int64_t)t0 - 1) * a.N + n;   // of the end before a batch's first step; not read for step 0
 #pragma unroll
-      for (int u = 0; u < kBack; ++u) next_flag[u] = flagged && t + u < last ? flag_at(a, t + u, n) : (uint8_t)0;
+    for (int u = 0; u < kBack; ++u) next_flag[u] = 0;
+    auto fetch_flags = [&](int t) {
+      if (!flagged) return;
+      if (t > 0 && t + kBack <= last && a.done) {
+#pragma unroll
+        for (int u = 0; u < kBack; ++u) next_flag[u] = done[u * a.N];
+      } else {
+#pragma unroll
+        for (int u = 0; u < kBack; ++u) next_flag[u] = t + u < last ? flag_at(a, t + u, n) : (uint8_t)0;
+      }
+      done += kBack * a.N;
     };
 #pragma unroll
     for (int i = 0; i < kRing - 1; ++i) copy(t0 + i * kBack);
@@ -396,26 +424,29 @@ __global__ void __launch_bounds__(kBackward, K <= 4 ? 4 : 2) k_conv_back(Conv a,
 }
 
 // out[c] = sum over rows of partial[row][c], columns 0 .. split - 1 to one array and the rest to another.
-constexpr int kSumGroups = 32;
-__global__ void __launch_bounds__(1024) k_conv_sums(const float* partial, int rows, int64_t cols, int64_t split, float* first,
-                                                    float* second) {
-  __shared__ float part[kSumGroups][33];
+constexpr int kSumCols = 8, kSumThreads = 512, kSumGroups = kSumThreads / kSumCols;
+__global__ void __launch_bounds__(kSumThreads) k_conv_sums(const float* partial, int rows, int64_t cols, int64_t split, float* first,
+                                                           float* second) {
+  __shared__ float part[kSumThreads / 32][kSumCols];
   after_previous();
-  const int lane = threadIdx.x % 32, group = threadIdx.x / 32;
-  const int64_t c = blockIdx.x * (int64_t)32 + lane;
+  const int lane = threadIdx.x % kSumCols, group = threadIdx.x / kSumCols;
+  const int64_t c = blockIdx.x * (int64_t)kSumCols + lane;
   float v = 0.0f;
-  if (c < cols)
-    for (int r = group; r < rows; r += kSumGroups) v += partial[r * cols + c];
-  part[group][lane] = v;
-  __syncthreads();
-  v = part[lane][group];
-#pragma unroll
-  for (int o = 16; o; o /= 2) v += __shfl_down_sync(0xffffffffu, v, o);
-  const int64_t k = blockIdx.x * (int64_t)32 + group;
-  if (lane == 0 && k < cols) {
-    float* const to = k < split ? first : second;
-    if (to) to[k < split ? k : k - split] = v;
+  if (c < cols) {
+    const float* p = partial + group * cols + c;
+#pragma unroll 4
+    for (int r = group; r < rows; r += kSumGroups, p += kSumGroups * cols) v += *p;
   }
+#pragma unroll
+  for (int o = 16; o >= kSumCols; o /= 2) v += __shfl_down_sync(0xffffffffu, v, o);
+  if (threadIdx.x % 32 < kSumCols) part[threadIdx.x / 32][lane] = v;
+  __syncthreads();
+  if (threadIdx.x >= kSumCols || c >= cols) return;
+  v = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kSumThreads / 32; ++w) v += part[w][lane];
+  float* const to = c < split ? first : second;
+  if (to) to[c < split ? c : c - split] = v;
 }
 
 // T = 0: the state passes as it is.
@@ -454,7 +485,7 @@ BackPlan back_plan(int64_t T, int64_t N, int64_t D, int e) {
   p.tiles = (per + p.side - 1) / p.side;
   p.chunk = chunk_of(T, N * per);
   p.chunks = (int)((T + p.chunk - 1) / p.chunk);
-  const int64_t items = N * p.chunks, most = std::max<int64_t>(1, (int64_t)sm_count() * 8 / p.tiles);
+  const int64_t items = N * p.chunks, most = std::max<int64_t>(1, (int64_t)sm_count() * 4 / p.tiles);
   p.blocks = std::max<int64_t>(1, std::min((items + p.slots - 1) / p.slots, std::min<int64_t>(most, 65535)));
   return p;
 }
@@ -496,7 +527,8 @@ cudaError_t launch_taps(Conv& a, bool back, bool act, float* dw, float* dbias, c
   e = cudaGetLastError();
   if (e != cudaSuccess || !a.partial) return e;
   const int64_t cols = (K + 1) * a.D;
-  return launch_after(k_conv_sums, dim3((unsigned)((cols + 31) / 32)), 1024, 0, s, a.partial, (int)p.blocks, cols, K * a.D, dw,
+  return launch_after(k_conv_sums, dim3((unsigned)((cols + kSumCols - 1) / kSumCols)), kSumThreads, 0, s, a.partial, (int)p.blocks, cols,
+                      K * a.D, dw,
                       dbias);
   }
 }

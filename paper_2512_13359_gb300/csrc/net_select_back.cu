@@ -450,11 +450,12 @@ __global__ void __launch_bounds__(32 * back_warps(L::SW), 1) k_select_back(Selec
 }
 
 // The pieces' gradients from 0 behind them, and their sums of step sizes, as forward.
-constexpr int kFoldWarps = 4;
+constexpr int kFoldWarps = 4, kFoldBatch = 4;
 template <typename T, typename L>
 __global__ void __launch_bounds__(32 * kFoldWarps) k_select_fold_back(Select a) {
   constexpr int SP = L::SP, LS = L::LS, CC = L::CC, SW = L::SW;
-  __shared__ __align__(16) float rows[kFoldWarps][kKeep * SW];
+  using In = Staged<T, SW, kFoldBatch>;
+  __shared__ __align__(16) float rows[kFoldWarps][kFoldBatch * SW];
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   int64_t id = blockIdx.x * (int64_t)kFoldWarps + warp;
   if (id >= a.N * a.G * a.tiles * a.pieces) return;
@@ -489,57 +490,75 @@ __global__ void __launch_bounds__(32 * kFoldWarps) k_select_fold_back(Select a) 
       A2[c][i] = A2[c][i] * pair(kLog2e, kLog2e);
     }
   const float bias = live && a.dt_bias ? a.dt_bias[d] : 0.0f;
+  const bool gated = a.gate.data, flagged = a.done || a.done_prev;
   float sum = 0.0f;
   bool cut = false;
-  for (int ts = t0 + (t1 - 1 - t0) / kKeep * kKeep; ts >= t0; ts -= kKeep) {
-    const int steps = min(kKeep, t1 - ts);
-    const uint32_t ends = ends_of(a, ts, n, lane);
-    stage<T, SW>(a, a.C, ts, steps, n, g, lane, Cs);
-    __syncwarp();
-#pragma unroll 1
-    for (int k0 = steps > 8 ? 8 : 0; k0 >= 0; k0 -= 8) {
-      T rdt[8], rgate[8], rdy[8];
+  // the last batch first, its inputs on their way while the one behind it is gone through
+  const int last = t0 + (t1 - 1 - t0) / kFoldBatch * kFoldBatch;
+  const T* pdt = row_at<T>(a.dt, last, n, d);
+  const T* pdy = row_at<T>(a.dy, last, n, d);
+  const T* pgate = gated ? row_at<T>(a.gate, last, n, d) : pdy;
+  const T* pC = row_at<T>(a.C, last + lane / In::kSide, n, (int64_t)g * a.S + lane % In::kSide);
+  T rdt[kFoldBatch], rgate[kFoldBatch], rdy[kFoldBatch];
+  In rC;
+  uint8_t rend = 0;
+  auto fetch = [&](int t) {
+    if (t < t0) return;
+    const int steps = min(kFoldBatch, t1 - t);
+    rend = flagged && lane < steps ? flag_at(a, t + lane, n) : (uint8_t)0;
+    rC.load(pC, a.C.outer, steps, a.S, lane);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        from_float(0.0f, rdt[k]);
-        rgate[k] = rdy[k] = rdt[k];
-        if (live && k0 + k < steps) {
-          const int t = ts + k0 + k;
-          rdt[k] = *row_at<T>(a.dt, t, n, d);
-          rdy[k] = *row_at<T>(a.dy, t, n, d);
-          if (a.gate.data) rgate[k] = *row_at<T>(a.gate, t, n, d);
-        }
-      }
-#pragma unroll
-      for (int k = 7; k >= 0; --k) {
-        if (k0 + k < steps) {
-          float p = to_float(rdy[k]);
-          const float e = live ? softplus(to_float(rdt[k]) + bias) : 0.0f;
-          if (a.gate.data) {
-            const float z = to_float(rgate[k]);
-            float s, o;
-            gates(z, s, o);
-            p *= z * s;
-          }
-          float es[CC], ps[CC];
-          to_lanes<CC>(e, es);
-          to_lanes<CC>(p, ps);
-          F2 C[SP / 2];
-          load_pairs<SP>(Cs + (k0 + k) * SW + s0, C);
-          const bool end = ends >> (k0 + k) & 1u;
-          cut = cut || end;
-          sum += e;
-#pragma unroll
-          for (int c = 0; c < CC; ++c) {
-            const F2 e2 = pair(es[c], es[c]), p2 = pair(ps[c], ps[c]);
-#pragma unroll
-            for (int i = 0; i < SP / 2; ++i)
-              G[c][i] = end ? pair(0.0f, 0.0f) : ex2(e2 * A2[c][i]) * fma2(p2, C[i], G[c][i]);
-          }
-        }
+    for (int k = 0; k < kFoldBatch; ++k) {
+      from_float(0.0f, rdt[k]);
+      rgate[k] = rdy[k] = rdt[k];
+      if (live && k < steps) {
+        rdt[k] = pdt[k * a.dt.outer], rdy[k] = pdy[k * a.dy.outer];
+        if (gated) rgate[k] = pgate[k * a.gate.outer];
       }
     }
+    pdt -= kFoldBatch * a.dt.outer, pdy -= kFoldBatch * a.dy.outer, pC -= kFoldBatch * a.C.outer;
+    if (gated) pgate -= kFoldBatch * a.gate.outer;
+  };
+  fetch(last);
+#pragma unroll 1
+  for (int ts = last; ts >= t0; ts -= kFoldBatch) {
+    const int steps = t1 - ts;
+    __syncwarp();                                             // the last batch's rows are read
+    rC.put(Cs, lane);
+    const uint32_t ends = flagged ? __ballot_sync(0xffffffffu, rend != 0) : 0u;
+    float e[kFoldBatch], p[kFoldBatch];
+#pragma unroll
+    for (int k = 0; k < kFoldBatch; ++k) {
+      e[k] = softplus(to_float(rdt[k]) + bias);
+      p[k] = to_float(rdy[k]);
+      if (gated) {
+        const float z = to_float(rgate[k]);
+        float s, o;
+        gates(z, s, o);
+        p[k] *= z * s;
+      }
+    }
+    fetch(ts - kFoldBatch);
     __syncwarp();
+    cut = cut || ends;
+#pragma unroll
+    for (int k = kFoldBatch - 1; k >= 0; --k) {
+      if (k < steps) {
+        float es[CC], ps[CC];
+        to_lanes<CC>(e[k], es);
+        to_lanes<CC>(p[k], ps);
+        F2 C[SP / 2];
+        load_pairs<SP>(Cs + k * SW + s0, C);
+        sum += e[k];
+#pragma unroll
+        for (int c = 0; c < CC; ++c) {
+          const F2 e2 = pair(es[c], es[c]), p2 = pair(ps[c], ps[c]);
+#pragma unroll
+          for (int i = 0; i < SP / 2; ++i) G[c][i] = ex2(e2 * A2[c][i]) * fma2(p2, C[i], G[c][i]);
+        }
+        if (ends >> k & 1u) clear(G);
+      }
+    }
   }
   store_states<SP, CC>(a.maps + piece * (a.N * a.D * a.S), at, there, s0, a.S, G);
   if (live && q < CC) a.sums[(int64_t)piece * a.N * a.D + n * a.D + d] = cut ? -1.0f : sum;
