@@ -167,7 +167,7 @@ __device__ __forceinline__ void wait_landed(uint64_t* b, uint32_t phase) {
 
 // One of a step's products: result rows x cols, contraction K; which operands run along M or N.
 struct Product {
-  int kind, rows, cols, K;
+  int kind, rows, cols, K, wide;   // wide: columns of a tile
   bool a_mn, b_mn;
 };
 
@@ -175,6 +175,7 @@ struct Steps {
   CUtensorMap x_rows[2], x_cols[2], p, q;   // boxes of 128 rows; x_cols: of 64
   int L, M, N, s, steps, ldx, lds;          // s: the shorter side
   bool wide;                                // M <= N
+  int tile[3];                              // columns of a tile of P, Q, X
   float a, b, c;
   __half *x[2], *P, *Q;                     // pieces [2][L][rows][ld]
   net_rows y;
@@ -183,14 +184,14 @@ struct Steps {
   unsigned* arrived;                        // blocks at the barriers between products
 };
 
-template <int BN>
-struct Tile {
-  static constexpr int kStages = BN > 128 ? 2 : 3;
-  static constexpr uint32_t kA = kBM * 128, kB = BN * 128;      // one piece of a stage
-  static constexpr uint32_t kStage = 2 * (kA + kB);
-  static constexpr uint32_t kTurn = 8 * 32 * 33 * 4;            // a 32 x 32 block a storing warp
-  static constexpr uint32_t kSmem = kStages * kStage + kTurn + 256 + 1024;
-};
+// Shared memory: a ring of two stages of 256-column tiles or of three of 128-column ones.
+constexpr uint32_t kA = kBM * 128;           // one piece of A in a stage; of B: 128 bytes a column
+constexpr uint32_t kRing = 196608, kTurn = 8 * 32 * 33 * 4;   // kTurn: a 32 x 32 block a storing warp
+constexpr uint32_t kSmem = kRing + kTurn + 256 + 1024;
+static_assert(kSmem <= 227 * 1024, "shared memory of a block");
+__host__ __device__ constexpr int stages_of(int wide) { return wide > 128 ? 2 : 3; }
+__host__ __device__ constexpr uint32_t stage_bytes(int wide) { return 2 * (kA + wide * 128); }
+static_assert(stages_of(256) * stage_bytes(256) == kRing && stages_of(128) * stage_bytes(128) == kRing, "the ring");
 struct Bars {
   uint64_t full[3], empty[3], sums[2], taken[2], drained;
   uint32_t tmem;
@@ -221,20 +222,20 @@ __device__ __forceinline__ void store_pieces(__half* hi, int64_t to_lo, const fl
   *reinterpret_cast<uint4*>(hi + to_lo) = make_uint4(o[0], o[1], o[2], o[3]);
 }
 
-// The block at (r0, c0) of a product that goes on as pieces, or with `other` its mirror image, from turn[row * 33 + column].
+// The block at (r0, c0) of a product that goes on as pieces, from turn[row * 33 + column]; with `mirror` its mirror image too.
 template <int AHEAD>
-__device__ __forceinline__ void store_block(const Steps& a, const Product& p, __half* out, int ld, int l, int r0, int c0, bool other,
-                                            const float* turn, int lane) {
+__device__ __forceinline__ void store_block(const Steps& a, const Product& p, __half* out, int ld, int l, int r0, int c0, bool mirror,
+                                            float* turn, int lane) {
   const int64_t to_lo = (int64_t)a.L * p.rows * ld, at = (int64_t)l * p.rows * ld;
-  const int q = lane % 4 * 8, c = (other ? r0 : c0) + q;
+  const int q = lane % 4 * 8;
   const float scale = p.kind == kP ? kScaleP / (kScaleX * kScaleX) : p.kind == kX ? 1.0f / kScaleQ : a.c * (kScaleQ / (kScaleP * kScaleP));
   const float fb = a.b * (kScaleQ / kScaleP);
   uint4 ph[AHEAD], po[AHEAD];                // P's values, on their way ahead of the stores
   auto fetch = [&](int i) {
-    const int r = (other ? c0 : r0) + i * 8 + lane / 4;
+    const int r = r0 + i * 8 + lane / 4;
     ph[i % AHEAD] = po[i % AHEAD] = make_uint4(0, 0, 0, 0);
-    if (r < p.rows && c < p.cols) {
-      const __half* const from = a.P + at + (int64_t)r * ld + c;
+    if (r < p.rows && c0 + q < p.cols) {
+      const __half* const from = a.P + at + (int64_t)r * ld + c0 + q;
       ph[i % AHEAD] = *reinterpret_cast<const uint4*>(from);
       po[i % AHEAD] = *reinterpret_cast<const uint4*>(from + to_lo);
     }
@@ -245,20 +246,33 @@ __device__ __forceinline__ void store_block(const Steps& a, const Product& p, __
 #pragma unroll
       for (int k = i; k < i + AHEAD; ++k) fetch(k);
     }
-    const int k = i * 8 + lane / 4, r = (other ? c0 : r0) + k;
+    const int k = i * 8 + lane / 4, r = r0 + k, c = c0 + q;
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = turn[k * 33 + q + e] * scale;
+    if (p.kind == kQ) {
+      float h[8], o[8];
+      unpack<__half, 8>(ph[i % AHEAD], h);
+      unpack<__half, 8>(po[i % AHEAD], o);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += fmaf(fb, h[e], fb * o[e]) + (c + e == r ? a.a * kScaleQ : 0.0f);
+    }
+    if (mirror) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) turn[k * 33 + q + e] = v[e];
+    }
+    if (r < p.rows && c < p.cols) store_pieces(out + at + (int64_t)r * ld + c, to_lo, v);
+  }
+  if (!mirror) return;
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int k = i * 8 + lane / 4, r = c0 + k, c = r0 + q;
     if (r < p.rows && c < p.cols) {
       float v[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = turn[other ? (q + e) * 33 + k : k * 33 + q + e] * scale;
-      const int64_t here = at + (int64_t)r * ld + c;
-      if (p.kind == kQ) {
-        float h[8], o[8];
-        unpack<__half, 8>(ph[i % AHEAD], h);
-        unpack<__half, 8>(po[i % AHEAD], o);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += fmaf(fb, h[e], fb * o[e]) + (c + e == r ? a.a * kScaleQ : 0.0f);
-      }
-      store_pieces(out + here, to_lo, v);
+      for (int e = 0; e < 8; ++e) v[e] = turn[(q + e) * 33 + k];
+      store_pieces(out + at + (int64_t)r * ld + c, to_lo, v);
     }
   }
 }
@@ -273,30 +287,27 @@ __device__ __forceinline__ void store_last(const Steps& a, int l, int r0, int c0
     if (r0 + i < a.M) from_float(turn[i * 33 + lane] * (1.0f / (kScaleQ * kScaleX)), *p);
 }
 
-// Tiles of a product: number, and the t-th of a matrix.  Of symmetric results those that reach the diagonal or lie below it.
-template <int BN>
-__device__ __forceinline__ int tiles_of(const Product& p) {
-  const int tm = (p.rows + kBM - 1) / kBM;
-  if (p.kind != kP && p.kind != kQ) return tm * ((p.cols + BN - 1) / BN);
-  if (BN == kBM) return tm * (tm + 1) / 2;
-  const int half = tm / 2;                       // 1, 1, 2, 2, 3, 3, ...
-  return half * (half + 1) + (tm & 1 ? half + 1 : 0);
+// Tiles of a product: number, and the t-th of a matrix.  Of symmetric results those that reach the diagonal or lie below
+// it: row i of tiles begins with number i (i + 1) / 2, or about i^2 / 4 of the wider ones.
+__host__ __device__ inline int start_of(int i, int wide) {
+  return wide == kBM ? i * (i + 1) / 2 : (i / 2) * (i / 2 + 1) + (i & 1 ? i / 2 + 1 : 0);
 }
-template <int BN>
+__host__ __device__ inline int tiles_of(int kind, int rows, int cols, int wide) {
+  const int tm = (rows + kBM - 1) / kBM;
+  return kind == kP || kind == kQ ? start_of(tm, wide) : tm * ((cols + wide - 1) / wide);
+}
 __device__ __forceinline__ void tile_at(const Product& p, int t, int& ti, int& tj) {
   if (p.kind != kP && p.kind != kQ) {
     // neighbours in groups of 8 tile rows: they read the same columns of B at about the same time
-    const int tm = (p.rows + kBM - 1) / kBM, tn = (p.cols + BN - 1) / BN, group = t / (8 * tn), first = group * 8;
+    const int tm = (p.rows + kBM - 1) / kBM, tn = (p.cols + p.wide - 1) / p.wide, group = t / (8 * tn), first = group * 8;
     const int high = min(8, tm - first), in = t - group * 8 * tn;
     ti = first + in % high, tj = in / high;
     return;
   }
-  // row ti's first tile is number ti (ti + 1) / 2, or about ti^2 / 4 of the wider ones
-  auto start = [](int i) { return BN == kBM ? i * (i + 1) / 2 : (i / 2) * (i / 2 + 1) + (i & 1 ? i / 2 + 1 : 0); };
-  ti = (int)sqrtf((BN == kBM ? 2.0f : 4.0f) * t);
-  while (start(ti) > t) --ti;
-  while (start(ti + 1) <= t) ++ti;
-  tj = t - start(ti);
+  ti = (int)sqrtf((p.wide == kBM ? 2.0f : 4.0f) * t);
+  while (start_of(ti, p.wide) > t) --ti;
+  while (start_of(ti + 1, p.wide) <= t) ++ti;
+  tj = t - start_of(ti, p.wide);
 }
 
 // Every block has arrived `round` times, and what they stored is seen, by TMA too.  Bounded.
@@ -323,15 +334,14 @@ __device__ __forceinline__ void all_blocks(const Steps& a, unsigned round, volat
 
 template <int BN>
 __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant__ Steps a) {
-  using TL = Tile<BN>;
   constexpr int kCols = BN / 2;              // of a storing warp's row
   extern __shared__ uint8_t smem_raw[];
   uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023u) & ~(uintptr_t)1023u);
-  Bars* const bar = reinterpret_cast<Bars*>(smem + TL::kStages * TL::kStage + TL::kTurn);
+  Bars* const bar = reinterpret_cast<Bars*>(smem + kRing + kTurn);
   volatile int* const abort = &bar->abort;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   if (tid == 0) {
-    for (int s = 0; s < TL::kStages; ++s) {
+    for (int s = 0; s < 3; ++s) {
       tc::mbar_init(&bar->full[s], 1);
       tc::mbar_init(&bar->empty[s], 1);
     }
@@ -357,6 +367,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant_
   const uint32_t tmem = bar->tmem;
   // The blocks' products and tiles, the same for every role: do(p, A, B, chunks, l, m0, n0, in).
   uint32_t chunk = 0;                        // of this block, over all tiles and products: each role counts its own
+  uint32_t used = 0, parity = 0;             // bit s: stage s has been filled; an odd number of times
   auto all_tiles = [&](auto&& work) {
     for (int k = 0; k < a.steps * 3; ++k) {
       const int in = k / 3 & 1;                // which of the two X is read
@@ -364,25 +375,26 @@ __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant_
       Product p;
       const CUtensorMap *A, *B;
       if (k % 3 == 0) {
-        p = {kP, a.s, a.s, a.wide ? a.N : a.M, !a.wide, !a.wide};
+        p = {kP, a.s, a.s, a.wide ? a.N : a.M, a.tile[0], !a.wide, !a.wide};
         A = B = a.wide ? &a.x_rows[in] : &a.x_cols[in];
       } else if (k % 3 == 1) {
-        p = {kQ, a.s, a.s, a.s, false, false};
+        p = {kQ, a.s, a.s, a.s, a.tile[1], false, false};
         A = B = &a.p;
       } else {
-        p = {last ? kLast : kX, a.M, a.N, a.s, false, a.wide};
+        p = {last ? kLast : kX, a.M, a.N, a.s, a.tile[2], false, a.wide};
         A = a.wide ? &a.q : &a.x_rows[in];
         B = a.wide ? &a.x_cols[in] : &a.q;
       }
-      const int chunks = (p.K + kBK - 1) / kBK, each = tiles_of<BN>(p);
+      const int chunks = (p.K + kBK - 1) / kBK, each = tiles_of(p.kind, p.rows, p.cols, p.wide);
+      int stage = 0;                           // the ring begins anew, with as many stages as these tiles leave
       const int64_t all = (int64_t)each * a.L;
       for (int64_t t = blockIdx.x; t < all; t += gridDim.x) {
         if (*abort) break;
         int ti, tj;
         const int l = (int)(t / each);
-        tile_at<BN>(p, (int)(t % each), ti, tj);
-        const int m0 = ti * kBM, n0 = tj * BN;
-        work(p, A, B, chunks, l, m0, n0, in);
+        tile_at(p, (int)(t % each), ti, tj);
+        const int m0 = ti * kBM, n0 = tj * p.wide;
+        work(p, A, B, chunks, l, m0, n0, in, stage);
       }
       if (k + 1 < a.steps * 3) all_blocks(a, (unsigned)k + 1, abort);
       if (*abort) break;                       // seen by all: behind a barrier, or at the end
@@ -390,12 +402,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant_
   };
   if (warp < kStorers) {
     more_registers();
-    all_tiles([&](const Product& p, const CUtensorMap*, const CUtensorMap*, int chunks, int l, int m0, int n0, int in) {
+    all_tiles([&](const Product& p, const CUtensorMap*, const CUtensorMap*, int chunks, int l, int m0, int n0, int in, int&) {
         float acc[kCols];
 #pragma unroll
         for (int i = 0; i < kCols; ++i) acc[i] = 0.0f;
         bool ok = true;
-        const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16, half = warp / 4 * kCols;
+        const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16, half = warp / 4 * (p.wide / 2);
 #pragma unroll 1
         for (int c = 0; c < chunks; ++c, ++chunk) {
           const uint32_t buf = chunk & 1u;
@@ -405,6 +417,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant_
           if (ok) {
 #pragma unroll
             for (int j = 0; j < kCols; j += 32) {
+              if (j >= p.wide / 2) break;
               uint32_t r[32];
               tc::tmem_ld32(tmem + lanes + buf * BN + half + j, r);
               tc::tmem_ld_wait(r);
@@ -417,9 +430,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant_
           if (lane == 0) tc::mbar_arrive(&bar->taken[buf]);
         }
         const int r0 = m0 + warp % 4 * 32;
-        float* const turn = reinterpret_cast<float*>(smem + TL::kStages * TL::kStage) + warp * 32 * 33;
+        float* const turn = reinterpret_cast<float*>(smem + kRing) + warp * 32 * 33;
 #pragma unroll
         for (int j = 0; j < kCols; j += 32) {
+          if (j >= p.wide / 2) break;
           const int col = n0 + (int)half + j;
           float* const v = acc + j;
           if (!ok) {
@@ -437,8 +451,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant_
             } else {
               __half* const out = p.kind == kP ? a.P : p.kind == kQ ? a.Q : a.x[in ^ 1];
               const int ld = p.kind == kX ? a.ldx : a.lds;
-              store_block<BN == 128 ? 4 : 1>(a, p, out, ld, l, r0, col, false, turn, lane);
-              if (p.kind != kX && col < r0) store_block<BN == 128 ? 4 : 1>(a, p, out, ld, l, r0, col, true, turn, lane);
+              store_block<BN == 128 ? 4 : 1>(a, p, out, ld, l, r0, col, p.kind != kX && col < r0, turn, lane);
             }
             __syncwarp();
           }
@@ -447,13 +460,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant_
   } else {
     fewer_registers();
     if (warp == kProducer) {
-      all_tiles([&](const Product& p, const CUtensorMap* A, const CUtensorMap* B, int chunks, int l, int m0, int n0, int) {
+      all_tiles([&](const Product& p, const CUtensorMap* A, const CUtensorMap* B, int chunks, int l, int m0, int n0, int, int& stage) {
         if (lane == 0)
-          for (int c = 0; c < chunks; ++c, ++chunk) {
-            const uint32_t s = chunk % TL::kStages, use = chunk / TL::kStages;
-            if (use && !tc::mbar_wait(&bar->empty[s], (use - 1) & 1u, abort, kWaitLimitNs)) break;
-            tc::mbar_arrive_expect_tx(&bar->full[s], TL::kStage);
-            uint8_t* to = smem + s * TL::kStage;
+          for (int c = 0; c < chunks; ++c) {
+            const int s = stage;
+            stage = s + 1 == stages_of(p.wide) ? 0 : s + 1;
+            if ((used >> s & 1u) && !tc::mbar_wait(&bar->empty[s], (parity >> s & 1u) ^ 1u, abort, kWaitLimitNs)) break;
+            used |= 1u << s, parity ^= 1u << s;
+            tc::mbar_arrive_expect_tx(&bar->full[s], stage_bytes(p.wide));
+            uint8_t* to = smem + s * stage_bytes(p.wide);
             const int kk = c * kBK;
 #pragma unroll
             for (int piece = 0; piece < 2; ++piece) {
@@ -464,41 +479,46 @@ __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant_
               } else {
                 tma_load_3d(to, A, kk, m0, z, &bar->full[s]);
               }
-              to += TL::kA;
+              to += kA;
             }
 #pragma unroll
             for (int piece = 0; piece < 2; ++piece) {
               const int z = l + piece * a.L;
               if (p.b_mn) {
 #pragma unroll
-                for (int j = 0; j < BN; j += 64) tma_load_3d(to + j * 128, B, n0 + j, kk, z, &bar->full[s]);
+                for (int j = 0; j < BN; j += 64)
+                  if (j < p.wide) tma_load_3d(to + j * 128, B, n0 + j, kk, z, &bar->full[s]);
               } else {
 #pragma unroll
-                for (int j = 0; j < BN; j += 128) tma_load_3d(to + j * 128, B, kk, n0 + j, z, &bar->full[s]);
+                for (int j = 0; j < BN; j += 128)
+                  if (j < p.wide) tma_load_3d(to + j * 128, B, kk, n0 + j, z, &bar->full[s]);
               }
-              to += TL::kB;
+              to += p.wide * 128;
             }
           }
         __syncwarp();
       });
     } else {
-      all_tiles([&](const Product& p, const CUtensorMap*, const CUtensorMap*, int chunks, int, int, int, int) {
+      all_tiles([&](const Product& p, const CUtensorMap*, const CUtensorMap*, int chunks, int, int, int, int, int& stage) {
         if (warp != kIssuer) return;
         if (lane == 0) {
-          const uint32_t id = idesc_f16(p.a_mn, p.b_mn, kBM, BN);
+          const uint32_t id = idesc_f16(p.a_mn, p.b_mn, kBM, p.wide);
           // 16 of K: 32 bytes along a row, or 16 rows of 128 bytes
           const uint32_t da = p.a_mn ? 2048 : 32, db = p.b_mn ? 2048 : 32, la = p.a_mn ? 8192 : 16, lb = p.b_mn ? 8192 : 16;
           for (int c = 0; c < chunks; ++c, ++chunk) {
-            const uint32_t s = chunk % TL::kStages, buf = chunk & 1u, to = tmem + buf * BN;
+            const int s = stage;
+            stage = s + 1 == stages_of(p.wide) ? 0 : s + 1;
+            const uint32_t buf = chunk & 1u, to = tmem + buf * BN;
             if (chunk >= 2 && !tc::mbar_wait(&bar->taken[buf], (chunk / 2 - 1) & 1u, abort, kWaitLimitNs)) break;
-            if (!tc::mbar_wait(&bar->full[s], chunk / TL::kStages & 1u, abort, kWaitLimitNs)) break;
+            if (!tc::mbar_wait(&bar->full[s], parity >> s & 1u, abort, kWaitLimitNs)) break;
+            parity ^= 1u << s;
             tc::tc_fence_after();
-            const uint32_t a0 = tc::smem_u32(smem + s * TL::kStage), b0 = a0 + 2 * TL::kA;
+            const uint32_t a0 = tc::smem_u32(smem + s * stage_bytes(p.wide)), b0 = a0 + 2 * kA, next_b = p.wide * 128;
             // the small products first: what the sum of the large ones is rounded by does not grow with them
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) {
-              const uint64_t ah = tile_desc(a0 + kk * da, la, 1024), al = tile_desc(a0 + TL::kA + kk * da, la, 1024);
-              const uint64_t bh = tile_desc(b0 + kk * db, lb, 1024), bl = tile_desc(b0 + TL::kB + kk * db, lb, 1024);
+              const uint64_t ah = tile_desc(a0 + kk * da, la, 1024), al = tile_desc(a0 + kA + kk * da, la, 1024);
+              const uint64_t bh = tile_desc(b0 + kk * db, lb, 1024), bl = tile_desc(b0 + next_b + kk * db, lb, 1024);
               tc::mma_ss(to, al, bh, id, kk > 0);
               tc::mma_ss(to, ah, bl, id, 1u);
             }
@@ -519,10 +539,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant_
     wait_landed(&bar->drained, 0);
   }
   if (warp == kProducer && lane == 0 && *abort)
-    for (uint32_t s = 0; s < TL::kStages; ++s) {
-      const uint32_t fills = chunk / TL::kStages + (s < chunk % TL::kStages ? 1 : 0);
-      if (fills) wait_landed(&bar->full[s], (fills - 1) & 1u);
-    }
+    for (int s = 0; s < 3; ++s)
+      if (used >> s & 1u) wait_landed(&bar->full[s], (parity >> s & 1u) ^ 1u);
   tc::tc_fence_before();
   __syncthreads();
   if (tid == 0 && bar->abort) *a.error = AUV_ERR_TIMEOUT;
@@ -627,15 +645,14 @@ int check(const net_ortho* p) {
 template <int BN>
 cudaError_t launch_products(const Steps& a, cudaStream_t s) {
   const auto kern = k_products<BN>;
-  static_assert(Tile<BN>::kSmem <= 227 * 1024, "shared memory of a block");
-  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Tile<BN>::kSmem);
+  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
   if (e != cudaSuccess) return e;
   // the blocks wait for each other: all of them, one an SM, or none; no more than the largest product has tiles
-  const int64_t tiles = (int64_t)((a.M + kBM - 1) / kBM) * ((a.N + BN - 1) / BN) * a.L;
+  const int64_t tiles = (int64_t)std::max(tiles_of(kX, a.M, a.N, a.tile[2]), tiles_of(kP, a.s, a.s, std::min(a.tile[0], a.tile[1]))) * a.L;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)std::min<int64_t>(sm_count(), std::max<int64_t>(1, tiles)));
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = Tile<BN>::kSmem;
+  cfg.dynamicSmemBytes = kSmem;
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeCooperative;
@@ -674,9 +691,18 @@ cudaError_t launch(const net_ortho* a, const Space& z, cudaStream_t s) {
     ok = make_map(&p.x_rows[i], at, a->N, a->M, z.ldx, a->L, kBM) && make_map(&p.x_cols[i], at, a->N, a->M, z.ldx, a->L, kBK);
   }
   if (!ok) return cudaErrorInvalidValue;
-  // wide tiles, which read less of shared memory for a product, where they still fill the device
-  const int64_t large = ((a->M + 127) / 128) * ((a->N + 255) / 256) * a->L;
-  return large >= sm_count() ? launch_products<256>(p, s) : launch_products<128>(p, s);
+  // Columns of a tile: 256 read less of shared memory for a product (64 of K: 1.3 us, 128 columns 0.7) and take longer to
+  // store (4.5 us, 2.5), and their rounds over the SMs are fewer and coarser.
+  const int kinds[3] = {kP, kQ, kX};
+  for (int k = 0; k < 3; ++k) {
+    const int K = k == 0 ? std::max(p.M, p.N) : p.s, rows = k < 2 ? p.s : p.M, cols = k < 2 ? p.s : p.N;
+    auto time = [&](int w) {
+      const int64_t rounds = ((int64_t)tiles_of(kinds[k], rows, cols, w) * p.L + sm_count() - 1) / sm_count();
+      return (double)rounds * ((K + kBK - 1) / kBK * (w == 256 ? 1.3 : 0.7) + (w == 256 ? 4.5 : 2.5));
+    };
+    p.tile[k] = time(256) < time(128) ? 256 : 128;
+  }
+  return p.tile[0] + p.tile[1] + p.tile[2] > 3 * 128 ? launch_products<256>(p, s) : launch_products<128>(p, s);
 }
 
 int run(const net_ortho* p, void* stream) {
