@@ -20,9 +20,10 @@ constexpr int kBatch = 4;       // steps whose inputs are on their way while as 
 // FOLD: only the piece's final state from 0, and the sum of its step sizes (-1 where an episode ends in it: nothing
 // passes through).
 template <typename T, typename L, bool FOLD>
-__global__ void __launch_bounds__(32 * kWarps, L::SP == 8 ? 4 : 6) k_select(Select a) {
-  constexpr int SP = L::SP, LS = L::LS, CC = L::CC, SW = L::SW;
+__global__ void __launch_bounds__(32 * kWarps, L::OWN > 1 ? 3 : L::SP == 8 ? 4 : 6) k_select(Select a) {
+  constexpr int SP = L::SP, LS = L::LS, CC = L::CC, SW = L::SW, OWN = L::OWN, kSides = CC / OWN;
   using In = Staged<T, SW, kBatch>;
+  using W = Raw<T, OWN>;
   __shared__ __align__(16) float rows[kWarps][FOLD ? 1 : 2][kBatch * SW];
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   int64_t id = blockIdx.x * (int64_t)kWarps + warp;
@@ -39,14 +40,14 @@ __global__ void __launch_bounds__(32 * kWarps, L::SP == 8 ? 4 : 6) k_select(Sele
 
   const int q = lane % LS, s0 = q * SP;
   const int first = tile * L::CW + lane / LS * CC;            // in the group
-  const int own = first + q % CC;
-  const bool live = own < a.per, writes = live && q < CC;
-  const int64_t d = (int64_t)g * a.per + own;                 // own channel
+  const int own = first + q % kSides * OWN;
+  const bool live = own < a.per, writes = live && q < kSides;   // OWN = 2: channels of a group are even in number
+  const int64_t d = (int64_t)g * a.per + own;                 // own channels
   int64_t at[CC], at_weight[CC];
   bool there[CC];
 #pragma unroll
   for (int c = 0; c < CC; ++c) {
-    const int k = first + (q % CC ^ c);
+    const int k = first + (q % kSides ^ c / OWN) * OWN + c % OWN;
     at_weight[c] = (int64_t)g * a.per + k;
     at[c] = n * a.D + at_weight[c];
     there[c] = k < a.per;
@@ -61,10 +62,11 @@ __global__ void __launch_bounds__(32 * kWarps, L::SP == 8 ? 4 : 6) k_select(Sele
   const int64_t in_row = (int64_t)g * a.S + lane % In::kSide;
   const T* pB = row_at<T>(a.B, t0 + lane / In::kSide, n, in_row);
   const T* pC = row_at<T>(a.C, t0 + lane / In::kSide, n, in_row);
-  T rx[kBatch], rdt[kBatch], rgate[kBatch];
+  W rx[kBatch], rdt[kBatch], rgate[kBatch];
   In rB, rC;
   uint8_t rend = 0;
   const bool all_live = __all_sync(0xffffffffu, live);
+  auto get = [](const T* p, int64_t at) { return *reinterpret_cast<const W*>(p + at); };
   auto fetch = [&](int t) {
     const int steps = t1 - t;
     if (steps <= 0) return;
@@ -73,19 +75,18 @@ __global__ void __launch_bounds__(32 * kWarps, L::SP == 8 ? 4 : 6) k_select(Sele
     if constexpr (!FOLD) rC.load(pC, a.C.outer, steps, a.S, lane);
     if (all_live && steps >= kBatch) {
 #pragma unroll
-      for (int k = 0; k < kBatch; ++k) rx[k] = px[k * a.x.outer], rdt[k] = pdt[k * a.dt.outer];
+      for (int k = 0; k < kBatch; ++k) rx[k] = get(px, k * a.x.outer), rdt[k] = get(pdt, k * a.dt.outer);
       if (gated) {
 #pragma unroll
-        for (int k = 0; k < kBatch; ++k) rgate[k] = pgate[k * a.gate.outer];
+        for (int k = 0; k < kBatch; ++k) rgate[k] = get(pgate, k * a.gate.outer);
       }
     } else {
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) {
-        from_float(0.0f, rx[k]);
-        rdt[k] = rgate[k] = rx[k];
+        rx[k] = rdt[k] = rgate[k] = W{};
         if (live && k < steps) {
-          rx[k] = px[k * a.x.outer], rdt[k] = pdt[k * a.dt.outer];
-          if (gated) rgate[k] = pgate[k * a.gate.outer];
+          rx[k] = get(px, k * a.x.outer), rdt[k] = get(pdt, k * a.dt.outer);
+          if (gated) rgate[k] = get(pgate, k * a.gate.outer);
         }
       }
     }
@@ -114,8 +115,13 @@ __global__ void __launch_bounds__(32 * kWarps, L::SP == 8 ? 4 : 6) k_select(Sele
   for (int c = 0; c < CC; ++c)
 #pragma unroll
     for (int i = 0; i < SP / 2; ++i) A2[c][i] = A2[c][i] * pair(kLog2e, kLog2e);
-  const float bias = live && a.dt_bias ? a.dt_bias[d] : 0.0f, skip = live && a.skip ? a.skip[d] : 0.0f;
-  float sum = 0.0f;
+  float bias[OWN], skip[OWN], sum[OWN];
+#pragma unroll
+  for (int j = 0; j < OWN; ++j) {
+    bias[j] = live && a.dt_bias ? a.dt_bias[d + j] : 0.0f;
+    skip[j] = live && a.skip ? a.skip[d + j] : 0.0f;
+    sum[j] = 0.0f;
+  }
   bool cut = false;
 
 #pragma unroll 1
@@ -125,20 +131,27 @@ __global__ void __launch_bounds__(32 * kWarps, L::SP == 8 ? 4 : 6) k_select(Sele
     rB.put(Bs, lane);
     if constexpr (!FOLD) rC.put(Cs, lane);
     const uint32_t ends = flagged ? __ballot_sync(0xffffffffu, rend != 0) : 0u;
-    float x[kBatch], e[kBatch], z[kBatch];
+    float x[kBatch][OWN], e[kBatch][OWN], z[kBatch][OWN];
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
-      x[k] = to_float(rx[k]);
-      e[k] = softplus(to_float(rdt[k]) + bias);
-      z[k] = 1.0f;
+      unpack<T, OWN>(rx[k], x[k]);
+      unpack<T, OWN>(rdt[k], e[k]);
+#pragma unroll
+      for (int j = 0; j < OWN; ++j) {
+        e[k][j] = softplus(e[k][j] + bias[j]);
+        z[k][j] = 1.0f;
+      }
     }
     if (gated) {
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) {
-        const float v = to_float(rgate[k]);
-        float s, o;
-        gates(v, s, o);
-        z[k] = v * s;
+        unpack<T, OWN>(rgate[k], z[k]);
+#pragma unroll
+        for (int j = 0; j < OWN; ++j) {
+          float s, o;
+          gates(z[k][j], s, o);
+          z[k][j] *= s;
+        }
       }
     }
     fetch(ts + kBatch);
@@ -151,9 +164,11 @@ __global__ void __launch_bounds__(32 * kWarps, L::SP == 8 ? 4 : 6) k_select(Sele
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) {
         if (!kPlain && k >= steps) break;
-        float es[CC], us[CC];
-        to_lanes<CC>(e[k], es);
-        to_lanes<CC>(e[k] * x[k], us);
+        float es[CC], us[CC], u[OWN];
+#pragma unroll
+        for (int j = 0; j < OWN; ++j) u[j] = e[k][j] * x[k][j];
+        to_lanes<CC, OWN>(e[k], es);
+        to_lanes<CC, OWN>(u, us);
         F2 B[SP / 2], C[SP / 2];
         load_pairs<SP>(Bs + k * SW + s0, B);
         if constexpr (!FOLD) load_pairs<SP>(Cs + k * SW + s0, C);
@@ -176,8 +191,17 @@ __global__ void __launch_bounds__(32 * kWarps, L::SP == 8 ? 4 : 6) k_select(Sele
           }
           y[c] = total(acc);
         }
-        if constexpr (FOLD) sum += e[k];
-        else store_if(writes, py + k * a.y.outer, fmaf(skip, x[k], over_states<LS, CC>(y)) * z[k]);
+        if constexpr (FOLD) {
+#pragma unroll
+          for (int j = 0; j < OWN; ++j) sum[j] += e[k][j];
+        } else {
+          float p[OWN];
+          over_states<LS, CC, OWN>(y, p);
+#pragma unroll
+          for (int j = 0; j < OWN; ++j) p[j] = fmaf(skip[j], x[k][j], p[j]) * z[k][j];
+          if constexpr (OWN == 1) store_if(writes, py + k * a.y.outer, p[0]);
+          else if (writes) store<T, OWN>(py + k * a.y.outer, p);
+        }
       }
     };
     if (steps >= kBatch && !ends) walk(std::true_type());
@@ -186,7 +210,10 @@ __global__ void __launch_bounds__(32 * kWarps, L::SP == 8 ? 4 : 6) k_select(Sele
   }
   if constexpr (FOLD) {
     store_states<SP, CC>(a.maps + piece * states, at, there, s0, a.S, h);
-    if (writes) a.sums[(int64_t)piece * a.N * a.D + n * a.D + d] = cut ? -1.0f : sum;
+    if (writes) {
+#pragma unroll
+      for (int j = 0; j < OWN; ++j) a.sums[(int64_t)piece * a.N * a.D + n * a.D + d + j] = cut ? -1.0f : sum[j];
+    }
   } else {
     if (a.hT && t1 == a.T) store_states<SP, CC>(a.hT, at, there, s0, a.S, h);
   }
@@ -369,8 +396,19 @@ cudaError_t launch_walk(const Select& a, cudaStream_t s) {
   return cudaGetLastError();
 }
 
+template <typename T, typename L>
+cudaError_t launch_all(const Select& a, cudaStream_t s) {
+  if (a.pieces > 1) {
+    cudaError_t e = launch_walk<T, L, true>(a, s);
+    if (e == cudaSuccess) e = launch_select_join(a, false, s);
+    if (e != cudaSuccess) return e;
+  }
+  return launch_walk<T, L, false>(a, s);
+}
+
 template <typename T>
 cudaError_t launch(const Select& a, cudaStream_t s) {
+  if (a.wide) return with_wide_lanes(a.S, [&](auto l) { return launch_all<T, decltype(l)>(a, s); });
   return with_lanes(a.S, [&](auto l) {
     using L = decltype(l);
     if (a.T == 1) {
@@ -386,12 +424,7 @@ cudaError_t launch(const Select& a, cudaStream_t s) {
       k_select_one<T, L><<<(unsigned)((envs * side + kOneWarps - 1) / kOneWarps), 32 * kOneWarps, 0, s>>>(a, wide);
       return cudaGetLastError();
     }
-    if (a.pieces > 1) {
-      cudaError_t e = launch_walk<T, L, true>(a, s);
-      if (e == cudaSuccess) e = launch_select_join(a, false, s);
-      if (e != cudaSuccess) return e;
-    }
-    return launch_walk<T, L, false>(a, s);
+    return launch_all<T, L>(a, s);
   });
 }
 
@@ -410,7 +443,7 @@ int check(const net_select* p) {
   return AUV_OK;
 }
 
-Select of(const net_select* p, bool back) {
+Select of(const net_select* p, bool back, bool narrow = false) {
   Select a = {};
   a.T = (int)p->T, a.S = (int)p->S, a.G = (int)p->G, a.per = (int)(p->D / p->G), a.N = p->N, a.D = p->D;
   a.x = p->x, a.dt = p->dt, a.gate = p->gate, a.y = p->y, a.B = p->B, a.C = p->C, a.dy = p->dy, a.dx = p->dx;
@@ -418,6 +451,14 @@ Select of(const net_select* p, bool back) {
   a.A = p->A, a.skip = p->skip, a.dt_bias = p->dt_bias, a.h0 = p->h0, a.hT = p->hT, a.kept = p->kept, a.dhT = p->dhT;
   a.dh0 = p->dh0, a.dA = p->dA, a.dskip = p->dskip, a.ddt_bias = p->ddt_bias, a.done = p->done, a.done_prev = p->done_prev;
   a.tiles = (a.per + lanes_channels(a.S) - 1) / lanes_channels(a.S);
+  // pairs of channels a lane where every access of two is aligned and enough warps are left: pieces of a long sequence are
+  // the shorter the more warps there are (65,521 steps of 250 channels x 13 fp32: 176 us in pairs, 161 not)
+  const net_rows* rows[] = {&a.x, &a.dt, &a.gate, &a.y};
+  const int z = type_size(p->dtype), tiles = (a.per + kWideChannels - 1) / kWideChannels;
+  bool pairs = !back && !narrow && a.T > 1 && a.S <= kMostWide && a.per % 2 == 0;
+  for (const net_rows* r : rows) pairs = pairs && aligned(*r, a.T, a.N, z, 2);
+  a.wide = pairs && a.N * a.G * tiles >= (int64_t)sm_count() * 12;
+  if (a.wide) a.tiles = tiles;
   select_pieces(a, back);
   return a;
 }
@@ -527,8 +568,8 @@ extern "C" {
 size_t net_select_scan_workspace_bytes(const net_select* p, int backward) {
   using namespace auv::net;
   if (!p || check(p) || !p->T || !p->N || !p->D) return 0;
-  Select a = of(p, backward);
-  return lay_out(a, backward, nullptr);
+  Select a = of(p, backward), b = of(p, backward, true);
+  return std::max(lay_out(a, backward, nullptr), lay_out(b, backward, nullptr));
 }
 
 int net_select_scan(const net_select* a, void* stream) { return auv::net::run(a, false, stream); }

@@ -18,6 +18,7 @@ struct Select {
   int T, S, G, per;             // per: channels of a group
   int piece, pieces;            // steps of a piece of the sequence, multiples of kKeep
   int tiles;                    // warps that a group's channels take
+  bool wide;                    // forward: twice as many channels a lane
   int64_t N, D;
   net_rows x, dt, gate, y, B, C, dy, dx, ddt, dgate, dB, dC;
   const float *A, *skip, *dt_bias, *h0;
@@ -59,25 +60,37 @@ __device__ __forceinline__ float softplus(float v, float* sigmoid = nullptr) {
   return fmaf(z, p, fmaxf(v, 0.0f));
 }
 
-// Sums over the lanes that share channels, of CC values a lane (one per channel, its own first): that of its own channel.
+// Sums over the lanes that share channels, of CC values a lane (its own OWN channels' first): those of its own.
+template <int LS, int CC, int OWN>
+__device__ __forceinline__ void over_states(const float (&v)[CC], float (&r)[OWN]) {
+#pragma unroll
+  for (int j = 0; j < OWN; ++j) {
+    r[j] = v[j];
+    if constexpr (CC > OWN) r[j] += __shfl_xor_sync(0xffffffffu, v[OWN + j], 1);
+#pragma unroll
+    for (int bit = CC / OWN; bit < LS; bit *= 2) r[j] += __shfl_xor_sync(0xffffffffu, r[j], bit);
+  }
+}
 template <int LS, int CC>
 __device__ __forceinline__ float over_states(const float (&v)[CC]) {
-  float r = v[0];
-  int bit = 1;
-  if constexpr (CC == 2) {
-    r += __shfl_xor_sync(0xffffffffu, v[1], 1);
-    bit = 2;
-  }
-#pragma unroll
-  for (; bit < LS; bit *= 2) r += __shfl_xor_sync(0xffffffffu, r, bit);
-  return r;
+  float r[1];
+  over_states<LS, CC, 1>(v, r);
+  return r[0];
 }
 
-// A value of the lane's own channel to the lanes that share it: r[c] is that of the lane's c-th channel, its own first.
+// Values of the lane's own channels to the lanes that share them: r[c] is that of the lane's c-th channel, its own first.
+template <int CC, int OWN>
+__device__ __forceinline__ void to_lanes(const float (&own)[OWN], float (&r)[CC]) {
+#pragma unroll
+  for (int j = 0; j < OWN; ++j) {
+    r[j] = own[j];
+    if constexpr (CC > OWN) r[OWN + j] = __shfl_xor_sync(0xffffffffu, own[j], 1);
+  }
+}
 template <int CC>
 __device__ __forceinline__ void to_lanes(float own, float (&r)[CC]) {
-  r[0] = own;
-  if constexpr (CC == 2) r[1] = __shfl_xor_sync(0xffffffffu, own, 1);
+  const float v[1] = {own};
+  to_lanes<CC, 1>(v, r);
 }
 
 template <typename T>
@@ -214,8 +227,8 @@ __device__ __forceinline__ void load_pairs(const float* p, F2 (&v)[SP / 2]) {
 }
 
 // How S states are laid over lanes.
-template <int SP_, int LS_, int CC_> struct Lanes {
-  static constexpr int SP = SP_, LS = LS_, CC = CC_;
+template <int SP_, int LS_, int CC_, int OWN_ = 1> struct Lanes {
+  static constexpr int SP = SP_, LS = LS_, CC = CC_, OWN = OWN_;   // CC: OWN, or twice that
   static constexpr int SW = SP * LS;          // states, padded
   static constexpr int CW = 32 / LS * CC;     // channels of a warp
 };
@@ -229,6 +242,14 @@ cudaError_t with_lanes(int S, F f) {
   return f(Lanes<8, 16, 2>());
 }
 inline int lanes_channels(int S) { return S <= 16 ? 32 : S <= 32 ? 16 : S <= 64 ? 8 : 4; }
+// Forward twice as many channels a lane: what a lane reads of B and C, and its addresses, serve twice the states (4,096 x 128
+// x 256 x 16 bf16: 683 us, 822 with half as many).
+template <typename F>
+cudaError_t with_wide_lanes(int S, F f) {
+  if (S <= 8) return f(Lanes<8, 1, 2, 2>());
+  return f(Lanes<8, 2, 4, 2>());
+}
+constexpr int kMostWide = 16, kWideChannels = 64;   // states; channels of a warp
 
 // The states before the pieces from the pieces' maps, in the maps' place (net_select.cu).
 cudaError_t launch_select_join(const Select& a, bool back, cudaStream_t s);

@@ -173,6 +173,13 @@ def test_scan_long(T, N, D, S, G, dt):
     _check_scan(T, N, D, S, G, dt, ends=0.002, seed=7)
 
 
+@pytest.mark.parametrize("T,N,D,S,G,dt,layout", [(19, 1900, 40, 16, 1, "bf16", "flat"), (5, 950, 96, 13, 1, "fp16", "half"), (6, 2000, 6, 8, 1, "fp32", "flat"),
+                                                 (18, 950, 12, 3, 2, "bf16", "pad"), (4, 2000, 34, 10, 1, "fp32", "odd")])
+def test_scan_of_many_envs(T, N, D, S, G, dt, layout):
+    """Enough warps for two channels a lane, or not aligned for it."""
+    _check_scan(T, N, D, S, G, dt, layout, seed=13)
+
+
 @pytest.mark.parametrize("T", [40, 20000])
 def test_scan_of_a_constant_input_reaches_its_limit(T):
     """dt = 0, no bias: e = log 2; with B x = 1 the state goes to e / (1 - exp(e A)) times 1 minus exp(e A T), whatever the
