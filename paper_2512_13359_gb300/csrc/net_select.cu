@@ -547,7 +547,7 @@ int run(const net_select* p, bool back, void* stream) {
 }  // namespace
 
 void select_pieces(Select& a, bool back) {
-  const int64_t warps = a.N * a.G * a.tiles, want = (int64_t)sm_count() * (back ? 8 : 16);
+  const int64_t warps = a.N * a.G * a.tiles, want = (int64_t)sm_count() * (!back ? 16 : a.S <= 8 ? 12 : 8);
   int64_t pieces = std::min(want / std::max<int64_t>(1, warps), (int64_t)a.T / 64);
   if (pieces < 2) pieces = 1;
   const int64_t piece = pieces == 1 ? a.T : ((a.T + pieces - 1) / pieces + kKeep - 1) / kKeep * kKeep;

@@ -20,14 +20,18 @@ namespace {
 constexpr int kHeld = 2, kSub = 4;
 
 // Warps of a block: shared memory grows with the padded states.
-constexpr int back_warps(int padded) { return padded <= 16 ? 8 : padded <= 64 ? 4 : 2; }
+constexpr int back_warps(int padded) { return padded <= 8 ? 4 : padded <= 16 ? 8 : padded <= 64 ? 4 : 2; }
+// Blocks of an SM: of up to 8 states a lane has one channel's, and three blocks of four warps fit (8,192 steps of 3 x 200
+// channels x 8 fp16: 147 us, 200 with one block of eight).
+constexpr int back_blocks(int padded) { return padded <= 8 ? 3 : 1; }
 
 // A warp's shared memory.  What multiplies pairs of states is there twice: copies in registers took a twelfth of all
 // instructions.
 template <typename L> struct Back {
   float B[kKeep][L::SW], C[kKeep][L::SW];
-  float4 eu[kKeep][32];                         // e, e, e x, e x of the lane's own channel
-  float2 pp[kKeep][32], xq[kKeep][32];          // p, p; x, dy silu'(gate)
+  static constexpr bool kTwice = L::CC == 2;    // one channel a lane: there is room for fewer, and copies are fewer too
+  float4 eu[kKeep][32];                         // of the lane's own channel e, e, e x, e x; or e, x, p, dy silu'(gate)
+  float2 pp[kTwice ? kKeep : 1][32], xq[kTwice ? kKeep : 1][32];   // p, p; x, dy silu'(gate)
   float slope[kKeep][32];                       // sigmoid(dt + dt_bias)
   float4 start[kKeep / kSub - 1][L::CC * L::SP / 4][32];   // the lane's states before steps 4, 8, 12
   float sums[kKeep][2][L::SW];                  // dB and dC over the warp's channels
@@ -161,7 +165,8 @@ __device__ __forceinline__ void prefetch(const void* p) { asm volatile("prefetch
 
 // rows: (env, group) pairs a block walks side by side, back_warps / rows warps each.
 template <typename T, typename L>
-__global__ void __launch_bounds__(32 * back_warps(L::SW), 1) k_select_back(Select a, int rows) {
+__global__ void __launch_bounds__(32 * back_warps(L::SW), back_blocks(L::SW)) k_select_back(Select a, int rows) {
+  constexpr bool kTwice = Back<L>::kTwice;
   constexpr int SP = L::SP, LS = L::LS, CC = L::CC, SW = L::SW, P = SP / 2;
   extern __shared__ __align__(16) uint8_t smem[];
   Back<L>* const all = reinterpret_cast<Back<L>*>(smem);
@@ -251,9 +256,13 @@ __global__ void __launch_bounds__(32 * back_warps(L::SW), 1) k_select_back(Selec
               p *= z * s;
             }
             const float x = to_float(rx[k]), u = e * x;
-            m.eu[k0 + k][lane] = live ? make_float4(e, e, u, u) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            m.pp[k0 + k][lane] = make_float2(p, p);
-            m.xq[k0 + k][lane] = make_float2(x, qy);
+            if constexpr (kTwice) {
+              m.eu[k0 + k][lane] = live ? make_float4(e, e, u, u) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+              m.pp[k0 + k][lane] = make_float2(p, p);
+              m.xq[k0 + k][lane] = make_float2(x, qy);
+            } else {
+              m.eu[k0 + k][lane] = make_float4(live ? e : 0.0f, x, p, qy);
+            }
             m.slope[k0 + k][lane] = slope;
           }
         }
@@ -272,15 +281,25 @@ __global__ void __launch_bounds__(32 * back_warps(L::SW), 1) k_select_back(Selec
         __syncwarp();
         // e, e x and p of step k, for both states of a pair
         auto inputs = [&](int k, F2 (&e)[CC], F2 (&u)[CC]) {
+          if constexpr (kTwice) {
 #pragma unroll
-          for (int c = 0; c < CC; ++c) {
-            const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(&m.eu[k][lane ^ c]);
-            e[c].v = w.x, u[c].v = w.y;
+            for (int c = 0; c < CC; ++c) {
+              const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(&m.eu[k][lane ^ c]);
+              e[c].v = w.x, u[c].v = w.y;
+            }
+          } else {
+            const float4 w = m.eu[k][lane];
+            e[0] = pair(w.x, w.x);
+            u[0] = pair(w.x * w.y, w.x * w.y);
           }
         };
         auto weights = [&](int k, F2 (&p)[CC]) {
+          if constexpr (kTwice) {
 #pragma unroll
-          for (int c = 0; c < CC; ++c) p[c].v = *reinterpret_cast<const uint64_t*>(&m.pp[k][lane ^ c]);
+            for (int c = 0; c < CC; ++c) p[c].v = *reinterpret_cast<const uint64_t*>(&m.pp[k][lane ^ c]);
+          } else {
+            p[0] = pair(m.eu[k][lane].z, m.eu[k][lane].z);
+          }
         };
         const int subs = (steps + kSub - 1) / kSub;
         // COUNT steps forward: the states behind them.  plain: no end is among them (and, below, all of them are there).
@@ -369,7 +388,9 @@ __global__ void __launch_bounds__(32 * back_warps(L::SW), 1) k_select_back(Selec
               float e1, p1, copy;
               split(e[0], e1, copy);
               split(p[0], p1, copy);
-              const float2 w = m.xq[i0][lane];
+              float2 w;
+              if constexpr (kTwice) w = m.xq[i0][lane];
+              else w = make_float2(m.eu[i0][lane].y, m.eu[i0][lane].w);
               const float du = fmaf(w.x, sumB, sumA) * m.slope[i0][lane];
               store_if(writes, pdx, fmaf(e1, sumB, skip * p1));
               store_if(writes, pddt, du);
@@ -613,7 +634,7 @@ int64_t select_slots(const Select& a, int64_t* blocks, int* rows) {
   *rows = warps / side;
   *blocks = (a.tiles + side - 1) / side;
   const int64_t items = (a.N * a.pieces + *rows - 1) / *rows;
-  const int64_t most = std::max<int64_t>(1, (int64_t)sm_count() / (*blocks * a.G));
+  const int64_t most = std::max<int64_t>(1, (int64_t)sm_count() * back_blocks(a.S) / (*blocks * a.G));
   // as many rounds as the fullest slot makes, spread evenly
   const int64_t rounds = (items + most - 1) / most;
   return std::min<int64_t>((items + rounds - 1) / rounds, 65535) * *rows;
@@ -634,7 +655,7 @@ cudaError_t launch_select_back(const Select& a, bool split, cudaStream_t s) {
     }
     const auto kern = k_select_back<T, L>;
     const int smem = (int)sizeof(Back<L>) * back_warps(L::SW);
-    static_assert(sizeof(Back<L>) * back_warps(L::SW) <= 227 * 1024, "shared memory of a block");
+    static_assert((sizeof(Back<L>) * back_warps(L::SW) + 1024) * back_blocks(L::SW) <= 228 * 1024, "shared memory of an SM");
     if ((e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess) return e;
     const dim3 grid((unsigned)(blocks * a.G), (unsigned)(slots / rows));
     if (split) return launch_after(kern, grid, 32 * back_warps(L::SW), smem, s, a, rows);
