@@ -297,26 +297,57 @@ __device__ __forceinline__ void load_row(const T* p, bool wide, int s0, int S, F
   for (int i = 0; i < SP / 2; ++i) v[i] = pair(x[2 * i], x[2 * i + 1]);
 }
 
-constexpr int kOneWarps = 8;
-template <typename T, typename L>
-__global__ void __launch_bounds__(32 * kOneWarps, 3) k_select_one(Select a, bool wide) {
+// whole: every lane's channels and states are there, and whole sectors; then the next env's are on their way while one is
+// computed.
+constexpr int kOneWarps = 4;
+template <int SP, int CC>
+__device__ __forceinline__ void load_whole(const float* p, const int (&at)[CC], F2 (&h)[CC][SP / 2]) {
+#pragma unroll
+  for (int c = 0; c < CC; ++c) {
+    if constexpr (SP == 8) {
+      asm volatile("ld.global.v4.b64 {%0, %1, %2, %3}, [%4];"
+                   : "=l"(h[c][0].v), "=l"(h[c][1].v), "=l"(h[c][2].v), "=l"(h[c][3].v)
+                   : "l"(p + at[c])
+                   : "memory");
+    } else {
+      const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(p + at[c]);
+      h[c][0].v = w.x, h[c][1].v = w.y;
+    }
+  }
+}
+template <int SP, int CC>
+__device__ __forceinline__ void store_whole(float* p, const int (&at)[CC], const F2 (&h)[CC][SP / 2]) {
+#pragma unroll
+  for (int c = 0; c < CC; ++c) {
+    if constexpr (SP == 8)
+      asm volatile("st.global.v4.b64 [%0], {%1, %2, %3, %4};" ::"l"(p + at[c]), "l"(h[c][0].v), "l"(h[c][1].v), "l"(h[c][2].v),
+                   "l"(h[c][3].v)
+                   : "memory");
+    else
+      *reinterpret_cast<ulonglong2*>(p + at[c]) = make_ulonglong2(h[c][0].v, h[c][1].v);
+  }
+}
+
+template <typename T, typename L, bool WHOLE>
+__global__ void __launch_bounds__(32 * kOneWarps, 4) k_select_one(Select a, bool wide) {
   constexpr int SP = L::SP, LS = L::LS, CC = L::CC, P = SP / 2;
   const int lane = threadIdx.x % 32;
-  const int64_t id = blockIdx.x * (int64_t)kOneWarps + threadIdx.x / 32, side = (int64_t)a.G * a.tiles;
-  const int64_t envs = gridDim.x * (int64_t)kOneWarps / side;           // walked side by side
-  int64_t n = id / side;
-  if (n >= min(envs, a.N)) return;
-  const int g = (int)(id % side / a.tiles), tile = (int)(id % a.tiles);
+  const int g = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles;
+  const int64_t envs = gridDim.y * (int64_t)kOneWarps;                  // walked side by side
+  int64_t n = blockIdx.y * (int64_t)kOneWarps + threadIdx.x / 32;
+  if (n >= a.N) return;
   const int q = lane % LS, s0 = q * SP;
   const int first = tile * L::CW + lane / LS * CC, own = first + q % CC;
   const bool live = own < a.per, writes = live && q < CC;
   const int64_t d = (int64_t)g * a.per + own;
   int64_t at_weight[CC];
+  int to[CC];                                                           // of an env's states
   bool there[CC];
 #pragma unroll
   for (int c = 0; c < CC; ++c) {
     const int k = first + (q % CC ^ c);
     at_weight[c] = (int64_t)g * a.per + k;
+    to[c] = (int)at_weight[c] * a.S + s0;
     there[c] = k < a.per;
   }
   F2 A2[CC][P];
@@ -326,58 +357,87 @@ __global__ void __launch_bounds__(32 * kOneWarps, 3) k_select_one(Select a, bool
   for (int c = 0; c < CC; ++c)
 #pragma unroll
     for (int i = 0; i < P; ++i) A2[c][i] = A2[c][i] * pair(kLog2e, kLog2e);
+  const int64_t in_row = (int64_t)g * a.S + s0, each = a.D * a.S;
+  const bool gated = a.gate.data;
+  T rx, rdt, rgate;
+  uint8_t rend = 0;
+  F2 next[CC][P], B[P], C[P];
+  auto fetch = [&](int64_t n) {
+    if constexpr (WHOLE) {
+      if (a.h0) {
+        load_whole<SP, CC>(a.h0 + n * each, to, next);
+      } else {
+#pragma unroll
+        for (int c = 0; c < CC; ++c)
+#pragma unroll
+          for (int i = 0; i < P; ++i) next[c][i] = pair(0.0f, 0.0f);
+      }
+    } else {
+      int64_t at[CC];
+#pragma unroll
+      for (int c = 0; c < CC; ++c) at[c] = n * a.D + at_weight[c];
+      load_states<SP, CC>(a.h0, at, there, s0, a.S, next);
+    }
+    from_float(0.0f, rx);
+    rdt = rgate = rx;
+    if (WHOLE || live) {
+      rx = *row_at<T>(a.x, 0, n, d);
+      rdt = *row_at<T>(a.dt, 0, n, d);
+      if (gated) rgate = *row_at<T>(a.gate, 0, n, d);
+    }
+    load_row<T, SP>(row_at<T>(a.B, 0, n, in_row), WHOLE || wide, s0, a.S, B);
+    load_row<T, SP>(row_at<T>(a.C, 0, n, in_row), WHOLE || wide, s0, a.S, C);
+    if (a.done_prev) rend = a.done_prev[n];
+  };
+  fetch(n);
   for (; n < a.N; n += envs) {
+    F2 h[CC][P];
     int64_t at[CC];
-    bool from[CC];
-    const uint8_t end = a.done_prev ? a.done_prev[n] : (uint8_t)0;
 #pragma unroll
     for (int c = 0; c < CC; ++c) {
       at[c] = n * a.D + at_weight[c];
-      from[c] = there[c];
+#pragma unroll
+      for (int i = 0; i < P; ++i) h[c][i] = next[c][i];
     }
-    F2 h[CC][P], B[P], C[P];
-    load_states<SP, CC>(a.h0, at, from, s0, a.S, h);
-    T rx, rdt, rgate;
-    from_float(0.0f, rx);
-    rdt = rgate = rx;
-    if (live) {
-      rx = *row_at<T>(a.x, 0, n, d);
-      rdt = *row_at<T>(a.dt, 0, n, d);
-      if (a.gate.data) rgate = *row_at<T>(a.gate, 0, n, d);
-    }
-    load_row<T, SP>(row_at<T>(a.B, 0, n, (int64_t)g * a.S + s0), wide, s0, a.S, B);
-    load_row<T, SP>(row_at<T>(a.C, 0, n, (int64_t)g * a.S + s0), wide, s0, a.S, C);
     if (a.kept) store_states<SP, CC>(a.kept, at, there, s0, a.S, h);
-    const float x = to_float(rx), e = live ? softplus(to_float(rdt) + bias) : 0.0f;
-    float es[CC], us[CC], y[CC];
-    to_lanes<CC>(e, es);
-    to_lanes<CC>(e * x, us);
-    if (end) {
+    const float x = to_float(rx), e = WHOLE || live ? softplus(to_float(rdt) + bias) : 0.0f;
+    float z = 1.0f;
+    if (gated) {
+      float s, o;
+      z = to_float(rgate);
+      gates(z, s, o);
+      z *= s;
+    }
+    if (rend) {
 #pragma unroll
       for (int c = 0; c < CC; ++c)
 #pragma unroll
         for (int i = 0; i < P; ++i) h[c][i] = pair(0.0f, 0.0f);
     }
+    F2 uB[P], oC[P];
+#pragma unroll
+    for (int i = 0; i < P; ++i) uB[i] = B[i], oC[i] = C[i];
+    if (WHOLE && n + envs < a.N) fetch(n + envs);
+    float es[CC], us[CC], y[CC];
+    to_lanes<CC>(e, es);
+    to_lanes<CC>(e * x, us);
 #pragma unroll
     for (int c = 0; c < CC; ++c) {
       const F2 e2 = pair(es[c], es[c]), u2 = pair(us[c], us[c]);
       F2 acc;
 #pragma unroll
       for (int i = 0; i < P; ++i) {
-        h[c][i] = fma2(ex2(e2 * A2[c][i]), h[c][i], u2 * B[i]);
-        acc = i ? fma2(C[i], h[c][i], acc) : C[i] * h[c][i];
+        h[c][i] = fma2(ex2(e2 * A2[c][i]), h[c][i], u2 * uB[i]);
+        acc = i ? fma2(oC[i], h[c][i], acc) : oC[i] * h[c][i];
       }
       y[c] = total(acc);
     }
-    if (a.hT) store_states<SP, CC>(a.hT, at, there, s0, a.S, h);
-    float p = fmaf(skip, x, over_states<LS, CC>(y));
-    if (a.gate.data) {
-      const float z = to_float(rgate);
-      float s, o;
-      gates(z, s, o);
-      p *= z * s;
+    if (a.hT) {
+      if constexpr (WHOLE) store_whole<SP, CC>(a.hT + n * each, to, h);
+      else store_states<SP, CC>(a.hT, at, there, s0, a.S, h);
     }
-    store_if(writes, const_cast<T*>(row_at<T>(a.y, 0, n, d)), p);
+    store_if(writes, const_cast<T*>(row_at<T>(a.y, 0, n, d)), fmaf(skip, x, over_states<LS, CC>(y)) * z);
+    if (!WHOLE && n + envs < a.N) fetch(n + envs);
   }
 }
 
@@ -417,11 +477,14 @@ cudaError_t launch(const Select& a, cudaStream_t s) {
       const net_rows* rows[] = {&a.B, &a.C};
       bool wide = a.S % L::SP == 0;
       for (const net_rows* r : rows) wide = wide && aligned(*r, 1, a.N, z, std::min(L::SP, 16 / z));
-      // a warp takes two to four envs where there are enough: fewer leave A's load unused, more leave warps out
-      const int64_t blocks = (side * a.N + kOneWarps - 1) / kOneWarps, few = (int64_t)sm_count() * 3;
-      const int64_t turns = std::max<int64_t>(1, std::min<int64_t>(4, blocks / (4 * few)));
-      const int64_t envs = (a.N + turns - 1) / turns;
-      k_select_one<T, L><<<(unsigned)((envs * side + kOneWarps - 1) / kOneWarps), 32 * kOneWarps, 0, s>>>(a, wide);
+      auto sectors = [&](const void* p) { return reinterpret_cast<uintptr_t>(p) % (4 * L::SP) == 0; };
+      const bool whole = wide && a.S == L::SW && a.per % L::CW == 0 && sectors(a.h0) && sectors(a.hT);
+      // as many warps as the SMs hold at a time walk the envs
+      const int64_t few = (int64_t)sm_count() * 4, all = (a.N + kOneWarps - 1) / kOneWarps;
+      const int64_t blocks = std::min<int64_t>(65535, std::max<int64_t>(1, std::min(all, (few + side - 1) / side)));
+      const dim3 grid((unsigned)side, (unsigned)blocks);
+      if (whole) k_select_one<T, L, true><<<grid, 32 * kOneWarps, 0, s>>>(a, true);
+      else k_select_one<T, L, false><<<grid, 32 * kOneWarps, 0, s>>>(a, wide);
       return cudaGetLastError();
     }
     return launch_all<T, L>(a, s);
