@@ -159,6 +159,50 @@ __device__ __forceinline__ uint64_t tile_desc(uint32_t saddr, uint32_t lbo, uint
 __host__ __device__ constexpr uint32_t idesc_f16(bool a_mn, bool b_mn, int M, int N) {
   return (1u << 4) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
+// A pair of blocks (a cluster of two) on one 256 x 256 tile: each loads its 128 rows of A and half of B's columns, and
+// signals the first one's barrier.
+__device__ __forceinline__ void tma_load_pair(void* dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+          tc::smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
+      : "memory");
+}
+template <bool PAIR>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t more) {
+  if constexpr (PAIR)
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a),
+                 "l"(b), "r"(id), "r"(more)
+                 : "memory");
+  else
+    tc::mma_ss(d, a, b, id, more);
+}
+// The barrier, of both blocks of a pair, when all products issued so far are done.
+template <bool PAIR>
+__device__ __forceinline__ void commit(uint64_t* bar) {
+  if constexpr (PAIR)
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+                     tc::smem_u32(bar)),
+                 "h"((uint16_t)3)
+                 : "memory");
+  else
+    tc::mma_commit(bar);
+}
+template <bool PAIR>
+__device__ __forceinline__ void alloc(uint32_t* dst, uint32_t cols) {
+  if constexpr (PAIR) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(dst)), "r"(cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  } else {
+    tc::tmem_alloc(dst, cols);
+    tc::tmem_relinquish();
+  }
+}
+template <bool PAIR>
+__device__ __forceinline__ void dealloc(uint32_t at, uint32_t cols) {
+  if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(cols) : "memory");
+  else tc::tmem_dealloc(at, cols);
+}
 __device__ __forceinline__ void wait_landed(uint64_t* b, uint32_t phase) {
   const uint64_t t0 = tc::global_timer_ns();
   while (!tc::mbar_test(b, phase) && tc::global_timer_ns() - t0 < kWaitLimitNs) {
@@ -167,7 +211,7 @@ __device__ __forceinline__ void wait_landed(uint64_t* b, uint32_t phase) {
 
 // One of a step's products: result rows x cols, contraction K; which operands run along M or N.
 struct Product {
-  int kind, rows, cols, K, wide;   // wide: columns of a tile
+  int kind, rows, cols, K, high, wide;   // high, wide: of a tile
   bool a_mn, b_mn;
 };
 
@@ -287,27 +331,27 @@ __device__ __forceinline__ void store_last(const Steps& a, int l, int r0, int c0
     if (r0 + i < a.M) from_float(turn[i * 33 + lane] * (1.0f / (kScaleQ * kScaleX)), *p);
 }
 
-// Tiles of a product: number, and the t-th of a matrix.  Of symmetric results those that reach the diagonal or lie below
-// it: row i of tiles begins with number i (i + 1) / 2, or about i^2 / 4 of the wider ones.
-__host__ __device__ inline int start_of(int i, int wide) {
-  return wide == kBM ? i * (i + 1) / 2 : (i / 2) * (i / 2 + 1) + (i & 1 ? i / 2 + 1 : 0);
+// Tiles of a product, of high x wide: number, and the t-th of a matrix.  Of symmetric results those that reach the diagonal
+// or lie below it: row i of square tiles begins with number i (i + 1) / 2, of tiles twice as wide with about i^2 / 4.
+__host__ __device__ inline int start_of(int i, int high, int wide) {
+  return wide == high ? i * (i + 1) / 2 : (i / 2) * (i / 2 + 1) + (i & 1 ? i / 2 + 1 : 0);
 }
-__host__ __device__ inline int tiles_of(int kind, int rows, int cols, int wide) {
-  const int tm = (rows + kBM - 1) / kBM;
-  return kind == kP || kind == kQ ? start_of(tm, wide) : tm * ((cols + wide - 1) / wide);
+__host__ __device__ inline int tiles_of(int kind, int rows, int cols, int high, int wide) {
+  const int tm = (rows + high - 1) / high;
+  return kind == kP || kind == kQ ? start_of(tm, high, wide) : tm * ((cols + wide - 1) / wide);
 }
 __device__ __forceinline__ void tile_at(const Product& p, int t, int& ti, int& tj) {
   if (p.kind != kP && p.kind != kQ) {
     // neighbours in groups of 8 tile rows: they read the same columns of B at about the same time
-    const int tm = (p.rows + kBM - 1) / kBM, tn = (p.cols + p.wide - 1) / p.wide, group = t / (8 * tn), first = group * 8;
-    const int high = min(8, tm - first), in = t - group * 8 * tn;
-    ti = first + in % high, tj = in / high;
+    const int tm = (p.rows + p.high - 1) / p.high, tn = (p.cols + p.wide - 1) / p.wide, group = t / (8 * tn), first = group * 8;
+    const int most = min(8, tm - first), in = t - group * 8 * tn;
+    ti = first + in % most, tj = in / most;
     return;
   }
-  ti = (int)sqrtf((p.wide == kBM ? 2.0f : 4.0f) * t);
-  while (start_of(ti, p.wide) > t) --ti;
-  while (start_of(ti + 1, p.wide) <= t) ++ti;
-  tj = t - start_of(ti, p.wide);
+  ti = (int)sqrtf((p.wide == p.high ? 2.0f : 4.0f) * t);
+  while (start_of(ti, p.high, p.wide) > t) --ti;
+  while (start_of(ti + 1, p.high, p.wide) <= t) ++ti;
+  tj = t - start_of(ti, p.high, p.wide);
 }
 
 // Every block has arrived `round` times, and what they stored is seen, by TMA too.  Bounded.
@@ -332,9 +376,12 @@ __device__ __forceinline__ void all_blocks(const Steps& a, unsigned round, volat
   asm volatile("fence.proxy.async.global;" ::: "memory");
 }
 
-template <int BN>
+// PAIR: blocks in clusters of two, each with 128 of a tile's 256 rows; the first one issues the products of both.
+template <int BN, bool PAIR>
 __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant__ Steps a) {
   constexpr int kCols = BN / 2;              // of a storing warp's row
+  constexpr int kBlocks = PAIR ? 2 : 1, kHigh = kBlocks * kBM;
+  const int rank = PAIR ? (int)tc::cluster_rank() : 0;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023u) & ~(uintptr_t)1023u);
   Bars* const bar = reinterpret_cast<Bars*>(smem + kRing + kTurn);
@@ -347,7 +394,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant_
     }
     for (int b = 0; b < 2; ++b) {
       tc::mbar_init(&bar->sums[b], 1);
-      tc::mbar_init(&bar->taken[b], kStorers);
+      tc::mbar_init(&bar->taken[b], kStorers * kBlocks);
     }
     tc::mbar_init(&bar->drained, 1);
     bar->abort = 0;
@@ -358,11 +405,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant_
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(maps[lane])) : "memory");
   }
   if (warp == kIssuer) {
-    tc::tmem_alloc(&bar->tmem, 2 * BN);
-    tc::tmem_relinquish();
+    alloc<PAIR>(&bar->tmem, 2 * BN);
   }
   tc::tc_fence_before();
   __syncthreads();
+  if constexpr (PAIR) tc::cluster_sync();    // the other block's barriers are there
   tc::tc_fence_after();
   const uint32_t tmem = bar->tmem;
   // The blocks' products and tiles, the same for every role: do(p, A, B, chunks, l, m0, n0, in).
@@ -375,25 +422,25 @@ __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant_
       Product p;
       const CUtensorMap *A, *B;
       if (k % 3 == 0) {
-        p = {kP, a.s, a.s, a.wide ? a.N : a.M, a.tile[0], !a.wide, !a.wide};
+        p = {kP, a.s, a.s, a.wide ? a.N : a.M, kHigh, a.tile[0], !a.wide, !a.wide};
         A = B = a.wide ? &a.x_rows[in] : &a.x_cols[in];
       } else if (k % 3 == 1) {
-        p = {kQ, a.s, a.s, a.s, a.tile[1], false, false};
+        p = {kQ, a.s, a.s, a.s, kHigh, a.tile[1], false, false};
         A = B = &a.p;
       } else {
-        p = {last ? kLast : kX, a.M, a.N, a.s, a.tile[2], false, a.wide};
+        p = {last ? kLast : kX, a.M, a.N, a.s, kHigh, a.tile[2], false, a.wide};
         A = a.wide ? &a.q : &a.x_rows[in];
         B = a.wide ? &a.x_cols[in] : &a.q;
       }
-      const int chunks = (p.K + kBK - 1) / kBK, each = tiles_of(p.kind, p.rows, p.cols, p.wide);
+      const int chunks = (p.K + kBK - 1) / kBK, each = tiles_of(p.kind, p.rows, p.cols, p.high, p.wide);
       int stage = 0;                           // the ring begins anew, with as many stages as these tiles leave
       const int64_t all = (int64_t)each * a.L;
-      for (int64_t t = blockIdx.x; t < all; t += gridDim.x) {
+      for (int64_t t = blockIdx.x / kBlocks; t < all; t += gridDim.x / kBlocks) {
         if (*abort) break;
         int ti, tj;
         const int l = (int)(t / each);
         tile_at(p, (int)(t % each), ti, tj);
-        const int m0 = ti * kBM, n0 = tj * p.wide;
+        const int m0 = ti * kHigh + rank * kBM, n0 = tj * p.wide;
         work(p, A, B, chunks, l, m0, n0, in, stage);
       }
       if (k + 1 < a.steps * 3) all_blocks(a, (unsigned)k + 1, abort);
@@ -416,18 +463,28 @@ __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant_
           tc::tc_fence_after();
           if (ok) {
 #pragma unroll
-            for (int j = 0; j < kCols; j += 32) {
+            for (int j = 0; j < kCols; j += 64) {        // 64 columns on their way at a time
               if (j >= p.wide / 2) break;
-              uint32_t r[32];
+              uint32_t r[32], q[32];
               tc::tmem_ld32(tmem + lanes + buf * BN + half + j, r);
+              tc::tmem_ld32(tmem + lanes + buf * BN + half + j + 32, q);
               tc::tmem_ld_wait(r);
+              tc::tmem_ld_wait(q);
 #pragma unroll
-              for (int i = 0; i < 32; ++i) acc[j + i] += __uint_as_float(r[i]);
+              for (int i = 0; i < 32; ++i) {
+                acc[j + i] += __uint_as_float(r[i]);
+                acc[j + 32 + i] += __uint_as_float(q[i]);
+              }
             }
           }
           tc::tc_fence_before();
           __syncwarp();
-          if (lane == 0) tc::mbar_arrive(&bar->taken[buf]);
+          if (lane == 0) {
+            // nothing but tensor memory has been read: no release at cluster scope, which waited 1 us for it to mean nothing
+            if constexpr (PAIR)
+              asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(tc::mapa(tc::smem_u32(&bar->taken[buf]), 0)) : "memory");
+            else tc::mbar_arrive(&bar->taken[buf]);
+          }
         }
         const int r0 = m0 + warp % 4 * 32;
         float* const turn = reinterpret_cast<float*>(smem + kRing) + warp * 32 * 33;
@@ -464,20 +521,25 @@ __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant_
         if (lane == 0)
           for (int c = 0; c < chunks; ++c) {
             const int s = stage;
-            stage = s + 1 == stages_of(p.wide) ? 0 : s + 1;
+            const int held = p.wide / kBlocks;        // columns of B in this block
+            stage = s + 1 == stages_of(held) ? 0 : s + 1;
             if ((used >> s & 1u) && !tc::mbar_wait(&bar->empty[s], (parity >> s & 1u) ^ 1u, abort, kWaitLimitNs)) break;
             used |= 1u << s, parity ^= 1u << s;
-            tc::mbar_arrive_expect_tx(&bar->full[s], stage_bytes(p.wide));
-            uint8_t* to = smem + s * stage_bytes(p.wide);
+            if (rank == 0) tc::mbar_arrive_expect_tx(&bar->full[s], kBlocks * stage_bytes(held));
+            uint8_t* to = smem + s * stage_bytes(held);
+            auto load = [&](void* dst, const CUtensorMap* map, int x, int y, int z) {
+              if constexpr (PAIR) tma_load_pair(dst, map, x, y, z, tc::mapa(tc::smem_u32(&bar->full[s]), 0));
+              else tma_load_3d(dst, map, x, y, z, &bar->full[s]);
+            };
             const int kk = c * kBK;
 #pragma unroll
             for (int piece = 0; piece < 2; ++piece) {
               const int z = l + piece * a.L;
               if (p.a_mn) {
-                tma_load_3d(to, A, m0, kk, z, &bar->full[s]);
-                tma_load_3d(to + 8192, A, m0 + 64, kk, z, &bar->full[s]);
+                load(to, A, m0, kk, z);
+                load(to + 8192, A, m0 + 64, kk, z);
               } else {
-                tma_load_3d(to, A, kk, m0, z, &bar->full[s]);
+                load(to, A, kk, m0, z);
               }
               to += kA;
             }
@@ -487,46 +549,46 @@ __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant_
               if (p.b_mn) {
 #pragma unroll
                 for (int j = 0; j < BN; j += 64)
-                  if (j < p.wide) tma_load_3d(to + j * 128, B, n0 + j, kk, z, &bar->full[s]);
+                  if (j < held) load(to + j * 128, B, n0 + rank * held + j, kk, z);
               } else {
 #pragma unroll
                 for (int j = 0; j < BN; j += 128)
-                  if (j < p.wide) tma_load_3d(to + j * 128, B, kk, n0 + j, z, &bar->full[s]);
+                  if (j < held) load(to + j * 128, B, kk, n0 + rank * held + j, z);
               }
-              to += p.wide * 128;
+              to += held * 128;
             }
           }
         __syncwarp();
       });
     } else {
       all_tiles([&](const Product& p, const CUtensorMap*, const CUtensorMap*, int chunks, int, int, int, int, int& stage) {
-        if (warp != kIssuer) return;
+        if (warp != kIssuer || rank) return;
         if (lane == 0) {
-          const uint32_t id = idesc_f16(p.a_mn, p.b_mn, kBM, p.wide);
+          const uint32_t id = idesc_f16(p.a_mn, p.b_mn, kHigh, p.wide);
           // 16 of K: 32 bytes along a row, or 16 rows of 128 bytes
           const uint32_t da = p.a_mn ? 2048 : 32, db = p.b_mn ? 2048 : 32, la = p.a_mn ? 8192 : 16, lb = p.b_mn ? 8192 : 16;
           for (int c = 0; c < chunks; ++c, ++chunk) {
-            const int s = stage;
-            stage = s + 1 == stages_of(p.wide) ? 0 : s + 1;
+            const int s = stage, held = p.wide / kBlocks;
+            stage = s + 1 == stages_of(held) ? 0 : s + 1;
             const uint32_t buf = chunk & 1u, to = tmem + buf * BN;
             if (chunk >= 2 && !tc::mbar_wait(&bar->taken[buf], (chunk / 2 - 1) & 1u, abort, kWaitLimitNs)) break;
             if (!tc::mbar_wait(&bar->full[s], parity >> s & 1u, abort, kWaitLimitNs)) break;
             parity ^= 1u << s;
             tc::tc_fence_after();
-            const uint32_t a0 = tc::smem_u32(smem + s * stage_bytes(p.wide)), b0 = a0 + 2 * kA, next_b = p.wide * 128;
+            const uint32_t a0 = tc::smem_u32(smem + s * stage_bytes(held)), b0 = a0 + 2 * kA, next_b = held * 128;
             // the small products first: what the sum of the large ones is rounded by does not grow with them
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) {
               const uint64_t ah = tile_desc(a0 + kk * da, la, 1024), al = tile_desc(a0 + kA + kk * da, la, 1024);
               const uint64_t bh = tile_desc(b0 + kk * db, lb, 1024), bl = tile_desc(b0 + next_b + kk * db, lb, 1024);
-              tc::mma_ss(to, al, bh, id, kk > 0);
-              tc::mma_ss(to, ah, bl, id, 1u);
+              mma<PAIR>(to, al, bh, id, kk > 0);
+              mma<PAIR>(to, ah, bl, id, 1u);
             }
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk)
-              tc::mma_ss(to, tile_desc(a0 + kk * da, la, 1024), tile_desc(b0 + kk * db, lb, 1024), id, 1u);
-            tc::mma_commit(&bar->empty[s]);
-            tc::mma_commit(&bar->sums[buf]);
+              mma<PAIR>(to, tile_desc(a0 + kk * da, la, 1024), tile_desc(b0 + kk * db, lb, 1024), id, 1u);
+            commit<PAIR>(&bar->empty[s]);
+            commit<PAIR>(&bar->sums[buf]);
           }
         }
         __syncwarp();
@@ -535,18 +597,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant_
   }
   // on the way out after a wait that gave up: nothing may land when the block has left
   if (warp == kIssuer && lane == 0) {
-    tc::mma_commit(&bar->drained);
+    if (rank == 0) commit<PAIR>(&bar->drained);
     wait_landed(&bar->drained, 0);
   }
-  if (warp == kProducer && lane == 0 && *abort)
+  if (warp == kProducer && lane == 0 && *abort && rank == 0)     // those of both blocks signal here
     for (int s = 0; s < 3; ++s)
       if (used >> s & 1u) wait_landed(&bar->full[s], (parity >> s & 1u) ^ 1u);
   tc::tc_fence_before();
   __syncthreads();
+  if constexpr (PAIR) tc::cluster_sync();    // neither leaves while the other's memory is asked for
   if (tid == 0 && bar->abort) *a.error = AUV_ERR_TIMEOUT;
   if (warp == kIssuer) {
     tc::tc_fence_after();
-    tc::tmem_dealloc(tmem, 2 * BN);
+    dealloc<PAIR>(tmem, 2 * BN);
   }
 }
 
@@ -642,23 +705,34 @@ int check(const net_ortho* p) {
   return AUV_OK;
 }
 
-template <int BN>
+template <int BN, bool PAIR>
 cudaError_t launch_products(const Steps& a, cudaStream_t s) {
-  const auto kern = k_products<BN>;
+  const auto kern = k_products<BN, PAIR>;
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
   if (e != cudaSuccess) return e;
   // the blocks wait for each other: all of them, one an SM, or none; no more than the largest product has tiles
-  const int64_t tiles = (int64_t)std::max(tiles_of(kX, a.M, a.N, a.tile[2]), tiles_of(kP, a.s, a.s, std::min(a.tile[0], a.tile[1]))) * a.L;
+  const int blocks = PAIR ? 2 : 1, high = blocks * kBM;
+  const int64_t tiles =
+      (int64_t)std::max(tiles_of(kX, a.M, a.N, high, a.tile[2]), tiles_of(kP, a.s, a.s, high, std::min(a.tile[0], a.tile[1]))) * a.L;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)std::min<int64_t>(sm_count(), std::max<int64_t>(1, tiles)));
+  cfg.gridDim = dim3((unsigned)(std::min<int64_t>(sm_count() / blocks, std::max<int64_t>(1, tiles)) * blocks));
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = kSmem;
   cfg.stream = s;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeCooperative;
   attr[0].val.cooperative = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = blocks;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = PAIR ? 2 : 1;
+  if (PAIR) {                                // as many pairs as the device holds at a time: an SM may lie apart
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess) cudaGetLastError();
+    if (n < 1) return cudaErrorInvalidConfiguration;
+    cfg.gridDim.x = std::min<unsigned>(cfg.gridDim.x, 2u * (unsigned)n);
+  }
   return cudaLaunchKernelEx(&cfg, kern, a);
 }
 
@@ -691,18 +765,28 @@ cudaError_t launch(const net_ortho* a, const Space& z, cudaStream_t s) {
     ok = make_map(&p.x_rows[i], at, a->N, a->M, z.ldx, a->L, kBM) && make_map(&p.x_cols[i], at, a->N, a->M, z.ldx, a->L, kBK);
   }
   if (!ok) return cudaErrorInvalidValue;
-  // Columns of a tile: 256 read less of shared memory for a product (64 of K: 1.3 us, 128 columns 0.7) and take longer to
-  // store (4.5 us, 2.5), and their rounds over the SMs are fewer and coarser.
+  // Tiles: 128 x 256 read less of shared memory for a product than 128 x 128 (64 of K: 1.3 us of an SM, 0.7) and take longer to
+  // store (4.5 us, 2.5), pairs of blocks on 256 x 256 read less still (1.0 us for both); the larger, the fewer and coarser are the
+  // rounds over the SMs.  Of one form all three products of a step are, wide or narrow is each.
   const int kinds[3] = {kP, kQ, kX};
+  double alone = 0.0, paired = 0.0;
   for (int k = 0; k < 3; ++k) {
     const int K = k == 0 ? std::max(p.M, p.N) : p.s, rows = k < 2 ? p.s : p.M, cols = k < 2 ? p.s : p.N;
-    auto time = [&](int w) {
-      const int64_t rounds = ((int64_t)tiles_of(kinds[k], rows, cols, w) * p.L + sm_count() - 1) / sm_count();
-      return (double)rounds * ((K + kBK - 1) / kBK * (w == 256 ? 1.3 : 0.7) + (w == 256 ? 4.5 : 2.5));
+    auto time = [&](int high, int wide, double chunk, double store) {
+      const int64_t at_once = sm_count() / (high / kBM);
+      const int64_t rounds = ((int64_t)tiles_of(kinds[k], rows, cols, high, wide) * p.L + at_once - 1) / at_once;
+      return (double)rounds * ((K + kBK - 1) / kBK * chunk + store);
     };
-    p.tile[k] = time(256) < time(128) ? 256 : 128;
+    const double wide = time(kBM, 256, 1.3, 4.5), narrow = time(kBM, 128, 0.7, 2.5);
+    p.tile[k] = wide < narrow ? 256 : 128;
+    alone += std::min(wide, narrow);
+    paired += time(2 * kBM, 256, 1.0, 4.5);
   }
-  return p.tile[0] + p.tile[1] + p.tile[2] > 3 * 128 ? launch_products<256>(p, s) : launch_products<128>(p, s);
+  if (paired < alone) {
+    p.tile[0] = p.tile[1] = p.tile[2] = 256;
+    return launch_products<256, true>(p, s);
+  }
+  return p.tile[0] + p.tile[1] + p.tile[2] > 3 * 128 ? launch_products<256, false>(p, s) : launch_products<128, false>(p, s);
 }
 
 int run(const net_ortho* p, void* stream) {

@@ -337,6 +337,13 @@ def test_update_large():
     _check_ortho(2, 1100, 600, "bf16", seed=2)
 
 
+@pytest.mark.parametrize("L,M,N,dt,layout", [(24, 512, 640, "fp32", "flat"), (20, 700, 400, "bf16", "pad"), (24, 515, 1000, "fp32", "odd"),
+                                             (24, 1000, 515, "fp16", "odd"), (20, 512, 1024, "fp32", "flat")])
+def test_update_of_stacks(L, M, N, dt, layout):
+    """Enough tiles for pairs of blocks, whole and ragged, either way round."""
+    _check_ortho(L, M, N, dt, layout, seed=L)
+
+
 def test_update_of_zeros_and_of_nothing():
     torch, nets, _ = _t()
     z = torch.zeros(2, 10, 20, device="cuda")
