@@ -508,7 +508,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant_
             } else {
               __half* const out = p.kind == kP ? a.P : p.kind == kQ ? a.Q : a.x[in ^ 1];
               const int ld = p.kind == kX ? a.ldx : a.lds;
-              store_block<BN == 128 ? 4 : 1>(a, p, out, ld, l, r0, col, p.kind != kX && col < r0, turn, lane);
+              store_block<4>(a, p, out, ld, l, r0, col, p.kind != kX && col < r0, turn, lane);
             }
             __syncwarp();
           }
