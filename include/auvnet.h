@@ -318,6 +318,7 @@ int net_select_scan_backward(const net_select* a, void* stream);
  * steps an update's singular values come to lie about 1.  Where M > N the
  * products are x (b P + c P P) with P = x^T x, the same polynomial.  Norms are
  * taken in range whatever the scale of x.  steps = 0: y = x / (|x| + eps).
+ * y may be x.  A matrix with a value that is not finite comes out as NaN.
  *
  * The products are taken of two fp16 pieces of every value (22 bits) with sums
  * in fp32, so the coefficients have to keep what is between them in fp16's

@@ -447,6 +447,14 @@ __global__ void k_select_none(int64_t m, const float* from, float* to) {
   if (i < m) to[i] = from ? from[i] : 0.0f;
 }
 
+// No channels: sums over nothing.
+template <typename T>
+__global__ void k_select_no_channels(net_rows r, int64_t T_, int64_t N, int64_t k) {
+  const int64_t step = gridDim.x * (int64_t)256;
+  for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < T_ * N * k; i += step)
+    from_float(0.0f, *const_cast<T*>(row_at<T>(r, i / (N * k), i / k % N, i % k)));
+}
+
 template <typename T, typename L, bool FOLD>
 cudaError_t launch_walk(const Select& a, cudaStream_t s) {
   const int64_t warps = a.N * a.G * a.tiles * a.pieces;
@@ -550,10 +558,22 @@ size_t lay_out(Select& a, bool back, char* at) {
 int run(const net_select* p, bool back, void* stream) {
   int rc = check(p);
   if (rc) return rc;
-  if (p->D == 0 || (p->N == 0 && !back)) return AUV_OK;
   const int z = type_size(p->dtype);
-  const bool gate = p->gate.data != nullptr;
   const int64_t GS = p->G * p->S;
+  if (p->D == 0) {
+    const int64_t all = back ? p->T * p->N * GS : 0;
+    const net_rows* const sums[] = {&p->dB, &p->dC};
+    for (int i = 0; i < 2 && all; ++i) {
+      if ((rc = need_rows(*sums[i], i ? "dC" : "dB", p->T, p->N, GS, z, true))) return rc;
+      const unsigned blocks = (unsigned)std::min<int64_t>((all + 255) / 256, 65535);
+      if (z == 4) k_select_no_channels<float><<<blocks, 256, 0, static_cast<cudaStream_t>(stream)>>>(*sums[i], p->T, p->N, GS);
+      else k_select_no_channels<__half><<<blocks, 256, 0, static_cast<cudaStream_t>(stream)>>>(*sums[i], p->T, p->N, GS);
+    }
+    const cudaError_t e = all ? cudaGetLastError() : cudaSuccess;
+    return e == cudaSuccess ? AUV_OK : cuda_fail(e, "net_select_scan_backward");
+  }
+  if (p->N == 0 && !back) return AUV_OK;
+  const bool gate = p->gate.data != nullptr;
   struct { const net_rows* r; const char* name; bool out, used; int64_t k; } rows[] = {
       {&p->x, "x", false, true, p->D},        {&p->dt, "dt", false, true, p->D},   {&p->gate, "gate", false, gate, p->D},
       {&p->B, "B", false, true, GS},          {&p->C, "C", false, true, GS},       {&p->y, "y", true, !back, p->D},

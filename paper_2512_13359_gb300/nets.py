@@ -42,6 +42,7 @@ _CONV = struct.Struct("@4I4q" + 4 * _ROWS + "11PN")
 _SELECT = struct.Struct("@II5q" + 12 * _ROWS + "14PN")
 _ORTHO = struct.Struct("@3I4fI3q" + 2 * _ROWS + "PN")
 _NO_ROWS = (0, 0, 0)
+_NO_GRADIENTS = 6 * _NO_ROWS
 
 _lib = None
 
@@ -84,7 +85,7 @@ def _call(fn, args, index, stream, scratch):
             stream.wait_stream(current)
             for t in scratch:
                 t.record_stream(stream)
-    if index == torch.cuda.current_device():
+    if index == torch._C._cuda_getDevice():
         rc = fn(args, handle)
     else:
         with torch.cuda.device(index):
@@ -333,9 +334,12 @@ def causal_conv(x, w, bias=None, state=None, *, done=None, done_prev=None, act="
     if new_state is None:
         new_state = _new(states, dtype, index, scratch)
     fields = (_CONV.size, NET_DTYPE[dtype], NET_ACT[act], 0, T, N, D, K, *_rows(x, "x", like), *_rows(y, "y", like), *_NO_ROWS,
-              *_NO_ROWS, _flat(w, "w", (K, D), torch.float32, index), _flat(bias, "bias", (D,), torch.float32, index),
-              _flat(state, "state", states, dtype, index), _flat(new_state, "new_state", states, dtype, index), 0, 0, 0, 0,
-              _flags(done, "done", (T, N), index), _flags(done_prev, "done_prev", (N,), index))
+              *_NO_ROWS, _flat(w, "w", (K, D), torch.float32, index),
+              0 if bias is None else _flat(bias, "bias", (D,), torch.float32, index),
+              0 if state is None else _flat(state, "state", states, dtype, index),
+              _flat(new_state, "new_state", states, dtype, index), 0, 0, 0, 0,
+              0 if done is None else _flags(done, "done", (T, N), index),
+              0 if done_prev is None else _flags(done_prev, "done_prev", (N,), index))
     _call_packed(lib().net_causal_conv, _CONV, fields, index, stream, scratch)
     return y, new_state
 
@@ -406,10 +410,13 @@ def select_scan(x, dt, A, B, C, *, skip=None, dt_bias=None, gate=None, h0=None, 
         kept = _new(kept_shape, f32, index, scratch)
     fields = (_SELECT.size, NET_DTYPE[dtype], T, N, D, S, G, *_rows(x, "x", like), *_rows(dt, "dt", like),
               *(_NO_ROWS if gate is None else _rows(gate, "gate", like)), *_rows(y, "y", like), *_rows(B, "B", rows),
-              *_rows(C, "C", rows), *(6 * _NO_ROWS), _flat(A, "A", (D, S), f32, index), _flat(skip, "skip", (D,), f32, index),
-              _flat(dt_bias, "dt_bias", (D,), f32, index), _flat(h0, "h0", states, f32, index),
-              _flat(hT, "hT", states, f32, index), _flat(kept, "kept", kept_shape, f32, index), 0, 0, 0, 0, 0,
-              _flags(done, "done", (T, N), index), _flags(done_prev, "done_prev", (N,), index))
+              *_rows(C, "C", rows), *_NO_GRADIENTS, _flat(A, "A", (D, S), f32, index),
+              0 if skip is None else _flat(skip, "skip", (D,), f32, index),
+              0 if dt_bias is None else _flat(dt_bias, "dt_bias", (D,), f32, index),
+              0 if h0 is None else _flat(h0, "h0", states, f32, index), _flat(hT, "hT", states, f32, index),
+              0 if kept is None else _flat(kept, "kept", kept_shape, f32, index), 0, 0, 0, 0, 0,
+              0 if done is None else _flags(done, "done", (T, N), index),
+              0 if done_prev is None else _flags(done_prev, "done_prev", (N,), index))
     L = lib()
     if T < 128:                       # short sequences need no workspace
         _call_packed(L.net_select_scan, _SELECT, fields, index, stream, scratch)
@@ -461,7 +468,7 @@ def select_scan_backward(x, dt, A, B, C, kept, dy, *, skip=None, dt_bias=None, g
 def orthogonalise(x, steps=5, *, coef=(3.4445, -4.775, 2.0315), eps=1e-7, y=None, stream=None):
     """Each of the matrices x [L, M, N] with its singular values v, over their norm, taken `steps` times through
     a v + b v^3 + c v^5 (coef): with the usual coefficients and five steps they come to lie about 1, and the singular
-    vectors stay.  Returns y [L, M, N] of x's type."""
+    vectors stay.  Returns y [L, M, N] of x's type; y may be x."""
     scratch = []
     shape, dtype, index = like = _activation(x, "x")
     if y is None:

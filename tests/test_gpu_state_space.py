@@ -229,6 +229,16 @@ def test_scan_without_steps_or_envs():
     assert not nets.select_scan_backward(z, z, A, b, b, kept, z)[2].any()
 
 
+def test_scan_without_channels():
+    torch, nets, types = _t()
+    for dt in DT:
+        z, b = torch.empty(3, 2, 0, device="cuda", dtype=types[dt]), torch.ones(3, 2, 8, device="cuda", dtype=types[dt])
+        A, dB, dC = torch.empty(0, 4, device="cuda"), torch.ones_like(b), torch.ones(3, 2, 16, device="cuda", dtype=types[dt])[..., 8:]
+        y, _, kept = nets.select_scan(z, z, A, b, b, kept=True)
+        nets.select_scan_backward(z, z, A, b, b, kept, y, dB=dB, dC=dC)
+        assert not dB.any() and not dC.any()
+
+
 @pytest.mark.parametrize("T", [6, 400])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 def test_nothing_of_an_ended_episode_passes(T, bad):
@@ -353,6 +363,38 @@ def test_update_of_zeros_and_of_nothing():
     assert not y[0].any() and torch.isnan(y[1]).all()
     for shape in ((0, 4, 4), (2, 0, 4), (2, 4, 0)):
         assert nets.orthogonalise(torch.zeros(shape, device="cuda")).shape == shape
+
+
+def test_update_in_place_and_of_infinite_values():
+    torch, nets, types = _t()
+    g = torch.Generator(device="cuda").manual_seed(4)
+    for steps in (0, 1, 5):
+        for dt in DT:
+            x = torch.randn(3, 40, 60, device="cuda", generator=g).to(types[dt])
+            want = nets.orthogonalise(x, steps)
+            assert nets.orthogonalise(x, steps, y=x) is x and torch.equal(x, want)
+    x = torch.randn(2, 40, 60, device="cuda", generator=g)
+    x[1, 3, 7] = float("inf")
+    y = nets.orthogonalise(x)
+    assert torch.isfinite(y[0]).all() and torch.isnan(y[1]).all()
+
+
+def test_updates_on_two_streams_at_once():
+    """Each takes the whole device and its blocks wait for one another."""
+    torch, nets, _ = _t()
+    g = torch.Generator(device="cuda").manual_seed(5)
+    xs = [torch.randn(24, 512, 640, device="cuda", generator=g), torch.randn(3, 900, 1100, device="cuda", generator=g)]
+    want = [nets.orthogonalise(x) for x in xs]
+    torch.cuda.synchronize()
+    low, high = torch.cuda.Stream(), torch.cuda.Stream(priority=-1)
+    got = []
+    for _ in range(4):
+        for x, s in zip(xs, (low, high)):
+            with torch.cuda.stream(s):
+                got.append((nets.orthogonalise(x), torch.randn(2048, 2048, device="cuda") @ torch.randn(2048, 2048, device="cuda")))
+    torch.cuda.synchronize()
+    for i, (y, _) in enumerate(got):
+        assert torch.equal(y, want[i % 2])
 
 
 def test_update_of_many_small_ones():
