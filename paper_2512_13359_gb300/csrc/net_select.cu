@@ -25,27 +25,28 @@ constexpr int kBatch = 4;       // steps whose inputs are on their way while as 
 // passes through).
 template <typename T, typename L, bool FOLD>
 __global__ void __launch_bounds__(32 * kWarps, L::OWN > 1 ? 3 : L::SP == 8 ? 4 : 6) k_select(Select a) {
-  constexpr int SP = L::SP, LS = L::LS, CC = L::CC, SW = L::SW, OWN = L::OWN, kSides = CC / OWN;
-  using In = Staged<T, SW, kBatch>;
+  constexpr int SP = L::SP, LS = L::LS, CC = L::CC, SW = L::SW, OWN = L::OWN, kSides = CC / OWN, R = L::R, RL = L::RL;
+  using In = Staged<T, SW, kBatch, RL>;
   using W = Raw<T, OWN>;
-  __shared__ __align__(16) float rows[kWarps][FOLD ? 1 : 2][kBatch * SW];
+  __shared__ __align__(16) float rows[kWarps][FOLD ? 1 : 2][R][kBatch * SW];
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   int64_t id = blockIdx.x * (int64_t)kWarps + warp;
-  const int64_t envs_groups = a.N * a.G;
+  const int64_t envs_groups = (a.N * a.G + R - 1) / R;         // rows, or fours of them
   if (id >= envs_groups * a.tiles * a.pieces) return;
-  const int tile = (int)(id % a.tiles);
+  const int tile = (int)(id % a.tiles), side = lane / RL, mine = lane % RL;
   id /= a.tiles;
-  const int g = (int)(id % a.G);
-  id /= a.G;
-  const int64_t n = id % a.N;
-  const int piece = (int)(id / a.N);
-  float* const Bs = rows[warp][0];
-  float* const Cs = rows[warp][FOLD ? 0 : 1];
+  const int64_t row = id % envs_groups * R + side;
+  const bool row_there = R == 1 || row < a.N * a.G;
+  const int g = row_there ? (int)(row % a.G) : 0;
+  const int64_t n = row_there ? row / a.G : 0;
+  const int piece = (int)(id / envs_groups);
+  float* const Bs = rows[warp][0][side];
+  float* const Cs = rows[warp][FOLD ? 0 : 1][side];
 
-  const int q = lane % LS, s0 = q * SP;
-  const int first = tile * L::CW + lane / LS * CC;            // in the group
+  const int q = mine % LS, s0 = q * SP;
+  const int first = tile * L::CW + mine / LS * CC;            // in the group
   const int own = first + q % kSides * OWN;
-  const bool live = own < a.per, writes = live && q < kSides;   // OWN = 2: channels of a group are even in number
+  const bool live = row_there && own < a.per, writes = live && q < kSides;   // OWN = 2: channels of a group are even in number
   const int64_t d = (int64_t)g * a.per + own;                 // own channels
   int64_t at[CC], at_weight[CC];
   bool there[CC];
@@ -54,7 +55,7 @@ __global__ void __launch_bounds__(32 * kWarps, L::OWN > 1 ? 3 : L::SP == 8 ? 4 :
     const int k = first + (q % kSides ^ c / OWN) * OWN + c % OWN;
     at_weight[c] = (int64_t)g * a.per + k;
     at[c] = n * a.D + at_weight[c];
-    there[c] = k < a.per;
+    there[c] = row_there && k < a.per;
   }
   const int t0 = piece * a.piece, t1 = min(a.T, t0 + a.piece);
   const int64_t states = a.N * a.D * a.S;
@@ -63,9 +64,9 @@ __global__ void __launch_bounds__(32 * kWarps, L::OWN > 1 ? 3 : L::SP == 8 ? 4 :
   const T* pdt = row_at<T>(a.dt, t0, n, d);
   const T* pgate = gated ? row_at<T>(a.gate, t0, n, d) : px;
   T* py = FOLD ? nullptr : const_cast<T*>(row_at<T>(a.y, t0, n, d));
-  const int64_t in_row = (int64_t)g * a.S + lane % In::kSide;
-  const T* pB = row_at<T>(a.B, t0 + lane / In::kSide, n, in_row);
-  const T* pC = row_at<T>(a.C, t0 + lane / In::kSide, n, in_row);
+  const int64_t in_row = (int64_t)g * a.S + mine % In::kSide;
+  const T* pB = row_at<T>(a.B, t0 + mine / In::kSide, n, in_row);
+  const T* pC = row_at<T>(a.C, t0 + mine / In::kSide, n, in_row);
   W rx[kBatch], rdt[kBatch], rgate[kBatch];
   In rB, rC;
   uint8_t rend = 0;
@@ -74,9 +75,9 @@ __global__ void __launch_bounds__(32 * kWarps, L::OWN > 1 ? 3 : L::SP == 8 ? 4 :
   auto fetch = [&](int t) {
     const int steps = t1 - t;
     if (steps <= 0) return;
-    rend = flagged && lane < min(kBatch, steps) ? flag_at(a, t + lane, n) : (uint8_t)0;
-    rB.load(pB, a.B.outer, steps, a.S, lane);
-    if constexpr (!FOLD) rC.load(pC, a.C.outer, steps, a.S, lane);
+    rend = flagged && mine < min(kBatch, steps) ? flag_at(a, t + mine, n) : (uint8_t)0;
+    rB.load(pB, a.B.outer, steps, a.S, mine);
+    if constexpr (!FOLD) rC.load(pC, a.C.outer, steps, a.S, mine);
     if (all_live && steps >= kBatch) {
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) rx[k] = get(px, k * a.x.outer), rdt[k] = get(pdt, k * a.dt.outer);
@@ -132,9 +133,9 @@ __global__ void __launch_bounds__(32 * kWarps, L::OWN > 1 ? 3 : L::SP == 8 ? 4 :
   for (int ts = t0; ts < t1; ts += kBatch) {
     const int steps = t1 - ts;
     __syncwarp();                                             // the last batch's rows are read
-    rB.put(Bs, lane);
-    if constexpr (!FOLD) rC.put(Cs, lane);
-    const uint32_t ends = flagged ? __ballot_sync(0xffffffffu, rend != 0) : 0u;
+    rB.put(Bs, mine);
+    if constexpr (!FOLD) rC.put(Cs, mine);
+    const uint32_t any_ends = flagged ? __ballot_sync(0xffffffffu, rend != 0) : 0u, ends = any_ends >> (side * RL % 32);
     float x[kBatch][OWN], e[kBatch][OWN], z[kBatch][OWN];
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
@@ -208,7 +209,7 @@ __global__ void __launch_bounds__(32 * kWarps, L::OWN > 1 ? 3 : L::SP == 8 ? 4 :
         }
       }
     };
-    if (steps >= kBatch && !ends) walk(std::true_type());
+    if (steps >= kBatch && !any_ends) walk(std::true_type());
     else walk(std::false_type());
     py += kBatch * a.y.outer;
   }
@@ -224,22 +225,23 @@ __global__ void __launch_bounds__(32 * kWarps, L::OWN > 1 ? 3 : L::SP == 8 ? 4 :
 }
 
 // The states before the pieces (backward: their gradients behind the pieces), in the place of the pieces' own.  A block has
-// eight states and all pieces: each of its 64 groups of eight lanes folds adjacent pieces to one, those are joined over the
-// block, and the groups go through their pieces once more from the state they begin with (293 pieces of 4,000 states: 40 us
-// by one thread a state).  The product of a piece's decays is kept from 0: an infinite state does not become NaN by a long
+// some states and all pieces: each of its groups of threads folds adjacent pieces to one, those are joined over the block, and
+// the groups go through their pieces once more from the state they begin with.  293 pieces of 4,000 states: 12 us in 64 groups,
+// 40 by one thread a state, which is enough for a few pieces.  The product of a piece's decays is kept from 0: an infinite state does not become NaN by a long
 // piece.
-constexpr int kJoin = 512, kJoinStates = 8, kJoinGroups = kJoin / kJoinStates, kJoinAhead = 4;
+constexpr int kJoin = 512, kJoinGroups = 64, kJoinAhead = 4;
 __device__ __forceinline__ float decay_of(float A2, float sum) { return fmaxf(ex2(A2 * sum), 1.17549435e-38f); }
-__global__ void __launch_bounds__(kJoin) k_select_join(Select a, bool back) {
-  __shared__ float sums[kJoinGroups][kJoinStates], owns[kJoinGroups][kJoinStates];
+__global__ void __launch_bounds__(kJoin) k_select_join(Select a, bool back, int groups) {
+  __shared__ float sums[kJoin], owns[kJoin];
   after_previous();
-  const int64_t m = a.N * a.D * a.S, i = blockIdx.x * (int64_t)kJoinStates + threadIdx.x % kJoinStates;
-  const int k = threadIdx.x % kJoinStates, group = threadIdx.x / kJoinStates;
+  const int side = kJoin / groups;                              // states of the block
+  const int k = threadIdx.x % side, group = threadIdx.x / side;
+  const int64_t m = a.N * a.D * a.S, i = blockIdx.x * (int64_t)side + k;
   const bool live = i < m;
   const int64_t nd = live ? i / a.S : 0, all = a.N * a.D;
   const float A2 = live ? a.A[nd % a.D * a.S + i % a.S] * kLog2e : 0.0f;
   // pieces in the chain's order: backward the last one first
-  const int each = (a.pieces + kJoinGroups - 1) / kJoinGroups, p0 = min(a.pieces, group * each);
+  const int each = (a.pieces + groups - 1) / groups, p0 = min(a.pieces, group * each);
   const int n = live ? min(a.pieces, p0 + each) - p0 : 0;
   const int64_t first = back ? a.pieces - 1 - p0 : p0, by = back ? -1 : 1;
   float total = 0.0f, state = 0.0f;
@@ -261,21 +263,21 @@ __global__ void __launch_bounds__(kJoin) k_select_join(Select a, bool back) {
         }
     }
   };
-  through(false);
-  sums[group][k] = total, owns[group][k] = state;
+  if (groups > 1) through(false);
+  sums[threadIdx.x] = total, owns[threadIdx.x] = state;
   __syncthreads();
   if (group == 0) {
     const float* const from = back ? a.dhT : a.h0;
     float h = live && from ? from[i] : 0.0f;
 #pragma unroll 4
-    for (int q = 0; q < kJoinGroups; ++q) {
-      const float sum = sums[q][k], own = owns[q][k];
-      owns[q][k] = h;
+    for (int q = 0; q < groups; ++q) {
+      const float sum = sums[q * side + k], own = owns[q * side + k];
+      owns[q * side + k] = h;
       h = sum < 0.0f ? own : fmaf(decay_of(A2, sum), h, own);
     }
   }
   __syncthreads();
-  state = owns[group][k];
+  state = owns[threadIdx.x];
   through(true);
 }
 
@@ -462,7 +464,7 @@ __global__ void k_select_no_channels(net_rows r, int64_t T_, int64_t N, int64_t 
 
 template <typename T, typename L, bool FOLD>
 cudaError_t launch_walk(const Select& a, cudaStream_t s) {
-  const int64_t warps = a.N * a.G * a.tiles * a.pieces;
+  const int64_t warps = (a.N * a.G + L::R - 1) / L::R * a.tiles * a.pieces;
   const dim3 grid((unsigned)((warps + kWarps - 1) / kWarps));
   if (!FOLD && a.pieces > 1) return launch_after(k_select<T, L, FOLD>, grid, 32 * kWarps, 0, s, a);
   k_select<T, L, FOLD><<<grid, 32 * kWarps, 0, s>>>(a);
@@ -481,6 +483,7 @@ cudaError_t launch_all(const Select& a, cudaStream_t s) {
 
 template <typename T>
 cudaError_t launch(const Select& a, cudaStream_t s) {
+  if (a.rows > 1) return with_narrow_lanes(a.S, [&](auto l) { return launch_all<T, decltype(l)>(a, s); });
   if (a.wide) return with_wide_lanes(a.S, [&](auto l) { return launch_all<T, decltype(l)>(a, s); });
   return with_lanes(a.S, [&](auto l) {
     using L = decltype(l);
@@ -535,6 +538,9 @@ Select of(const net_select* p, bool back, bool narrow = false) {
   for (const net_rows* r : rows) pairs = pairs && aligned(*r, a.T, a.N, z, 2);
   a.wide = pairs && a.N * a.G * tiles >= (int64_t)sm_count() * 12;
   if (a.wide) a.tiles = tiles;
+  // narrow groups: lanes that would be idle take other rows (TALL)
+  a.rows = (back || a.T > 1) && a.per <= kNarrow && a.S <= kMostWide ? kSide4 : 1;
+  if (a.rows > 1) a.wide = false, a.tiles = 1;
   select_pieces(a, back);
   return a;
 }
@@ -635,7 +641,7 @@ int run(const net_select* p, bool back, void* stream) {
 }  // namespace
 
 void select_pieces(Select& a, bool back) {
-  const int64_t warps = a.N * a.G * a.tiles, want = (int64_t)sm_count() * (!back ? 16 : a.S <= 8 ? 12 : 8);
+  const int64_t warps = (a.N * a.G + a.rows - 1) / a.rows * a.tiles, want = (int64_t)sm_count() * (!back ? 16 : a.S <= 8 ? 12 : 8);
   int64_t pieces = std::min(want / std::max<int64_t>(1, warps), (int64_t)a.T / 64);
   if (pieces < 2) pieces = 1;
   const int64_t piece = pieces == 1 ? a.T : ((a.T + pieces - 1) / pieces + kKeep - 1) / kKeep * kKeep;
@@ -645,7 +651,10 @@ void select_pieces(Select& a, bool back) {
 
 cudaError_t launch_select_join(const Select& a, bool back, cudaStream_t s) {
   const int64_t m = a.N * a.D * a.S;
-  return launch_after(k_select_join, dim3((unsigned)((m + kJoinStates - 1) / kJoinStates)), kJoin, 0, s, a, back);
+  int groups = 1;
+  while (groups < kJoinGroups && a.pieces > 4 * groups) groups *= 2;
+  const int side = kJoin / groups;
+  return launch_after(k_select_join, dim3((unsigned)((m + side - 1) / side)), kJoin, 0, s, a, back, groups);
 }
 
 }  // namespace net

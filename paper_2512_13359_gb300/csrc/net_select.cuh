@@ -19,6 +19,7 @@ struct Select {
   int piece, pieces;            // steps of a piece of the sequence, multiples of kKeep
   int tiles;                    // warps that a group's channels take
   bool wide;                    // forward: twice as many channels a lane
+  int rows;                     // (env, group) pairs of a warp
   int64_t N, D;
   net_rows x, dt, gate, y, B, C, dy, dx, ddt, dgate, dB, dC;
   const float *A, *skip, *dt_bias, *h0;
@@ -171,9 +172,9 @@ __device__ __forceinline__ void store_states(float* p, const int64_t (&at)[CC], 
 }
 
 // The rows of B or C of up to 16 steps from t on, into [16][SW] fp32, zeros past S.
-template <typename T, int SW>
+template <typename T, int SW, int RL>
 __device__ __forceinline__ void stage(const Select& a, const net_rows& r, int t, int steps, int64_t n, int g, int lane, float* to) {
-  constexpr int kSide = SW < 32 ? SW : 32, kRows = 32 / kSide;        // a lane's state stays, its rows are kRows apart
+  constexpr int kSide = SW < RL ? SW : RL, kRows = RL / kSide;        // a lane's states stay, its rows are kRows apart
   const int s = lane % kSide, k = lane / kSide;
   const T* p = row_at<T>(r, t + k, n, (int64_t)g * a.S + s);
   const int64_t by = kRows * r.outer;
@@ -181,15 +182,16 @@ __device__ __forceinline__ void stage(const Select& a, const net_rows& r, int t,
   for (int j = 0; j < kKeep / kRows; ++j) {
 #pragma unroll
     for (int i = 0; i < SW / kSide; ++i)
-      to[(k + j * kRows) * SW + s + i * 32] = k + j * kRows < steps && s + i * 32 < a.S ? to_float(p[i * 32]) : 0.0f;
+      to[(k + j * kRows) * SW + s + i * kSide] = k + j * kRows < steps && s + i * kSide < a.S ? to_float(p[i * kSide]) : 0.0f;
     p += by;
   }
 }
 
 // The same for STEPS steps, in two parts: the loads, of a lane's values, and their way into shared memory.
-template <typename T, int SW, int STEPS>
+// RL: lanes that a row's states are loaded by.
+template <typename T, int SW, int STEPS, int RL = 32>
 struct Staged {
-  static constexpr int kSide = SW < 32 ? SW : 32, kRows = 32 / kSide;
+  static constexpr int kSide = SW < RL ? SW : RL, kRows = RL / kSide;
   static constexpr int kDown = (STEPS + kRows - 1) / kRows, kAcross = SW / kSide;
   T v[kDown][kAcross];
   __device__ __forceinline__ void load(const T* p, int64_t by, int steps, int S, int lane) {   // p: the lane's first value
@@ -199,7 +201,7 @@ struct Staged {
 #pragma unroll
       for (int i = 0; i < kAcross; ++i) {
         from_float(0.0f, v[j][i]);
-        if (k + j * kRows < steps && s + i * 32 < S) v[j][i] = p[i * 32];
+        if (k + j * kRows < steps && s + i * kSide < S) v[j][i] = p[i * kSide];
       }
       p += kRows * by;
     }
@@ -210,7 +212,7 @@ struct Staged {
     for (int j = 0; j < kDown; ++j)
       if (STEPS % kRows == 0 || k + j * kRows < STEPS) {
 #pragma unroll
-        for (int i = 0; i < kAcross; ++i) to[(k + j * kRows) * SW + s + i * 32] = to_float(v[j][i]);
+        for (int i = 0; i < kAcross; ++i) to[(k + j * kRows) * SW + s + i * kSide] = to_float(v[j][i]);
       }
   }
 };
@@ -227,11 +229,20 @@ __device__ __forceinline__ void load_pairs(const float* p, F2 (&v)[SP / 2]) {
 }
 
 // How S states are laid over lanes.
-template <int SP_, int LS_, int CC_, int OWN_ = 1> struct Lanes {
+// R: envs (with the same group, or groups) that a warp has side by side, of narrow groups, RL lanes each.
+template <int SP_, int LS_, int CC_, int OWN_ = 1, int R_ = 1> struct Lanes {
   static constexpr int SP = SP_, LS = LS_, CC = CC_, OWN = OWN_;   // CC: OWN, or twice that
+  static constexpr int R = R_, RL = 32 / R;
   static constexpr int SW = SP * LS;          // states, padded
-  static constexpr int CW = 32 / LS * CC;     // channels of a warp
+  static constexpr int CW = RL / LS * CC;     // channels of a warp, or of a row of it
 };
+constexpr int kNarrow = 8, kSide4 = 4;         // groups of up to 8 channels, of up to 16 states: four rows a warp
+template <typename F>
+cudaError_t with_narrow_lanes(int S, F f) {
+  if (S <= 4) return f(Lanes<4, 1, 1, 1, kSide4>());
+  if (S <= 8) return f(Lanes<8, 1, 1, 1, kSide4>());
+  return f(Lanes<8, 2, 2, 1, kSide4>());
+}
 template <typename F>
 cudaError_t with_lanes(int S, F f) {
   if (S <= 4) return f(Lanes<4, 1, 1>());

@@ -24,21 +24,23 @@ namespace {
 constexpr int kHeld = 2, kSub = 4;
 
 // Warps of a block: shared memory grows with the padded states.
-constexpr int back_warps(int padded) { return padded <= 8 ? 4 : padded <= 16 ? 8 : padded <= 64 ? 4 : 2; }
+constexpr int back_warps(int padded, int rows) {
+  return rows > 1 ? 5 : padded <= 8 ? 4 : padded <= 16 ? 8 : padded <= 64 ? 4 : 2;
+}
 // Blocks of an SM: of up to 8 states a lane has one channel's, and three blocks of four warps fit (8,192 steps of 3 x 200
 // channels x 8 fp16: 147 us, 200 with one block of eight).
-constexpr int back_blocks(int padded) { return padded <= 8 ? 3 : 1; }
+constexpr int back_blocks(int padded, int rows) { return padded > 8 ? 1 : rows > 1 ? 2 : 3; }
 
 // A warp's shared memory.  What multiplies pairs of states is there twice: copies in registers took a twelfth of all
 // instructions.
 template <typename L> struct Back {
-  float B[kKeep][L::SW], C[kKeep][L::SW];
+  float B[L::R][kKeep][L::SW], C[L::R][kKeep][L::SW];
   static constexpr bool kTwice = L::CC == 2;    // one channel a lane: there is room for fewer, and copies are fewer too
   float4 eu[kKeep][32];                         // of the lane's own channel e, e, e x, e x; or e, x, p, dy silu'(gate)
   float2 pp[kTwice ? kKeep : 1][32], xq[kTwice ? kKeep : 1][32];   // p, p; x, dy silu'(gate)
   float slope[kKeep][32];                       // sigmoid(dt + dt_bias)
   float4 start[kKeep / kSub - 1][L::CC * L::SP / 4][32];   // the lane's states before steps 4, 8, 12
-  float sums[kKeep][2][L::SW];                  // dB and dC over the warp's channels
+  float sums[L::R][kKeep][2][L::SW];            // dB and dC over a row's channels
 };
 
 // The order of a lane's pairs of states.  Sums over channels go over the lanes with the same q; at each level a lane keeps
@@ -47,7 +49,7 @@ template <typename L> struct Back {
 template <typename L>
 __device__ __forceinline__ int pair_order(int lane) {
   int order = 0;
-  int bit = 16;
+  int bit = L::RL / 2;
 #pragma unroll
   for (int n = L::SP / 4; n >= 1 && bit >= L::LS; n /= 2, bit /= 2) order |= lane & bit ? n : 0;
   return order;
@@ -61,7 +63,7 @@ __device__ __forceinline__ F2 other(F2 v, int bit) {
 template <typename L>
 __device__ __forceinline__ void put_sums(F2 (&v)[L::SP / 2], int lane, int order, float* to) {
   constexpr int P = L::SP / 2, LS = L::LS;
-  int n = P, bit = 16;
+  int n = P, bit = L::RL / 2;
 #pragma unroll
   for (int k = 0; k < 5; ++k)
     if (n > 1 && bit >= LS) {
@@ -169,22 +171,22 @@ __device__ __forceinline__ void prefetch(const void* p) { asm volatile("prefetch
 
 // rows: (env, group) pairs a block walks side by side, back_warps / rows warps each.
 template <typename T, typename L>
-__global__ void __launch_bounds__(32 * back_warps(L::SW), back_blocks(L::SW)) k_select_back(Select a, int rows) {
+__global__ void __launch_bounds__(32 * back_warps(L::SW, L::R), back_blocks(L::SW, L::R)) k_select_back(Select a, int rows) {
   constexpr bool kTwice = Back<L>::kTwice;
-  constexpr int SP = L::SP, LS = L::LS, CC = L::CC, SW = L::SW, P = SP / 2;
+  constexpr int SP = L::SP, LS = L::LS, CC = L::CC, SW = L::SW, P = SP / 2, R = L::R, RL = L::RL;
   extern __shared__ __align__(16) uint8_t smem[];
   Back<L>* const all = reinterpret_cast<Back<L>*>(smem);
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   Back<L>& m = all[warp];
-  const int side = back_warps(SW) / rows;                    // warps of a row
-  const int row = warp / side;
+  const int side = back_warps(SW, R) / rows;                    // warps of a row
+  const int row = warp / side, sub = lane / RL, mine = lane % RL;
   const int blocks = (a.tiles + side - 1) / side;             // blocks along a group's channels
   const int g = blockIdx.x / blocks, block = blockIdx.x % blocks;
   const int tile = block * side + warp % side;
 
-  const int q = lane % LS, s0 = q * SP, order = pair_order<L>(lane);
-  const int first = tile * L::CW + lane / LS * CC, own = first + q % CC;
-  const bool live = own < a.per, writes = live && q < CC;
+  const int q = mine % LS, s0 = q * SP, order = pair_order<L>(lane);
+  const int first = tile * L::CW + mine / LS * CC, own = first + q % CC;
+  const bool channel = own < a.per;
   const int64_t d = (int64_t)g * a.per + own;
   int64_t at_weight[CC];
   bool there[CC];
@@ -202,14 +204,14 @@ __global__ void __launch_bounds__(32 * back_warps(L::SW), back_blocks(L::SW)) k_
 #pragma unroll
     for (int i = 0; i < P; ++i) A2[c][i] = A2[c][i] * pair(kLog2e, kLog2e);
   clear(dA);
-  const float bias = live && a.dt_bias ? a.dt_bias[d] : 0.0f, skip = live && a.skip ? a.skip[d] : 0.0f;
+  const float bias = channel && a.dt_bias ? a.dt_bias[d] : 0.0f, skip = channel && a.skip ? a.skip[d] : 0.0f;
   float dskip = 0.0f, dbias = 0.0f;
   const bool gated = a.gate.data, gate_out = a.dgate.data;
-  const int64_t states = a.N * a.D * a.S, items = a.N * a.pieces;
-  float* const slot = a.weights + (blockIdx.y * (int64_t)rows + row) * a.D * (a.S + 2);
+  const int64_t states = a.N * a.D * a.S, envs = (a.N + R - 1) / R, items = envs * a.pieces;
+  float* const slot = a.weights + ((blockIdx.y * (int64_t)rows + row) * R + sub) * a.D * (a.S + 2);
   auto put_weights = [&] {
     store_ordered<SP, CC>(slot, at_weight, there, s0, order, a.S, dA);
-    if (writes) {
+    if (channel && q < CC) {
       slot[a.D * a.S + d] = dskip;
       slot[a.D * (a.S + 1) + d] = dbias;
     }
@@ -218,24 +220,33 @@ __global__ void __launch_bounds__(32 * back_warps(L::SW), back_blocks(L::SW)) k_
   for (int64_t item0 = blockIdx.y * (int64_t)rows; item0 < items; item0 += gridDim.y * (int64_t)rows) {
     const bool real = item0 + row < items;
     const int64_t item = real ? item0 + row : 0;
-    const int64_t n = item % a.N;
-    const int piece = (int)(item / a.N);
+    const int64_t env = item % envs * R + sub;
+    const bool env_there = R == 1 || env < a.N;
+    const int64_t n = env_there ? env : 0;
+    const bool live = channel && env_there, writes = live && q < CC;
+    const int piece = (int)(item / envs);
     const int t0 = piece * a.piece, t1 = real ? min(a.T, t0 + a.piece) : t0;
     const int segments = (min(a.T, a.piece) + kKeep - 1) / kKeep;       // of the longest piece
     int64_t at[CC];
+    bool held[CC];                                        // the lane's channels of this env
 #pragma unroll
-    for (int c = 0; c < CC; ++c) at[c] = n * a.D + at_weight[c];
+    for (int c = 0; c < CC; ++c) {
+      at[c] = n * a.D + at_weight[c];
+      held[c] = there[c] && env_there;
+    }
     F2 G[CC][P];
-    load_ordered<SP, CC>(a.pieces > 1 ? a.maps + piece * states : a.dhT, at, there, s0, order, a.S, G);
+    load_ordered<SP, CC>(a.pieces > 1 ? a.maps + piece * states : a.dhT, at, held, s0, order, a.S, G);
 
     for (int seg = segments - 1; seg >= 0; --seg) {
       const int ts = t0 + seg * kKeep, steps = min(kKeep, t1 - ts);
       if (steps > 0) {
-        const uint8_t rend = (a.done || a.done_prev) && lane < steps ? flag_at(a, ts + lane, n) : (uint8_t)0;
+        const bool flagged = a.done || a.done_prev;
+        const uint8_t rend = flagged && mine < steps ? flag_at(a, ts + mine, n) : (uint8_t)0;
+        const uint8_t rend8 = R > 1 && flagged && mine + 8 < steps ? flag_at(a, ts + mine + 8, n) : (uint8_t)0;
         F2 h[CC][P];
-        load_ordered<SP, CC>(a.kept + ts / kKeep * states, at, there, s0, order, a.S, h);
-        stage<T, SW>(a, a.B, ts, steps, n, g, lane, m.B[0]);
-        stage<T, SW>(a, a.C, ts, steps, n, g, lane, m.C[0]);
+        load_ordered<SP, CC>(a.kept + ts / kKeep * states, at, held, s0, order, a.S, h);
+        stage<T, SW, RL>(a, a.B, ts, steps, n, g, mine, m.B[sub][0]);
+        stage<T, SW, RL>(a, a.C, ts, steps, n, g, mine, m.C[sub][0]);
         const T* px = row_at<T>(a.x, ts, n, d);
         const T* pdt = row_at<T>(a.dt, ts, n, d);
         const T* pdy = row_at<T>(a.dy, ts, n, d);
@@ -289,7 +300,15 @@ __global__ void __launch_bounds__(32 * back_warps(L::SW), back_blocks(L::SW)) k_
           }
           prefetch(a.kept + (ts / kKeep - 1) * states + at[0] * a.S);
         }
-        const uint32_t ends = __ballot_sync(0xffffffffu, rend != 0);
+        // ends of the lane's env, and of any of the warp's
+        uint32_t ends = __ballot_sync(0xffffffffu, rend != 0), any_ends = ends;
+        if constexpr (R > 1) {
+          static_assert(RL == 8, "two flags a lane");
+          const uint32_t upper = __ballot_sync(0xffffffffu, rend8 != 0);
+          any_ends = (ends | ends >> 16) | (upper | upper >> 16) << 16;
+          any_ends = ((any_ends | any_ends >> 8) & 255u) | ((any_ends >> 16 | any_ends >> 24) & 255u) << 8;
+          ends = (ends >> (sub * RL) & 255u) | (upper >> (sub * RL) & 255u) << 8;
+        }
         __syncwarp();
         // e, e x and p of step k, for both states of a pair
         auto inputs = [&](int k, F2 (&e)[CC], F2 (&u)[CC]) {
@@ -322,7 +341,7 @@ __global__ void __launch_bounds__(32 * back_warps(L::SW), back_blocks(L::SW)) k_
             const int i0 = first_step + k;
             F2 e[CC], u[CC], B[P];
             inputs(i0, e, u);
-            load_pairs(m.B[i0] + s0, order, B);
+            load_pairs(m.B[sub][i0] + s0, order, B);
             if (!kPlain && (ends >> i0 & 1u)) clear(h);
 #pragma unroll
             for (int c = 0; c < CC; ++c)
@@ -347,8 +366,8 @@ __global__ void __launch_bounds__(32 * back_warps(L::SW), back_blocks(L::SW)) k_
               F2 e[CC], u[CC], p[CC], B[P], C[P], sC[P];
               inputs(i0, e, u);
               weights(i0, p);
-              load_pairs(m.B[i0] + s0, order, B);
-              load_pairs(m.C[i0] + s0, order, C);
+              load_pairs(m.B[sub][i0] + s0, order, B);
+              load_pairs(m.C[sub][i0] + s0, order, C);
               if (!kPlain && (ends >> i0 & 1u)) clear(h);
 #pragma unroll
               for (int c = 0; c < CC; ++c) {
@@ -364,7 +383,7 @@ __global__ void __launch_bounds__(32 * back_warps(L::SW), back_blocks(L::SW)) k_
                 yc[c] = total(acc);
               }
               y[k] = over_states<LS, CC>(yc);
-              put_sums<L>(sC, lane, order, &m.sums[i0][1][s0]);
+              put_sums<L>(sC, lane, order, &m.sums[sub][i0][1][s0]);
             }
           }
 #pragma unroll
@@ -377,8 +396,8 @@ __global__ void __launch_bounds__(32 * back_warps(L::SW), back_blocks(L::SW)) k_
               F2 e[CC], u[CC], p[CC], B[P], C[P], sB[P];
               inputs(i0, e, u);
               weights(i0, p);
-              load_pairs(m.B[i0] + s0, order, B);
-              load_pairs(m.C[i0] + s0, order, C);
+              load_pairs(m.B[sub][i0] + s0, order, B);
+              load_pairs(m.C[sub][i0] + s0, order, C);
 #pragma unroll
               for (int c = 0; c < CC; ++c) {
                 F2 accB, accA;
@@ -396,7 +415,7 @@ __global__ void __launch_bounds__(32 * back_warps(L::SW), back_blocks(L::SW)) k_
               }
               if (!kPlain && (ends >> i0 & 1u)) clear(G);
               const float sumB = over_states<LS, CC>(by_B), sumA = over_states<LS, CC>(by_A) * kLn2;
-              put_sums<L>(sB, lane, order, &m.sums[i0][0][s0]);
+              put_sums<L>(sB, lane, order, &m.sums[sub][i0][0][s0]);
               float e1, p1, copy;
               split(e[0], e1, copy);
               split(p[0], p1, copy);
@@ -417,9 +436,9 @@ __global__ void __launch_bounds__(32 * back_warps(L::SW), back_blocks(L::SW)) k_
         const auto two = std::integral_constant<int, kHeld>();
         const auto four = std::integral_constant<int, kSub>();
 #pragma unroll 1
-        for (int sub = 0; sub + 1 < subs; ++sub) {        // the states before every 4th step but the first
-          if (ends >> (sub * kSub) & 15u) ahead(any, four, sub * kSub);
-          else ahead(plain, four, sub * kSub);
+        for (int block4 = 0; block4 + 1 < subs; ++block4) {        // the states before every 4th step but the first
+          if (any_ends >> (block4 * kSub) & 15u) ahead(any, four, block4 * kSub);
+          else ahead(plain, four, block4 * kSub);
 #pragma unroll
           for (int c = 0; c < CC; ++c)
 #pragma unroll
@@ -427,25 +446,25 @@ __global__ void __launch_bounds__(32 * back_warps(L::SW), back_blocks(L::SW)) k_
               float4 w;
               split(h[c][i], w.x, w.y);
               split(h[c][i + 1], w.z, w.w);
-              m.start[sub][(c * SP + 2 * i) / 4][lane] = w;
+              m.start[block4][(c * SP + 2 * i) / 4][lane] = w;
             }
         }
 #pragma unroll 1
         for (int half = subs * 2 - 1; half >= 0; --half) {
-          const int sub = half / 2, at0 = half * kHeld;
-          if (sub) {
+          const int block4 = half / 2, at0 = half * kHeld;
+          if (block4) {
 #pragma unroll
             for (int c = 0; c < CC; ++c)
 #pragma unroll
               for (int i = 0; i < P; i += 2) {
-                const float4 w = m.start[sub - 1][(c * SP + 2 * i) / 4][lane];
+                const float4 w = m.start[block4 - 1][(c * SP + 2 * i) / 4][lane];
                 h[c][i] = pair(w.x, w.y);
                 h[c][i + 1] = pair(w.z, w.w);
               }
           } else {
-            load_ordered<SP, CC>(a.kept + ts / kKeep * states, at, there, s0, order, a.S, h);
+            load_ordered<SP, CC>(a.kept + ts / kKeep * states, at, held, s0, order, a.S, h);
           }
-          if ((ends >> (sub * kSub) & 15u) || at0 + kHeld > steps) {
+          if ((any_ends >> (block4 * kSub) & 15u) || at0 + kHeld > steps) {
             if (half & 1) ahead(any, two, at0 - kHeld);
             through(any, at0);
           } else {
@@ -456,21 +475,26 @@ __global__ void __launch_bounds__(32 * back_warps(L::SW), back_blocks(L::SW)) k_
       }
       __syncthreads();
       // dB and dC of the segment over the row's warps, in their order
-      if (steps > 0) {
+      if (R > 1 && steps > 0 && env_there) {
+        for (int i = mine; i < steps * 2 * a.S; i += RL) {
+          const int k = i / (2 * a.S), j = i % (2 * a.S), which = j >= a.S, s = which ? j - a.S : j;
+          from_float(m.sums[sub][k][which][s], *const_cast<T*>(row_at<T>(which ? a.dC : a.dB, ts + k, n, (int64_t)g * a.S + s)));
+        }
+      } else if (R == 1 && steps > 0) {
         const int threads = 32 * side, me = threadIdx.x % threads;
         const Back<L>* const from = all + row * side;
         const int live_warps = min(side, a.tiles - block * side);
         for (int i = me; i < steps * 2 * a.S; i += threads) {
           const int k = i / (2 * a.S), j = i % (2 * a.S), which = j >= a.S, s = which ? j - a.S : j, t = ts + k;
           float v = 0.0f;
-          for (int w = 0; w < live_warps; ++w) v += from[w].sums[k][which][s];
+          for (int w = 0; w < live_warps; ++w) v += from[w].sums[0][k][which][s];
           if (blocks > 1) a.parts[((((int64_t)block * a.T + t) * a.N + n) * a.G + g) * 2 * a.S + j] = v;
           else from_float(v, *const_cast<T*>(row_at<T>(which ? a.dC : a.dB, t, n, (int64_t)g * a.S + s)));
         }
       }
       __syncthreads();
     }
-    if (a.dh0 && piece == 0 && real) store_ordered<SP, CC>(a.dh0, at, there, s0, order, a.S, G);
+    if (a.dh0 && piece == 0 && real) store_ordered<SP, CC>(a.dh0, at, held, s0, order, a.S, G);
     // weight gradients are summed over an item in registers, over a slot's items in memory: one chain through all of them
     // rounded away three times as much (4,096 x 128: 1.4e-6 of dA)
     if (real) {
@@ -481,7 +505,7 @@ __global__ void __launch_bounds__(32 * back_warps(L::SW), back_blocks(L::SW)) k_
         for (int c = 0; c < CC; ++c)
 #pragma unroll
           for (int i = 0; i < P; ++i) dA[c][i] = dA[c][i] + before[c][i];
-        if (writes) {
+        if (channel && q < CC) {
           dskip += slot[a.D * a.S + d];
           dbias += slot[a.D * (a.S + 1) + d];
         }
@@ -498,22 +522,24 @@ __global__ void __launch_bounds__(32 * back_warps(L::SW), back_blocks(L::SW)) k_
 constexpr int kFoldWarps = 4, kFoldBatch = 4;
 template <typename T, typename L>
 __global__ void __launch_bounds__(32 * kFoldWarps) k_select_fold_back(Select a) {
-  constexpr int SP = L::SP, LS = L::LS, CC = L::CC, SW = L::SW;
-  using In = Staged<T, SW, kFoldBatch>;
-  __shared__ __align__(16) float rows[kFoldWarps][kFoldBatch * SW];
+  constexpr int SP = L::SP, LS = L::LS, CC = L::CC, SW = L::SW, R = L::R, RL = L::RL;
+  using In = Staged<T, SW, kFoldBatch, RL>;
+  __shared__ __align__(16) float rows[kFoldWarps][R][kFoldBatch * SW];
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   int64_t id = blockIdx.x * (int64_t)kFoldWarps + warp;
-  if (id >= a.N * a.G * a.tiles * a.pieces) return;
-  const int tile = (int)(id % a.tiles);
+  const int64_t envs_groups = (a.N * a.G + R - 1) / R;         // rows, or fours of them
+  if (id >= envs_groups * a.tiles * a.pieces) return;
+  const int tile = (int)(id % a.tiles), sub = lane / RL, mine = lane % RL;
   id /= a.tiles;
-  const int g = (int)(id % a.G);
-  id /= a.G;
-  const int64_t n = id % a.N;
-  const int piece = (int)(id / a.N);
-  float* const Cs = rows[warp];
-  const int q = lane % LS, s0 = q * SP;
-  const int first = tile * L::CW + lane / LS * CC, own = first + q % CC;
-  const bool live = own < a.per;
+  const int64_t row = id % envs_groups * R + sub;
+  const bool row_there = R == 1 || row < a.N * a.G;
+  const int g = row_there ? (int)(row % a.G) : 0;
+  const int64_t n = row_there ? row / a.G : 0;
+  const int piece = (int)(id / envs_groups);
+  float* const Cs = rows[warp][sub];
+  const int q = mine % LS, s0 = q * SP;
+  const int first = tile * L::CW + mine / LS * CC, own = first + q % CC;
+  const bool live = row_there && own < a.per;
   const int64_t d = (int64_t)g * a.per + own;
   int64_t at[CC], at_weight[CC];
   bool there[CC];
@@ -522,7 +548,7 @@ __global__ void __launch_bounds__(32 * kFoldWarps) k_select_fold_back(Select a) 
     const int k = first + (q % CC ^ c);
     at_weight[c] = (int64_t)g * a.per + k;
     at[c] = n * a.D + at_weight[c];
-    there[c] = k < a.per;
+    there[c] = row_there && k < a.per;
   }
   const int t0 = piece * a.piece, t1 = min(a.T, t0 + a.piece);
   F2 G[CC][SP / 2], A2[CC][SP / 2];
@@ -543,15 +569,15 @@ __global__ void __launch_bounds__(32 * kFoldWarps) k_select_fold_back(Select a) 
   const T* pdt = row_at<T>(a.dt, last, n, d);
   const T* pdy = row_at<T>(a.dy, last, n, d);
   const T* pgate = gated ? row_at<T>(a.gate, last, n, d) : pdy;
-  const T* pC = row_at<T>(a.C, last + lane / In::kSide, n, (int64_t)g * a.S + lane % In::kSide);
+  const T* pC = row_at<T>(a.C, last + mine / In::kSide, n, (int64_t)g * a.S + mine % In::kSide);
   T rdt[kFoldBatch], rgate[kFoldBatch], rdy[kFoldBatch];
   In rC;
   uint8_t rend = 0;
   auto fetch = [&](int t) {
     if (t < t0) return;
     const int steps = min(kFoldBatch, t1 - t);
-    rend = flagged && lane < steps ? flag_at(a, t + lane, n) : (uint8_t)0;
-    rC.load(pC, a.C.outer, steps, a.S, lane);
+    rend = flagged && mine < steps ? flag_at(a, t + mine, n) : (uint8_t)0;
+    rC.load(pC, a.C.outer, steps, a.S, mine);
 #pragma unroll
     for (int k = 0; k < kFoldBatch; ++k) {
       from_float(0.0f, rdt[k]);
@@ -569,8 +595,8 @@ __global__ void __launch_bounds__(32 * kFoldWarps) k_select_fold_back(Select a) 
   for (int ts = last; ts >= t0; ts -= kFoldBatch) {
     const int steps = t1 - ts;
     __syncwarp();                                             // the last batch's rows are read
-    rC.put(Cs, lane);
-    const uint32_t ends = flagged ? __ballot_sync(0xffffffffu, rend != 0) : 0u;
+    rC.put(Cs, mine);
+    const uint32_t ends = flagged ? __ballot_sync(0xffffffffu, rend != 0) >> (sub * RL % 32) & 15u : 0u;
     float e[kFoldBatch], p[kFoldBatch];
 #pragma unroll
     for (int k = 0; k < kFoldBatch; ++k) {
@@ -652,16 +678,16 @@ __global__ void __launch_bounds__(256) k_select_rows(Select a, int64_t blocks) {
 
 // How many partial sums of the weight gradients there are; *blocks: along a group's channels; *rows: of a block.
 int64_t select_slots(const Select& a, int64_t* blocks, int* rows) {
-  const int warps = back_warps(a.S);
+  const int warps = back_warps(a.S, a.rows);
   int side = 1;
-  while (side < a.tiles && side < warps) side *= 2;
+  while (a.rows == 1 && side < a.tiles && side < warps) side *= 2;
   *rows = warps / side;
   *blocks = (a.tiles + side - 1) / side;
-  const int64_t items = (a.N * a.pieces + *rows - 1) / *rows;
-  const int64_t most = std::max<int64_t>(1, (int64_t)sm_count() * back_blocks(a.S) / (*blocks * a.G));
+  const int64_t items = ((a.N + a.rows - 1) / a.rows * a.pieces + *rows - 1) / *rows;
+  const int64_t most = std::max<int64_t>(1, (int64_t)sm_count() * back_blocks(a.S, a.rows) / (*blocks * a.G));
   // as many rounds as the fullest slot makes, spread evenly
   const int64_t rounds = (items + most - 1) / most;
-  return std::min<int64_t>((items + rounds - 1) / rounds, 65535) * *rows;
+  return std::min<int64_t>((items + rounds - 1) / rounds, 65535) * *rows * a.rows;
 }
 
 template <typename T>
@@ -669,23 +695,25 @@ cudaError_t launch_select_back(const Select& a, bool split, cudaStream_t s) {
   int64_t blocks;
   int rows;
   const int64_t slots = select_slots(a, &blocks, &rows);
-  cudaError_t e = with_lanes(a.S, [&](auto l) -> cudaError_t {
+  auto all = [&](auto l) -> cudaError_t {
     using L = decltype(l);
     cudaError_t e;
     if (split) {
-      const int64_t warps = a.N * a.G * a.tiles * a.pieces;
+      const int64_t warps = (a.N * a.G + L::R - 1) / L::R * a.tiles * a.pieces;
       k_select_fold_back<T, L><<<(unsigned)((warps + kFoldWarps - 1) / kFoldWarps), 32 * kFoldWarps, 0, s>>>(a);
       if ((e = cudaGetLastError()) != cudaSuccess || (e = launch_select_join(a, true, s)) != cudaSuccess) return e;
     }
     const auto kern = k_select_back<T, L>;
-    const int smem = (int)sizeof(Back<L>) * back_warps(L::SW);
-    static_assert((sizeof(Back<L>) * back_warps(L::SW) + 1024) * back_blocks(L::SW) <= 228 * 1024, "shared memory of an SM");
+    constexpr int kWarps = back_warps(L::SW, L::R);
+    const int smem = (int)sizeof(Back<L>) * kWarps;
+    static_assert((sizeof(Back<L>) * kWarps + 1024) * back_blocks(L::SW, L::R) <= 228 * 1024, "shared memory of an SM");
     if ((e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess) return e;
-    const dim3 grid((unsigned)(blocks * a.G), (unsigned)(slots / rows));
-    if (split) return launch_after(kern, grid, 32 * back_warps(L::SW), smem, s, a, rows);
-    kern<<<grid, 32 * back_warps(L::SW), smem, s>>>(a, rows);
+    const dim3 grid((unsigned)(blocks * a.G), (unsigned)(slots / (rows * L::R)));
+    if (split) return launch_after(kern, grid, 32 * kWarps, smem, s, a, rows);
+    kern<<<grid, 32 * kWarps, smem, s>>>(a, rows);
     return cudaGetLastError();
-  });
+  };
+  cudaError_t e = a.rows > 1 ? with_narrow_lanes(a.S, all) : with_lanes(a.S, all);
   if (e != cudaSuccess) return e;
   if (a.dA || a.dskip || a.ddt_bias) {
     e = launch_after(k_select_weights, dim3((unsigned)((a.D * (a.S + 2) + 31) / 32)), 32 * kGroups, 0, s, a, slots);

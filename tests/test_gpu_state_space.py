@@ -180,6 +180,14 @@ def test_scan_of_many_envs(T, N, D, S, G, dt, layout):
     _check_scan(T, N, D, S, G, dt, layout, seed=13)
 
 
+@pytest.mark.parametrize("T,N,D,S,G,dt,layout", [(37, 50, 8, 16, 1, "bf16", "flat"), (40, 7, 16, 16, 2, "fp16", "half"), (19, 900, 2, 13, 1, "fp32", "odd"),
+                                                 (33, 6, 12, 4, 3, "bf16", "swap"), (700, 2, 6, 8, 1, "fp32", "flat"), (900, 1, 7, 16, 1, "bf16", "pad"),
+                                                 (16, 3, 32, 8, 4, "fp32", "flat"), (130, 5, 1, 1, 1, "fp16", "flat"), (65, 601, 8, 5, 1, "fp32", "pad")])
+def test_scan_of_narrow_groups(T, N, D, S, G, dt, layout):
+    """Four rows a warp, the last of them without rows for all."""
+    _check_scan(T, N, D, S, G, dt, layout, ends=0.05, seed=14)
+
+
 @pytest.mark.parametrize("T", [40, 20000])
 def test_scan_of_a_constant_input_reaches_its_limit(T):
     """dt = 0, no bias: e = log 2; with B x = 1 the state goes to e / (1 - exp(e A)) times 1 minus exp(e A T), whatever the
