@@ -35,11 +35,21 @@ __global__ void __launch_bounds__(32 * kWarps, L::OWN > 1 ? 3 : L::SP == 8 ? 4 :
   if (id >= envs_groups * a.tiles * a.pieces) return;
   const int tile = (int)(id % a.tiles), side = lane / RL, mine = lane % RL;
   id /= a.tiles;
-  const int64_t row = id % envs_groups * R + side;
-  const bool row_there = R == 1 || row < a.N * a.G;
-  const int g = row_there ? (int)(row % a.G) : 0;
-  const int64_t n = row_there ? row / a.G : 0;
-  const int piece = (int)(id / envs_groups);
+  int g, piece;
+  int64_t n;
+  bool row_there = true;
+  if constexpr (R == 1) {                                     // as below, but every lane's the same
+    g = (int)(id % a.G);
+    id /= a.G;
+    n = id % a.N;
+    piece = (int)(id / a.N);
+  } else {
+    const int64_t row = id % envs_groups * R + side;
+    row_there = row < a.N * a.G;
+    g = row_there ? (int)(row % a.G) : 0;
+    n = row_there ? row / a.G : 0;
+    piece = (int)(id / envs_groups);
+  }
   float* const Bs = rows[warp][0][side];
   float* const Cs = rows[warp][FOLD ? 0 : 1][side];
 
@@ -227,7 +237,8 @@ __global__ void __launch_bounds__(32 * kWarps, L::OWN > 1 ? 3 : L::SP == 8 ? 4 :
 // The states before the pieces (backward: their gradients behind the pieces), in the place of the pieces' own.  A block has
 // some states and all pieces: each of its groups of threads folds adjacent pieces to one, those are joined over the block, and
 // the groups go through their pieces once more from the state they begin with.  293 pieces of 4,000 states: 12 us in 64 groups,
-// 40 by one thread a state, which is enough for a few pieces.  The product of a piece's decays is kept from 0: an infinite state does not become NaN by a long
+// 40 by one thread a state, which is enough for a few pieces.  The product of a piece's decays is kept from 0: an infinite state
+// does not become NaN by a long
 // piece.
 constexpr int kJoin = 512, kJoinGroups = 64, kJoinAhead = 4;
 __device__ __forceinline__ float decay_of(float A2, float sum) { return fmaxf(ex2(A2 * sum), 1.17549435e-38f); }
@@ -538,7 +549,8 @@ Select of(const net_select* p, bool back, bool narrow = false) {
   for (const net_rows* r : rows) pairs = pairs && aligned(*r, a.T, a.N, z, 2);
   a.wide = pairs && a.N * a.G * tiles >= (int64_t)sm_count() * 12;
   if (a.wide) a.tiles = tiles;
-  // narrow groups: lanes that would be idle take other rows (TALL)
+  // narrow groups: lanes that would be idle take other rows (1,374 steps of 1,137 envs x 2 groups of 8 channels x 16 fp32: 288 us,
+  // 2,139 with a row a warp)
   a.rows = (back || a.T > 1) && a.per <= kNarrow && a.S <= kMostWide ? kSide4 : 1;
   if (a.rows > 1) a.wide = false, a.tiles = 1;
   select_pieces(a, back);
