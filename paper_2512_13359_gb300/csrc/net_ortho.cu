@@ -224,6 +224,7 @@ struct Steps {
   int L, M, N, s, steps, ldx, lds;          // s: the shorter side
   bool wide;                                // M <= N
   int tile[3];                              // columns of a tile of P, Q, X
+  bool single;                              // a matrix is one tile of each
   float a, b, c;
   __half *x[2], *P, *Q;                     // pieces [2][L][rows][ld]
   net_rows y;
@@ -380,6 +381,15 @@ __device__ __forceinline__ void all_blocks(const Steps& a, unsigned round, volat
   asm volatile("fence.proxy.async.global;" ::: "memory");
 }
 
+// The same where every matrix is one tile of each product, always the same block's.
+__device__ __forceinline__ void this_block() {
+  asm volatile("fence.proxy.async.global;" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0) __threadfence();
+  __syncthreads();
+  asm volatile("fence.proxy.async.global;" ::: "memory");
+}
+
 // PAIR: blocks in clusters of two, each with 128 of a tile's 256 rows; the first one issues the products of both.
 template <int BN, bool PAIR>
 __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant__ Steps a) {
@@ -447,7 +457,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant_
         const int m0 = ti * kHigh + rank * kBM, n0 = tj * p.wide;
         work(p, A, B, chunks, l, m0, n0, in, stage);
       }
-      if (k + 1 < a.steps * 3) all_blocks(a, (unsigned)k + 1, abort);
+      if (k + 1 < a.steps * 3) {
+        if (a.single) this_block();
+        else all_blocks(a, (unsigned)k + 1, abort);
+      }
       if (*abort) break;                       // seen by all: behind a barrier, or at the end
     }
   };
@@ -790,6 +803,8 @@ cudaError_t launch(const net_ortho* a, const Space& z, cudaStream_t s) {
     p.tile[0] = p.tile[1] = p.tile[2] = 256;
     return launch_products<256, true>(p, s);
   }
+  p.single = p.M <= 128 && p.N <= 128;
+  if (p.single) p.tile[0] = p.tile[1] = p.tile[2] = 128;
   return p.tile[0] + p.tile[1] + p.tile[2] > 3 * 128 ? launch_products<256, false>(p, s) : launch_products<128, false>(p, s);
 }
 

@@ -237,9 +237,8 @@ __global__ void __launch_bounds__(32 * kWarps, L::OWN > 1 ? 3 : L::SP == 8 ? 4 :
 // The states before the pieces (backward: their gradients behind the pieces), in the place of the pieces' own.  A block has
 // some states and all pieces: each of its groups of threads folds adjacent pieces to one, those are joined over the block, and
 // the groups go through their pieces once more from the state they begin with.  293 pieces of 4,000 states: 12 us in 64 groups,
-// 40 by one thread a state, which is enough for a few pieces.  The product of a piece's decays is kept from 0: an infinite state
-// does not become NaN by a long
-// piece.
+// 40 by one thread a state, which is enough for a few pieces.  The product of a piece's decays is kept from 0: an infinite
+// state does not become NaN by a long piece.
 constexpr int kJoin = 512, kJoinGroups = 64, kJoinAhead = 4;
 __device__ __forceinline__ float decay_of(float A2, float sum) { return fmaxf(ex2(A2 * sum), 1.17549435e-38f); }
 __global__ void __launch_bounds__(kJoin) k_select_join(Select a, bool back, int groups) {
