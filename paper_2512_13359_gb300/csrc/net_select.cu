@@ -293,11 +293,14 @@ __global__ void __launch_bounds__(kJoin) k_select_join(Select a, bool back, int 
 
 // One step, as in a rollout: the states are read, changed and written, so few registers and no staging; a warp takes its
 // channels of one env after the other, A in registers (65,536 envs x 256 x 16 of bf16: 351 us, 6.5 TB/s).  wide: B's and C's
-// values of a lane are aligned vectors.
+// values of a lane are aligned vectors, of a lane that has states (there); one past them (S = 24: the last of four) has zeros.
 template <typename T, int SP>
-__device__ __forceinline__ void load_row(const T* p, bool wide, int s0, int S, F2 (&v)[SP / 2]) {
+__device__ __forceinline__ void load_row(const T* p, bool wide, bool there, int s0, int S, F2 (&v)[SP / 2]) {
   float x[SP];
-  if (wide) {
+  if (!there) {
+#pragma unroll
+    for (int i = 0; i < SP; ++i) x[i] = 0.0f;
+  } else if (wide) {
     constexpr int E = SP * sizeof(T) > 16 ? 16 / sizeof(T) : SP;
 #pragma unroll
     for (int i = 0; i < SP; i += E) {
@@ -402,8 +405,8 @@ __global__ void __launch_bounds__(32 * kOneWarps, 4) k_select_one(Select a, bool
       rdt = *row_at<T>(a.dt, 0, n, d);
       if (gated) rgate = *row_at<T>(a.gate, 0, n, d);
     }
-    load_row<T, SP>(row_at<T>(a.B, 0, n, in_row), WHOLE || wide, s0, a.S, B);
-    load_row<T, SP>(row_at<T>(a.C, 0, n, in_row), WHOLE || wide, s0, a.S, C);
+    load_row<T, SP>(row_at<T>(a.B, 0, n, in_row), WHOLE || wide, WHOLE || s0 < a.S, s0, a.S, B);
+    load_row<T, SP>(row_at<T>(a.C, 0, n, in_row), WHOLE || wide, WHOLE || s0 < a.S, s0, a.S, C);
     if (a.done_prev) rend = a.done_prev[n];
   };
   fetch(n);

@@ -224,6 +224,38 @@ def test_scan_steps_in_place_are_one_pass():
         assert torch.equal(torch.cat(parts), y) and torch.equal(h, hT)
 
 
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("G", [1, 2])
+@pytest.mark.parametrize("S", [1, 3, 4, 8, 13, 16, 20, 24, 32, 40, 48, 56, 64, 72, 88, 96, 120, 128])
+def test_single_steps_of_any_number_of_states(S, G, dt):
+    """Against the formulas; rows that belong to nobody hold NaN; and two steps in place are a pass of two, bit for bit."""
+    torch, nets, types = _t()
+    t, N, D = types[dt], 37, 40
+    g, a, opt, h0 = _scan_args(torch, t, 2, N, D, S, G, "flat", 0.2, S)
+    for k in ("B", "C"):                                         # rows 16 apart, and one behind the last, aligned as before
+        room = torch.full((2, N + 1, G * S + 16), float("nan"), device="cuda", dtype=t)
+        room[:, :N, :G * S] = a[k]
+        a[k] = room[:, :N, :G * S]
+    first = {k: v if k == "A" else v[:1] for k, v in a.items()}
+    gate, done, prev = opt.pop("gate"), opt.pop("done"), opt.pop("done_prev")
+    y, h, kept = nets.select_scan(**first, **opt, gate=gate[:1], h0=h0, done_prev=prev, kept=True)
+    q = R.Scan(*(_nn(v) for v in (first["x"], first["dt"], a["A"], first["B"], first["C"], opt["skip"], opt["dt_bias"], gate[:1], h0, None, prev)))
+    _within(y, q.y, q.Ey, dt)
+    _within(h, q.hT, q.EhT)
+    assert torch.equal(kept[0], h0)
+    want, hT, _ = nets.select_scan(**a, **opt, gate=gate, h0=h0, done=done, done_prev=prev)
+    second = {k: v if k == "A" else v[1:] for k, v in a.items()}
+    y2, out, _ = nets.select_scan(**second, **opt, gate=gate[1:], h0=h, done_prev=done[0], hT=h)
+    assert out is h and torch.equal(y[0], want[0]) and torch.equal(y2[0], want[1]) and torch.equal(h, hT)
+
+
+@pytest.mark.parametrize("N,D,S,G,dt,layout", [(5000, 12, 24, 1, "bf16", "flat"), (5000, 24, 40, 2, "fp32", "odd"), (3, 600, 48, 1, "fp16", "pad"),
+                                               (1, 4, 120, 1, "fp32", "flat"), (2500, 16, 96, 4, "bf16", "half"), (7, 1, 24, 1, "fp16", "swap")])
+def test_single_steps_of_padded_states(N, D, S, G, dt, layout):
+    """More envs than warps walk side by side, odd strides, a single row; the states' gradients too."""
+    _check_scan(1, N, D, S, G, dt, layout, ends=0.2, seed=S)
+
+
 def test_scan_without_steps_or_envs():
     torch, nets, _ = _t()
     h0, A = torch.randn(3, 8, 4, device="cuda"), -torch.ones(8, 4, device="cuda")
