@@ -327,7 +327,14 @@ int net_select_scan_backward(const net_select* a, void* stream);
  *
  * workspace: net_orthogonalise_workspace_bytes(a) bytes, 256-byte aligned.  Its
  * first 32-bit word is AUV_OK after the call has run, or AUV_ERR_TIMEOUT where
- * a wait inside a kernel gave up (2 s); y then holds NaN.
+ * a wait inside a kernel gave up (2 s); y then holds NaN in the place of every
+ * value that finished products have not come to.
+ *
+ * net_orthogonalise_selftest_timeout: failure-detection self-test.  The same
+ * call, but that behind the product-th of its 3 * steps products (1 on, ahead
+ * of the last) one block waits for something that never comes, and all waits
+ * give up after limit_us microseconds (1 .. 5e6).  Matrices of one tile
+ * (M, N <= 128) have no such wait: the call is then net_orthogonalise.
  */
 typedef struct net_ortho {
   uint32_t struct_size;           /* sizeof(net_ortho): version guard         */
@@ -343,6 +350,7 @@ typedef struct net_ortho {
 } net_ortho;
 size_t net_orthogonalise_workspace_bytes(const net_ortho* a);
 int net_orthogonalise(const net_ortho* a, void* stream);
+int net_orthogonalise_selftest_timeout(const net_ortho* a, uint32_t product, uint32_t limit_us, void* stream);
 
 const char* net_last_error(void);
 

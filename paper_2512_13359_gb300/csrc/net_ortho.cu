@@ -230,7 +230,9 @@ struct Steps {
   net_rows y;
   int dtype;
   int* error;
-  unsigned* arrived;                        // blocks at the barriers between products
+  unsigned* arrived;                        // blocks at the barriers between products, and kGaveUp
+  uint64_t limit;                           // of a wait, in ns
+  int stuck;                                // self-test: the first block waits in vain behind this product
 };
 
 // Shared memory: a ring of two stages of 256-column tiles or of three of 128-column ones.
@@ -359,35 +361,56 @@ __device__ __forceinline__ void tile_at(const Product& p, int t, int& ti, int& t
   tj = t - start_of(ti, p.high, p.wide);
 }
 
-// Every block has arrived `round` times, and what they stored is seen, by TMA too.  Bounded.
-__device__ __forceinline__ void all_blocks(const Steps& a, unsigned round, volatile int* abort) {
+// Every block has arrived `round` times, and what they stored is seen, by TMA too.  Bounded.  A block that gave up, here or in
+// the product before, says so ahead of its arrival, and the others give up with it: none goes on from a product that is not
+// whole.  Returns whether to go on, the same to all threads.
+constexpr unsigned kGaveUp = 1u << 31;
+__device__ __forceinline__ bool all_blocks(const Steps& a, unsigned round, volatile int* abort) {
   asm volatile("fence.proxy.async.global;" ::: "memory");
   __syncthreads();
   if (threadIdx.x == 0) {
+    const bool in_vain = (int)round == a.stuck && blockIdx.x == 0;
+    auto give_up = [&] {
+      *abort = 1;
+      asm volatile("red.relaxed.gpu.global.or.b32 [%0], %1;" ::"l"(a.arrived), "r"(kGaveUp) : "memory");
+    };
     __threadfence();
+    if (*abort) give_up();
     asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(a.arrived) : "memory");
     const uint64_t t0 = tc::global_timer_ns();
-    for (unsigned it = 1;; ++it) {
+    for (unsigned it = 1; !*abort; ++it) {
       unsigned v;
       asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(a.arrived) : "memory");
-      if (v >= round * gridDim.x) break;
-      if ((it & 63u) == 0 && tc::global_timer_ns() - t0 > kWaitLimitNs) {
-        *abort = 1;
-        break;
-      }
+      if (v & kGaveUp) *abort = 1;
+      else if (v >= round * gridDim.x && !in_vain) break;
+      else if ((it & 63u) == 0 && tc::global_timer_ns() - t0 > a.limit) give_up();
     }
   }
-  __syncthreads();
+  const bool on = !__syncthreads_or(threadIdx.x == 0 && *abort);
   asm volatile("fence.proxy.async.global;" ::: "memory");
+  return on;
 }
 
 // The same where every matrix is one tile of each product, always the same block's.
-__device__ __forceinline__ void this_block() {
+__device__ __forceinline__ bool this_block(volatile int* abort) {
   asm volatile("fence.proxy.async.global;" ::: "memory");
   __syncthreads();
   if (threadIdx.x == 0) __threadfence();
-  __syncthreads();
+  const bool on = !__syncthreads_or(threadIdx.x == 0 && *abort);
   asm volatile("fence.proxy.async.global;" ::: "memory");
+  return on;
+}
+
+// After a wait that gave up: NaN in y where this block's tiles lie, whichever of them were stored.
+template <typename T>
+__device__ __forceinline__ void spoil(const Steps& a, int l, int m0, int n0, int wide) {
+  T nan;
+  from_float(__uint_as_float(0x7fc00000u), nan);
+  T* const p = reinterpret_cast<T*>(a.y.data) + l * a.y.outer;
+  for (int i = threadIdx.x; i < kBM * wide; i += kStorers * 32) {
+    const int r = m0 + i / wide, c = n0 + i % wide;
+    if (r < a.M && c < a.N) p[r * a.y.inner + c] = nan;
+  }
 }
 
 // PAIR: blocks in clusters of two, each with 128 of a tile's 256 rows; the first one issues the products of both.
@@ -457,11 +480,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant_
         const int m0 = ti * kHigh + rank * kBM, n0 = tj * p.wide;
         work(p, A, B, chunks, l, m0, n0, in, stage);
       }
-      if (k + 1 < a.steps * 3) {
-        if (a.single) this_block();
-        else all_blocks(a, (unsigned)k + 1, abort);
-      }
-      if (*abort) break;                       // seen by all: behind a barrier, or at the end
+      if (k + 1 < a.steps * 3 && !(a.single ? this_block(abort) : all_blocks(a, (unsigned)k + 1, abort))) break;
     }
   };
   if (warp < kStorers) {
@@ -475,7 +494,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant_
 #pragma unroll 1
         for (int c = 0; c < chunks; ++c, ++chunk) {
           const uint32_t buf = chunk & 1u;
-          ok = ok && tc::mbar_wait(&bar->sums[buf], chunk / 2 & 1u, abort, kWaitLimitNs);
+          ok = ok && tc::mbar_wait(&bar->sums[buf], chunk / 2 & 1u, abort, a.limit);
           if (!__all_sync(0xffffffffu, ok)) ok = false;
           tc::tc_fence_after();
           if (ok) {
@@ -540,7 +559,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant_
             const int s = stage;
             const int held = p.wide / kBlocks;        // columns of B in this block
             stage = s + 1 == stages_of(held) ? 0 : s + 1;
-            if ((used >> s & 1u) && !tc::mbar_wait(&bar->empty[s], (parity >> s & 1u) ^ 1u, abort, kWaitLimitNs)) break;
+            if ((used >> s & 1u) && !tc::mbar_wait(&bar->empty[s], (parity >> s & 1u) ^ 1u, abort, a.limit)) break;
             used |= 1u << s, parity ^= 1u << s;
             if (rank == 0) tc::mbar_arrive_expect_tx(&bar->full[s], kBlocks * stage_bytes(held));
             uint8_t* to = smem + s * stage_bytes(held);
@@ -588,8 +607,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant_
             const int s = stage, held = p.wide / kBlocks;
             stage = s + 1 == stages_of(held) ? 0 : s + 1;
             const uint32_t buf = chunk & 1u, to = tmem + buf * BN;
-            if (chunk >= 2 && !tc::mbar_wait(&bar->taken[buf], (chunk / 2 - 1) & 1u, abort, kWaitLimitNs)) break;
-            if (!tc::mbar_wait(&bar->full[s], parity >> s & 1u, abort, kWaitLimitNs)) break;
+            if (chunk >= 2 && !tc::mbar_wait(&bar->taken[buf], (chunk / 2 - 1) & 1u, abort, a.limit)) break;
+            if (!tc::mbar_wait(&bar->full[s], parity >> s & 1u, abort, a.limit)) break;
             parity ^= 1u << s;
             tc::tc_fence_after();
             const uint32_t a0 = tc::smem_u32(smem + s * stage_bytes(held)), b0 = a0 + 2 * kA, next_b = held * 128;
@@ -624,6 +643,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_products(const __grid_constant_
   __syncthreads();
   if constexpr (PAIR) tc::cluster_sync();    // neither leaves while the other's memory is asked for
   if (tid == 0 && bar->abort) *a.error = AUV_ERR_TIMEOUT;
+  if (warp < kStorers && bar->abort) {
+    const Product p = {kLast, a.M, a.N, a.s, kHigh, a.tile[2], false, a.wide};
+    const int each = tiles_of(kLast, a.M, a.N, kHigh, p.wide);
+    for (int64_t t = blockIdx.x / kBlocks; t < (int64_t)each * a.L; t += gridDim.x / kBlocks) {
+      int ti, tj;
+      tile_at(p, (int)(t % each), ti, tj);
+      const int l = (int)(t / each), m0 = ti * kHigh + rank * kBM, n0 = tj * p.wide;
+      if (a.dtype == NET_FP32) spoil<float>(a, l, m0, n0, p.wide);
+      else if (a.dtype == NET_BF16) spoil<__nv_bfloat16>(a, l, m0, n0, p.wide);
+      else spoil<__half>(a, l, m0, n0, p.wide);
+    }
+  }
   if (warp == kIssuer) {
     tc::tc_fence_after();
     dealloc<PAIR>(tmem, 2 * BN);
@@ -754,7 +785,7 @@ cudaError_t launch_products(const Steps& a, cudaStream_t s) {
 }
 
 template <typename T>
-cudaError_t launch(const net_ortho* a, const Space& z, cudaStream_t s) {
+cudaError_t launch(const net_ortho* a, const Space& z, int stuck, uint64_t limit, cudaStream_t s) {
   char* const ws = static_cast<char*>(a->workspace);
   float* const partial = reinterpret_cast<float*>(ws + z.partial);
   __half* const x[2] = {reinterpret_cast<__half*>(ws + z.x[0]), reinterpret_cast<__half*>(ws + z.x[1])};
@@ -776,6 +807,7 @@ cudaError_t launch(const net_ortho* a, const Space& z, cudaStream_t s) {
   p.x[0] = x[0], p.x[1] = x[1], p.P = P, p.Q = Q;
   p.y = a->y, p.dtype = (int)a->dtype;
   p.error = reinterpret_cast<int*>(ws), p.arrived = reinterpret_cast<unsigned*>(ws) + 1;
+  p.limit = limit, p.stuck = stuck;
   bool ok = make_map(&p.p, P, z.s, z.s, z.lds, a->L, kBM) && make_map(&p.q, Q, z.s, z.s, z.lds, a->L, kBM);
   for (int i = 0; i < 2 && ok; ++i) {
     const __half* const at = x[a->steps > 1 ? i : 0];
@@ -808,7 +840,7 @@ cudaError_t launch(const net_ortho* a, const Space& z, cudaStream_t s) {
   return p.tile[0] + p.tile[1] + p.tile[2] > 3 * 128 ? launch_products<256, false>(p, s) : launch_products<128, false>(p, s);
 }
 
-int run(const net_ortho* p, void* stream) {
+int run(const net_ortho* p, void* stream, int stuck = 0, uint64_t limit = kWaitLimitNs) {
   int rc = check(p);
   if (rc) return rc;
   if (!p->L || !p->M || !p->N) return AUV_OK;
@@ -818,9 +850,9 @@ int run(const net_ortho* p, void* stream) {
   if (p->workspace_bytes < w.bytes) return fail(AUV_ERR_SIZE, "workspace of %zu bytes, %zu needed", p->workspace_bytes, w.bytes);
   if ((rc = need(p->workspace, "workspace", 256))) return rc;
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = p->dtype == NET_FP32   ? launch<float>(p, w, s)
-                        : p->dtype == NET_BF16 ? launch<__nv_bfloat16>(p, w, s)
-                                               : launch<__half>(p, w, s);
+  const cudaError_t e = p->dtype == NET_FP32   ? launch<float>(p, w, stuck, limit, s)
+                        : p->dtype == NET_BF16 ? launch<__nv_bfloat16>(p, w, stuck, limit, s)
+                                               : launch<__half>(p, w, stuck, limit, s);
   return e == cudaSuccess ? AUV_OK : cuda_fail(e, "net_orthogonalise");
 }
 
@@ -836,5 +868,14 @@ size_t net_orthogonalise_workspace_bytes(const net_ortho* a) {
 }
 
 int net_orthogonalise(const net_ortho* a, void* stream) { return auv::net::run(a, stream); }
+
+int net_orthogonalise_selftest_timeout(const net_ortho* a, uint32_t product, uint32_t limit_us, void* stream) {
+  using namespace auv::net;
+  const int rc = check(a);
+  if (rc) return rc;
+  if (product < 1 || product >= a->steps * 3) return fail(AUV_ERR_INVALID, "product %u: not from 1 on and ahead of the last", product);
+  if (limit_us < 1 || limit_us > 5000000) return fail(AUV_ERR_INVALID, "limit_us outside [1, 5e6]");
+  return run(a, stream, (int)product, limit_us * 1000ull);
+}
 
 }  // extern "C"

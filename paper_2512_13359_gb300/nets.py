@@ -31,7 +31,7 @@ EXPORTED = ("net_gate_scan_workspace_bytes", "net_gate_scan", "net_gate_scan_bac
             "net_group_norm_workspace_bytes", "net_group_norm", "net_group_norm_backward", "net_dropout",
             "net_causal_conv_workspace_bytes", "net_causal_conv", "net_causal_conv_backward",
             "net_select_scan_workspace_bytes", "net_select_scan", "net_select_scan_backward",
-            "net_orthogonalise_workspace_bytes", "net_orthogonalise", "net_last_error")
+            "net_orthogonalise_workspace_bytes", "net_orthogonalise", "net_orthogonalise_selftest_timeout", "net_last_error")
 
 # The argument blocks, field by field as in the header (native alignment).
 _ROWS = "Pqq"
@@ -63,6 +63,8 @@ def lib():
             getattr(L, name).restype = C.c_size_t
         L.net_orthogonalise_workspace_bytes.argtypes = [C.c_char_p]
         L.net_orthogonalise_workspace_bytes.restype = C.c_size_t
+        L.net_orthogonalise_selftest_timeout.argtypes = [C.c_char_p, C.c_uint32, C.c_uint32, C.c_void_p]
+        L.net_orthogonalise_selftest_timeout.restype = C.c_int
         L.net_last_error.restype = C.c_char_p
         _lib = L
     return _lib
@@ -468,7 +470,8 @@ def select_scan_backward(x, dt, A, B, C, kept, dy, *, skip=None, dt_bias=None, g
 def orthogonalise(x, steps=5, *, coef=(3.4445, -4.775, 2.0315), eps=1e-7, y=None, stream=None):
     """Each of the matrices x [L, M, N] with its singular values v, over their norm, taken `steps` times through
     a v + b v^3 + c v^5 (coef): with the usual coefficients and five steps they come to lie about 1, and the singular
-    vectors stay.  Returns y [L, M, N] of x's type; y may be x."""
+    vectors stay.  Returns y [L, M, N] of x's type; y may be x.  A matrix with a value that is not finite comes out as NaN, and so
+    do values that a wait inside the kernel, given up after 2 s, has kept from being computed."""
     scratch = []
     shape, dtype, index = like = _activation(x, "x")
     if y is None:

@@ -437,6 +437,34 @@ def test_updates_on_two_streams_at_once():
         assert torch.equal(y, want[i % 2])
 
 
+@pytest.mark.parametrize("dt,L,M,N", [("fp32", 2, 300, 200), ("bf16", 3, 150, 700), ("fp32", 24, 512, 640), ("fp16", 24, 640, 512)])
+def test_update_whose_wait_gives_up(dt, L, M, N):
+    """One block waits behind a product for what never comes (20 ms): the code says so, no value of y is anything but right or
+    NaN, none is right where products were still to come for all blocks, and the next call is as ever.  By single blocks and by
+    pairs."""
+    torch, nets, types = _t()
+    from paper_2512_13359_gb300.nets import NET_DTYPE, _ORTHO
+    lib, t, steps = nets.lib(), types[dt], 2
+    g = torch.Generator(device="cuda").manual_seed(M)
+    x = torch.randn(L, M, N, device="cuda", generator=g).to(t)
+    want = nets.orthogonalise(x, steps)
+    y = torch.empty_like(x)
+    fields = (_ORTHO.size, NET_DTYPE[t], steps, 1e-7, 3.4445, -4.775, 2.0315, 0, L, M, N, x.data_ptr(), M * N, N, y.data_ptr(), M * N, N)
+    need = lib.net_orthogonalise_workspace_bytes(_ORTHO.pack(*fields, 0, 0))
+    work = torch.empty(need, device="cuda", dtype=torch.uint8)
+    args = _ORTHO.pack(*fields, work.data_ptr(), need)
+    code = lambda: int(work[:4].view(torch.int32).item())         # noqa: E731
+    for product in range(1, 3 * steps):
+        y.zero_()
+        assert lib.net_orthogonalise_selftest_timeout(args, product, 20000, torch.cuda.current_stream().cuda_stream) == 0
+        assert code() == -4
+        gone = torch.isnan(y)
+        assert gone.any() and torch.equal(y[~gone], want[~gone])
+        assert gone.all() or product == 3 * steps - 1
+    assert lib.net_orthogonalise(args, torch.cuda.current_stream().cuda_stream) == 0
+    assert code() == 0 and torch.equal(y, want)
+
+
 def test_update_of_many_small_ones():
     torch, nets, _ = _t()
     g = torch.Generator(device="cuda").manual_seed(3)

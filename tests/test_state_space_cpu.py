@@ -79,6 +79,15 @@ def test_workspaces(nets):
                 assert L.net_causal_conv_workspace_bytes(form.pack(*f), 1) == 0         # no weight gradients asked for
 
 
+@pytest.mark.parametrize("product,limit,msg", [(0, 20000, "product"), (15, 20000, "product"), (1, 0, "limit_us"), (14, 5000001, "limit_us"),
+                                               (14, 20000, "x is NULL")])
+def test_bad_limits_of_the_self_test_are_rejected(nets, product, limit, msg):
+    form, fields = _blocks(nets)["net_orthogonalise"]
+    assert nets.lib().net_orthogonalise_selftest_timeout(form.pack(*fields), product, limit, None) == -1
+    assert msg in nets.lib().net_last_error().decode()
+    assert nets.lib().net_orthogonalise_selftest_timeout(None, 1, 20000, None) == -1
+
+
 def test_wrong_tensors_are_rejected(nets):
     import torch
     from paper_2512_13359_gb300.auvenv import AuvError
