@@ -317,11 +317,14 @@ int net_select_scan_backward(const net_select* a, void* stream);
  * singular vectors: with coef (a, b, c) = (3.4445, -4.775, 2.0315) and five
  * steps an update's singular values come to lie about 1.  Where M > N the
  * products are x (b P + c P P) with P = x^T x, the same polynomial.  Norms are
- * taken in range whatever the scale of x.  steps = 0: y = x / (|x| + eps).
- * y may be x.  A matrix with a value that is not finite comes out as NaN.
+ * taken in range whatever the scale of x, from the smallest subnormal to the
+ * largest number.  steps = 0: y = x / (|x| + eps).  y may be x.  A matrix with a
+ * value that is not finite comes out as NaN, whatever the steps; so does one of
+ * zeros with eps = 0.
  *
- * The products are taken of two fp16 pieces of every value (22 bits) with sums
- * in fp32, so the coefficients have to keep what is between them in fp16's
+ * The products are taken of two fp16 pieces of every value (22 bits, and not
+ * below 2^-37 for a value of x / (|x| + eps): where |x| is far below eps, that is
+ * less) with sums in fp32, so the coefficients have to keep what is between them in fp16's
  * range: from v in [0, 1] no singular value may come above 8, nor
  * |a| + |b| v^2 + |c| v^4 above 1000 (AUV_ERR_UNSUPPORTED; the usual ones reach 1.3 and 15).
  *

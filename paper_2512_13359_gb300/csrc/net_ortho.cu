@@ -40,8 +40,11 @@ constexpr uint64_t kWaitLimitNs = 2000000000ull;
 enum Kind { kP, kQ, kX, kLast };
 
 // ---- sums of squares ----
-// Of x, and of x times 2^64 and 2^-64: one of the three is in range wherever the largest |x| is.
-constexpr float kUp = 18446744073709551616.0f, kDown = 1.0f / 18446744073709551616.0f;
+// Of x, and of x times 2^100 and 2^-96: one of the three is in range wherever the largest |x| is, of up to 2^36 values.  2^-96:
+// squares of the largest, 2^64, sum up to 2^100.  2^100: those of the smallest subnormal are 2^-98, and of sums below 1e-24
+// (kLow) they come to less than 2^121.  What a sum from kLow on, or the scaled one of a sum from kHigh on, loses of squares
+// below 2^-149 is 2^-34 of it at most.
+constexpr float kUp = 0x1p100f, kDown = 0x1p-96f, kLow = 1e-24f, kHigh = 1e36f;
 constexpr int kNormThreads = 256;
 
 template <typename T>
@@ -92,7 +95,8 @@ __global__ void __launch_bounds__(kNormThreads) k_squares(net_rows x, int64_t M,
   }
 }
 
-// 1 / (|x| + eps) as two factors, from the blocks' sums (every thread of a block; fixed order).
+// 1 / (|x| + eps) as two factors, from the blocks' sums (every thread of a block; fixed order).  Multiplied one after the other
+// they keep x in range.  NaN where a value is not finite.
 __device__ __forceinline__ float2 inverse_norm(const float* partial, int blocks, float eps) {
   __shared__ float part[3][kNormThreads / 32];
   float s[3] = {0.0f, 0.0f, 0.0f};
@@ -111,8 +115,11 @@ __device__ __forceinline__ float2 inverse_norm(const float* partial, int blocks,
     s[k] = 0.0f;
     for (int w = 0; w < kNormThreads / 32; ++w) s[k] += part[k][w];
   }
-  if (s[0] >= 1e30f) return make_float2(kDown, 1.0f / (sqrtf(s[2]) + eps * kDown));     // also infinite sums; NaN falls through
-  if (s[0] < 1e-30f) return make_float2(kUp, 1.0f / (sqrtf(s[1]) + eps * kUp));
+  if (s[0] >= kHigh) {                       // also infinite sums; NaN falls through
+    if (isinf(s[2])) return make_float2(__uint_as_float(0x7fc00000u), 1.0f);
+    return make_float2(1.0f / (sqrtf(s[2]) + eps * kDown), kDown);
+  }
+  if (s[0] < kLow && !isinf(eps * kUp)) return make_float2(kUp, 1.0f / (sqrtf(s[1]) + eps * kUp));     // else |x| is nothing to eps
   return make_float2(1.0f, 1.0f / (sqrtf(s[0]) + eps));
 }
 

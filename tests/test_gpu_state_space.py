@@ -382,6 +382,38 @@ def test_update_whatever_the_scale(scale):
         _check_ortho(1, 20, 30, "bf16", scale=scale, seed=8)
 
 
+@pytest.mark.parametrize("L,M,N,dt,scale,steps", [(2, 64, 80, "fp32", 5e37, 5), (1, 300, 500, "fp32", 5e37, 0), (2, 300, 500, "bf16", 5e37, 2),
+                                                  (2, 64, 80, "fp32", 1e16, 1), (2, 64, 80, "fp32", 1e-14, 1), (2, 100, 70, "fp32", 1e-42, 5),
+                                                  (2, 100, 70, "fp32", 1e-42, 0), (1, 40, 1000, "bf16", 1e-38, 1), (2, 20, 30, "fp32", 3e-45, 1)])
+def test_update_of_the_largest_and_smallest_values(L, M, N, dt, scale, steps):
+    """Sums of squares far out of fp32's range, subnormals, and either side of where another scale takes over."""
+    _check_ortho(L, M, N, dt, scale=scale, steps=steps, eps=0.0, seed=N)
+
+
+@pytest.mark.parametrize("steps", [0, 1, 5])
+@pytest.mark.parametrize("dt", DT)
+def test_update_of_values_that_are_not_finite(dt, steps):
+    torch, nets, types = _t()
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.randn(5, 40, 60, device="cuda", generator=g).to(types[dt])
+    for i, bad in ((1, float("inf")), (2, -float("inf")), (3, float("nan"))):
+        x[i, 3 * i, 7] = bad
+    y = nets.orthogonalise(x, steps)
+    assert torch.isfinite(y[0]).all() and torch.isfinite(y[4]).all() and torch.isnan(y[1:4]).all()
+    assert torch.isnan(nets.orthogonalise(torch.zeros(1, 4, 5, device="cuda", dtype=types[dt]), steps, eps=0.0)).all()
+
+
+def test_update_beside_a_large_eps():
+    torch, nets, _ = _t()
+    g = torch.Generator(device="cuda").manual_seed(6)
+    x = torch.randn(2, 20, 30, device="cuda", generator=g) * 1e-25
+    for eps in (1e-3, 1e5, 1e10):
+        # a sum, a quotient and two products, 4 U; |x| is 2^-70 of eps or less; a result below 2^-126 (x of 1e-28 over 1e10) is
+        # rounded to a multiple of 2^-149, off by half of that
+        want = _np(x) / eps
+        assert (np.abs(_np(nets.orthogonalise(x, 0, eps=eps)) - want) <= 4 * R.U * np.abs(want) + 2.0 ** -150).all()
+
+
 def test_update_large():
     _check_ortho(1, 1024, 1300, "fp32", seed=1)
     _check_ortho(2, 1100, 600, "bf16", seed=2)
