@@ -237,10 +237,17 @@ __global__ void __launch_bounds__(32 * kWarps, L::OWN > 1 ? 3 : L::SP == 8 ? 4 :
 // The states before the pieces (backward: their gradients behind the pieces), in the place of the pieces' own.  A block has
 // some states and all pieces: each of its groups of threads folds adjacent pieces to one, those are joined over the block, and
 // the groups go through their pieces once more from the state they begin with.  293 pieces of 4,000 states: 12 us in 64 groups,
-// 40 by one thread a state, which is enough for a few pieces.  The product of a piece's decays is kept from 0: an infinite
-// state does not become NaN by a long piece.
+// 40 by one thread a state, which is enough for a few pieces.
 constexpr int kJoin = 512, kJoinGroups = 64, kJoinAhead = 4;
-__device__ __forceinline__ float decay_of(float A2, float sum) { return fmaxf(ex2(A2 * sum), 1.17549435e-38f); }
+// A state behind a piece: that before it times the product of the piece's decays, 2^(A2 sum), and the piece's own.  The product
+// may be out of fp32's range where the state behind it is not (2^140 of one of 2^-100): as 2^126, or 2^-126, and twice the root
+// of the rest, so none of the factors is 0 or infinite, and a state of 0 stays 0 and an infinite one infinite, as step by step.
+// 2^360 takes the smallest number past the largest, and 2^-360 the other way.  (Where the power is NaN, so is the piece's own.)
+__device__ __forceinline__ float through_piece(float A2, float sum, float state, float own) {
+  const float power = A2 * sum, most = fminf(fmaxf(power, -126.0f), 126.0f);
+  const float root = ex2(fminf(fmaxf((power - most) * 0.5f, -117.0f), 117.0f));     // 1, mostly
+  return fmaf(ex2(most), state * root * root, own);
+}
 __global__ void __launch_bounds__(kJoin) k_select_join(Select a, bool back, int groups) {
   __shared__ float sums[kJoin], owns[kJoin];
   after_previous();
@@ -269,7 +276,7 @@ __global__ void __launch_bounds__(kJoin) k_select_join(Select a, bool back, int 
         if (q + u < n) {
           if (put) a.maps[(first + (q + u) * by) * m + i] = state;
           else total = sum[u] < 0.0f || total < 0.0f ? -1.0f : total + sum[u];
-          state = sum[u] < 0.0f ? own[u] : fmaf(decay_of(A2, sum[u]), state, own[u]);
+          state = sum[u] < 0.0f ? own[u] : through_piece(A2, sum[u], state, own[u]);
         }
     }
   };
@@ -283,7 +290,7 @@ __global__ void __launch_bounds__(kJoin) k_select_join(Select a, bool back, int 
     for (int q = 0; q < groups; ++q) {
       const float sum = sums[q * side + k], own = owns[q * side + k];
       owns[q * side + k] = h;
-      h = sum < 0.0f ? own : fmaf(decay_of(A2, sum), h, own);
+      h = sum < 0.0f ? own : through_piece(A2, sum, h, own);
     }
   }
   __syncthreads();

@@ -188,6 +188,55 @@ def test_scan_of_narrow_groups(T, N, D, S, G, dt, layout):
     _check_scan(T, N, D, S, G, dt, layout, ends=0.05, seed=14)
 
 
+def _against_formulas(a, h0, dy=None):
+    """select_scan of inputs without ends, gate or bias, and its gradients, against the 64-bit reference."""
+    torch, nets, _ = _t()
+    y, hT, kept = nets.select_scan(**a, h0=h0, kept=True)
+    q = R.Scan(*(_np(a[k]) for k in ("x", "dt", "A", "B", "C")), None, None, None, _nn(h0), None, None)
+    _within(y, q.y, q.Ey)
+    _within(hT, q.hT, q.EhT)
+    if dy is not None:
+        names = ("dx", "ddt", "dA", "dB", "dC", "dskip", "ddt_bias", "dgate", "dh0")
+        got, ref = dict(zip(names, nets.select_scan_backward(*(a[k] for k in ("x", "dt", "A", "B", "C")), kept, dy))), q.backward(_np(dy), None)
+        for k in ref:
+            _within(got[k], *ref[k])
+    return hT
+
+
+@pytest.mark.parametrize("D,S", [(8, 4), (40, 16)])
+@pytest.mark.parametrize("T", [1000, 20000])
+def test_scan_of_growing_states(T, D, S):
+    """A > 0: over a piece of a long sequence a state would grow past fp32's range, but it is 0 until the last steps (and its
+    gradient from the first steps on)."""
+    torch, nets, types = _t()
+    g, a, _, _ = _scan_args(torch, types["fp32"], T, 1, D, S, 1, "flat", None, 3)
+    a["A"], a["dt"] = 0.5 + 0.5 * torch.rand(D, S, device="cuda", generator=g), 1.0 + 0.1 * a["dt"]
+    late, early = torch.zeros(2, T, 1, D, device="cuda")
+    late[-20:], early[:20] = a["x"][-20:], a["x"][:20]
+    hT = _against_formulas(dict(a, x=late), None)
+    assert hT.abs().max() > 1e3
+    _against_formulas(dict(a, x=torch.zeros_like(late)), None, early)
+
+
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("T", [160, 1000])
+def test_scan_of_states_that_pass_a_range_of_their_own(T, sign):
+    """From 2^-100 up by 2^140, or from 2^100 down by as much, in the first piece of a sequence: in fp32's range at both ends."""
+    torch, nets, types = _t()
+    D, S = 8, 4
+    g, a, _, _ = _scan_args(torch, types["fp32"], T, 1, D, S, 1, "flat", None, 5)
+    a["dt"].fill_(-20.0)
+    a["dt"][:60] = 1.0
+    steps = 60 * np.log1p(np.e)                                   # the sum of the step sizes that count
+    a["A"] = torch.full((D, S), sign * 140 * np.log(2.0) / steps, device="cuda")
+    a["x"].zero_()
+    h0 = torch.randn(1, D, S, device="cuda", generator=g) * 2.0 ** (-100 * sign)
+    hT = _against_formulas(a, h0)
+    assert (hT.double() / h0.double()).log2().sub(140 * sign).abs().max() < 0.1
+    h0[0, 0] = float("inf")
+    assert torch.isinf(nets.select_scan(**a, h0=h0)[1][0, 0]).all()
+
+
 @pytest.mark.parametrize("T", [40, 20000])
 def test_scan_of_a_constant_input_reaches_its_limit(T):
     """dt = 0, no bias: e = log 2; with B x = 1 the state goes to e / (1 - exp(e A)) times 1 minus exp(e A T), whatever the
