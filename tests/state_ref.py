@@ -187,3 +187,49 @@ def orthogonalise(x, steps, coef, eps):
         X = Q @ X if wide else X @ Q
         E += 2.0 ** -22 * f(X)
     return X, E
+
+
+# Sizes at which both pieces of X, of P and of Q weigh, and coefficients that give P P its part.
+RANK_ONE = [(115, 110), (120, 125), (493, 874), (1044, 487), (493, 804), (518, 493), (991, 895), (613, 212), (630, 493), (493, 917)]
+RANK_ONE_COEF = (0.2, 0.2, 0.6)
+
+
+def _pieces(v):
+    hi = np.float64(np.float16(v))
+    return hi, np.float64(np.float16(v - hi))
+
+
+def rank_one_update(M, N, steps, coef, lost=None):
+    """One value of the update of a matrix of ones, whose result is v / sqrt(M N) everywhere, by the two fp16 pieces of each
+    value and three products of them (scaled by 4096, 512 and 64), sums exact; lost: "P", "Q" or "X" and "hl" or "lh" for a
+    product of pieces that is left out.  Every sum is of equal terms, so what a piece is to the result does not average out."""
+    a, b, c = coef
+    s, n = min(M, N), max(M, N)
+
+    def product(u, v, which):
+        (uh, ul), (vh, vl) = _pieces(u), _pieces(v)
+        return uh * vh + (lost != which + "hl") * uh * vl + (lost != which + "lh") * ul * vh
+    x = 4096 / np.sqrt(M * N)
+    for _ in range(steps):
+        p = n * product(x, x, "P") * 512 / 4096 ** 2
+        q = b * sum(_pieces(p)) / 512 + c * s * product(p, p, "Q") / 512 ** 2
+        x = ((s - 1) * product(64 * q, x, "X") + product(64 * (q + a), x, "X")) / 64
+    return x / 4096
+
+
+def rank_one_bound(M, N, steps, coef):
+    """Relative bound of the same in fp32 and tensor products, for coefficients >= 0 that sum up to 1 (v stays 1, no sum
+    cancels).  A value in two pieces is off by 2^-22 of itself and 2^-25 of its scaled unit; a product leaves 2^-22 of a term
+    out, adds 16 terms in a tensor instruction and twelve of those to a sum over 64 of K, of which each may cut 2^-22 (those of
+    the large pieces; the small ones' are 2^-11 of that), and rounds once for each 64 of K."""
+    a, b, c = coef
+    s, n = min(M, N), max(M, N)
+    piece = lambda v: 2.0 ** -22 + 2.0 ** -25 / v                  # noqa: E731
+    eta = lambda K: 13 * 2.0 ** -22 + np.ceil(K / 64) * U          # noqa: E731
+    r = 80 * U                                                     # norm, a root of sums of up to 128 values in a row, and quotient
+    for _ in range(steps):
+        r += piece(4096 / np.sqrt(M * N))
+        p = 2 * r + eta(n) + 4 * U + piece(512 / s)
+        q = (b * p + c * (2 * p + eta(s))) / (b + c) + 4 * U + piece(64 * (b + c) / s)
+        r += (b + c) * q + a * piece(64 * a) + eta(s) + 4 * U
+    return r

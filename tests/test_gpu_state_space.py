@@ -475,6 +475,20 @@ def test_update_of_stacks(L, M, N, dt, layout):
     _check_ortho(L, M, N, dt, layout, seed=L)
 
 
+@pytest.mark.parametrize("steps", [1, 2])
+@pytest.mark.parametrize("L,M,N", list(zip((20, 54, 4, 27, 9, 55, 19, 52, 18, 19), *zip(*R.RANK_ONE))))
+def test_update_has_all_pieces_of_its_products(L, M, N, steps):
+    """Matrices of one rank with random signs, at sizes that take all kinds of tiles (one tile, narrow and wide ones, pairs of
+    blocks): every value to 3e-5 of itself (1.4e-4 after two steps), a third of what a lost product of pieces would be."""
+    torch, nets, _ = _t()
+    g = torch.Generator(device="cuda").manual_seed(L)
+    sign = lambda *s: torch.randint(0, 2, s, device="cuda", generator=g).float() * 2 - 1      # noqa: E731
+    signs = sign(L, M, 1) * sign(L, 1, N)
+    y = nets.orthogonalise(signs * 1e-3, steps, coef=R.RANK_ONE_COEF, eps=0.0)
+    off = np.abs(_np(y * signs) * np.sqrt(M * N) - 1).max()
+    assert off <= R.rank_one_bound(M, N, steps, R.RANK_ONE_COEF), off
+
+
 def test_update_of_zeros_and_of_nothing():
     torch, nets, _ = _t()
     z = torch.zeros(2, 10, 20, device="cuda")

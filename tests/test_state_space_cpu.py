@@ -181,6 +181,19 @@ def test_reference_update_moves_singular_values(M, N):
     assert np.allclose(y, u * v @ w, atol=1e-12)
 
 
+@pytest.mark.parametrize("M,N", R.RANK_ONE)
+def test_bound_of_an_update_sees_a_lost_piece(M, N):
+    """What the GPU's update of a matrix of one rank is held to is a third of what any of its products of pieces is to it."""
+    assert np.isclose(R.rank_one_update(M, N, 1, R.RANK_ONE_COEF) * np.sqrt(M * N), 1.0, rtol=1e-6)
+    for steps in (1, 2):
+        bound = R.rank_one_bound(M, N, steps, R.RANK_ONE_COEF)
+        whole = R.rank_one_update(M, N, steps, R.RANK_ONE_COEF) * np.sqrt(M * N) - 1
+        assert abs(whole) < bound
+        for lost in ("Phl", "Plh", "Qhl", "Qlh", "Xhl", "Xlh"):
+            off = R.rank_one_update(M, N, steps, R.RANK_ONE_COEF, lost) * np.sqrt(M * N) - 1
+            assert abs(off) > 3 * bound, (steps, lost, off / bound)
+
+
 def test_reference_activation_is_the_operators():
     u = np.linspace(-20, 20, 41)
     assert np.allclose(act(u, "silu")[0], u / (1 + np.exp(-u)))
