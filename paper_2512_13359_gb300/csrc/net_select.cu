@@ -201,7 +201,7 @@ __global__ void __launch_bounds__(32 * kWarps, L::OWN > 1 ? 3 : L::SP == 8 ? 4 :
           F2 acc = pair(0.0f, 0.0f);
 #pragma unroll
           for (int i = 0; i < SP / 2; ++i) {
-            h[c][i] = fma2(ex2(e2 * A2[c][i]), h[c][i], u2 * B[i]);
+            h[c][i] = fma2(decay_of(e2, A2[c][i]), h[c][i], u2 * B[i]);
             if constexpr (!FOLD) acc = i ? fma2(C[i], h[c][i], acc) : C[i] * h[c][i];
           }
           y[c] = total(acc);
@@ -450,11 +450,11 @@ __global__ void __launch_bounds__(32 * kOneWarps, 4) k_select_one(Select a, bool
     to_lanes<CC>(e * x, us);
 #pragma unroll
     for (int c = 0; c < CC; ++c) {
-      const F2 e2 = pair(es[c], es[c]), u2 = pair(us[c], us[c]);
+      const F2 u2 = pair(us[c], us[c]);
       F2 acc;
 #pragma unroll
       for (int i = 0; i < P; ++i) {
-        h[c][i] = fma2(ex2(e2 * A2[c][i]), h[c][i], u2 * uB[i]);
+        h[c][i] = fma2(decay_of(es[c], A2[c][i]), h[c][i], u2 * uB[i]);
         acc = i ? fma2(oC[i], h[c][i], acc) : oC[i] * h[c][i];
       }
       y[c] = total(acc);

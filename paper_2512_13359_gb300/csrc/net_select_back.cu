@@ -346,7 +346,7 @@ __global__ void __launch_bounds__(32 * back_warps(L::SW, L::R), back_blocks(L::S
 #pragma unroll
             for (int c = 0; c < CC; ++c)
 #pragma unroll
-              for (int i = 0; i < P; ++i) h[c][i] = fma2(ex2(e[c] * A2[c][i]), h[c][i], u[c] * B[i]);
+              for (int i = 0; i < P; ++i) h[c][i] = fma2(decay_of(e[c], A2[c][i]), h[c][i], u[c] * B[i]);
           }
         };
         T* pdx = const_cast<T*>(row_at<T>(a.dx, ts + subs * kSub, n, d));
@@ -374,7 +374,7 @@ __global__ void __launch_bounds__(32 * back_warps(L::SW, L::R), back_blocks(L::S
                 F2 acc;
 #pragma unroll
                 for (int i = 0; i < P; ++i) {
-                  decay[k][c][i] = ex2(e[c] * A2[c][i]);
+                  decay[k][c][i] = decay_of(e[c], A2[c][i]);
                   passed[k][c][i] = decay[k][c][i] * h[c][i];
                   h[c][i] = fma2(u[c], B[i], passed[k][c][i]);
                   acc = i ? fma2(C[i], h[c][i], acc) : C[i] * h[c][i];
@@ -625,7 +625,7 @@ __global__ void __launch_bounds__(32 * kFoldWarps) k_select_fold_back(Select a) 
         for (int c = 0; c < CC; ++c) {
           const F2 e2 = pair(es[c], es[c]), p2 = pair(ps[c], ps[c]);
 #pragma unroll
-          for (int i = 0; i < SP / 2; ++i) G[c][i] = ex2(e2 * A2[c][i]) * fma2(p2, C[i], G[c][i]);
+          for (int i = 0; i < SP / 2; ++i) G[c][i] = decay_of(e2, A2[c][i]) * fma2(p2, C[i], G[c][i]);
         }
         if (ends >> k & 1u) clear(G);
       }
