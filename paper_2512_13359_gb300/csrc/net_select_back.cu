@@ -153,20 +153,6 @@ __device__ __forceinline__ void clear(F2 (&h)[CC][P]) {
 #pragma unroll
     for (int i = 0; i < P; ++i) h[c][i] = pair(0.0f, 0.0f);
 }
-// One value, where `on`, without a branch.
-template <typename T>
-__device__ __forceinline__ void store_if(bool on, T* p, float v) {
-  T t;
-  from_float(v, t);
-  if constexpr (sizeof(T) == 4)
-    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t@q st.global.b32 [%0], %1;\n\t}" ::"l"(p), "r"(__float_as_uint(v)),
-                 "r"((int)on)
-                 : "memory");
-  else
-    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t@q st.global.b16 [%0], %1;\n\t}" ::"l"(p),
-                 "h"(*reinterpret_cast<const uint16_t*>(&t)), "r"((int)on)
-                 : "memory");
-}
 __device__ __forceinline__ void prefetch(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
 // rows: (env, group) pairs a block walks side by side, back_warps / rows warps each.
