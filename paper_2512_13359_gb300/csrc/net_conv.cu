@@ -4,8 +4,9 @@
 // to step but the last K - 1 rows, so a sequence is cut into chunks of steps that know nothing of each other: a thread
 // walks E adjacent channels of one env through one chunk with those rows in registers, and reads the K - 1 rows ahead of
 // its chunk once more (backward: also those behind it, whose outputs the chunk's rows are part of).  128 steps of 4,096 envs x
-// 256 channels of bf16, K = 4, silu: 114 us (4.8 TB/s) and 185 us (4.5 TB/s); both wait for chains of dependent products, with
-// 16 warps an SM.
+// 256 channels of bf16, K = 4, silu: 115 us (4.8 TB/s) and 185 us (4.5 TB/s), of 81 and 122 that the bytes take.  What bounds
+// them is not established: issue slots are half used and DRAM less than half busy, and what warps wait for most are their own
+// products, but neither more warps nor more bytes on their way (below) made them faster.
 #include <algorithm>
 
 #include "net_common.cuh"

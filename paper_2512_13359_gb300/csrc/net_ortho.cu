@@ -17,9 +17,9 @@
 // K = 4096 came to 9e-5 of the result.  So a sum runs over 64 of K there, small products first, and those sums are added in
 // registers, rounded to nearest, while the next 64 run into the other half of tensor memory (1e-6; 8 % of the time).
 //
-// 4,096 x 4,096 fp32, five steps: 3.0 ms, 71 % of the measured bf16 rate in products (three for one, symmetric ones by half):
-// large products are taken by pairs of blocks (below).  24 x 1,000 x 515 bf16: 775 us; 4 x 256 x 256 fp32: 159 us, latency of
-// 15 products and barriers.
+// 4,096 x 4,096 fp32, five steps: 3.0 to 3.1 ms on several boxes, 68 to 71 % of the measured bf16 rate in products (three for
+// one, symmetric ones by half): large products are taken by pairs of blocks (below).  24 x 1,000 x 515 bf16: 780 to 790 us;
+// 4 x 256 x 256 fp32: 162 us, latency of 15 products and barriers.
 #include <cuda.h>
 
 #include <algorithm>

@@ -2,14 +2,14 @@
 //
 // Per channel and state a chain h = a c + u B with a = exp(e A), u = e x: S exponentials and 4 S products and sums a value
 // of x, against 8 to 16 bytes of it, so with S = 16 the multi-function unit, the fp32 pipe and HBM are all near their
-// limits.  k_select walks the steps with the states in registers (layout: net_select.cuh), B and C of 16 steps staged in
+// limits.  k_select walks the steps with the states in registers (layout: net_select.cuh), B and C of four steps staged in
 // shared memory by each warp for itself.  Sequences of few channels are cut into pieces: each is walked from 0 for its
 // final state and the sum of its step sizes (the product of its decays is exp(A sum)), those are joined to the states
 // before the pieces (k_select_join), and the pieces are walked from these.
 //
-// 128 steps of 4,096 envs x 256 channels x 16 states of bf16, states kept: 682 us (HBM alone 262, exponentials 230): 12 warps
-// an SM, two channels a lane each, wait for their own instructions half of the time.  65,521 steps of 250 x 13 fp32: 161 us, of
-// which 60 the fold, 12 the join and 85 the walk.
+// 128 steps of 4,096 envs x 256 channels x 16 states of bf16, states kept: 671 us (HBM alone 262, exponentials 230): 12 warps
+// an SM, two channels a lane each, wait for their own instructions half of the time.  65,521 steps of 250 x 13 fp32: 162 us, of
+// which 60 the fold, 85 the walk and the rest the join.
 #include <algorithm>
 
 #include "net_select.cuh"
@@ -299,7 +299,7 @@ __global__ void __launch_bounds__(kJoin) k_select_join(Select a, bool back, int 
 }
 
 // One step, as in a rollout: the states are read, changed and written, so few registers and no staging; a warp takes its
-// channels of one env after the other, A in registers (65,536 envs x 256 x 16 of bf16: 351 us, 6.5 TB/s).  wide: B's and C's
+// channels of one env after the other, A in registers (65,536 envs x 256 x 16 of bf16: 350 us, 6.5 TB/s).  wide: B's and C's
 // values of a lane are aligned vectors, of a lane that has states (there); one past them (S = 24: the last of four) has zeros.
 template <typename T, int SP>
 __device__ __forceinline__ void load_row(const T* p, bool wide, bool there, int s0, int S, F2 (&v)[SP / 2]) {

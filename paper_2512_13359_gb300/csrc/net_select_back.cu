@@ -9,8 +9,8 @@
 // block's warps in shared memory at the end of a segment; groups wider than a block leave partial sums, which k_select_rows
 // adds.  Weight gradients stay in registers over an env's piece.  Every sum has a fixed order.
 //
-// 128 steps of 4,096 envs x 256 channels x 16 states of bf16: 4.0 ms (the fp32 pipe alone 0.7): 255 registers leave 8 warps an
-// SM, which wait for each other's latencies.  One channel a lane with 16 warps took 5.1 ms (every lane does a whole channel's
+// 128 steps of 4,096 envs x 256 channels x 16 states of bf16: 3.9 ms (the fp32 pipe alone 0.7): 255 registers a thread and 28 KB
+// of shared memory a warp, either of them, leave 8 warps an SM, which wait for each other's latencies.  One channel a lane with 16 warps took 5.1 ms (every lane does a whole channel's
 // and step's own work), four steps held instead of two 4.2 (spills).
 #include <algorithm>
 
